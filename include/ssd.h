@@ -381,6 +381,172 @@ int ssd_decode_step_split_rope(ssd_cache *cache, int layer_begin, int layer_end,
                                int compress, const float *cos, const float *sin, int rope_layout,
                                void *const *streams, int n_streams, int sync);
 
+/* ---- serving batches of unequal lengths: a cache in pages ------------------ */
+
+/*
+ * The calls above keep a cache whose sequences advance together.  A server's
+ * sequences do not: they come and go, have lengths of their own, and their
+ * rows lie in pages handed out from one pool.  The calls below work on such a
+ * cache.  They keep no descriptor and no counters: the lengths, the positions
+ * and the block table are device arrays of the caller, read when the call's
+ * kernels run, so that a step can be enqueued (or captured in a graph) before
+ * the lengths are known on the host.
+ *
+ *   pool        : K and V rows at  k_pages + page * page_stride + kv_head *
+ *                 head_stride + place * row_stride  (elements; d consecutive
+ *                 elements per row), page 0..n_pages-1, place 0..page_size-1;
+ *                 v_pages likewise.
+ *   block_table : dev int32 [n_seqs, max_blocks]; slot i of sequence b is place
+ *                 i % page_size of page block_table[b, i / page_size].  Entries
+ *                 past a sequence's last block are not read.  Sequences may
+ *                 share pages that are only read.  An entry outside
+ *                 0..n_pages-1 names no page: its rows are neither read nor
+ *                 written, and count as masked.
+ *   seq_len     : dev int32 [n_seqs], rows the sequence holds, the new token
+ *                 (or new tokens) of the call included; 0 is allowed, a value
+ *                 outside 0..max_len (0..max_blocks * page_size) is taken as
+ *                 the nearer end.
+ *   seq_pos     : dev int32 [n_seqs], tokens seen so far (the next position),
+ *                 evicted ones included; NULL: as seq_len.
+ *   pos, weight : dev int32 / float [n_pages, n_kv_heads, page_size], dense:
+ *                 position and accumulated attention weight of the row at each
+ *                 place.  Either may be NULL where a call says so: a cache
+ *                 from which nothing is evicted needs neither.
+ *   Grouped queries: query heads kv*G .. kv*G + G-1, G = n_heads / n_kv_heads,
+ *   read key / value head kv.
+ */
+typedef struct ssd_paged_config {
+    int32_t n_seqs;        /* B: 1..65535                                                  */
+    int32_t n_heads;       /* query heads: a multiple of n_kv_heads, at most 1024           */
+    int32_t n_kv_heads;    /* key / value heads: 1..1024                                    */
+    int32_t head_dim;      /* d: 64 or 128                                                 */
+    int32_t dtype;         /* ssd_dtype of q, k, v, the pool and the output                */
+    int32_t page_size;     /* places per page: 1..65536                                    */
+    int32_t n_pages;       /* pages of the pool: >= 1                                      */
+    int32_t max_blocks;    /* columns of block_table: >= 1, max_blocks * page_size <= 2^30 */
+    float   softmax_scale; /* 0 selects 1/sqrt(d)                                          */
+    int32_t reserved[3];   /* must be 0                                                    */
+    int64_t page_stride;   /* elements; multiples of 16 bytes, at least d.  All three 0:   */
+    int64_t head_stride;   /*   [n_pages, n_kv_heads, page_size, d], dense                 */
+    int64_t row_stride;
+    int64_t q_stride;      /* elements from a sequence's n_heads * d queries to the next's, 0: dense  */
+    int64_t new_stride;    /* elements from a new token's n_kv_heads * d elements to the next's (k_new and
+                              v_new alike), 0: dense.  Both: multiples of 16 bytes           */
+} ssd_paged_config;
+
+/*
+ * Write new tokens' rows into the pages: prompts of unequal lengths, or one
+ * token per sequence.
+ *   k_new, v_new : dev [n_new, n_kv_heads, d]
+ *   new_start    : dev int32 [n_seqs + 1], ascending from 0 to n_new: sequence b's tokens are
+ *                  rows new_start[b] .. new_start[b+1]-1; NULL: one token per
+ *                  sequence (n_new = n_seqs)
+ *   Token j of the n_b new ones goes to slot seq_len[b] - n_b + j, with position
+ *   seq_pos[b] - n_b + j and weight weight_new[row, kv_head] (dev float
+ *   [n_new, n_kv_heads]; NULL: 0).  Tokens whose slot is outside the sequence's rows
+ *   (0 .. min(seq_len[b], max_blocks * page_size) - 1) are left out, so is a
+ *   token of a sequence that holds nothing.
+ *   pos, weight : may be NULL (then not written)
+ */
+int ssd_paged_append(const ssd_paged_config *cfg, void *k_pages, void *v_pages, int32_t *pos, float *weight,
+                     const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos,
+                     const void *k_new, const void *v_new, const int32_t *new_start, int n_new,
+                     const float *weight_new, void *stream);
+
+/*
+ * Attention of one new token per sequence over the sequence's rows:
+ *     out[b, h] = sum_j p[h, j] v[j],  p[h, .] = softmax_j(scale * q[b, h] . k[j]),
+ *     lse[b, h] = log sum_j exp(scale * q[b, h] . k[j])   (natural logarithm)
+ * A sequence without rows gives out = 0 and lse = -infinity.
+ *   q, out     : dev [n_seqs, n_heads, d] (q with q_stride)
+ *   lse        : dev float [n_seqs, n_heads], or NULL.  Joins this result with one over other rows
+ *   weight_in, weight_out : both NULL, or tables shaped as `weight`:
+ *                weight_out[row] = weight_in[row] + sum of p[h, row] over the row's query heads,
+ *                for every row of every sequence; other places keep what they hold.  They may be
+ *                the same array (then no page may belong to two sequences)
+ *   max_len    : no sequence holds more rows than this (0: max_blocks * page_size); it bounds the
+ *                launch and the workspace.  A longer sequence is cut to it
+ *   workspace  : dev scratch, 256-byte aligned, at least ssd_paged_workspace_bytes(cfg, max_len,
+ *                weight_out != NULL) bytes; may be NULL if that is 0.  Nothing in it has to be
+ *                kept or cleared between calls
+ * Logits that are NaN or infinite are the caller's; they reach the outputs of
+ * their own sequence and heads only.  What lies in a page past a sequence's end is
+ * never used, whatever bits it holds.
+ */
+size_t ssd_paged_workspace_bytes(const ssd_paged_config *cfg, int max_len, int with_weights);
+int ssd_paged_decode_attn(const ssd_paged_config *cfg, const void *q, const void *k_pages, const void *v_pages,
+                          const float *weight_in, float *weight_out, const int32_t *block_table, const int32_t *seq_len,
+                          void *out, float *lse, int max_len, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ssd_paged_append of one token per sequence (weight 0), then ssd_paged_decode_attn:
+ * the same rows, tables and results, with the rows written on the way.  weight_in is not read at the
+ * new token's place.  pos may be NULL.  No page that holds a sequence's last row may belong to two sequences.
+ */
+int ssd_paged_decode_step(const ssd_paged_config *cfg, const void *q, const void *k_new, const void *v_new,
+                          void *k_pages, void *v_pages, int32_t *pos, const float *weight_in, float *weight_out,
+                          const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos,
+                          void *out, float *lse, int max_len, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Eviction by accumulated attention weight (the top-M rule of Algorithm 1, with
+ * the sinks and the recent tokens of Sec. 3.3 protected): every (sequence, kv
+ * head) keeps n' = min(seq_len[b], budget[b]) of its rows (a budget below 0 is 0).  Order: protected
+ * tokens (position < n_sink, or >= seq_pos[b] - recent) before the others, then the
+ * higher weight (NaN below everything, +0 = -0), then the lower position, then the lower
+ * slot.  Kept rows in slots below n' stay where they are; those in slots n' and above move, in
+ * slot order, into the slots that became free: afterwards the sequence's rows are its slots
+ * 0..n'-1, and its pages from block ceil(n' / page_size) on are the caller's again.
+ *   pos_in, weight_in   : the tables before; read in slots below seq_len[b]
+ *   pos_out, weight_out : the tables after; written in slots below n'.  May be the same arrays as pos_in, weight_in
+ *                         (both or neither)
+ *   budget       : dev int32 [n_seqs]
+ *   seq_len_out  : dev int32 [n_seqs], n' per sequence; may be NULL, must not be seq_len
+ *   max_len, workspace : as ssd_paged_decode_attn (ssd_paged_evict_workspace_bytes)
+ * The rows of K and V move in place; slots n' and above keep their contents.  Sequences that share
+ * a page must not be evicted from.  Rows of entries that name no page count like others and are not moved;
+ * their weight is taken as NaN, their position as 0.
+ */
+size_t ssd_paged_evict_workspace_bytes(const ssd_paged_config *cfg, int max_len);
+int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, const int32_t *block_table,
+                    const int32_t *seq_len, const int32_t *seq_pos, const int32_t *budget, int n_sink, int recent,
+                    const int32_t *pos_in, int32_t *pos_out, const float *weight_in, float *weight_out,
+                    int32_t *seq_len_out, int max_len, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * From a step's logits to those a token is sampled from.  Per output row i and
+ * vocabulary entry v, in fp32 and in this order:
+ *     x = logits[i, v], or guided:  c + gamma (c - u), c = logits[2i, v], u = logits[2i+1, v]  (Eq. 1)
+ *     x += bias[i, v]
+ *     v among the row's tokens:          x = x > 0 ? x / repetition[i] : x * repetition[i]
+ *     n = times v is among the row's tokens from n_prompt[i] on:
+ *                                        x -= frequency[i] * n + (n > 0 ? presence[i] : 0)
+ *     x /= temperature[i]
+ *     mask bit 0:                        x = -infinity, whatever it was
+ * A row whose mask leaves nothing is -infinity throughout.
+ */
+typedef struct ssd_logits_params {
+    const int32_t *tokens;      /* dev [n_rows, token_stride >= longest row] tokens so far, prompt first; NULL: none.
+                                   Entries outside 0..V-1 are ignored */
+    const int32_t *n_tokens;    /* dev [n_rows], 0..token_stride (values outside: the nearer end)  */
+    const int32_t *n_prompt;    /* dev [n_rows] how many of them are the prompt's; NULL: 0 */
+    const float *repetition;    /* dev [n_rows] each, NULL: 1, 0, 0, 1.  repetition and temperature that are */
+    const float *presence;      /*   not above 0 are taken as 1                                    */
+    const float *frequency;
+    const float *temperature;
+    const float *bias;          /* dev [n_rows, bias_stride], bias_stride 0: one row for all; NULL: none */
+    const uint32_t *mask;       /* dev [n_rows, mask_stride] words, bit v % 32 of word v / 32 allows v; mask_stride 0: one
+                                   row for all; NULL: everything is allowed */
+    int64_t token_stride, bias_stride, mask_stride;   /* elements */
+} ssd_logits_params;
+/*   logits  : dev, row r at r * logits_stride elements (0: V) of `dtype`; n_rows rows, or 2 * n_rows if guided
+ *   out     : dev float [n_rows, V] with out_stride (0: V).  May be logits where these are fp32, not guided, and the strides agree
+ *   guided  : 0 or 1; gamma (finite) is used if 1
+ *   n_rows  : 1..65535;  V : 1 .. 2^24
+ */
+int ssd_logits_process(const void *logits, int n_rows, int V, int dtype, int64_t logits_stride, int guided, float gamma,
+                       const ssd_logits_params *params, float *out, int64_t out_stride, void *stream);
+
 /* ---- exports for tests and benchmarks (not steps of the method) ------------ */
 
 /*

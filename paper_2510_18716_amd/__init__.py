@@ -12,4 +12,6 @@ from .binding import (  # noqa: F401
     SSD_ROPE_HALF, SSD_ROPE_INTERLEAVED, ssd_decode_step_rope,
     SSD_MAX_SPLIT, SSD_SPLIT_FORK, SSD_SPLIT_JOIN, ssd_decode_step_split, ssd_decode_step_split_rope, stream_array,
     ssd_dense_decode_attn, ssd_dense_decode_attn_static, SSD_DENSE_STATIC_SCRATCH_BYTES, ssd_dense_workspace_bytes, ssd_last_error, ssd_prefill_scores, ssd_version,
+    SsdLogitsParams, SsdPagedConfig, make_paged_config, ssd_logits_process, ssd_paged_append, ssd_paged_decode_attn, ssd_paged_decode_step,
+    ssd_paged_evict, ssd_paged_evict_workspace_bytes, ssd_paged_workspace_bytes,
 )

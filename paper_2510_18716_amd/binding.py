@@ -435,3 +435,118 @@ def ssd_dense_decode_attn_static(q, K, V, out, B: int, H: int, d: int, dtype, n_
     _check(lib.ssd_dense_decode_attn_static(_ptr(q), _ptr(K), _ptr(V), _ptr(out), B, H, d, _dtype_code(dtype), n_cap, n,
                                             float(softmax_scale), _ptr(far), _ptr(tot), mass_stride, vis_start, w,
                                             _stream(stream)), "ssd_dense_decode_attn_static")
+
+
+# ---- serving batches of unequal lengths: the cache in pages, the step's logits ----
+
+class SsdPagedConfig(C.Structure):
+    _fields_ = [
+        ("n_seqs", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_blocks", C.c_int32), ("softmax_scale", C.c_float),
+        ("reserved", C.c_int32 * 3), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("row_stride", C.c_int64),
+        ("q_stride", C.c_int64), ("new_stride", C.c_int64),
+    ]
+
+
+class SsdLogitsParams(C.Structure):
+    _fields_ = [
+        ("tokens", _vp), ("n_tokens", _vp), ("n_prompt", _vp), ("repetition", _vp), ("presence", _vp), ("frequency", _vp),
+        ("temperature", _vp), ("bias", _vp), ("mask", _vp), ("token_stride", C.c_int64), ("bias_stride", C.c_int64),
+        ("mask_stride", C.c_int64),
+    ]
+
+
+_pcfg = C.POINTER(SsdPagedConfig)
+lib.ssd_paged_append.argtypes = [_pcfg] + [_vp] * 10 + [C.c_int, _vp, _vp]
+lib.ssd_paged_append.restype = C.c_int
+lib.ssd_paged_workspace_bytes.argtypes = [_pcfg, C.c_int, C.c_int]
+lib.ssd_paged_workspace_bytes.restype = C.c_size_t
+lib.ssd_paged_decode_attn.argtypes = [_pcfg] + [_vp] * 9 + [C.c_int, _vp, C.c_size_t, _vp]
+lib.ssd_paged_decode_attn.restype = C.c_int
+lib.ssd_paged_decode_step.argtypes = [_pcfg] + [_vp] * 13 + [C.c_int, _vp, C.c_size_t, _vp]
+lib.ssd_paged_decode_step.restype = C.c_int
+lib.ssd_paged_evict_workspace_bytes.argtypes = [_pcfg, C.c_int]
+lib.ssd_paged_evict_workspace_bytes.restype = C.c_size_t
+lib.ssd_paged_evict.argtypes = [_pcfg] + [_vp] * 6 + [C.c_int, C.c_int] + [_vp] * 5 + [C.c_int, _vp, C.c_size_t, _vp]
+lib.ssd_paged_evict.restype = C.c_int
+lib.ssd_logits_process.argtypes = [_vp, C.c_int, C.c_int, C.c_int, C.c_int64, C.c_int, C.c_float, C.POINTER(SsdLogitsParams), _vp,
+                                   C.c_int64, _vp]
+lib.ssd_logits_process.restype = C.c_int
+
+
+def make_paged_config(B, H, H_kv, d, dtype, page_size, n_pages, max_blocks, softmax_scale=0.0, page_stride=0, head_stride=0,
+                      row_stride=0, q_stride=0, new_stride=0) -> SsdPagedConfig:
+    cfg = SsdPagedConfig()
+    cfg.n_seqs, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim = B, H, H_kv, d
+    cfg.dtype = _dtype_code(dtype)
+    cfg.page_size, cfg.n_pages, cfg.max_blocks, cfg.softmax_scale = page_size, n_pages, max_blocks, softmax_scale
+    cfg.page_stride, cfg.head_stride, cfg.row_stride = page_stride, head_stride, row_stride
+    cfg.q_stride, cfg.new_stride = q_stride, new_stride
+    return cfg
+
+
+def _strided(t) -> Optional[int]:
+    """Address of a tensor whose outer strides the config gives: rows alone have to be dense."""
+    if t is None or isinstance(t, int):
+        return t
+    assert t.stride(-1) == 1, "rows handed to the library must be dense"
+    return t.data_ptr()
+
+
+def _size(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def ssd_paged_append(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len, k_new, v_new, pos=None, weight=None, seq_pos=None,
+                     new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
+    """n_new: tokens in k_new; None: its first dimension."""
+    n = int(k_new.shape[0] if n_new is None else n_new)
+    _check(lib.ssd_paged_append(C.byref(cfg), _strided(k_pages), _strided(v_pages), _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len),
+                                _ptr(seq_pos), _strided(k_new), _strided(v_new), _ptr(new_start), n, _ptr(weight_new), _stream(stream)),
+           "ssd_paged_append")
+
+
+def ssd_paged_workspace_bytes(cfg: SsdPagedConfig, max_len: int = 0, with_weights: bool = False) -> int:
+    return lib.ssd_paged_workspace_bytes(C.byref(cfg), int(max_len), int(bool(with_weights)))
+
+
+def ssd_paged_decode_attn(cfg: SsdPagedConfig, q, k_pages, v_pages, block_table, seq_len, out, lse=None, weight_in=None, weight_out=None,
+                          max_len: int = 0, workspace=None, stream=None) -> None:
+    _check(lib.ssd_paged_decode_attn(C.byref(cfg), _strided(q), _strided(k_pages), _strided(v_pages), _ptr(weight_in), _ptr(weight_out),
+                                     _ptr(block_table), _ptr(seq_len), _ptr(out), _ptr(lse), int(max_len), _ptr(workspace), _size(workspace),
+                                     _stream(stream)), "ssd_paged_decode_attn")
+
+
+def ssd_paged_decode_step(cfg: SsdPagedConfig, q, k_new, v_new, k_pages, v_pages, block_table, seq_len, out, pos=None, seq_pos=None, lse=None,
+                          weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
+    _check(lib.ssd_paged_decode_step(C.byref(cfg), _strided(q), _strided(k_new), _strided(v_new), _strided(k_pages), _strided(v_pages),
+                                     _ptr(pos), _ptr(weight_in), _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(out),
+                                     _ptr(lse), int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_decode_step")
+
+
+def ssd_paged_evict_workspace_bytes(cfg: SsdPagedConfig, max_len: int = 0) -> int:
+    return lib.ssd_paged_evict_workspace_bytes(C.byref(cfg), int(max_len))
+
+
+def ssd_paged_evict(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len, budget, pos_in, pos_out, weight_in, weight_out, seq_len_out=None,
+                    n_sink: int = 0, recent: int = 0, seq_pos=None, max_len: int = 0, workspace=None, stream=None) -> None:
+    _check(lib.ssd_paged_evict(C.byref(cfg), _strided(k_pages), _strided(v_pages), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(budget),
+                               int(n_sink), int(recent), _ptr(pos_in), _ptr(pos_out), _ptr(weight_in), _ptr(weight_out), _ptr(seq_len_out),
+                               int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_evict")
+
+
+def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[float] = None, tokens=None, n_tokens=None, n_prompt=None,
+                       repetition=None, presence=None, frequency=None, temperature=None, bias=None, bias_shared: bool = False, mask=None,
+                       mask_shared: bool = False, logits_stride: int = 0, out_stride: int = 0, token_stride: Optional[int] = None,
+                       stream=None) -> None:
+    """gamma: guidance strength, None: no guidance.  bias [n_rows, V] and mask [n_rows, ceil(V / 32)], or one row of either for all
+    (bias_shared, mask_shared).  token_stride: places per row of tokens, None: its last dimension."""
+    p = SsdLogitsParams()
+    p.tokens, p.n_tokens, p.n_prompt = _ptr(tokens), _ptr(n_tokens), _ptr(n_prompt)
+    p.repetition, p.presence, p.frequency, p.temperature = _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(temperature)
+    p.bias, p.mask = _ptr(bias), _ptr(mask)
+    p.token_stride = int((0 if tokens is None else tokens.shape[-1]) if token_stride is None else token_stride)
+    p.bias_stride = 0 if bias_shared else int(V)
+    p.mask_stride = 0 if mask_shared else -(-int(V) // 32)
+    _check(lib.ssd_logits_process(_strided(logits), int(n_rows), int(V), _dtype_code(dtype), int(logits_stride), int(gamma is not None),
+                                  float(gamma or 0.0), C.byref(p), _strided(out), int(out_stride), _stream(stream)), "ssd_logits_process")

@@ -1,0 +1,63 @@
+// What the kernels of the paged cache share: the pool as they see it, slot to address, and the checks of a config.
+#pragma once
+
+#include "ssd_device.h"
+
+namespace ssd {
+
+// Everything a kernel needs to find a row.  Strides in bytes.
+struct PagedGeom {
+    int64_t page_stride, head_stride, row_stride;
+    const int32_t *block_table;
+    const int32_t *seq_len;
+    const int32_t *seq_pos;          // may be seq_len
+    int32_t n_seqs, n_kv, page_size, n_pages, max_blocks;
+    int32_t max_len;                 // min(caller's bound, max_blocks * page_size)
+    int32_t page_log2;               // log2 of page_size, or -1 where it is no power of two
+};
+
+static __device__ __forceinline__ int clamp_len(const PagedGeom &g, int b) {
+    const int n = g.seq_len[b];
+    return n < 0 ? 0 : n > g.max_len ? g.max_len : n;
+}
+
+// Block and place of a slot, by a shift where the page size allows it.
+static __device__ __forceinline__ void split_slot(const PagedGeom &g, int slot, int &block, int &place) {
+    if (g.page_log2 >= 0) {
+        block = slot >> g.page_log2;
+        place = slot & (g.page_size - 1);
+    } else {
+        block = (int)((unsigned)slot / (unsigned)g.page_size);
+        place = slot - block * g.page_size;
+    }
+}
+
+// The page a slot lies in, or -1 where the table names none.  slot < max_blocks * page_size.
+static __device__ __forceinline__ int page_of(const PagedGeom &g, int b, int block) {
+    const int p = g.block_table[(size_t)b * (size_t)g.max_blocks + (size_t)block];
+    return (unsigned)p < (unsigned)g.n_pages ? p : -1;
+}
+static __device__ __forceinline__ int64_t row_offset(const PagedGeom &g, int page, int kv, int place) {
+    return (int64_t)page * g.page_stride + (int64_t)kv * g.head_stride + (int64_t)place * g.row_stride;
+}
+static __device__ __forceinline__ int64_t table_index(const PagedGeom &g, int page, int kv, int place) {
+    return ((int64_t)page * g.n_kv + kv) * g.page_size + place;
+}
+
+// Checks of the config (with the error text set), then the geometry; max_len <= 0 selects the table's reach.
+int check_paged(const ssd_paged_config *c);
+PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, int max_len);
+int check_max_len(const ssd_paged_config *c, int max_len);
+static inline int paged_reach(const ssd_paged_config *c, int max_len) {
+    const int64_t all = (int64_t)c->max_blocks * c->page_size;
+    return max_len > 0 && max_len < all ? max_len : (int)all;
+}
+static inline size_t paged_esize(const ssd_paged_config *c) { return c->dtype == SSD_F32 ? 4 : 2; }
+static inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+// the launch behind ssd_paged_append, all arguments checked (ssd_paged_decode_step takes it too)
+int launch_paged_append(const ssd_paged_config *c, void *k_pages, void *v_pages, int32_t *pos, float *weight, const int32_t *block_table,
+                        const int32_t *seq_len, const int32_t *seq_pos, int max_len, const void *k_new, const void *v_new,
+                        const int32_t *new_start, int n_new, const float *weight_new, hipStream_t s);
+
+}  // namespace ssd

@@ -1,0 +1,460 @@
+"""GPU parity of the paged cache's calls against plain 64-bit implementations, through the C ABI."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2510_18716_amd as ssd
+from oracle import paged
+from paged_harness import TORCH, Batch, attend, check_attend
+
+pytestmark = pytest.mark.gpu
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("H,n_kv", [(2, 2), (8, 2), (3, 1)])
+def test_attention_at_the_edges_of_tiles(dtype, d, H, n_kv):
+    say("edges", dtype, d, H, n_kv)
+    bt = Batch(EDGES, H, n_kv, d, dtype, 16, seed=d + H)
+    check_attend(bt, attend(bt))
+
+
+@pytest.mark.parametrize("H,n_kv", [(1, 1), (2, 1), (5, 1), (7, 1), (16, 2), (16, 1), (17, 1), (24, 1), (40, 1), (32, 32), (64, 2)])
+def test_groups_of_query_heads(H, n_kv):
+    for dtype, d in (("bf16", 128), ("f32", 64)):
+        say("group", H, n_kv, dtype, d)
+        bt = Batch([70, 5, 0, 131], H, n_kv, d, dtype, 32, seed=H)
+        check_attend(bt, attend(bt))
+
+
+@pytest.mark.parametrize("page", [1, 3, 7, 8, 16, 24, 48, 64, 100, 256])
+@pytest.mark.parametrize("layout", ["heads", "rows", "both", "wide"])
+def test_pages_and_strides(page, layout):
+    for dtype, d in (("bf16", 128), ("f32", 128), ("bf16", 64)):
+        say("pages", page, layout, dtype, d)
+        bt = Batch([100, 1, 37, 0, 258], 4, 2, d, dtype, page, seed=page, layout=layout, q_gap=64)
+        check_attend(bt, attend(bt))
+
+
+@pytest.mark.parametrize("dtype,d,H,n_kv", [("bf16", 128, 8, 2), ("f32", 64, 4, 4), ("bf16", 64, 2, 2), ("f32", 128, 8, 1)])
+def test_long_rows_are_split_and_joined(dtype, d, H, n_kv):
+    say("long", dtype, d, H, n_kv)
+    bt = Batch([2500, 3, 1023, 0, 1537], H, n_kv, d, dtype, 16, seed=7, qs=2.0)
+    check_attend(bt, attend(bt))
+    check_attend(bt, attend(bt, weights=False, lse=False), weights=False)
+
+
+def test_many_sequences_of_one_head_and_few_rows():
+    bt = Batch([(i * 7) % 50 for i in range(300)], 1, 1, 64, "bf16", 8, seed=3)
+    check_attend(bt, attend(bt))
+
+
+def test_one_long_sequence_of_one_head():
+    bt = Batch([9001], 1, 1, 64, "bf16", 64, seed=4)
+    check_attend(bt, attend(bt))
+
+
+def test_max_len_cuts_and_a_length_below_zero_is_none():
+    bt = Batch([96, 33, 64, 10], 4, 2, 128, "bf16", 16, seed=5)
+    bt.lend = torch.tensor([96, 33, 64, -5], dtype=torch.int32, device="cuda")
+    got = attend(bt, max_len=40)
+    check_attend(bt, got, max_len=40, lens=[96, 33, 64, 0])
+    bt.lend = torch.tensor([1 << 30, 33, 64, 10], dtype=torch.int32, device="cuda")      # the table's reach bounds it: blocks named -1 count as masked
+    check_attend(bt, attend(bt), lens=[bt.max_blocks * 16, 33, 64, 10])
+
+
+def test_blocks_that_name_no_page_count_as_masked():
+    for dtype in ("bf16", "f32"):
+        bt = Batch([100, 40, 48, 300], 4, 2, 64, dtype, 16, seed=6)
+        bt.table[0, 2] = -1
+        bt.table[1, :] = bt.n_pages
+        bt.table[2, 0], bt.table[2, 2] = 1 << 30, -(1 << 31)
+        bt.table[3, 3:19] = -5
+        bt.tabled = torch.from_numpy(bt.table).cuda()
+        check_attend(bt, attend(bt))
+
+
+def test_a_page_read_by_two_sequences():
+    bt = Batch([64, 64], 4, 2, 128, "bf16", 16, seed=8)
+    bt.table[1, :2] = bt.table[0, :2]
+    bt.tabled = torch.from_numpy(bt.table).cuda()
+    check_attend(bt, attend(bt, weights=False), weights=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_of_any_size(dtype):
+    """Queries so large that one row takes everything, late rows above all earlier ones, all logits far below zero, a scale of the
+    caller's."""
+    n = 400
+    bt = Batch([n, n, n, 40], 2, 1, 64, dtype, 16, seed=9)
+    ramp = torch.linspace(-1, 1, n)
+    for b, (f, sign) in enumerate([(200.0, 1), (60.0, -1), (30.0, 1)]):
+        bt.q[b] = torch.tensor([f] + [0.0] * 63).to(TORCH[dtype])
+        for j in range(n):
+            x = ramp[j] * sign - (3.0 if b == 2 else 0.0)
+            bt.k[bt.table[b, j // 16], :, j % 16, 0] = x.to(TORCH[dtype])
+    bt.kd, bt.qd = bt.k.cuda(), bt.q.cuda()
+    check_attend(bt, attend(bt))
+    bt.cfg.softmax_scale = 0.7
+    check_attend(bt, attend(bt), scale=0.7)
+
+
+def test_a_sequence_whose_logits_are_no_numbers_keeps_them_to_itself():
+    bt = Batch([50, 50, 50], 4, 2, 64, "bf16", 16, seed=10)
+    clean = attend(bt)
+    bt.kd[int(bt.table[1, 1]), 0, 3, 0] = float("nan")
+    bt.kd[int(bt.table[1, 2]), 1, 3, 0] = float("inf")
+    out, lse, w = attend(bt)
+    assert torch.isnan(out[1, :2].float()).all() and torch.isnan(lse[1, :2]).all()
+    for b in (0, 2):
+        assert torch.equal(out[b], clean[0][b]) and torch.equal(lse[b], clean[1][b])
+
+
+def test_results_do_not_change_from_call_to_call():
+    bt = Batch([700, 3, 90, 2000], 8, 2, 128, "bf16", 16, seed=11)
+    a, b = attend(bt), attend(bt)
+    for x, y in zip(a, b):
+        assert torch.equal(x.nan_to_num(9.0), y.nan_to_num(9.0))
+
+
+def test_weights_may_be_updated_in_place():
+    bt = Batch([300, 20], 4, 2, 64, "f32", 16, seed=12)
+    ref = attend(bt)
+    w = bt.weight.cuda()
+    out = torch.empty_like(ref[0])
+    ws = bt.scratch(ssd.ssd_paged_workspace_bytes(bt.cfg, 0, True))
+    ssd.ssd_paged_decode_attn(bt.cfg, bt.qd, bt.kd, bt.vd, bt.tabled, bt.lend, out, weight_in=w, weight_out=w, workspace=ws)
+    got = ref[2]
+    held = got != -3.0
+    assert torch.equal(w[held], got[held]) and torch.equal(out, ref[0])
+
+
+def test_rows_beyond_four_gigabytes():
+    """A pool of more than 2^32 bytes and 2^31 elements: the last pages are read and written where they are."""
+    d, page, n_kv = 128, 64, 1
+    n_pages = (9 << 30) // (page * d * 4)
+    k = torch.zeros((n_pages, n_kv, page, d), device="cuda")
+    bt = Batch([130, 70], 1, n_kv, d, "f32", page, seed=13)
+    small_k, small_v, small_table = bt.kd, bt.vd, bt.tabled
+    v = torch.zeros_like(k)
+    for p in range(bt.n_pages):
+        k[n_pages - 1 - p], v[n_pages - 1 - p] = small_k[p], small_v[p]
+    table = torch.where(small_table >= 0, n_pages - 1 - small_table, small_table).contiguous()
+    cfg = ssd.make_paged_config(2, 1, n_kv, d, "f32", page, n_pages, bt.max_blocks)
+    out, ref = torch.zeros((2, 1, d), device="cuda"), attend(bt, weights=False)
+    ws = bt.scratch(ssd.ssd_paged_workspace_bytes(cfg, 0, False))
+    ssd.ssd_paged_decode_attn(cfg, bt.qd, k, v, table, bt.lend, out, workspace=ws)
+    assert torch.equal(out, ref[0])
+    new = torch.randn((2, n_kv, d), device="cuda")
+    ssd.ssd_paged_append(cfg, k, v, table, bt.lend, new, -new)
+    for b, n in enumerate(bt.lens):
+        at = int(table[b, (n - 1) // page])
+        assert torch.equal(k[at, 0, (n - 1) % page], new[b, 0]) and torch.equal(v[at, 0, (n - 1) % page], -new[b, 0])
+
+
+# ---- append, step -------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("layout", ["heads", "rows", "both", "wide"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("bf16", 64), ("f32", 128)])
+def test_append_of_ragged_prompts(layout, dtype, d):
+    lens, new = [40, 0, 17, 1, 100, 6], [40, 0, 5, 1, 33, 0]
+    for page in (16, 7):
+        say("append", layout, dtype, d, page)
+        bt = Batch(lens, 3, 3, d, dtype, page, seed=page, layout=layout)
+        g = torch.Generator().manual_seed(1)
+        total = sum(new)
+        big = torch.randn((total, 2, 3 * d + 32), generator=g).to(TORCH[dtype])
+        start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        seq_pos = np.array(lens) + 9
+        wn = torch.rand((total, 3), generator=g)
+        bigd = big.cuda()
+        bt.cfg.new_stride = 2 * (3 * d + 32)
+        pos, weight = bt.pos.cuda(), bt.weight.cuda()
+        ssd.ssd_paged_append(bt.cfg, bt.kd, bt.vd, bt.tabled, bt.lend, bigd[:, 0], bigd[:, 1], pos=pos, weight=weight,
+                             seq_pos=torch.from_numpy(seq_pos.astype(np.int32)).cuda(), new_start=torch.from_numpy(start).cuda(), weight_new=wn.cuda())
+        k, v, rp, rw = bt.k.float().numpy(), bt.v.float().numpy(), bt.pos.numpy().copy(), bt.weight.numpy().copy()
+        kn, vn = (big[:, i, :3 * d].float().numpy().reshape(total, 3, d) for i in (0, 1))
+        paged.paged_append(k, v, rp, rw, bt.table, lens, seq_pos, kn, vn, start, wn.numpy())
+        np.testing.assert_array_equal(bt.kd.float().cpu().numpy(), k)
+        np.testing.assert_array_equal(bt.vd.float().cpu().numpy(), v)
+        np.testing.assert_array_equal(pos.cpu().numpy(), rp)
+        np.testing.assert_array_equal(weight.cpu().numpy(), rw)
+
+
+def test_append_leaves_out_what_has_no_place():
+    """Lengths beyond the table, tokens before slot 0, blocks that name no page; tables that are not wanted."""
+    bt = Batch([20, 5, 16, 0], 2, 2, 64, "f32", 8, seed=2)
+    bt.table[2, 1] = bt.n_pages + 3
+    lens = [1000, 2, 16, 0]
+    new = [3, 5, 4, 2]
+    start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    kn = torch.randn((14, 2, 64))
+    k, v = bt.k.numpy().copy(), bt.v.numpy().copy()
+    paged.paged_append(k, v, None, None, bt.table, lens, lens, kn.numpy(), -kn.numpy(), start, None)
+    ssd.ssd_paged_append(bt.cfg, bt.kd, bt.vd, torch.from_numpy(bt.table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), kn.cuda(), -kn.cuda(),
+                         new_start=torch.from_numpy(start).cuda())
+    np.testing.assert_array_equal(bt.kd.cpu().numpy(), k)
+    np.testing.assert_array_equal(bt.vd.cpu().numpy(), v)
+
+
+def test_append_of_many_tokens_and_sequences():
+    """More tokens than a grid dimension holds."""
+    lens = [1] * 3000 + [67000]
+    d, page = 64, 64
+    n_pages = 3000 + 1048
+    table = torch.full((3001, 1048), -1, dtype=torch.int32)
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(3)).to(torch.int32)
+    table[:3000, 0] = order[:3000]
+    table[3000, :1047] = order[3000:4047]
+    total = sum(lens)
+    kn = torch.arange(total, dtype=torch.float32, device="cuda")[:, None, None].expand(total, 1, d).contiguous()
+    k = torch.full((n_pages, 1, page, d), -1.0, device="cuda")
+    v = k.clone()
+    cfg = ssd.make_paged_config(3001, 1, 1, d, "f32", page, n_pages, 1048)
+    start = torch.from_numpy(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)).cuda()
+    pos = torch.full((n_pages, 1, page), -1, dtype=torch.int32, device="cuda")
+    ssd.ssd_paged_append(cfg, k, v, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), kn, kn + 0.5, pos=pos, new_start=start)
+    first = table[:3000, 0].long().cuda()
+    assert torch.equal(k[first, 0, 0, 5], torch.arange(3000, device="cuda").float()) and bool((k[first, 0, 1:] == -1).all())
+    rest = table[3000, :1047].long().cuda()
+    got = v[rest, 0].reshape(-1, d)[:67000]
+    assert torch.equal(got[:, 63], torch.arange(3000, 70000, device="cuda") + 0.5)
+    assert torch.equal(pos[rest, 0].reshape(-1)[:67000], torch.arange(67000, device="cuda", dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype,d,H,n_kv,page", [("bf16", 128, 8, 2, 16), ("f32", 64, 3, 3, 7), ("bf16", 64, 16, 1, 64), ("f32", 128, 6, 2, 32)])
+def test_step_is_append_and_attention(dtype, d, H, n_kv, page):
+    lens = [1, 0, 16, 17, 65, 300, 2, 1200]
+    for layout, weights in (("heads", True), ("rows", True), ("both", False)):
+        say("step", dtype, d, H, n_kv, page, layout)
+        bt = Batch(lens, H, n_kv, d, dtype, page, seed=H, layout=layout)
+        g = torch.Generator().manual_seed(4)
+        big = torch.randn((len(lens), 2, n_kv * d + 64), generator=g).to(TORCH[dtype]).cuda()
+        bt.cfg.new_stride = 2 * (n_kv * d + 64)
+        seq_pos = bt.lend + 5
+        out = torch.empty((len(lens), H, d), dtype=TORCH[dtype], device="cuda")
+        lse = torch.empty((len(lens), H), device="cuda")
+        pos, w_in = bt.pos.cuda(), bt.weight.cuda()
+        w_out = torch.full_like(w_in, -3.0)
+        ws = bt.scratch(ssd.ssd_paged_workspace_bytes(bt.cfg, 0, weights))
+        for b, n in enumerate(lens):          # what weight_in holds at the new token's place is not read
+            if n:
+                w_in[int(bt.table[b, (n - 1) // page]), :, (n - 1) % page] = float("nan")
+        more = dict(weight_in=w_in, weight_out=w_out) if weights else {}
+        ssd.ssd_paged_decode_step(bt.cfg, bt.qd, big[:, 0], big[:, 1], bt.kd, bt.vd, bt.tabled, bt.lend, out, pos=pos, seq_pos=seq_pos, lse=lse,
+                                  workspace=ws, **more)
+        # the rows and positions by the plain implementation
+        rk, rv, rp, rw = bt.k.float().numpy(), bt.v.float().numpy(), bt.pos.numpy().copy(), bt.weight.numpy().copy()
+        kn, vn = (big[:, i, :n_kv * d].float().cpu().numpy().reshape(-1, n_kv, d) for i in (0, 1))
+        paged.paged_append(rk, rv, rp, rw, bt.table, lens, seq_pos.tolist(), kn, vn, None, None)
+        np.testing.assert_array_equal(bt.kd.float().cpu().numpy(), rk)
+        np.testing.assert_array_equal(bt.vd.float().cpu().numpy(), rv)
+        np.testing.assert_array_equal(pos.cpu().numpy(), rp)
+        bt.k, bt.v = torch.from_numpy(rk).to(TORCH[dtype]), torch.from_numpy(rv).to(TORCH[dtype])
+        check_attend(bt, (out, lse, w_out if weights else None), weight_before=torch.from_numpy(rw))
+
+
+# ---- eviction -----------------------------------------------------------------------------------------------------
+
+def _evict_case(lens, budgets, n_kv, d, dtype, page, sink, recent, seed, layout="heads", in_place=False, weight_of=None, pos_of=None, max_len=0, more=0):
+    say("evict", lens, budgets, n_kv, d, dtype, page, sink, recent, seed, layout, in_place)
+    bt = Batch(lens, n_kv, n_kv, d, dtype, page, seed=seed, layout=layout)
+    rng = np.random.default_rng(seed)
+    seq_pos = [n + more for n in lens]
+    for b, n in enumerate(lens):
+        for kv in range(n_kv):
+            p = np.arange(n) if pos_of is None else pos_of(rng, n, seq_pos[b])
+            w = rng.random(n).astype(np.float32) if weight_of is None else weight_of(rng, n)
+            for j in range(n):
+                bt.pos[bt.table[b, j // page], kv, j % page] = int(p[j])
+                bt.weight[bt.table[b, j // page], kv, j % page] = float(w[j])
+    pos, weight = bt.pos.cuda(), bt.weight.cuda()
+    pos_out = pos if in_place else torch.full_like(pos, -9)
+    weight_out = weight if in_place else torch.full_like(weight, -3.0)
+    len_out = torch.full_like(bt.lend, -1)
+    ws = bt.scratch(ssd.ssd_paged_evict_workspace_bytes(bt.cfg, max_len))
+    ssd.ssd_paged_evict(bt.cfg, bt.kd, bt.vd, bt.tabled, bt.lend, torch.tensor(budgets, dtype=torch.int32, device="cuda"), pos, pos_out, weight,
+                        weight_out, len_out, n_sink=sink, recent=recent, seq_pos=torch.tensor(seq_pos, dtype=torch.int32, device="cuda"),
+                        max_len=max_len, workspace=ws)
+    rk, rv = bt.k.float().numpy().copy(), bt.v.float().numpy().copy()
+    rp, rw = (bt.pos.numpy().copy(), bt.weight.numpy().copy()) if in_place else (np.full(pos.shape, -9, np.int32), np.full(pos.shape, -3.0, np.float32))
+    stays = []
+    for b, n in enumerate(lens):
+        n = min(n, max_len) if max_len else n
+        places = [paged.slot_place(bt.table[b], j, page) for j in range(n)]
+        stay = min(n, max(0, budgets[b]))
+        for kv in range(n_kv):
+            p = np.array([bt.pos[i, kv, j] for i, j in places])
+            w = np.array([bt.weight[i, kv, j] for i, j in places], dtype=np.float32)
+            stay, moves = paged.evict_moves(p, w, seq_pos[b], budgets[b], sink, recent)
+            source = list(range(stay))
+            for to, at in moves:
+                source[to] = at
+            for to, at in enumerate(source):
+                (ti, tj), (fi, fj) = places[to], places[at]
+                rk[ti, kv, tj], rv[ti, kv, tj] = bt.k[fi, kv, fj].float().numpy(), bt.v[fi, kv, fj].float().numpy()
+                rp[ti, kv, tj], rw[ti, kv, tj] = p[at], w[at]
+        stays.append(stay)
+    assert len_out.tolist() == stays
+    np.testing.assert_array_equal(pos_out.cpu().numpy(), rp)
+    np.testing.assert_array_equal(weight_out.cpu().numpy(), rw)
+    np.testing.assert_array_equal(bt.kd.float().cpu().numpy(), rk)
+    np.testing.assert_array_equal(bt.vd.float().cpu().numpy(), rv)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype,d,layout", [("bf16", 128, "heads"), ("f32", 64, "rows"), ("bf16", 64, "both"), ("f32", 128, "wide")])
+def test_eviction_of_unequal_lengths(dtype, d, layout, in_place):
+    _evict_case([100, 0, 1, 33, 250, 64, 65, 64], [40, 5, 1, 32, 17, 64, 64, 0], 3, d, dtype, 16, 2, 5, 1, layout, in_place)
+    _evict_case([700, 30], [699, -1], 2, d, dtype, 7, 0, 0, 2, layout, in_place, more=11)
+
+
+@pytest.mark.parametrize("n,m", [(2, 1), (64, 63), (65, 64), (129, 128), (129, 127), (257, 250), (1025, 1024), (1030, 3), (1500, 700), (2100, 2099), (5000, 1200)])
+def test_eviction_at_sizes_of_its_passes(n, m):
+    _evict_case([n, n // 2 + 1], [m, m], 2, 64, "bf16", 16, 1, 8, n)
+
+
+@pytest.mark.parametrize("name", ["zeros", "steps", "close", "signs", "huge"])
+def test_eviction_with_ties_and_unusual_weights(name):
+    def weight_of(rng, n):
+        if name == "zeros":
+            return np.zeros(n, np.float32)
+        if name == "steps":
+            return rng.integers(0, 4, n).astype(np.float32)
+        if name == "close":                                       # neighbours among the representable numbers
+            return (np.float32(1.0).view(np.int32) + rng.integers(0, 50, n)).astype(np.int32).view(np.float32)
+        if name == "signs":
+            return np.where(rng.random(n) < 0.3, np.float32(-0.0), rng.standard_normal(n).astype(np.float32) * (rng.random(n) < 0.7))
+        w = rng.choice(np.array([np.inf, -np.inf, np.nan, 3e38, 1e-45, 0.0, 1.0], np.float32), n)
+        return w.astype(np.float32)
+
+    def pos_of(rng, n, total):
+        return rng.permutation(total)[:n]
+    _evict_case([200, 600, 1300], [90, 599, 100], 2, 64, "f32", 16, 1, 3, 5, weight_of=weight_of)
+    _evict_case([200, 600, 1300], [90, 301, 1299], 2, 64, "f32", 16, 1, 3, 6, weight_of=weight_of, pos_of=pos_of, more=50)
+
+
+def test_eviction_where_more_is_protected_than_stays():
+    _evict_case([100, 100, 100, 50], [10, 20, 21, 3], 2, 64, "f32", 8, 4, 16, 7)
+    _evict_case([100, 100], [10, 99], 2, 64, "f32", 8, 0, 1000, 8)
+
+
+def test_eviction_with_positions_held_twice_goes_by_slot():
+    _evict_case([150, 40], [70, 10], 2, 64, "bf16", 16, 0, 0, 9, weight_of=lambda r, n: np.ones(n, np.float32), pos_of=lambda r, n, t: np.full(n, 3))
+
+
+def test_eviction_below_max_len():
+    _evict_case([100, 30], [20, 20], 2, 64, "bf16", 16, 1, 4, 10, max_len=50)
+
+
+def test_eviction_of_a_long_sequence():
+    """Selection over 40000 rows, exactly, by the tables alone (rows that carry their own slot)."""
+    n, m, page, n_kv, d = 40000, 6000, 64, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    blocks = n // page
+    table = torch.randperm(blocks, device="cuda", generator=g).to(torch.int32)[None].contiguous()
+    k = torch.zeros((blocks, n_kv, page, d), device="cuda")
+    slot = torch.arange(n, device="cuda").reshape(blocks, page)
+    k[table[0].long()] = slot[:, None, :, None].float().expand(blocks, n_kv, page, d)
+    v = k + 0.5
+    weight = torch.rand((blocks, n_kv, page), device="cuda", generator=g)
+    weight[weight < 0.3] = 0.0
+    pos = torch.zeros((blocks, n_kv, page), dtype=torch.int32, device="cuda")
+    pos[table[0].long()] = slot[:, None].to(torch.int32).expand(blocks, n_kv, page)
+    cfg = ssd.make_paged_config(1, n_kv, n_kv, d, "f32", page, blocks, blocks)
+    ws = torch.empty(ssd.ssd_paged_evict_workspace_bytes(cfg, 0), dtype=torch.uint8, device="cuda")
+    w_slot = weight[table[0].long()].transpose(0, 1).reshape(n_kv, n).cpu().numpy()
+    ln = torch.zeros(1, dtype=torch.int32, device="cuda")
+    one = torch.tensor([n], dtype=torch.int32, device="cuda")
+    for budget in (m, n - 1, 30000):
+        kk, vv, pp, ww = k.clone(), v.clone(), torch.full_like(pos, -9), torch.zeros_like(weight)
+        ssd.ssd_paged_evict(cfg, kk, vv, table, one, torch.tensor([budget], dtype=torch.int32, device="cuda"), pos, pp, weight, ww, ln, n_sink=2, recent=100,
+                            workspace=ws)
+        for kv in range(n_kv):
+            w = w_slot[kv].astype(np.float64)
+            w[:2] = w[-100:] = np.inf
+            kept = np.lexsort((np.arange(n), -w))[:budget]
+            src = np.arange(budget)
+            src[~np.isin(src, kept)] = np.sort(kept[kept >= budget])
+            got = pp[table[0].long()].transpose(0, 1).reshape(n_kv, n)[kv, :budget].cpu().numpy()
+            np.testing.assert_array_equal(got, src)
+            rows = kk[table[0].long()].transpose(0, 1).reshape(n_kv, n, d)[kv, :budget]
+            assert torch.equal(rows, torch.from_numpy(src).cuda().float()[:, None].expand(budget, d))
+            rows = vv[table[0].long()].transpose(0, 1).reshape(n_kv, n, d)[kv, :budget]
+            assert torch.equal(rows, torch.from_numpy(src).cuda().float()[:, None].expand(budget, d) + 0.5)
+        assert ln.tolist() == [budget]
+
+
+# ---- streams, graphs ------------------------------------------------------------------------------------------------
+
+def test_calls_run_on_the_stream_they_are_given():
+    bt = Batch([300, 40, 0], 8, 2, 128, "bf16", 16, seed=14)
+    ref = attend(bt)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    big = torch.randn((4096, 4096), device="cuda")
+    q = bt.qd.clone()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(4):
+            big = big @ big * 1e-2                      # the stream is busy when the call comes
+        bt.qd = q * 1
+        got = attend(bt)
+    s.synchronize()
+    for x, y in zip(ref, got):
+        assert torch.equal(x.nan_to_num(9.0), y.nan_to_num(9.0))
+
+
+def test_a_step_in_a_graph_follows_the_lengths_on_the_device():
+    """Captured once, replayed while sequences grow: lengths, positions and the table are read when the kernels run."""
+    lens = [30, 5, 0]
+    bt = Batch([64, 64, 64], 4, 2, 64, "f32", 16, seed=15)
+    bt.lend.copy_(torch.tensor(lens, dtype=torch.int32))
+    q = torch.zeros((3, 4, 64), device="cuda")
+    kn, vn = (torch.zeros((3, 2, 64), device="cuda") for _ in range(2))
+    out, pos, w = torch.zeros_like(q), bt.pos.cuda(), bt.weight.cuda()
+    budget = torch.tensor([36, 8, 100], dtype=torch.int32, device="cuda")
+    after = torch.zeros_like(bt.lend)
+    ws = torch.empty(ssd.ssd_paged_workspace_bytes(bt.cfg, 64, True), dtype=torch.uint8, device="cuda")
+    we = torch.empty(ssd.ssd_paged_evict_workspace_bytes(bt.cfg, 64), dtype=torch.uint8, device="cuda")
+    seq_pos = bt.lend.clone()
+
+    def step(k, v, pos, w, out, length, total, after):
+        length += 1
+        total += 1
+        ssd.ssd_paged_decode_step(bt.cfg, q, kn, vn, k, v, bt.tabled, length, out, pos=pos, seq_pos=total, weight_in=w, weight_out=w, max_len=64, workspace=ws)
+        ssd.ssd_paged_evict(bt.cfg, k, v, bt.tabled, length, budget, pos, pos, w, w, after, n_sink=1, recent=2, seq_pos=total, max_len=64, workspace=we)
+        length.copy_(after)
+
+    eager = [x.clone() for x in (bt.kd, bt.vd, pos, w, out, bt.lend, seq_pos, after)]
+    inputs = [bt.kd, bt.vd, pos, w, out, bt.lend, seq_pos, after]
+    keep = [x.clone() for x in inputs]
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*inputs)                                   # once outside, so that capture meets nothing for the first time
+    torch.cuda.current_stream().wait_stream(side)
+    for x, y in zip(inputs, keep):
+        x.copy_(y)
+    with torch.cuda.graph(graph):
+        step(*inputs)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    for i in range(12):
+        for x in (q, kn, vn):
+            x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        graph.replay()
+        torch.cuda.synchronize()
+        step(*eager)
+        torch.cuda.synchronize()
+        for x, y in zip(inputs, eager):
+            assert torch.equal(x.nan_to_num(5.0) if x.is_floating_point() else x, y.nan_to_num(5.0) if y.is_floating_point() else y), i
+    assert bt.lend.tolist() == [36, 8, 12] and seq_pos.tolist() == [42, 17, 12]
