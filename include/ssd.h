@@ -421,7 +421,7 @@ typedef struct ssd_paged_config {
     int32_t n_kv_heads;    /* key / value heads: 1..1024                                    */
     int32_t head_dim;      /* d: 64 or 128                                                 */
     int32_t dtype;         /* ssd_dtype of q, k, v, the pool and the output                */
-    int32_t page_size;     /* places per page: 1..65536                                    */
+    int32_t page_size;     /* places per page: 1..32768                                    */
     int32_t n_pages;       /* pages of the pool: >= 1                                      */
     int32_t max_blocks;    /* columns of block_table: >= 1, max_blocks * page_size <= 2^30 */
     float   softmax_scale; /* 0 selects 1/sqrt(d)                                          */

@@ -16,7 +16,7 @@ int check_paged(const ssd_paged_config *c) {
         return fail(SSD_ERR_INVALID_ARG, "n_heads=%d must be a multiple of n_kv_heads=%d, at most 1024", c->n_heads, c->n_kv_heads);
     if (c->head_dim != 64 && c->head_dim != 128) return fail(SSD_ERR_INVALID_ARG, "head_dim=%d, supported: 64, 128", c->head_dim);
     if (c->dtype != SSD_F32 && c->dtype != SSD_BF16) return fail(SSD_ERR_INVALID_ARG, "dtype=%d is neither SSD_F32 nor SSD_BF16", c->dtype);
-    if (c->page_size < 1 || c->page_size > 65536) return fail(SSD_ERR_INVALID_ARG, "page_size=%d outside 1..65536", c->page_size);
+    if (c->page_size < 1 || c->page_size > 32768) return fail(SSD_ERR_INVALID_ARG, "page_size=%d outside 1..32768", c->page_size);
     if (c->n_pages < 1) return fail(SSD_ERR_INVALID_ARG, "n_pages=%d must be >= 1", c->n_pages);
     if (c->max_blocks < 1 || (int64_t)c->max_blocks * c->page_size > (1ll << 30))
         return fail(SSD_ERR_INVALID_ARG, "max_blocks=%d must be >= 1, with max_blocks * page_size at most 2^30", c->max_blocks);
