@@ -41,22 +41,23 @@ struct PagedAttnArgs {
     int n_heads, group, q_tiles;
     int chunk, n_split;
     int whole;                // every sequence is one chunk and every group one tile: this launch writes the outputs
-    uint32_t page_magic;      // ceil(2^32 / page_size)
+    uint32_t page_magic, single;   // ceil(2^32 / page_size) and 0, or 0 and 1 where that is 2^32
     float scale;              // softmax scale * log2 e
 };
 
 static constexpr int WAVES = 4;
 static constexpr int CHUNK_MAX = 1024;
 static constexpr int HEADS = 16;                                   // heads of a tile
+static constexpr int64_t NO_PAGE = -(1ll << 62);
 static constexpr float LN2 = 0.6931471805599453f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // block of a row: x / page_size for x < 2^16 (a chunk's rows and what lies before them in its first page), page_size <= 2^15:
-// the rounded-up reciprocal is exact while x * page_size < 2^32
+// the rounded-up reciprocal is exact while x * page_size < 2^32.  For pages of one row it is 0 and `single` 1.
 static __device__ __forceinline__ int block_of(const PagedAttnArgs &a, int x) {
-    return a.g.page_log2 >= 0 ? x >> a.g.page_log2 : (int)__umulhi((uint32_t)x, a.page_magic);
+    return (int)(__umulhi((uint32_t)x, a.page_magic) + __umul24((uint32_t)x, a.single));
 }
 
 // Where a lane finds its rows of a tile.  K: rows lane % 16 (and + 16); V and the logits: rows 4 g .. 4 g + 3 (and + 16), g = lane / 16.
@@ -70,39 +71,50 @@ template <bool BF16, bool QUADS> struct TileRows {
     uint32_t there;                                                // bit 4 t + i: row 16 t + 4 g + i
 };
 
-// One row's byte offset in the pool, -1 if it does not exist.  x: row of the chunk.
+// One row's byte offset in the pool, negative if it does not exist.  x: row of the chunk.
 static __device__ __forceinline__ int64_t row_at(const PagedAttnArgs &a, const int64_t *pages, int lead, int rows, int x) {
-    const int y = x < rows ? x : rows - 1;
-    const int block = block_of(a, y + lead), place = y + lead - block * a.g.page_size;
-    const int64_t base = pages[block];
-    return base < 0 ? -1 : base + (int64_t)place * a.g.row_stride;
+    const int y = (x < rows ? x : rows - 1) + lead;
+    const int block = block_of(a, y), place = y - block * a.g.page_size;
+    return pages[block] + (int64_t)place * a.g.row_stride;         // a block without a page: NO_PAGE, far below zero
 }
 
 template <bool BF16, bool QUADS>
-static __device__ __forceinline__ void find_rows(const PagedAttnArgs &a, const int64_t *pages, int lead, int rows, int first, int lane,
-                                                 TileRows<BF16, QUADS> &t) {
-    const int r = lane & 15, g = lane >> 4;
+static __device__ __forceinline__ void find_k(const PagedAttnArgs &a, const int64_t *pages, int lead, int rows, int first, int lane,
+                                              TileRows<BF16, QUADS> &t) {
+#pragma unroll
+    for (int s = 0; s < TileRows<BF16, QUADS>::SUB; ++s) {
+        const int64_t k = row_at(a, pages, lead, rows, first + 16 * s + (lane & 15));
+        t.k[s] = k < 0 ? 0 : k;
+    }
+}
+
+template <bool BF16, bool QUADS>
+static __device__ __forceinline__ void find_v(const PagedAttnArgs &a, const int64_t *pages, int lead, int rows, int first, int lane,
+                                              TileRows<BF16, QUADS> &t) {
     t.there = 0;
 #pragma unroll
     for (int s = 0; s < TileRows<BF16, QUADS>::SUB; ++s) {
-        const int64_t k = row_at(a, pages, lead, rows, first + 16 * s + r);
-        t.k[s] = k < 0 ? 0 : k;
-        const int x = first + 16 * s + 4 * g;
+        const int x = first + 16 * s + 4 * (lane >> 4);
         if constexpr (QUADS) {                                     // the chunk's first row and the page size are multiples of four
             const int64_t v = row_at(a, pages, lead, rows, x < rows ? x : (rows - 1) & ~3);
             t.v[s] = v < 0 ? 0 : v;
-            const int left = rows - x;
-            if (v >= 0 && left > 0) t.there |= (left >= 4 ? 15u : (1u << left) - 1u) << (4 * s);
+            const int left = v < 0 ? 0 : rows - x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.there |= i < left ? 1u << (4 * s + i) : 0u;
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int64_t v = row_at(a, pages, lead, rows, x + i);
                 t.v[4 * s + i] = v < 0 ? 0 : v;
-                if (v >= 0 && x + i < rows) t.there |= 1u << (4 * s + i);
+                t.there |= v >= 0 && x + i < rows ? 1u << (4 * s + i) : 0u;
             }
         }
     }
 }
+
+// Makes an address wait for a result, for the compiler: requests that it moves up across the products that still read the registers they
+// are to fill need a second set of them, which then goes to scratch memory (attn over 290000 rows 0.2 -> 0.54 ms).
+static __device__ __forceinline__ void after(int64_t &address, float result) { asm volatile("" : "+v"(address) : "v"(result)); }
 
 // ---- a tile's operands and products, by element type --------------------------------------------------------------
 
@@ -214,7 +226,7 @@ template <typename T> static __device__ __forceinline__ void store_out(char *out
 }
 
 // grid = (chunks, kv heads * tiles of query heads, sequences)
-template <typename T, int D, bool QUADS, bool STEP>
+template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS>
 __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs a) {
     typedef Tile<T, D> TT;
     constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
@@ -243,7 +255,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     const int blocks = block_of(a, rows - 1 + lead) + 1;
     for (int i = threadIdx.x; i < blocks; i += 64 * WAVES) {
         const int page = page_of(a.g, b, block0 + i);
-        pages[i] = page < 0 ? -1 : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
+        pages[i] = page < 0 ? NO_PAGE : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
     }
     typename TT::Q q;
     TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (r < heads ? r : 0)) * (D * sizeof(T)), lane, q);
@@ -282,26 +294,24 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         }
     };
     const int tiles = (rows + TT::ROWS - 1) / TT::ROWS;
-    float *zrow = a.z ? a.z + ((int64_t)b * a.n_heads + head0 + (r < heads ? r : 0)) * a.z_stride + row0 : nullptr;
-    if (wave < tiles) {
-        find_rows(a, pages, lead, rows, wave * TT::ROWS, lane, at);
-        request_k(wave * TT::ROWS);
-        request_v(wave * TT::ROWS);
-    }
-    for (int i = wave; i < tiles; i += WAVES) {
-        const int first = i * TT::ROWS, next = first + WAVES * TT::ROWS;
-        const bool more = i + WAVES < tiles;
+    float *zrow = WEIGHTS ? a.z + ((int64_t)b * a.n_heads + head0 + (r < heads ? r : 0)) * a.z_stride + row0 : nullptr;
+    // One tile: its products and softmax step.  LAST: no tile follows.  Outside the last one every request is made without a condition, or
+    // the compiler would wait for all that is in flight wherever it waits for anything.
+    auto tile = [&](int first, auto last) {
+        constexpr bool LAST = decltype(last)::value;
+        const int next = first + WAVES * TT::ROWS;
         float z[NZ];
         t.logits(q, z);
         const uint32_t there = at.there;
-        if (more) {
-            find_rows(a, pages, lead, rows, next, lane, at);
+        if constexpr (!LAST) {
+            find_k(a, pages, lead, rows, next, lane, at);
+#pragma unroll
+            for (int s = 0; s < at.SUB; ++s) after(at.k[s], z[NZ - 1]);
             request_k(next);
         }
-        float top = m;
 #pragma unroll
         for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
-        if (zrow && r < heads)
+        if constexpr (WEIGHTS)                                      // lanes without a head repeat the first head's: the same values
 #pragma unroll
             for (int e = 0; e < NZ; e += 4) *reinterpret_cast<f32x4 *>(zrow + first + 4 * e + 4 * g) = f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]};
         const bool all = __all(there == (1u << NZ) - 1u);
@@ -309,6 +319,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
 #pragma unroll
             for (int e = 0; e < NZ; ++e) z[e] = there >> e & 1 ? z[e] : NEG_BIG;
         }
+        float top = m;
 #pragma unroll
         for (int e = 0; e < NZ; ++e) top = fmaxf(top, z[e]);
         {
@@ -339,7 +350,24 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
 #pragma unroll
         for (int e = 0; e < NZ; ++e) l += p[e];
         t.accumulate(p, o);
-        if (more) request_v(next);
+        if constexpr (!LAST) {
+            find_v(a, pages, lead, rows, next, lane, at);
+#pragma unroll
+            for (int i = 0; i < at.NV; ++i) after(at.v[i], o[TT::NV - 1][0]);
+            request_v(next);
+            asm volatile("" ::: "memory");                          // or the requests would move to the loop's head, behind K's
+        }
+    };
+    if (wave < tiles) {
+        int first = wave * TT::ROWS;
+        find_k(a, pages, lead, rows, first, lane, at);
+        request_k(first);
+        find_v(a, pages, lead, rows, first, lane, at);
+        request_v(first);
+        asm volatile("" ::: "memory");
+#pragma unroll 1
+        for (int i = wave; i + WAVES < tiles; i += WAVES, first += WAVES * TT::ROWS) tile(first, std::false_type{});
+        tile(first, std::true_type{});
     }
 
     // the newest row goes where it belongs
@@ -404,7 +432,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             if (d == 0) a.part_ml[bh * a.n_split + blockIdx.x] = make_float2(top, sum);
         }
     }
-    if (!whole || !a.weight_out) return;
+    if (!WEIGHTS || !whole) return;
     __syncthreads();
     for (int j = threadIdx.x; j < rows; j += 64 * WAVES) {
         const int block = block_of(a, j + lead), place = j + lead - block * a.g.page_size;
@@ -531,8 +559,11 @@ template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(con
     const int heads = a.group < HEADS ? a.group : HEADS;
     const size_t lds = (size_t)WAVES * heads * (D + 4) * sizeof(float);
     const dim3 grid((unsigned)sh.n_split, (unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs);
-    if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true>), grid, dim3(64 * WAVES), lds, s, a);
-    else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false>), grid, dim3(64 * WAVES), lds, s, a);
+    const dim3 wg(64 * WAVES);
+    if (step && a.weight_out) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true>), grid, wg, lds, s, a);
+    else if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, false>), grid, wg, lds, s, a);
+    else if (a.weight_out) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, true>), grid, wg, lds, s, a);
+    else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, false>), grid, wg, lds, s, a);
     if (!sh.whole) {
         const unsigned pieces = a.weight_out ? (unsigned)(a.g.max_len + 1023) / 1024 : 0;
         hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)a.group + pieces, (unsigned)a.g.n_kv, (unsigned)a.g.n_seqs), dim3(256),
@@ -590,6 +621,7 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     a.chunk = shape.chunk;
     a.n_split = shape.n_split;
     a.whole = shape.whole;
+    a.single = cfg->page_size == 1;
     a.page_magic = (uint32_t)((0xffffffffull + (unsigned)cfg->page_size) / (unsigned)cfg->page_size);
     a.q_stride = (cfg->q_stride ? cfg->q_stride : (int64_t)cfg->n_heads * cfg->head_dim) * (int64_t)paged_esize(cfg);
     a.n_heads = cfg->n_heads;
