@@ -423,7 +423,7 @@ typedef struct ssd_paged_config {
     int32_t dtype;         /* ssd_dtype of q, k, v, the pool and the output                */
     int32_t page_size;     /* places per page: 1..32768                                    */
     int32_t n_pages;       /* pages of the pool: >= 1                                      */
-    int32_t max_blocks;    /* columns of block_table: >= 1, max_blocks * page_size <= 2^30 */
+    int32_t max_blocks;    /* columns of block_table: >= 1, max_blocks * page_size <= 2^25 */
     float   softmax_scale; /* 0 selects 1/sqrt(d)                                          */
     int32_t reserved[3];   /* must be 0                                                    */
     int64_t page_stride;   /* elements; multiples of 16 bytes, at least d.  All three 0:   */

@@ -18,8 +18,8 @@ int check_paged(const ssd_paged_config *c) {
     if (c->dtype != SSD_F32 && c->dtype != SSD_BF16) return fail(SSD_ERR_INVALID_ARG, "dtype=%d is neither SSD_F32 nor SSD_BF16", c->dtype);
     if (c->page_size < 1 || c->page_size > 32768) return fail(SSD_ERR_INVALID_ARG, "page_size=%d outside 1..32768", c->page_size);
     if (c->n_pages < 1) return fail(SSD_ERR_INVALID_ARG, "n_pages=%d must be >= 1", c->n_pages);
-    if (c->max_blocks < 1 || (int64_t)c->max_blocks * c->page_size > (1ll << 30))
-        return fail(SSD_ERR_INVALID_ARG, "max_blocks=%d must be >= 1, with max_blocks * page_size at most 2^30", c->max_blocks);
+    if (c->max_blocks < 1 || (int64_t)c->max_blocks * c->page_size > (1ll << 25))
+        return fail(SSD_ERR_INVALID_ARG, "max_blocks=%d must be >= 1, with max_blocks * page_size at most 2^25", c->max_blocks);
     if (!(c->softmax_scale >= 0.f) || !std::isfinite(c->softmax_scale)) return fail(SSD_ERR_INVALID_ARG, "softmax_scale must be finite and >= 0");
     for (int i = 0; i < 3; ++i)
         if (c->reserved[i] != 0) return fail(SSD_ERR_INVALID_ARG, "reserved[%d] must be 0", i);

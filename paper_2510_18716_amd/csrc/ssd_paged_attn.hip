@@ -40,7 +40,6 @@ struct PagedAttnArgs {
     int64_t z_stride;         // rows, a multiple of the chunk
     int n_heads, group, q_tiles;
     int chunk, n_split;
-    int whole;                // every sequence is one chunk and every group one tile: this launch writes the outputs
     uint32_t page_magic, single;   // ceil(2^32 / page_size) and 0, or 0 and 1 where that is 2^32
     float scale;              // softmax scale * log2 e
 };
@@ -225,7 +224,13 @@ template <typename T> static __device__ __forceinline__ void store_out(char *out
     else reinterpret_cast<uint16_t *>(out)[i] = (uint16_t)f32_to_bf16_bits(x);
 }
 
-// grid = (chunks, kv heads * tiles of query heads, sequences)
+// Which piece a workgroup takes.
+struct Piece { int b, chunk, head_tile; };
+static __device__ __forceinline__ Piece piece_of() {
+    const unsigned z = blockIdx.z;
+    return {(int)((blockIdx.y + z) % gridDim.y), (int)z, (int)((blockIdx.x + z) % gridDim.x)};
+}
+
 template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS>
 __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs a) {
     typedef Tile<T, D> TT;
@@ -236,14 +241,15 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     __shared__ float sm_lse[HEADS];
     extern __shared__ float sm_o[];                                 // [WAVES][heads][LD]
 
-    const int b = blockIdx.z, kv = (int)blockIdx.y / a.q_tiles, qt = (int)blockIdx.y - kv * a.q_tiles;
+    const Piece pc = piece_of();
+    const int b = pc.b, kv = pc.head_tile / a.q_tiles, qt = pc.head_tile - kv * a.q_tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int n = clamp_len(a.g, b);
-    const int row0 = (int)blockIdx.x * a.chunk;
+    const int row0 = pc.chunk * a.chunk;
     const int heads = a.group - qt * HEADS < HEADS ? a.group - qt * HEADS : HEADS, head0 = kv * a.group + qt * HEADS;
-    const bool whole = a.whole;
+    const bool whole = n <= a.chunk && a.q_tiles == 1;              // this workgroup writes the outputs
     if (row0 >= n) {
-        if (whole) {                                                // a sequence without rows
+        if (n == 0 && row0 == 0 && whole) {                         // a sequence without rows
             for (int i = threadIdx.x; i < heads * D; i += 64 * WAVES) store_out<T>(a.out, ((int64_t)b * a.n_heads + head0) * D + i, 0.f);
             if (a.lse && (int)threadIdx.x < heads) a.lse[(int64_t)b * a.n_heads + head0 + threadIdx.x] = -INFINITY;
         }
@@ -428,8 +434,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                 sm_lse[h] = sum == 0.f ? INFINITY : lse;
             }
         } else {
-            a.part_o[(bh * a.n_split + blockIdx.x) * D + d] = acc;
-            if (d == 0) a.part_ml[bh * a.n_split + blockIdx.x] = make_float2(top, sum);
+            a.part_o[(bh * a.n_split + pc.chunk) * D + d] = acc;
+            if (d == 0) a.part_ml[bh * a.n_split + pc.chunk] = make_float2(top, sum);
         }
     }
     if (!WEIGHTS || !whole) return;
@@ -445,72 +451,80 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     }
 }
 
-// Joins the chunks of a (sequence, query head): blockIdx.x < group.  The workgroups beyond bring the weights of 1024 rows each up to date.
-// grid = (group + pieces of 1024 rows, kv heads, sequences)
+// Maximum over the lanes of a wave.
+static __device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, dpp_f<0xB1>(v));
+    v = fmaxf(v, dpp_f<0x4E>(v));
+    v = fmaxf(v, dpp_f<0x141>(v));
+    v = fmaxf(v, dpp_f<0x140>(v));
+    return across_groups_max<16>(v);
+}
+
+// Joins the chunks of a (sequence, query head): blockIdx.z < group.  The workgroups beyond bring the weights of 1024 rows each up to date.
+// Sequences of one chunk are complete already.
+// grid = (kv heads, sequences, group + pieces of 1024 rows)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int step) {
-    __shared__ float red[4];
-    __shared__ float part[256 / D][D];
+    constexpr int FR = D / 4, PAR = 256 / FR;                       // 16-byte pieces of a chunk's sums, chunks read side by side
+    constexpr int SEG = 512;                                        // chunks whose factors are in LDS at a time
+    __shared__ float factor[SEG];
+    __shared__ float red[8];
+    __shared__ f32x4 part[PAR][FR];
     extern __shared__ float lse2[];                                 // [group]
-    const int kv = blockIdx.y, b = blockIdx.z;
+    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
     const int n = clamp_len(a.g, b), chunks = (n + a.chunk - 1) / a.chunk;
-    if ((int)blockIdx.x < a.group) {
-        const int64_t bh = (int64_t)b * a.n_heads + kv * a.group + blockIdx.x;
+    if (chunks == 1 && a.q_tiles == 1) return;
+    if ((int)blockIdx.z < a.group) {
+        const int64_t bh = (int64_t)b * a.n_heads + kv * a.group + blockIdx.z;
         const float2 *ml = a.part_ml + bh * a.n_split;
-        float top = NEG_BIG;
-        for (int c = threadIdx.x; c < chunks; c += 256) top = fmaxf(top, ml[c].x);
-        top = across_groups_max<16>(top);
-        top = fmaxf(top, dpp_f<0xB1>(top));
-        top = fmaxf(top, dpp_f<0x4E>(top));
-        top = fmaxf(top, dpp_f<0x141>(top));
-        top = fmaxf(top, dpp_f<0x140>(top));
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+        const float *po = a.part_o + bh * a.n_split * D + 4 * (tid % FR);
+        float top = NEG_BIG, sum = 0.f;
+        for (int c = tid; c < chunks; c += 256) top = fmaxf(top, ml[c].x);
+        top = wave_max(top);
+        if ((tid & 63) == 0) red[tid >> 6] = top;
         __syncthreads();
         top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-        constexpr int P = 256 / D;
-        const int d = threadIdx.x % D, lane = threadIdx.x / D;
-        float acc = 0.f, sum = 0.f;
-        for (int c = lane; c < chunks; c += P) {
-            const float2 x = ml[c];
-            const float f = fast_exp2(x.x - top);
-            sum = fmaf(x.y, f, sum);
-            acc = fmaf(a.part_o[(bh * a.n_split + c) * D + d], f, acc);
-        }
-        part[lane][d] = acc;
-        __shared__ float sums[P];
-        if (d == 0) sums[lane] = sum;
-        __syncthreads();
-        if (lane == 0) {
-            sum = 0.f;
-            acc = 0.f;
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                sum += sums[i];
-                acc += part[i][d];
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < chunks; c0 += SEG) {
+            const int end = chunks - c0 < SEG ? chunks - c0 : SEG;
+            __syncthreads();
+            for (int c = tid; c < end; c += 256) {
+                const float2 x = ml[c0 + c];
+                factor[c] = fast_exp2(x.x - top);
+                sum = fmaf(x.y, factor[c], sum);
             }
-            store_out<T>(a.out, bh * D + d, sum == 0.f ? 0.f : acc / sum);
-            if (d == 0 && a.lse) a.lse[bh] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+            __syncthreads();
+#pragma unroll 4
+            for (int c = tid / FR; c < end; c += PAR) acc += factor[c] * *reinterpret_cast<const f32x4 *>(po + (int64_t)(c0 + c) * D);
         }
+        sum = across_groups_sum<16>(group_sum<16>(sum));
+        if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
+        part[tid / FR][tid % FR] = acc;
+        __syncthreads();
+        sum = (red[4] + red[5]) + (red[6] + red[7]);
+        if (tid < D) {
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < PAR; ++i) x += reinterpret_cast<const float *>(part[i])[tid];
+            store_out<T>(a.out, bh * D + tid, sum == 0.f ? 0.f : x / sum);
+        }
+        if (tid == 0 && a.lse) a.lse[bh] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
         return;
     }
-    const int j0 = ((int)blockIdx.x - a.group) * 1024;
+    const int j0 = ((int)blockIdx.z - a.group) * 1024;
     if (j0 >= n) return;
-    for (int h = threadIdx.x >> 6; h < a.group; h += 4) {           // a wave sums a head's chunks
+    for (int h = tid >> 6; h < a.group; h += 4) {                   // a wave sums a head's chunks
         const float2 *ml = a.part_ml + ((int64_t)b * a.n_heads + kv * a.group + h) * a.n_split;
         float top = NEG_BIG, sum = 0.f;
-        for (int c = threadIdx.x & 63; c < chunks; c += 64) top = fmaxf(top, ml[c].x);
-        top = across_groups_max<16>(top);
-        top = fmaxf(top, dpp_f<0xB1>(top));
-        top = fmaxf(top, dpp_f<0x4E>(top));
-        top = fmaxf(top, dpp_f<0x141>(top));
-        top = fmaxf(top, dpp_f<0x140>(top));
-        for (int c = threadIdx.x & 63; c < chunks; c += 64) sum += ml[c].y * fast_exp2(ml[c].x - top);
+        for (int c = tid & 63; c < chunks; c += 64) top = fmaxf(top, ml[c].x);
+        top = wave_max(top);
+        for (int c = tid & 63; c < chunks; c += 64) sum += ml[c].y * fast_exp2(ml[c].x - top);
         sum = across_groups_sum<16>(group_sum<16>(sum));
-        if ((threadIdx.x & 63) == 0) lse2[h] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
+        if ((tid & 63) == 0) lse2[h] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
     }
     __syncthreads();
     const int end = n - j0 < 1024 ? n : j0 + 1024;
-    for (int j = j0 + (int)threadIdx.x; j < end; j += 256) {
+    for (int j = j0 + tid; j < end; j += 256) {
         int block, place;
         split_slot(a.g, j, block, place);
         const int page = page_of(a.g, b, block);
@@ -540,6 +554,7 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     while (s.chunk > 128 && units * ((reach + s.chunk - 1) / s.chunk) < 8192) s.chunk /= 2;
     s.n_split = (reach + s.chunk - 1) / s.chunk;
     s.whole = s.n_split == 1 && s.q_tiles == 1;
+
     return s;
 }
 
@@ -558,7 +573,7 @@ static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s
 template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(const PagedAttnArgs &a, const PagedShape &sh, bool step, hipStream_t s) {
     const int heads = a.group < HEADS ? a.group : HEADS;
     const size_t lds = (size_t)WAVES * heads * (D + 4) * sizeof(float);
-    const dim3 grid((unsigned)sh.n_split, (unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs);
+    const dim3 grid((unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs, (unsigned)sh.n_split);
     const dim3 wg(64 * WAVES);
     if (step && a.weight_out) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true>), grid, wg, lds, s, a);
     else if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, false>), grid, wg, lds, s, a);
@@ -566,7 +581,7 @@ template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(con
     else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, false>), grid, wg, lds, s, a);
     if (!sh.whole) {
         const unsigned pieces = a.weight_out ? (unsigned)(a.g.max_len + 1023) / 1024 : 0;
-        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)a.group + pieces, (unsigned)a.g.n_kv, (unsigned)a.g.n_seqs), dim3(256),
+        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs, (unsigned)a.group + pieces), dim3(256),
                            (size_t)a.group * sizeof(float), s, a, step ? 1 : 0);
     }
     return hipGetLastError();
@@ -620,7 +635,7 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     a.q_tiles = shape.q_tiles;
     a.chunk = shape.chunk;
     a.n_split = shape.n_split;
-    a.whole = shape.whole;
+
     a.single = cfg->page_size == 1;
     a.page_magic = (uint32_t)((0xffffffffull + (unsigned)cfg->page_size) / (unsigned)cfg->page_size);
     a.q_stride = (cfg->q_stride ? cfg->q_stride : (int64_t)cfg->n_heads * cfg->head_dim) * (int64_t)paged_esize(cfg);

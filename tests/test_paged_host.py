@@ -22,7 +22,7 @@ def test_struct_sizes_agree_with_the_header():
 
 
 BAD_CONFIG = [dict(n_seqs=0), dict(n_seqs=65536), dict(n_kv_heads=0), dict(n_kv_heads=3), dict(n_heads=0), dict(n_heads=2048), dict(head_dim=96),
-              dict(dtype=2), dict(page_size=0), dict(page_size=32769), dict(n_pages=0), dict(max_blocks=0), dict(max_blocks=1 << 27),
+              dict(dtype=2), dict(page_size=0), dict(page_size=32769), dict(n_pages=0), dict(max_blocks=0), dict(max_blocks=1 << 22),
               dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")), dict(page_stride=1024), dict(page_stride=4096, head_stride=2048, row_stride=120),
               dict(page_stride=4096, head_stride=2052, row_stride=128), dict(page_stride=1 << 49, head_stride=128, row_stride=128),
               dict(page_stride=-4096, head_stride=2048, row_stride=128), dict(q_stride=8), dict(q_stride=1028), dict(new_stride=100), dict(new_stride=-256)]
