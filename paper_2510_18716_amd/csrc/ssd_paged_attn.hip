@@ -34,18 +34,21 @@ struct PagedAttnArgs {
     char *out;
     float *lse;
     float *z;                 // logits (base 2) [n_seqs, n_heads, z_stride]; only where weights are wanted
-    float *part_o;            // [n_seqs, n_heads, n_split, D] sums of a chunk, relative to its maximum
-    float2 *part_ml;          // [n_seqs, n_heads, n_split] maximum (base 2) and sum of a chunk
+    float *lse2;              // [n_seqs, n_heads] lse (base 2) of units that one workgroup completed; only where weights are wanted
+    float *part_o;            // [2 * workgroups, heads of a tile, D] sums of a unit's part, relative to its maximum
+    float2 *part_ml;          // [2 * workgroups, heads of a tile] its maximum (base 2) and sum
     int64_t q_stride, new_stride;   // bytes
-    int64_t z_stride;         // rows, a multiple of the chunk
+    int64_t z_stride;         // rows, a multiple of a round
     int n_heads, group, q_tiles;
-    int chunk, n_split;
+    int tile_heads;           // min(group, 16)
+    int workgroups;           // 0: a workgroup takes a whole unit
+    int stage;                // rows whose part of the block table is in LDS at a time: a multiple of a round
     uint32_t page_magic, single;   // ceil(2^32 / page_size) and 0, or 0 and 1 where that is 2^32
     float scale;              // softmax scale * log2 e
 };
 
 static constexpr int WAVES = 4;
-static constexpr int CHUNK_MAX = 1024;
+static constexpr int BLOCKS = 1024;                                // entries of the block table in LDS
 static constexpr int HEADS = 16;                                   // heads of a tile
 static constexpr int64_t NO_PAGE = -(1ll << 62);
 static constexpr float LN2 = 0.6931471805599453f;
@@ -224,230 +227,358 @@ template <typename T> static __device__ __forceinline__ void store_out(char *out
     else reinterpret_cast<uint16_t *>(out)[i] = (uint16_t)f32_to_bf16_bits(x);
 }
 
-// Which piece a workgroup takes.
-struct Piece { int b, chunk, head_tile; };
-static __device__ __forceinline__ Piece piece_of() {
-    const unsigned z = blockIdx.z;
-    return {(int)((blockIdx.y + z) % gridDim.y), (int)z, (int)((blockIdx.x + z) % gridDim.x)};
+// ---- who works on what -------------------------------------------------------------------------------------------------
+//
+// A unit is a (sequence, key / value head, tile of query heads); its rows are counted in rounds of WAVES tiles.  All units' rounds, in the order
+// sequence, head, row, are dealt to the workgroups in equal runs, so that the chip is evenly loaded whatever the lengths are: a
+// workgroup finishes one unit, goes through some and begins another.  The lengths are known on the device only; every wave adds them
+// up for itself, 64 sequences (or runs of them) at a time, and finds its place by a ballot.  A unit in more than one workgroup leaves parts
+// for the second launch; a workgroup leaves at most two, the one it begins with and the one it ends with.
+
+static __device__ __forceinline__ int rounds_of(int n, int round) { return n == 0 ? 1 : (n + round - 1) / round; }
+
+static __device__ __forceinline__ uint32_t wave_sum_u32(uint32_t v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += (uint32_t)__shfl_xor((int)v, o);
+    return v;
 }
+static __device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t w = (uint32_t)__shfl_up((int)v, o);
+        v += lane >= o ? w : 0;
+    }
+    return v;
+}
+static __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
-template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS>
-__global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs a) {
-    typedef Tile<T, D> TT;
-    constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
-    constexpr int LD = D + 4;                                       // row of the merge area
-    __shared__ int64_t pages[CHUNK_MAX + 1];
-    __shared__ float sm_ml[WAVES][HEADS][2];
-    __shared__ float sm_lse[HEADS];
-    extern __shared__ float sm_o[];                                 // [WAVES][heads][LD]
+// The runs: `all` rounds over at most `most` workgroups, none below two rounds where there are 256 workgroups without.
+struct Runs {
+    uint32_t q, rem;
+    __device__ __forceinline__ Runs(uint32_t all, uint32_t most) {
+        uint32_t w = all / 2 > 256 ? all / 2 : 256;
+        w = w < most ? w : most;
+        w = w < all ? w : all;
+        q = all / w;
+        rem = all - q * w;
+    }
+    __device__ __forceinline__ uint32_t start(uint32_t w) const { return w * q + (w < rem ? w : rem); }
+    __device__ __forceinline__ uint32_t owner(uint32_t r) const {
+        const uint32_t longer = rem * (q + 1);
+        return r < longer ? r / (q + 1) : rem + (r - longer) / q;
+    }
+};
 
-    const Piece pc = piece_of();
-    const int b = pc.b, kv = pc.head_tile / a.q_tiles, qt = pc.head_tile - kv * a.q_tiles;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int n = clamp_len(a.g, b);
-    const int row0 = pc.chunk * a.chunk;
-    const int heads = a.group - qt * HEADS < HEADS ? a.group - qt * HEADS : HEADS, head0 = kv * a.group + qt * HEADS;
-    const bool whole = n <= a.chunk && a.q_tiles == 1;              // this workgroup writes the outputs
-    if (row0 >= n) {
-        if (n == 0 && row0 == 0 && whole) {                         // a sequence without rows
-            for (int i = threadIdx.x; i < heads * D; i += 64 * WAVES) store_out<T>(a.out, ((int64_t)b * a.n_heads + head0) * D + i, 0.f);
-            if (a.lse && (int)threadIdx.x < heads) a.lse[(int64_t)b * a.n_heads + head0 + threadIdx.x] = -INFINITY;
-        }
+// Accumulated weights of rows j .. j + 3, j a multiple of four, n the sequence's rows; p their probabilities.  newest: the row without a
+// weight so far, or -1.
+template <bool QUADS>
+static __device__ __forceinline__ void add_weights(const PagedAttnArgs &a, int b, int kv, int j, int n, const f32x4 &p, int newest) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    int block, place;
+    split_slot(a.g, j, block, place);
+    if (QUADS && j + 4 <= n) {
+        const int page = page_of(a.g, b, block);
+        if (page < 0) return;
+        const int64_t i = table_index(a.g, page, kv, place);
+        f32x4 w = *reinterpret_cast<const f32x4_any *>(a.weight_in + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (j + e == newest ? 0.f : w[e]) + p[e];
+        *reinterpret_cast<f32x4_any *>(a.weight_out + i) = w;
         return;
     }
-    const int rows = n - row0 < a.chunk ? n - row0 : a.chunk;
-    int block0, lead;
-    split_slot(a.g, row0, block0, lead);
-    const int blocks = block_of(a, rows - 1 + lead) + 1;
-    for (int i = threadIdx.x; i < blocks; i += 64 * WAVES) {
-        const int page = page_of(a.g, b, block0 + i);
-        pages[i] = page < 0 ? NO_PAGE : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (j + e >= n) return;
+        if (e > 0 && ++place == a.g.page_size) {
+            place = 0;
+            ++block;
+        }
+        const int page = page_of(a.g, b, block);
+        if (page < 0) continue;
+        const int64_t i = table_index(a.g, page, kv, place);
+        a.weight_out[i] = (j + e == newest ? 0.f : a.weight_in[i]) + p[e];
     }
-    typename TT::Q q;
-    TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (r < heads ? r : 0)) * (D * sizeof(T)), lane, q);
-    __syncthreads();
+}
 
-    // step: the sequence's last row, if it lies here
-    const bool newest = STEP && a.g.seq_len[b] == n && row0 + rows == n;
-    const char *k_new = nullptr, *v_new = nullptr;
-    if (STEP && newest) {
-        k_new = a.k_new + (int64_t)b * a.new_stride + (int64_t)kv * (D * sizeof(T));
-        v_new = a.v_new + (int64_t)b * a.new_stride + (int64_t)kv * (D * sizeof(T));
+// The arguments, to be read from their segment again: what one phase of the kernel needs of them does not have to stay in scalar
+// registers through the others (there are too few: they would be kept in vector registers' lanes, and those in scratch memory).
+static __device__ __forceinline__ const PagedAttnArgs &arguments() {
+    typedef const PagedAttnArgs __attribute__((address_space(4))) *args_t;
+    args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const PagedAttnArgs *)p;
+}
+
+// grid = (workgroups), or (kv heads * tiles of query heads, sequences) where a workgroup takes a whole unit
+template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS>
+__global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs) {
+    typedef Tile<T, D> TT;
+    constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
+    constexpr int ROUND = WAVES * TT::ROWS;
+    constexpr int LD = D + 4;                                       // row of the merge area
+    __shared__ int64_t pages[BLOCKS];
+    __shared__ float sm_ml[WAVES][HEADS][2];
+    extern __shared__ float sm_o[];                                 // [WAVES][tile_heads][LD]
+
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    int b, ht, t;                                                   // sequence, head tile, round of the unit
+    uint32_t left;                                                  // rounds of the run
+    {
+    const PagedAttnArgs &a = arguments();
+    const uint32_t K = (uint32_t)(a.g.n_kv * a.q_tiles);
+    if (a.workgroups == 0) {
+        b = (int)blockIdx.y;
+        ht = (int)((blockIdx.x + blockIdx.y) % K);
+        t = 0;
+        left = (uint32_t)rounds_of(clamp_len(a.g, b), ROUND);
+    } else {
+        const int run = (a.g.n_seqs + 63) / 64;                     // sequences of a lane
+        uint32_t mine = 0;
+        for (int i = 0; i < run; ++i) {
+            const int seq = lane * run + i;
+            if (seq < a.g.n_seqs) mine += (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
+        }
+        uint32_t upto = wave_scan_u32(mine, lane);
+        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * K;
+        const Runs runs(all, (uint32_t)a.workgroups);
+        const uint32_t r0 = runs.start(blockIdx.x), r1 = runs.start(blockIdx.x + 1);
+        if (r0 >= r1 || r0 >= all) return;
+        left = r1 - r0;
+        const uint32_t at = r0 / K;                                 // in rounds of one head
+        int l = (int)__popcll(__ballot(upto <= at));
+        uint32_t before = l == 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)upto, l - 1);
+        b = l * run;
+        for (int i0 = 0; run > 1; i0 += 64) {                       // the run's sequences, 64 at a time
+            const int seq = l * run + i0 + lane;
+            const bool ours = i0 + lane < run && seq < a.g.n_seqs;
+            const uint32_t up = wave_scan_u32(ours ? (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND) : 0u, lane) + before;
+            const int k = (int)__popcll(__ballot(up <= at));
+            if (k < 64) {
+                b = l * run + i0 + k;
+                if (k > 0) before = (uint32_t)__builtin_amdgcn_readlane((int)up, k - 1);
+                break;
+            }
+            before = (uint32_t)__builtin_amdgcn_readlane((int)up, 63);
+        }
+        const uint32_t tb = uniform((uint32_t)rounds_of(clamp_len(a.g, b), ROUND)), into = r0 - before * K;
+        ht = (int)(into / tb);
+        t = (int)(into - (uint32_t)ht * tb);
     }
-    const char *kp = a.k_pages, *vp = a.v_pages;
+    }
+    b = (int)uniform((uint32_t)b);
+    ht = (int)uniform((uint32_t)ht);
+    t = (int)uniform((uint32_t)t);
+    left = uniform(left);
 
-    float m = NEG_BIG, l = 0.f;
-    f32x4 o[TT::NV];
-#pragma unroll
-    for (int j = 0; j < TT::NV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (bool first_unit = true;; first_unit = false) {
+        const PagedAttnArgs &a = arguments();
+        const int kv = ht / a.q_tiles, qt = ht - kv * a.q_tiles;
+        const int heads = a.group - qt * HEADS < HEADS ? a.group - qt * HEADS : HEADS, head0 = kv * a.group + qt * HEADS;
+        const int n = clamp_len(a.g, b), rounds = rounds_of(n, ROUND);
+        const int take = (uint32_t)(rounds - t) < left ? rounds - t : (int)left;
+        const int begin = t * ROUND, end = begin + take * ROUND < n ? begin + take * ROUND : n;
+        const bool whole = take == rounds;                          // this workgroup writes the outputs
+        const bool newest = STEP && end == n && n > 0 && a.g.seq_len[b] == n;      // the row of this call is among them
+        const char *k_new = nullptr, *v_new = nullptr;
+        if (STEP && newest) {
+            k_new = a.k_new + (int64_t)b * a.new_stride + (int64_t)kv * (D * sizeof(T));
+            v_new = a.v_new + (int64_t)b * a.new_stride + (int64_t)kv * (D * sizeof(T));
+        }
+        typename TT::Q q;
+        TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (r < heads ? r : 0)) * (D * sizeof(T)), lane, q);
+        float *z_unit = WEIGHTS ? a.z + ((int64_t)b * a.n_heads + head0) * a.z_stride : nullptr;
+        const uint32_t z_lane = WEIGHTS ? (uint32_t)(r < heads ? r : 0) * (uint32_t)a.z_stride + 4u * (uint32_t)g : 0;
 
-    TT t;
-    TileRows<TT::BF16, QUADS> at;
-    auto request_k = [&](int first) {
+        float m = NEG_BIG, l = 0.f;
+        f32x4 o[TT::NV];
 #pragma unroll
-        for (int s = 0; s < at.SUB; ++s) {
-            const char *row = kp + at.k[s];
-            if (STEP && newest && first + 16 * s + r >= rows - 1) row = k_new;
-            t.load_k(s, row, lane);
+        for (int j = 0; j < TT::NV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        for (int row0 = begin; row0 < end;) {
+            const PagedAttnArgs &a = arguments();
+            const int rows = end - row0 < a.stage ? end - row0 : a.stage;
+            int block0, lead;
+            split_slot(a.g, row0, block0, lead);
+            const int blocks = block_of(a, rows - 1 + lead) + 1;
+            __syncthreads();                                        // the last stage's entries, and a unit's merge area, have been read
+            for (int i = threadIdx.x; i < blocks; i += 64 * WAVES) {
+                const int page = page_of(a.g, b, block0 + i);
+                pages[i] = page < 0 ? NO_PAGE : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
+            }
+            __syncthreads();
+            const int last_row = newest && row0 + rows == n ? rows - 1 : 0x7fffffff;
+
+            TT tl;
+            TileRows<TT::BF16, QUADS> at;
+            auto request_k = [&](int first) {
+#pragma unroll
+                for (int s = 0; s < at.SUB; ++s) {
+                    const char *row = a.k_pages + at.k[s];
+                    if (STEP && first + 16 * s + r >= last_row) row = k_new;
+                    tl.load_k(s, row, lane);
+                }
+            };
+            auto request_v = [&](int first) {
+#pragma unroll
+                for (int i = 0; i < NZ; ++i) {
+                    const char *row = a.v_pages + (QUADS ? at.v[i / 4] + (i % 4) * a.g.row_stride : at.v[i]);
+                    if (STEP && first + 16 * (i / 4) + 4 * g + i % 4 >= last_row) row = v_new;
+                    tl.load_v(i, row, lane);
+                }
+            };
+            // One tile: its products and softmax step.  LAST: no tile follows.  Outside the last one every request is made without a condition,
+            // or the compiler would wait for all that is in flight wherever it waits for anything.
+            auto tile = [&](int first, auto last) {
+                constexpr bool LAST = decltype(last)::value;
+                const int next = first + ROUND;
+                float z[NZ];
+                tl.logits(q, z);
+                const uint32_t there = at.there;
+                if constexpr (!LAST) {
+                    find_k(a, pages, lead, rows, next, lane, at);
+#pragma unroll
+                    for (int s = 0; s < at.SUB; ++s) after(at.k[s], z[NZ - 1]);
+                    request_k(next);
+                }
+#pragma unroll
+                for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
+                if constexpr (WEIGHTS)                              // lanes without a head repeat the first head's: the same values
+#pragma unroll
+                    for (int e = 0; e < NZ; e += 4)
+                        *reinterpret_cast<f32x4 *>(z_unit + (z_lane + (uint32_t)(row0 + first + 4 * e))) = f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]};
+                const bool all = __all(there == (1u << NZ) - 1u);
+                if (!all) {
+#pragma unroll
+                    for (int e = 0; e < NZ; ++e) z[e] = there >> e & 1 ? z[e] : NEG_BIG;
+                }
+                float top = m;
+#pragma unroll
+                for (int e = 0; e < NZ; ++e) top = fmaxf(top, z[e]);
+                {
+                    float x, y;
+                    rows_pair(top, x, y);
+                    top = fmaxf(x, y);
+                    halves_pair(top, x, y);
+                    top = fmaxf(x, y);
+                }
+                if (__any(top > m)) {                               // a larger logit: what is summed so far shrinks
+                    const float f = fast_exp2(m - top);
+                    l *= f;
+#pragma unroll
+                    for (int j = 0; j < TT::NV; ++j) o[j] *= f;
+                    m = top;
+                }
+                float p[NZ];
+#pragma unroll
+                for (int e = 0; e < NZ; ++e) p[e] = fast_exp2(z[e] - m);
+                if (!all) {                                         // rows that do not exist: neither their p nor their V may count
+#pragma unroll
+                    for (int e = 0; e < NZ; ++e)
+                        if (!(there >> e & 1)) {
+                            p[e] = 0.f;
+                            tl.zero_v(e);
+                        }
+                }
+#pragma unroll
+                for (int e = 0; e < NZ; ++e) l += p[e];
+                tl.accumulate(p, o);
+                if constexpr (!LAST) {
+                    find_v(a, pages, lead, rows, next, lane, at);
+#pragma unroll
+                    for (int i = 0; i < at.NV; ++i) after(at.v[i], o[TT::NV - 1][0]);
+                    request_v(next);
+                    asm volatile("" ::: "memory");                  // or the requests would move to the loop's head, behind K's
+                }
+            };
+            const int tiles = (rows + TT::ROWS - 1) / TT::ROWS;
+            if (wave < tiles) {
+                int first = wave * TT::ROWS;
+                find_k(a, pages, lead, rows, first, lane, at);
+                request_k(first);
+                find_v(a, pages, lead, rows, first, lane, at);
+                request_v(first);
+                asm volatile("" ::: "memory");
+#pragma unroll 1
+                for (int i = wave; i + WAVES < tiles; i += WAVES, first += ROUND) tile(first, std::false_type{});
+                tile(first, std::true_type{});
+            }
+            row0 += rows;
         }
-    };
-    auto request_v = [&](int first) {
-#pragma unroll
-        for (int i = 0; i < NZ; ++i) {
-            const char *row = vp + (QUADS ? at.v[i / 4] + (i % 4) * a.g.row_stride : at.v[i]);
-            if (STEP && newest && first + 16 * (i / 4) + 4 * g + i % 4 >= rows - 1) row = v_new;
-            t.load_v(i, row, lane);
+
+        {
+        const PagedAttnArgs &a = arguments();
+        // the newest row goes where it belongs
+        if (STEP && newest && qt == 0 && wave == 0) {
+            int block, place;
+            split_slot(a.g, n - 1, block, place);
+            const int page = page_of(a.g, b, block);
+            if (page >= 0) {
+                constexpr int FR = D * (int)sizeof(T) / 16;
+                if (lane < 2 * FR) {
+                    const bool v = lane >= FR;
+                    const int sub = (v ? lane - FR : lane) * 16;
+                    *reinterpret_cast<uint4 *>((v ? a.v_dst : a.k_dst) + row_offset(a.g, page, kv, place) + sub) =
+                        *reinterpret_cast<const uint4 *>((v ? v_new : k_new) + sub);
+                }
+                if (lane == 0 && a.pos) a.pos[table_index(a.g, page, kv, place)] = a.g.seq_pos[b] - 1;
+            }
         }
-    };
-    const int tiles = (rows + TT::ROWS - 1) / TT::ROWS;
-    float *zrow = WEIGHTS ? a.z + ((int64_t)b * a.n_heads + head0 + (r < heads ? r : 0)) * a.z_stride + row0 : nullptr;
-    // One tile: its products and softmax step.  LAST: no tile follows.  Outside the last one every request is made without a condition, or
-    // the compiler would wait for all that is in flight wherever it waits for anything.
-    auto tile = [&](int first, auto last) {
-        constexpr bool LAST = decltype(last)::value;
-        const int next = first + WAVES * TT::ROWS;
-        float z[NZ];
-        t.logits(q, z);
-        const uint32_t there = at.there;
-        if constexpr (!LAST) {
-            find_k(a, pages, lead, rows, next, lane, at);
-#pragma unroll
-            for (int s = 0; s < at.SUB; ++s) after(at.k[s], z[NZ - 1]);
-            request_k(next);
-        }
-#pragma unroll
-        for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
-        if constexpr (WEIGHTS)                                      // lanes without a head repeat the first head's: the same values
-#pragma unroll
-            for (int e = 0; e < NZ; e += 4) *reinterpret_cast<f32x4 *>(zrow + first + 4 * e + 4 * g) = f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]};
-        const bool all = __all(there == (1u << NZ) - 1u);
-        if (!all) {
-#pragma unroll
-            for (int e = 0; e < NZ; ++e) z[e] = there >> e & 1 ? z[e] : NEG_BIG;
-        }
-        float top = m;
-#pragma unroll
-        for (int e = 0; e < NZ; ++e) top = fmaxf(top, z[e]);
+
+        // the waves' states meet
         {
             float x, y;
-            rows_pair(top, x, y);
-            top = fmaxf(x, y);
-            halves_pair(top, x, y);
-            top = fmaxf(x, y);
+            rows_pair(l, x, y);
+            l = x + y;
+            halves_pair(l, x, y);
+            l = x + y;
         }
-        if (__any(top > m)) {                                       // a larger logit: what is summed so far shrinks
-            const float f = fast_exp2(m - top);
-            l *= f;
+        if (!first_unit) __syncthreads();                           // a unit without rows passes no other barrier
+        if (r < heads) {
+            if (g == 0) {
+                sm_ml[wave][r][0] = m;
+                sm_ml[wave][r][1] = l;
+            }
+            float *dst = sm_o + (wave * heads + r) * LD;
 #pragma unroll
-            for (int j = 0; j < TT::NV; ++j) o[j] *= f;
-            m = top;
+            for (int j = 0; j < TT::NV; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dst[TT::column(j, e, lane)] = o[j][e];
         }
-        float p[NZ];
+        __syncthreads();
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (first_unit ? 0 : 1);
+        for (int i = threadIdx.x; i < heads * D; i += 64 * WAVES) {
+            const int h = i / D, d = i % D;
+            float top = sm_ml[0][h][0], sum = 0.f, acc = 0.f;
 #pragma unroll
-        for (int e = 0; e < NZ; ++e) p[e] = fast_exp2(z[e] - m);
-        if (!all) {                                                 // rows that do not exist: neither their p nor their V may count
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm_ml[w][h][0]);
 #pragma unroll
-            for (int e = 0; e < NZ; ++e)
-                if (!(there >> e & 1)) {
-                    p[e] = 0.f;
-                    t.zero_v(e);
+            for (int w = 0; w < WAVES; ++w) {
+                const float f = fast_exp2(sm_ml[w][h][0] - top);
+                sum = fmaf(sm_ml[w][h][1], f, sum);
+                acc = fmaf(sm_o[(w * heads + h) * LD + d], f, acc);
+            }
+            const int64_t bh = (int64_t)b * a.n_heads + head0 + h;
+            if (whole) {
+                store_out<T>(a.out, bh * D + d, sum == 0.f ? 0.f : acc / sum);
+                if (d == 0) {
+                    const float lse = top + __builtin_amdgcn_logf(sum);
+                    if (a.lse) a.lse[bh] = sum == 0.f ? -INFINITY : lse * LN2;
+                    if (WEIGHTS) a.lse2[bh] = sum == 0.f ? INFINITY : lse;
                 }
-        }
-#pragma unroll
-        for (int e = 0; e < NZ; ++e) l += p[e];
-        t.accumulate(p, o);
-        if constexpr (!LAST) {
-            find_v(a, pages, lead, rows, next, lane, at);
-#pragma unroll
-            for (int i = 0; i < at.NV; ++i) after(at.v[i], o[TT::NV - 1][0]);
-            request_v(next);
-            asm volatile("" ::: "memory");                          // or the requests would move to the loop's head, behind K's
-        }
-    };
-    if (wave < tiles) {
-        int first = wave * TT::ROWS;
-        find_k(a, pages, lead, rows, first, lane, at);
-        request_k(first);
-        find_v(a, pages, lead, rows, first, lane, at);
-        request_v(first);
-        asm volatile("" ::: "memory");
-#pragma unroll 1
-        for (int i = wave; i + WAVES < tiles; i += WAVES, first += WAVES * TT::ROWS) tile(first, std::false_type{});
-        tile(first, std::true_type{});
-    }
-
-    // the newest row goes where it belongs
-    if (STEP && newest && qt == 0 && wave == 0) {
-        const int64_t to = row_at(a, pages, lead, rows, rows - 1);
-        if (to >= 0) {
-            constexpr int FR = D * (int)sizeof(T) / 16;
-            if (lane < 2 * FR) {
-                const bool v = lane >= FR;
-                const int sub = (v ? lane - FR : lane) * 16;
-                *reinterpret_cast<uint4 *>((v ? a.v_dst : a.k_dst) + to + sub) = *reinterpret_cast<const uint4 *>((v ? v_new : k_new) + sub);
-            }
-            if (lane == 0 && a.pos) {
-                int block, place;
-                split_slot(a.g, n - 1, block, place);
-                a.pos[table_index(a.g, page_of(a.g, b, block), kv, place)] = a.g.seq_pos[b] - 1;
+            } else {
+                a.part_o[(slot * a.tile_heads + h) * D + d] = acc;
+                if (d == 0) a.part_ml[slot * a.tile_heads + h] = make_float2(top, sum);
             }
         }
-    }
-
-    // the waves' states meet
-    {
-        float x, y;
-        rows_pair(l, x, y);
-        l = x + y;
-        halves_pair(l, x, y);
-        l = x + y;
-    }
-    if (r < heads) {
-        if (g == 0) {
-            sm_ml[wave][r][0] = m;
-            sm_ml[wave][r][1] = l;
+        left -= (uint32_t)take;
+        if (left == 0) return;
+        t = 0;
+        if (++ht == a.g.n_kv * a.q_tiles) {
+            ht = 0;
+            ++b;
         }
-        float *dst = sm_o + (wave * heads + r) * LD;
-#pragma unroll
-        for (int j = 0; j < TT::NV; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) dst[TT::column(j, e, lane)] = o[j][e];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < heads * D; i += 64 * WAVES) {
-        const int h = i / D, d = i % D;
-        float top = sm_ml[0][h][0], sum = 0.f, acc = 0.f;
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm_ml[w][h][0]);
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float f = fast_exp2(sm_ml[w][h][0] - top);
-            sum = fmaf(sm_ml[w][h][1], f, sum);
-            acc = fmaf(sm_o[(w * heads + h) * LD + d], f, acc);
         }
-        const int64_t bh = (int64_t)b * a.n_heads + head0 + h;
-        if (whole) {
-            store_out<T>(a.out, bh * D + d, sum == 0.f ? 0.f : acc / sum);
-            if (d == 0) {
-                const float lse = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
-                if (a.lse) a.lse[bh] = lse * LN2;
-                sm_lse[h] = sum == 0.f ? INFINITY : lse;
-            }
-        } else {
-            a.part_o[(bh * a.n_split + pc.chunk) * D + d] = acc;
-            if (d == 0) a.part_ml[bh * a.n_split + pc.chunk] = make_float2(top, sum);
-        }
-    }
-    if (!WEIGHTS || !whole) return;
-    __syncthreads();
-    for (int j = threadIdx.x; j < rows; j += 64 * WAVES) {
-        const int block = block_of(a, j + lead), place = j + lead - block * a.g.page_size;
-        if (pages[block] < 0) continue;
-        const float *z = a.z + ((int64_t)b * a.n_heads + head0) * a.z_stride + j;
-        float p = 0.f;
-        for (int h = 0; h < heads; ++h) p += fast_exp2(z[(int64_t)h * a.z_stride] - sm_lse[h]);
-        const int64_t i = table_index(a.g, page_of(a.g, b, block0 + block), kv, place);
-        a.weight_out[i] = (STEP && newest && j == rows - 1 ? 0.f : a.weight_in[i]) + p;
+        __syncthreads();
     }
 }
 
@@ -460,130 +591,195 @@ static __device__ __forceinline__ float wave_max(float v) {
     return across_groups_max<16>(v);
 }
 
-// Joins the chunks of a (sequence, query head): blockIdx.z < group.  The workgroups beyond bring the weights of 1024 rows each up to date.
-// Sequences of one chunk are complete already.
-// grid = (kv heads, sequences, group + pieces of 1024 rows)
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int step) {
-    constexpr int FR = D / 4, PAR = 256 / FR;                       // 16-byte pieces of a chunk's sums, chunks read side by side
-    constexpr int SEG = 512;                                        // chunks whose factors are in LDS at a time
-    __shared__ float factor[SEG];
-    __shared__ float red[8];
-    __shared__ f32x4 part[PAR][FR];
+// What the first launch leaves open: joins the parts of units that several workgroups share (blockIdx.z < head_blocks; a query head takes a
+// wave, or the whole workgroup where WIDE), and brings the rows' weights up to date (the workgroups beyond, 1024 rows at a time).
+// grid = (kv heads, sequences, head_blocks + a few)
+template <typename T, int D, bool QUADS, bool WIDE>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int step, int head_blocks) {
+    constexpr int ROUND = WAVES * Tile<T, D>::ROWS;
+    constexpr int FR = D / 4, PW = 64 / FR, NW = WIDE ? 4 : 1;      // 16-byte pieces of a part's sums; parts a wave reads side by side; waves
+    __shared__ float red[2][4];
+    __shared__ f32x4 sums[4][FR];
+    __shared__ float2 ml_lds[4][HEADS];
     extern __shared__ float lse2[];                                 // [group]
-    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const int n = clamp_len(a.g, b), chunks = (n + a.chunk - 1) / a.chunk;
-    if (chunks == 1 && a.q_tiles == 1) return;
-    if ((int)blockIdx.z < a.group) {
-        const int64_t bh = (int64_t)b * a.n_heads + kv * a.group + blockIdx.z;
-        const float2 *ml = a.part_ml + bh * a.n_split;
-        const float *po = a.part_o + bh * a.n_split * D + 4 * (tid % FR);
+    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = clamp_len(a.g, b);
+    const uint32_t K = (uint32_t)(a.g.n_kv * a.q_tiles), tb = (uint32_t)rounds_of(n, ROUND);
+    uint32_t all = 0, before = 0;
+    if (a.workgroups > 0) {
+        for (int seq = lane; seq < a.g.n_seqs; seq += 64) {
+            const uint32_t x = (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
+            all += x;
+            before += seq < b ? x : 0;
+        }
+        all = uniform(wave_sum_u32(all)) * K;
+        before = uniform(wave_sum_u32(before)) * K;
+    }
+    // the workgroups that share a unit, and where the first one's part lies
+    struct Parts { uint32_t w0, count, slot0; };
+    auto parts_of = [&](int tile) {
+        if (a.workgroups == 0) return Parts{0, 1, 0};
+        const Runs runs(all, (uint32_t)a.workgroups);
+        const uint32_t u0 = before + (uint32_t)(kv * a.q_tiles + tile) * tb, w0 = runs.owner(u0);
+        return Parts{w0, runs.owner(u0 + tb - 1) - w0 + 1, 2 * w0 + (runs.start(w0) < u0 ? 1 : 0)};
+    };
+    auto slot = [&](const Parts &p, uint32_t c) { return (int64_t)(c == 0 ? p.slot0 : 2 * (p.w0 + c)) * a.tile_heads; };
+
+    if ((int)blockIdx.z < head_blocks) {
+        const int head = WIDE ? (int)blockIdx.z : (int)blockIdx.z * 4 + wave, w = WIDE ? wave : 0;
+        if (head >= a.group) return;
+        const int h = head % HEADS;
+        const Parts p = parts_of(head / HEADS);
+        if (p.count == 1) return;
+        const int64_t bh = (int64_t)b * a.n_heads + kv * a.group + head;
         float top = NEG_BIG, sum = 0.f;
-        for (int c = tid; c < chunks; c += 256) top = fmaxf(top, ml[c].x);
+        for (uint32_t c = w * 64 + lane; c < p.count; c += 64 * NW) top = fmaxf(top, a.part_ml[slot(p, c) + h].x);
         top = wave_max(top);
-        if ((tid & 63) == 0) red[tid >> 6] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        if constexpr (WIDE) {
+            if (lane == 0) red[0][w] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+        }
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int c0 = 0; c0 < chunks; c0 += SEG) {
-            const int end = chunks - c0 < SEG ? chunks - c0 : SEG;
-            __syncthreads();
-            for (int c = tid; c < end; c += 256) {
-                const float2 x = ml[c0 + c];
-                factor[c] = fast_exp2(x.x - top);
-                sum = fmaf(x.y, factor[c], sum);
-            }
-            __syncthreads();
 #pragma unroll 4
-            for (int c = tid / FR; c < end; c += PAR) acc += factor[c] * *reinterpret_cast<const f32x4 *>(po + (int64_t)(c0 + c) * D);
+        for (uint32_t c = w * PW + lane / FR; c < p.count; c += PW * NW) {
+            const int64_t at = slot(p, c) + h;
+            const float2 x = a.part_ml[at];
+            const float f = fast_exp2(x.x - top);
+            sum = fmaf(x.y, f, sum);
+            acc += f * *reinterpret_cast<const f32x4 *>(a.part_o + at * D + 4 * (lane % FR));
         }
-        sum = across_groups_sum<16>(group_sum<16>(sum));
-        if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
-        part[tid / FR][tid % FR] = acc;
-        __syncthreads();
-        sum = (red[4] + red[5]) + (red[6] + red[7]);
-        if (tid < D) {
-            float x = 0.f;
+        if constexpr (PW == 4) {
+            sum = across_groups_sum<16>(sum);
 #pragma unroll
-            for (int i = 0; i < PAR; ++i) x += reinterpret_cast<const float *>(part[i])[tid];
-            store_out<T>(a.out, bh * D + tid, sum == 0.f ? 0.f : x / sum);
+            for (int e = 0; e < 4; ++e) acc[e] = across_groups_sum<16>(acc[e]);
+        } else {
+            float x, y;
+            halves_pair(sum, x, y);
+            sum = x + y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                halves_pair(acc[e], x, y);
+                acc[e] = x + y;
+            }
         }
-        if (tid == 0 && a.lse) a.lse[bh] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
+        if constexpr (WIDE) {
+            if (lane == 0) red[1][w] = sum;
+            if (lane < FR) sums[w][lane] = acc;
+            __syncthreads();
+            if (w > 0) return;
+            sum = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+            acc = (sums[0][lane % FR] + sums[1][lane % FR]) + (sums[2][lane % FR] + sums[3][lane % FR]);
+        }
+        if (lane < FR)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store_out<T>(a.out, bh * D + 4 * lane + e, sum == 0.f ? 0.f : acc[e] / sum);
+        if (lane == 0 && a.lse) a.lse[bh] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * LN2;
         return;
     }
-    const int j0 = ((int)blockIdx.z - a.group) * 1024;
-    if (j0 >= n) return;
-    for (int h = tid >> 6; h < a.group; h += 4) {                   // a wave sums a head's chunks
-        const float2 *ml = a.part_ml + ((int64_t)b * a.n_heads + kv * a.group + h) * a.n_split;
+    const int first = ((int)blockIdx.z - head_blocks) * 1024;
+    if (first >= n) return;
+    // the heads' lse: a lane takes a head of the tile and every sixteenth part
+    for (int tile = 0; tile < a.q_tiles; ++tile) {
+        const int h0 = tile * HEADS, h = lane & 15, heads = a.group - h0 < HEADS ? a.group - h0 : HEADS;
+        const Parts p = parts_of(tile);
+        if (p.count == 1) {
+            if (tid < heads) lse2[h0 + tid] = a.lse2[(int64_t)b * a.n_heads + kv * a.group + h0 + tid];
+            continue;
+        }
         float top = NEG_BIG, sum = 0.f;
-        for (int c = tid & 63; c < chunks; c += 64) top = fmaxf(top, ml[c].x);
-        top = wave_max(top);
-        for (int c = tid & 63; c < chunks; c += 64) sum += ml[c].y * fast_exp2(ml[c].x - top);
-        sum = across_groups_sum<16>(group_sum<16>(sum));
-        if ((tid & 63) == 0) lse2[h] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
+#pragma unroll 4
+        for (uint32_t c = tid >> 4; c < p.count; c += 16) {
+            const float2 x = a.part_ml[slot(p, c) + (h < heads ? h : 0)];
+            const float up = fmaxf(top, x.x);
+            sum = sum * fast_exp2(top - up) + x.y * fast_exp2(x.x - up);
+            top = up;
+        }
+        const float most = across_groups_max<16>(top);
+        sum = across_groups_sum<16>(sum * fast_exp2(top - most));
+        __syncthreads();
+        if (lane < 16) ml_lds[wave][h] = make_float2(most, sum);
+        __syncthreads();
+        if (tid < heads) {
+            top = fmaxf(fmaxf(ml_lds[0][tid].x, ml_lds[1][tid].x), fmaxf(ml_lds[2][tid].x, ml_lds[3][tid].x));
+            sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += ml_lds[i][tid].y * fast_exp2(ml_lds[i][tid].x - top);
+            lse2[h0 + tid] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
+        }
     }
     __syncthreads();
-    const int end = n - j0 < 1024 ? n : j0 + 1024;
-    for (int j = j0 + tid; j < end; j += 256) {
-        int block, place;
-        split_slot(a.g, j, block, place);
-        const int page = page_of(a.g, b, block);
-        if (page < 0) continue;
-        const float *z = a.z + ((int64_t)b * a.n_heads + kv * a.group) * a.z_stride + j;
-        float p = 0.f;
-        for (int h = 0; h < a.group; ++h) p += fast_exp2(z[(int64_t)h * a.z_stride] - lse2[h]);
-        const int64_t i = table_index(a.g, page, kv, place);
-        a.weight_out[i] = (step && j == a.g.seq_len[b] - 1 ? 0.f : a.weight_in[i]) + p;
+    const int newest = step && a.g.seq_len[b] == n ? n - 1 : -1;
+    const float *z0 = a.z + ((int64_t)b * a.n_heads + kv * a.group) * a.z_stride;
+    for (int j = first + 4 * tid; j < n; j += ((int)gridDim.z - head_blocks) * 1024) {
+        f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int h = 0; h < a.group; ++h) {
+            const f32x4 z = *reinterpret_cast<const f32x4 *>(z0 + (int64_t)h * a.z_stride + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] += fast_exp2(z[e] - lse2[h]);
+        }
+        add_weights<QUADS>(a, b, kv, j, n, p, newest);
     }
 }
 
 // ---- launch shapes ---------------------------------------------------------------------------------------------------
 
 struct PagedShape {
-    int q_tiles, chunk, n_split;
-    bool whole;
+    int round, q_tiles, tile_heads, workgroups, stage;
+    int64_t reach;            // rows, in whole rounds
 };
 
-// Rows of a chunk: as many as leave the chip enough workgroups, 128 (a tile for each wave) to 1024.
 static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     PagedShape s;
     const int reach = paged_reach(c, max_len), group = c->n_heads / c->n_kv_heads;
+    s.round = c->dtype == SSD_BF16 ? 128 : 64;
     s.q_tiles = (group + HEADS - 1) / HEADS;
-    const int64_t units = (int64_t)c->n_seqs * c->n_kv_heads * s.q_tiles;
-    s.chunk = CHUNK_MAX;
-    while (s.chunk > 128 && units * ((reach + s.chunk - 1) / s.chunk) < 8192) s.chunk /= 2;
-    s.n_split = (reach + s.chunk - 1) / s.chunk;
-    s.whole = s.n_split == 1 && s.q_tiles == 1;
-
+    s.tile_heads = group < HEADS ? group : HEADS;
+    const int64_t units = (int64_t)c->n_seqs * c->n_kv_heads * s.q_tiles, rounds = (reach + s.round - 1) / s.round;
+    s.reach = rounds * s.round;
+    // Units that nothing can divide, or so many short ones that the chip is evenly loaded without, are not counted and dealt but taken
+    // as they come; so are sums that 32 bits would not hold.
+    const bool plain = rounds == 1 || (units >= 2048 && rounds <= 8) || units * rounds >= 1ll << 31;
+    s.workgroups = plain ? 0 : (int)(units * rounds < 768 ? units * rounds : 768);
+    // a stage's blocks: its rows and what lies before them in the first one, in at most BLOCKS entries; block_of allows 2^16 rows
+    const int64_t most = (int64_t)(BLOCKS - 1) * c->page_size;
+    s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);
     return s;
 }
 
-struct PagedScratch { size_t z, o, ml, all; };
+struct PagedScratch { size_t z, lse2, o, ml, all; };
 
 static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s, bool weights) {
     PagedScratch w;
-    const size_t bh = (size_t)c->n_seqs * c->n_heads;
-    w.z = weights ? round256(bh * s.n_split * s.chunk * sizeof(float)) : 0;
-    w.o = s.whole ? 0 : round256(bh * s.n_split * c->head_dim * sizeof(float));
-    w.ml = s.whole ? 0 : round256(bh * s.n_split * sizeof(float2));
-    w.all = w.z + w.o + w.ml;
+    const size_t bh = (size_t)c->n_seqs * c->n_heads, parts = (size_t)2 * s.workgroups * s.tile_heads;
+    w.z = weights ? round256(bh * s.reach * sizeof(float)) : 0;
+    w.lse2 = weights ? round256(bh * sizeof(float)) : 0;
+    w.o = round256(parts * c->head_dim * sizeof(float));
+    w.ml = round256(parts * sizeof(float2));
+    w.all = w.z + w.lse2 + w.o + w.ml;
     return w;
 }
 
-template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(const PagedAttnArgs &a, const PagedShape &sh, bool step, hipStream_t s) {
-    const int heads = a.group < HEADS ? a.group : HEADS;
-    const size_t lds = (size_t)WAVES * heads * (D + 4) * sizeof(float);
-    const dim3 grid((unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs, (unsigned)sh.n_split);
-    const dim3 wg(64 * WAVES);
-    if (step && a.weight_out) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true>), grid, wg, lds, s, a);
+template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(PagedAttnArgs a, const PagedShape &sh, bool step, hipStream_t s) {
+    const bool weights = a.weight_out != nullptr;
+    const dim3 wg(64 * WAVES), grid = sh.workgroups ? dim3((unsigned)sh.workgroups) : dim3((unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs);
+    const size_t lds = (size_t)WAVES * a.tile_heads * (D + 4) * sizeof(float);
+    if (step && weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true>), grid, wg, lds, s, a);
     else if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, false>), grid, wg, lds, s, a);
-    else if (a.weight_out) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, true>), grid, wg, lds, s, a);
+    else if (weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, true>), grid, wg, lds, s, a);
     else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, false>), grid, wg, lds, s, a);
-    if (!sh.whole) {
-        const unsigned pieces = a.weight_out ? (unsigned)(a.g.max_len + 1023) / 1024 : 0;
-        hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs, (unsigned)a.group + pieces), dim3(256),
-                           (size_t)a.group * sizeof(float), s, a, step ? 1 : 0);
-    }
+    if (!sh.workgroups && !weights) return hipGetLastError();
+    const int64_t units = (int64_t)a.g.n_seqs * a.g.n_kv;
+    const bool wide = units * a.group < 1024;
+    const int head_blocks = !sh.workgroups ? 0 : wide ? a.group : (a.group + 3) / 4;
+    int64_t pieces = weights ? (sh.reach + 1023) / 1024 : 0;
+    const int64_t enough = 4096 / units + 1;
+    if (pieces > enough) pieces = enough;
+    const dim3 join((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs, (unsigned)(head_blocks + pieces));
+    const size_t lse = (size_t)a.group * sizeof(float);
+    if (wide) hipLaunchKernelGGL((paged_join_kernel<T, D, QUADS, true>), join, dim3(256), lse, s, a, step ? 1 : 0, head_blocks);
+    else hipLaunchKernelGGL((paged_join_kernel<T, D, QUADS, false>), join, dim3(256), lse, s, a, step ? 1 : 0, head_blocks);
     return hipGetLastError();
 }
 
@@ -622,20 +818,21 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     a.out = static_cast<char *>(out);
     a.lse = lse;
     char *ws = static_cast<char *>(workspace);
-    a.z = parts.z ? reinterpret_cast<float *>(ws) : nullptr;
-    a.part_o = reinterpret_cast<float *>(ws + parts.z);
-    a.part_ml = reinterpret_cast<float2 *>(ws + parts.z + parts.o);
+    a.z = reinterpret_cast<float *>(ws);
+    a.lse2 = reinterpret_cast<float *>(ws + parts.z);
+    a.part_o = reinterpret_cast<float *>(ws + parts.z + parts.lse2);
+    a.part_ml = reinterpret_cast<float2 *>(ws + parts.z + parts.lse2 + parts.o);
     a.k_new = static_cast<const char *>(k_new);
     a.v_new = static_cast<const char *>(v_new);
     a.k_dst = static_cast<char *>(k_pages);
     a.v_dst = static_cast<char *>(v_pages);
     a.pos = pos;
     a.new_stride = (cfg->new_stride ? cfg->new_stride : (int64_t)cfg->n_kv_heads * cfg->head_dim) * (int64_t)paged_esize(cfg);
-    a.z_stride = (int64_t)shape.n_split * shape.chunk;
+    a.z_stride = shape.reach;
     a.q_tiles = shape.q_tiles;
-    a.chunk = shape.chunk;
-    a.n_split = shape.n_split;
-
+    a.tile_heads = shape.tile_heads;
+    a.workgroups = shape.workgroups;
+    a.stage = shape.stage;
     a.single = cfg->page_size == 1;
     a.page_magic = (uint32_t)((0xffffffffull + (unsigned)cfg->page_size) / (unsigned)cfg->page_size);
     a.q_stride = (cfg->q_stride ? cfg->q_stride : (int64_t)cfg->n_heads * cfg->head_dim) * (int64_t)paged_esize(cfg);
