@@ -47,8 +47,8 @@ struct PagedAttnArgs {
     float scale;              // softmax scale * log2 e
 };
 
-static constexpr int WAVES = 4;
-static constexpr int BLOCKS = 1024;                                // entries of the block table in LDS
+// entries of the block table that a workgroup has in LDS
+static constexpr int blocks_of(int waves) { return 256 * waves; }
 static constexpr int HEADS = 16;                                   // heads of a tile
 static constexpr int64_t NO_PAGE = -(1ll << 62);
 static constexpr float LN2 = 0.6931471805599453f;
@@ -310,13 +310,13 @@ static __device__ __forceinline__ const PagedAttnArgs &arguments() {
 }
 
 // grid = (workgroups), or (kv heads * tiles of query heads, sequences) where a workgroup takes a whole unit
-template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS>
+template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs) {
     typedef Tile<T, D> TT;
     constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
     constexpr int ROUND = WAVES * TT::ROWS;
     constexpr int LD = D + 4;                                       // row of the merge area
-    __shared__ int64_t pages[BLOCKS];
+    __shared__ int64_t pages[blocks_of(WAVES)];
     __shared__ float sm_ml[WAVES][HEADS][2];
     extern __shared__ float sm_o[];                                 // [WAVES][tile_heads][LD]
 
@@ -596,7 +596,7 @@ static __device__ __forceinline__ float wave_max(float v) {
 // grid = (kv heads, sequences, head_blocks + a few)
 template <typename T, int D, bool QUADS, bool WIDE>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int step, int head_blocks) {
-    constexpr int ROUND = WAVES * Tile<T, D>::ROWS;
+    constexpr int ROUND = 4 * Tile<T, D>::ROWS;
     constexpr int FR = D / 4, PW = 64 / FR, NW = WIDE ? 4 : 1;      // 16-byte pieces of a part's sums; parts a wave reads side by side; waves
     __shared__ float red[2][4];
     __shared__ f32x4 sums[4][FR];
@@ -726,24 +726,28 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
 // ---- launch shapes ---------------------------------------------------------------------------------------------------
 
 struct PagedShape {
-    int round, q_tiles, tile_heads, workgroups, stage;
+    int waves, round, q_tiles, tile_heads, workgroups, stage;
     int64_t reach;            // rows, in whole rounds
 };
 
 static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     PagedShape s;
     const int reach = paged_reach(c, max_len), group = c->n_heads / c->n_kv_heads;
-    s.round = c->dtype == SSD_BF16 ? 128 : 64;
+    const int tile = c->dtype == SSD_BF16 ? 32 : 16;
     s.q_tiles = (group + HEADS - 1) / HEADS;
     s.tile_heads = group < HEADS ? group : HEADS;
-    const int64_t units = (int64_t)c->n_seqs * c->n_kv_heads * s.q_tiles, rounds = (reach + s.round - 1) / s.round;
-    s.reach = rounds * s.round;
-    // Units that nothing can divide, or so many short ones that the chip is evenly loaded without, are not counted and dealt but taken
-    // as they come; so are sums that 32 bits would not hold.
-    const bool plain = rounds == 1 || (units >= 2048 && rounds <= 8) || units * rounds >= 1ll << 31;
+    const int64_t units = (int64_t)c->n_seqs * c->n_kv_heads * s.q_tiles, rounds = (reach + 4 * tile - 1) / (4 * tile);
+    s.reach = rounds * 4 * tile;
+    // A unit of few rounds is taken whole (8 units of 512 rows 9.1 us whole and 10.6 dealt, 512 of 512 24 and 30); with more rounds only where
+    // units are many (512 of 1024 rows 44 and 51, of 10 to 1024 25 and 23, of 2048 84 and 91, of 10 to 2048 44 and 29; 128 of 1024 20 and 19),
+    // and where 32 bits would not hold the sums.
+    const bool plain = rounds <= 4 || (units >= 512 && rounds <= 8) || units * rounds >= 1ll << 31;
+    // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
+    s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
+    s.round = s.waves * tile;
     s.workgroups = plain ? 0 : (int)(units * rounds < 768 ? units * rounds : 768);
-    // a stage's blocks: its rows and what lies before them in the first one, in at most BLOCKS entries; block_of allows 2^16 rows
-    const int64_t most = (int64_t)(BLOCKS - 1) * c->page_size;
+    // a stage's blocks: its rows and what lies before them in the first one; block_of allows 2^16 rows
+    const int64_t most = (int64_t)(blocks_of(s.waves) - 1) * c->page_size;
     s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);
     return s;
 }
@@ -761,14 +765,20 @@ static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s
     return w;
 }
 
-template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(PagedAttnArgs a, const PagedShape &sh, bool step, hipStream_t s) {
+template <typename T, int D, bool QUADS, int WAVES> static void launch_paged_rows(const PagedAttnArgs &a, const PagedShape &sh, bool step, hipStream_t s) {
     const bool weights = a.weight_out != nullptr;
     const dim3 wg(64 * WAVES), grid = sh.workgroups ? dim3((unsigned)sh.workgroups) : dim3((unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs);
     const size_t lds = (size_t)WAVES * a.tile_heads * (D + 4) * sizeof(float);
-    if (step && weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true>), grid, wg, lds, s, a);
-    else if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, false>), grid, wg, lds, s, a);
-    else if (weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, true>), grid, wg, lds, s, a);
-    else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, false>), grid, wg, lds, s, a);
+    if (step && weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true, WAVES>), grid, wg, lds, s, a);
+    else if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, false, WAVES>), grid, wg, lds, s, a);
+    else if (weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, true, WAVES>), grid, wg, lds, s, a);
+    else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, false, WAVES>), grid, wg, lds, s, a);
+}
+
+template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(const PagedAttnArgs &a, const PagedShape &sh, bool step, hipStream_t s) {
+    const bool weights = a.weight_out != nullptr;
+    if (sh.waves == 1) launch_paged_rows<T, D, QUADS, 1>(a, sh, step, s);
+    else launch_paged_rows<T, D, QUADS, 4>(a, sh, step, s);
     if (!sh.workgroups && !weights) return hipGetLastError();
     const int64_t units = (int64_t)a.g.n_seqs * a.g.n_kv;
     const bool wide = units * a.group < 1024;
