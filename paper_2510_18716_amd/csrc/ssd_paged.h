@@ -55,9 +55,4 @@ static inline int paged_reach(const ssd_paged_config *c, int max_len) {
 static inline size_t paged_esize(const ssd_paged_config *c) { return c->dtype == SSD_F32 ? 4 : 2; }
 static inline size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-// the launch behind ssd_paged_append, all arguments checked (ssd_paged_decode_step takes it too)
-int launch_paged_append(const ssd_paged_config *c, void *k_pages, void *v_pages, int32_t *pos, float *weight, const int32_t *block_table,
-                        const int32_t *seq_len, const int32_t *seq_pos, int max_len, const void *k_new, const void *v_new,
-                        const int32_t *new_start, int n_new, const float *weight_new, hipStream_t s);
-
 }  // namespace ssd
