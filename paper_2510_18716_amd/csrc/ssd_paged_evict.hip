@@ -1,9 +1,11 @@
 // ssd_paged_evict: each (sequence, kv head) of a paged cache is cut to its budget; the rows of the largest accumulated attention weight
 // stay (the top-M rule of Algorithm 1, sinks and recent tokens protected as in Sec. 3.3).
 //
-// Two launches.  Selection: one workgroup per unit finds the key of the last row that stays by a radix descent over the keys
-// (weight, position) -- integer compares, so the set is exact -- and lists the slots that become free below n' and the kept rows
-// above, both in slot order.  Movement: the rows of the lists, 16-byte fragments.
+// A unit's selection is one workgroup's: the key of the last row that stays is found by a descent over the keys' bits (weight first,
+// then position; whole-number compares, so the set is exact), eight bits a step by a histogram in LDS, beginning at the first bit in which the
+// weights differ.  Up to 16384 rows a thread keeps its rows' keys in registers, and the tables are read once; longer units are read anew for every
+// step, eleven bits each.  Then every thread ranks its free slots below n' and its kept rows above by one scan over the workgroup, and the rows
+// move, in 16-byte fragments: by the same workgroup where units are many, by a second launch with more workgroups per unit otherwise.
 #include "ssd_paged.h"
 
 namespace ssd {
@@ -24,154 +26,80 @@ struct PagedEvictArgs {
 
 static __host__ __device__ inline int64_t moves_of(int cap, int64_t unit) { return unit * (2 * (int64_t)cap + 1); }
 
-// Larger is better: the weight, then the lower position.
-static __device__ __forceinline__ unsigned long long evict_key(float w, int pos) {
-    uint32_t u = __float_as_uint(w);
-    if ((u & 0x7fffffffu) > 0x7f800000u) u = 0;                                   // NaN: below everything
-    else if (u == 0x80000000u) u = 0x80000000u;                                   // -0 as +0
-    else u = u & 0x80000000u ? ~u : u | 0x80000000u;
-    return (unsigned long long)u << 32 | (uint32_t)~((uint32_t)pos ^ 0x80000000u);
+// Larger is better.  Weights: NaN below everything, -0 as +0, the rest by their bits turned into an ascending order.
+static __device__ __forceinline__ uint32_t weight_key(float w) {
+    const uint32_t u = __float_as_uint(w);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
+    if (u << 1 == 0) return 0x80000000u;
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+static __device__ __forceinline__ uint32_t pos_key(int pos) { return ~((uint32_t)pos ^ 0x80000000u); }
 
-struct EvictRow { unsigned long long key; bool safe; };
+struct Four { float w[4]; int pos[4]; };
 
-static __device__ __forceinline__ EvictRow evict_row(const PagedEvictArgs &a, int b, int kv, int j, int total) {
+// Weights and positions of rows j .. j + 3 (those below n).
+static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b, int kv, int j, int n) {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));
+    Four r;
     int block, place;
     split_slot(a.g, j, block, place);
-    const int page = page_of(a.g, b, block);
-    float w = __uint_as_float(0x7fc00000u);
-    int pos = 0;
-    if (page >= 0) {
-        const int64_t i = table_index(a.g, page, kv, place);
-        w = a.weight_in[i];
-        pos = a.pos_in[i];
-    }
-    return {evict_key(w, pos), pos < a.n_sink || (int64_t)pos >= (int64_t)total - a.recent};
-}
-
-// Position of this thread among those of the workgroup whose flag is set, and how many there are.
-static __device__ __forceinline__ int block_rank(bool flag, uint32_t *lds, int &all) {
-    const unsigned long long m = __ballot(flag);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    __syncthreads();
-    if (lane == 0) lds[wave] = (uint32_t)__popcll(m);
-    __syncthreads();
-    int before = 0;
-    all = 0;
-    for (int i = 0; i < (int)(blockDim.x >> 6); ++i) {
-        if (i < wave) before += (int)lds[i];
-        all += (int)lds[i];
-    }
-    return before + __popcll(m & ((1ull << lane) - 1));
-}
-
-__global__ __launch_bounds__(1024) void paged_select_kernel(PagedEvictArgs a) {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t lds[16];
-    __shared__ int found[3];
-    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-    const int n = clamp_len(a.g, b);
-    const int want = a.budget[b] < 0 ? 0 : a.budget[b];
-    const int stay = n < want ? n : want;
-    int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
-    if (kv == 0 && tid == 0 && a.len_out) a.len_out[b] = stay;
-    const bool copy = a.pos_out != a.pos_in;
-    const int total = a.g.seq_pos[b];
-    int count = 0, all;
-
-    // which rows compete, and for how many places
-    int safe_rows = 0;
-    if (stay < n)
-        for (int j0 = 0; j0 < n; j0 += 1024) {
-            const int j = j0 + tid;
-            block_rank(j < n && evict_row(a, b, kv, j, total).safe, lds, all);
-            safe_rows += all;
+    if (place + 4 <= a.g.page_size) {
+        const int page = page_of(a.g, b, block);
+        const int64_t i = table_index(a.g, page < 0 ? 0 : page, kv, place);
+        const f4 w = *reinterpret_cast<const f4 *>(a.weight_in + i);
+        const i4 p = *reinterpret_cast<const i4 *>(a.pos_in + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            r.w[e] = page < 0 ? __uint_as_float(0x7fc00000u) : w[e];
+            r.pos[e] = page < 0 ? 0 : p[e];
         }
-    const bool among_safe = safe_rows >= stay;
-    int left = among_safe ? stay : stay - safe_rows;
-
-    // the key of the last row that stays, and how many of its equals
-    unsigned long long last = 0;
-    int ties = 0;
-    if (stay < n && left > 0) {
-        int shift = 64;
-        while (shift > 0) {
-            shift -= 8;
-            for (int i = tid; i < 256; i += 1024) hist[i] = 0;
-            __syncthreads();
-            for (int j = tid; j < n; j += 1024) {
-                const EvictRow r = evict_row(a, b, kv, j, total);
-                if (r.safe == among_safe && (shift == 56 || r.key >> (shift + 8) == last >> (shift + 8)))
-                    atomicAdd(&hist[(int)(r.key >> shift) & 255], 1u);
-            }
-            __syncthreads();
-            if (tid == 0) {
-                int above = 0, digit = 255;
-                while (digit > 0 && above + (int)hist[digit] < left) above += (int)hist[digit--];
-                found[0] = digit;
-                found[1] = above;
-                found[2] = (int)hist[digit];
-            }
-            __syncthreads();
-            last |= (unsigned long long)found[0] << shift;
-            left -= found[1];
-            ties = left;
-            const bool whole = found[2] == left;
-            __syncthreads();
-            if (whole) {                       // all of them stay: nothing below needs looking at
-                ties = n;
-                break;
-            }
-        }
+        return r;
     }
-
-    int n_free = 0, n_move = 0, n_tie = 0;
-    for (int j0 = 0; j0 < n && (stay < n || copy); j0 += 1024) {
-        const int j = j0 + tid;
-        bool kept = j < n;
-        if (stay < n) {
-            const EvictRow r = evict_row(a, b, kv, j < n ? j : n - 1, total);
-            const bool competes = j < n && r.safe == among_safe && stay > 0 && (among_safe || stay > safe_rows);
-            const bool tie = competes && r.key == last;
-            const int rank = n_tie + block_rank(tie, lds, all);
-            n_tie += all;
-            kept = j < n && ((r.safe && !among_safe) || (competes && (r.key > last || (tie && rank < ties))));
-            const int f = n_free + block_rank(j < stay && !kept, lds, all);
-            n_free += all;
-            if (j < stay && !kept) list[1 + f] = j;
-            const int m = n_move + block_rank(j >= stay && kept, lds, all);
-            n_move += all;
-            if (j >= stay && kept) list[1 + a.cap + m] = j;
-        }
-        if (copy && kept && j < stay) {
-            int block, place;
-            split_slot(a.g, j, block, place);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        r.w[e] = __uint_as_float(0x7fc00000u);
+        r.pos[e] = 0;
+        if (j + e < n) {
+            split_slot(a.g, j + e, block, place);
             const int page = page_of(a.g, b, block);
             if (page >= 0) {
                 const int64_t i = table_index(a.g, page, kv, place);
-                a.pos_out[i] = a.pos_in[i];
-                a.weight_out[i] = a.weight_in[i];
+                r.w[e] = a.weight_in[i];
+                r.pos[e] = a.pos_in[i];
             }
         }
     }
-    count = n_move;
-    if (tid == 0) list[0] = count;
+    return r;
 }
 
-// grid = (pieces of the list, kv heads, sequences)
-__global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
-    const int kv = blockIdx.y, b = blockIdx.z;
-    const int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
-    const int count = list[0], lanes = 2 << a.lpr_log2;          // a row of K and one of V
-    const int per = 256 / lanes, lane = threadIdx.x & (lanes - 1);
+static __device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += (uint32_t)__shfl_xor((int)v, o);
+    return v;
+}
+static __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t w = (uint32_t)__shfl_up((int)v, o);
+        v += lane >= o ? w : 0;
+    }
+    return v;
+}
+
+// Rows from[i] to slots to[i], i = first, first + step, ..; K and V of a row by neighbouring threads, their table entries by the first of them.
+static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b, int kv, const int32_t *to, const int32_t *from, int count, int thread,
+                                                 int threads) {
+    const int lanes = 2 << a.lpr_log2, lane = thread & (lanes - 1);
     const bool v = lane >> a.lpr_log2;
     const int64_t sub = (int64_t)(lane & ((1 << a.lpr_log2) - 1)) * 16;
     char *pool = v ? a.v_pages : a.k_pages;
-    for (int i = (int)blockIdx.x * per + (int)threadIdx.x / lanes; i < count; i += (int)gridDim.x * per) {
-        const int to = list[1 + i], from = list[1 + a.cap + i];
+#pragma unroll 4
+    for (int i = thread / lanes; i < count; i += threads / lanes) {
         int tb, tp, fb, fp;
-        split_slot(a.g, to, tb, tp);
-        split_slot(a.g, from, fb, fp);
+        split_slot(a.g, to[i], tb, tp);
+        split_slot(a.g, from[i], fb, fp);
         const int tpage = page_of(a.g, b, tb), fpage = page_of(a.g, b, fb);
         if (tpage < 0 || fpage < 0) continue;
         *reinterpret_cast<uint4 *>(pool + row_offset(a.g, tpage, kv, tp) + sub) =
@@ -182,6 +110,272 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
             a.weight_out[t] = a.weight_in[f];
         }
     }
+}
+
+// KEYS: rows whose keys a thread keeps, consecutive ones; 0: none, the tables are read again for every step.  grid = (kv heads, sequences)
+template <int THREADS, int KEYS>
+__global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a, int move_here) {
+    constexpr int NW = THREADS / 64, BITS = KEYS ? 8 : 11, BINS = 1 << BITS, LEVELS = 2 * ((32 + BITS - 1) / BITS);
+    constexpr int HISTS = KEYS ? LEVELS : 1;                        // one histogram per step, or one that is cleared in between
+    __shared__ uint32_t hist[HISTS][BINS];
+    __shared__ uint32_t red[3][NW];
+    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = clamp_len(a.g, b);
+    const int want = a.budget[b] < 0 ? 0 : a.budget[b];
+    const int stay = n < want ? n : want;
+    const bool copy = a.pos_out != a.pos_in;
+    const int64_t total = a.g.seq_pos[b];
+    int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
+    if (kv == 0 && tid == 0 && a.len_out) a.len_out[b] = stay;
+    if (n == stay && !copy) {
+        if (tid == 0) list[0] = 0;
+        return;
+    }
+    for (int i = tid; i < HISTS * BINS; i += THREADS) (&hist[0][0])[i] = 0;
+
+    // what a thread looks at: its own rows in registers, or all rows of the unit with stride THREADS * 4, read again
+    uint32_t wk[KEYS ? KEYS : 1], pk[KEYS ? KEYS : 1], safe_bits = 0;
+    auto is_safe = [&](int pos) { return pos < a.n_sink || (int64_t)pos >= total - a.recent; };
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int k = 0; k < KEYS; k += 4) {
+            const int j = tid * KEYS + k;
+            if (j < n) {
+                const Four r = table_rows(a, b, kv, j, n);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    wk[k + e] = weight_key(r.w[e]);
+                    pk[k + e] = pos_key(r.pos[e]);
+                    safe_bits |= is_safe(r.pos[e]) ? 1u << (k + e) : 0u;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wk[k + e] = pk[k + e] = 0;
+            }
+        }
+    }
+    auto each = [&](auto f) {                                      // f(weight key, position key, safe)
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int k = 0; k < KEYS; ++k)
+                if (tid * KEYS + k < n) f(wk[k], pk[k], (safe_bits >> k & 1) != 0);
+        } else {
+#pragma unroll 2
+            for (int j = 4 * tid; j < n; j += 4 * THREADS) {
+                const Four r = table_rows(a, b, kv, j, n);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < n) f(weight_key(r.w[e]), pos_key(r.pos[e]), is_safe(r.pos[e]));
+            }
+        }
+    };
+
+    // which rows compete and for how many places; the bits in which the weights of each kind differ
+    uint32_t last_w = 0, last_p = 0;                               // keys of the last row that stays
+    int ties = 0;                                                  // how many rows with just these keys stay
+    bool among_safe = false, compete = false;
+    if (stay < n && stay > 0) {
+        uint32_t safe_rows = 0, or_s = 0, and_s = ~0u, or_o = 0, and_o = ~0u;
+        each([&](uint32_t w, uint32_t, bool safe) {
+            safe_rows += safe;
+            or_s |= safe ? w : 0;
+            and_s &= safe ? w : ~0u;
+            or_o |= safe ? 0 : w;
+            and_o &= safe ? ~0u : w;
+        });
+        safe_rows = wave_sum(safe_rows);
+        if (lane == 0) red[0][wave] = safe_rows;
+        __syncthreads();
+        safe_rows = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) safe_rows += red[0][i];
+        among_safe = (int)safe_rows >= stay;
+        int left = among_safe ? stay : stay - (int)safe_rows;
+        compete = left > 0;
+        uint32_t any = among_safe ? or_s : or_o, every = among_safe ? and_s : and_o;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            any |= (uint32_t)__shfl_xor((int)any, o);
+            every &= (uint32_t)__shfl_xor((int)every, o);
+        }
+        if (lane == 0) {
+            red[1][wave] = any;
+            red[2][wave] = every;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            any |= red[1][i];
+            every &= red[2][i];
+        }
+        const uint32_t differ = any ^ every;
+        int bits = differ ? 32 - __clz((int)differ) : 0;           // bits of the weight still open
+        last_w = bits == 32 ? 0 : every >> bits << bits;
+        bool on_pos = bits == 0, whole = false;
+        if (on_pos) bits = 32;
+        for (int level = 0; compete && !whole; ++level) {
+            const int take = bits < BITS ? bits : BITS, shift = bits - take;
+            uint32_t *h = hist[KEYS ? level : 0];
+            const uint32_t mask = (1u << take) - 1;
+            each([&](uint32_t w, uint32_t p, bool safe) {
+                const uint32_t key = on_pos ? p : w, ref = on_pos ? last_p : last_w;
+                const bool in = safe == among_safe && (!on_pos || w == last_w) && (bits == 32 || key >> bits == ref >> bits);
+                if (in) atomicAdd(&h[key >> shift & mask], 1u);
+            });
+            __syncthreads();
+            // the digit in which the place falls: every wave adds up the bins from the top, BINS / 64 a lane
+            constexpr int PER = BINS / 64;
+            uint32_t sum = 0, mine[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                mine[i] = h[BINS - 1 - (lane * PER + i)];
+                sum += mine[i];
+            }
+            const uint32_t upto = wave_scan(sum);
+            const int l = __ffsll((unsigned long long)__ballot(upto >= (uint32_t)left)) - 1;
+            uint32_t above = upto - sum, in_bin = 0;
+            int digit = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const bool here = above < (uint32_t)left && above + mine[i] >= (uint32_t)left;
+                if (here && in_bin == 0) {
+                    digit = BINS - 1 - (lane * PER + i);
+                    in_bin = mine[i];
+                }
+                if (in_bin == 0) above += mine[i];
+            }
+            digit = __builtin_amdgcn_readlane(digit, l);
+            above = (uint32_t)__builtin_amdgcn_readlane((int)above, l);
+            in_bin = (uint32_t)__builtin_amdgcn_readlane((int)in_bin, l);
+            left -= (int)above;
+            if (on_pos) last_p |= (uint32_t)digit << shift;
+            else last_w |= (uint32_t)digit << shift;
+            bits = shift;
+            whole = (int)in_bin == left;                           // all of them stay: nothing below needs looking at
+            if (bits == 0) {
+                if (on_pos) break;
+                on_pos = true;
+                bits = 32;
+            }
+            if constexpr (KEYS == 0) {
+                if (!whole) {
+                    __syncthreads();
+                    for (int i = tid; i < BINS; i += THREADS) hist[0][i] = 0;
+                    __syncthreads();
+                }
+            }
+        }
+        ties = whole ? n : left;
+    }
+    // Rows above the last one's keys stay; so do those equal to them while there are ties left.  Where the descent ended early, the bits
+    // below are 0 in the last keys, and everything at or above them stays.
+    auto level_of = [&](uint32_t w, uint32_t p) {                  // 2: stays, 1: equal, 0: goes
+        if (w != last_w) return w > last_w ? 2 : 0;
+        return p > last_p ? 2 : p == last_p ? 1 : 0;
+    };
+
+    // who stays, where slots become free, which rows move
+    constexpr int HAVE = KEYS ? KEYS : 4;
+    uint32_t seen_tie = 0, seen_free = 0, seen_move = 0;
+    for (int base = 0; base < n; base += THREADS * HAVE) {
+        const int j0 = base + tid * HAVE;
+        uint32_t kept = 0, tie = 0;
+        Four r;
+        if constexpr (KEYS == 0) {
+            if (j0 < n) r = table_rows(a, b, kv, j0, n);
+        }
+#pragma unroll
+        for (int k = 0; k < HAVE; ++k) {
+            if (j0 + k >= n) continue;
+            bool safe;
+            uint32_t w, p;
+            if constexpr (KEYS > 0) {
+                safe = safe_bits >> k & 1;
+                w = wk[k];
+                p = pk[k];
+            } else {
+                safe = is_safe(r.pos[k]);
+                w = weight_key(r.w[k]);
+                p = pos_key(r.pos[k]);
+            }
+            int lv = stay == n ? 2 : stay == 0 ? 0 : safe != among_safe ? (safe ? 2 : 0) : compete ? level_of(w, p) : 0;
+            kept |= lv == 2 ? 1u << k : 0u;
+            tie |= lv == 1 ? 1u << k : 0u;
+        }
+        if (stay < n) {
+            if (ties >= n) {
+                kept |= tie;
+            } else {                                               // equal keys: the lowest slots
+                const uint32_t c = (uint32_t)__popc(tie), up = wave_scan(c);
+                __syncthreads();
+                if (lane == 63) red[0][wave] = up;
+                __syncthreads();
+                uint32_t before = seen_tie + up - c;
+#pragma unroll
+                for (int i = 0; i < NW; ++i) {
+                    before += i < wave ? red[0][i] : 0;
+                    seen_tie += red[0][i];
+                }
+#pragma unroll
+                for (int k = 0; k < HAVE; ++k)
+                    if (tie >> k & 1) {
+                        kept |= (int)before < ties ? 1u << k : 0u;
+                        ++before;
+                    }
+            }
+            const int below = stay - j0 < 0 ? 0 : stay - j0 < HAVE ? stay - j0 : HAVE, there = n - j0 < 0 ? 0 : n - j0 < HAVE ? n - j0 : HAVE;
+            const uint32_t low = below == 32 ? ~0u : (1u << below) - 1, in = there == 32 ? ~0u : (1u << there) - 1;
+            const uint32_t free_bits = in & low & ~kept, move_bits = kept & ~low;
+            const uint32_t c = (uint32_t)__popc(free_bits) | (uint32_t)__popc(move_bits) << 16, up = wave_scan(c);
+            __syncthreads();
+            if (lane == 63) red[1][wave] = up;
+            __syncthreads();
+            uint32_t before = up - c, all = 0;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                before += i < wave ? red[1][i] : 0;
+                all += red[1][i];
+            }
+            uint32_t f = seen_free + (before & 0xffff), m = seen_move + (before >> 16);
+            seen_free += all & 0xffff;
+            seen_move += all >> 16;
+#pragma unroll
+            for (int k = 0; k < HAVE; ++k) {
+                if (free_bits >> k & 1) list[1 + f++] = j0 + k;
+                if (move_bits >> k & 1) list[1 + a.cap + m++] = j0 + k;
+            }
+        }
+        if (copy) {
+            int block, place;
+            split_slot(a.g, j0 < n ? j0 : 0, block, place);
+#pragma unroll
+            for (int k = 0; k < HAVE; ++k) {
+                if (j0 + k >= stay) break;
+                if (k > 0 && ++place == a.g.page_size) {
+                    place = 0;
+                    ++block;
+                }
+                if (!(kept >> k & 1)) continue;
+                const int page = page_of(a.g, b, block);
+                if (page < 0) continue;
+                const int64_t i = table_index(a.g, page, kv, place);
+                a.pos_out[i] = a.pos_in[i];
+                a.weight_out[i] = a.weight_in[i];
+            }
+        }
+    }
+    if (tid == 0) list[0] = (int32_t)seen_move;
+    if (move_here && seen_move > 0) {
+        __syncthreads();
+        move_rows(a, b, kv, list + 1, list + 1 + a.cap, (int)seen_move, tid, THREADS);
+    }
+}
+
+// grid = (kv heads, sequences, workgroups per unit)
+__global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
+    const int kv = blockIdx.x, b = blockIdx.y;
+    const int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
+    move_rows(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)(blockIdx.z * 256 + threadIdx.x), (int)gridDim.z * 256);
 }
 
 static int evict_cap(const ssd_paged_config *c, int max_len) { return paged_reach(c, max_len) / 2 + 1; }
@@ -234,9 +428,18 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     a.lpr_log2 = __builtin_ctz((unsigned)((size_t)cfg->head_dim * paged_esize(cfg) / 16));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 units((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs);
-    hipLaunchKernelGGL(paged_select_kernel, units, dim3(1024), 0, s, a);
-    const unsigned pieces = (unsigned)(a.cap + 127) / 128;
-    hipLaunchKernelGGL(paged_move_kernel, dim3(pieces < 256 ? pieces : 256, units.x, units.y), dim3(256), 0, s, a);
+    const int64_t n_units = (int64_t)units.x * units.y;
+    const int move_here = n_units >= 128;
+    const int reach = a.g.max_len;
+    if (reach <= 256) hipLaunchKernelGGL((paged_select_kernel<64, 4>), units, dim3(64), 0, s, a, move_here);
+    else if (reach <= 2048) hipLaunchKernelGGL((paged_select_kernel<256, 8>), units, dim3(256), 0, s, a, move_here);
+    else if (reach <= 8192) hipLaunchKernelGGL((paged_select_kernel<1024, 8>), units, dim3(1024), 0, s, a, move_here);
+    else if (reach <= 16384) hipLaunchKernelGGL((paged_select_kernel<1024, 16>), units, dim3(1024), 0, s, a, move_here);
+    else hipLaunchKernelGGL((paged_select_kernel<1024, 0>), units, dim3(1024), 0, s, a, move_here);
+    if (!move_here) {
+        const int64_t pieces = (a.cap + 31) / 32, enough = 2048 / n_units + 1;
+        hipLaunchKernelGGL(paged_move_kernel, dim3(units.x, units.y, (unsigned)(pieces < enough ? pieces : enough)), dim3(256), 0, s, a);
+    }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSD_OK : hip_fail(e, "paged eviction launch");
 }
