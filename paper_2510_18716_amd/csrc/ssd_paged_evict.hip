@@ -89,26 +89,54 @@ static __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
 }
 
 // Rows from[i] to slots to[i], i = first, first + step, ..; K and V of a row by neighbouring threads, their table entries by the first of them.
+// A thread has MOVES rows' loads in flight at each of the three stages (list, block table, row); past the end it repeats the last row, which
+// writes the same again.
+static constexpr int MOVES = 8;
 static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b, int kv, const int32_t *to, const int32_t *from, int count, int thread,
                                                  int threads) {
-    const int lanes = 2 << a.lpr_log2, lane = thread & (lanes - 1);
+    const int lanes = 2 << a.lpr_log2, lane = thread & (lanes - 1), step = threads / lanes;
     const bool v = lane >> a.lpr_log2;
-    const int64_t sub = (int64_t)(lane & ((1 << a.lpr_log2) - 1)) * 16;
-    char *pool = v ? a.v_pages : a.k_pages;
-#pragma unroll 4
-    for (int i = thread / lanes; i < count; i += threads / lanes) {
-        int tb, tp, fb, fp;
-        split_slot(a.g, to[i], tb, tp);
-        split_slot(a.g, from[i], fb, fp);
-        const int tpage = page_of(a.g, b, tb), fpage = page_of(a.g, b, fb);
-        if (tpage < 0 || fpage < 0) continue;
-        *reinterpret_cast<uint4 *>(pool + row_offset(a.g, tpage, kv, tp) + sub) =
-            *reinterpret_cast<const uint4 *>(pool + row_offset(a.g, fpage, kv, fp) + sub);
-        if (lane == 0) {
-            const int64_t t = table_index(a.g, tpage, kv, tp), f = table_index(a.g, fpage, kv, fp);
-            a.pos_out[t] = a.pos_in[f];
-            a.weight_out[t] = a.weight_in[f];
+    const int64_t sub = (int64_t)kv * a.g.head_stride + (int64_t)(lane & ((1 << a.lpr_log2) - 1)) * 16;
+    char *pool = (v ? a.v_pages : a.k_pages) + sub;
+    for (int i0 = thread / lanes; i0 < count; i0 += MOVES * step) {
+        int t[MOVES], f[MOVES], tp[MOVES], fp[MOVES], pages[2][MOVES];
+#pragma unroll
+        for (int m = 0; m < MOVES; ++m) {
+            const int i = i0 + m * step < count ? i0 + m * step : count - 1;
+            t[m] = to[i];
+            f[m] = from[i];
         }
+#pragma unroll
+        for (int m = 0; m < MOVES; ++m) {
+            int block;
+            split_slot(a.g, t[m], block, tp[m]);
+            pages[0][m] = page_of(a.g, b, block);
+            split_slot(a.g, f[m], block, fp[m]);
+            pages[1][m] = page_of(a.g, b, block);
+        }
+        u32x4_nt_t x[MOVES];
+        float w[MOVES];
+        int p[MOVES];
+#pragma unroll
+        for (int m = 0; m < MOVES; ++m) {
+            const int page = pages[1][m] < 0 ? 0 : pages[1][m];
+            x[m] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_nt_t *>(pool + (int64_t)page * a.g.page_stride + (int64_t)fp[m] * a.g.row_stride));
+            if (lane == 0) {
+                const int64_t i = table_index(a.g, page, kv, fp[m]);
+                w[m] = a.weight_in[i];
+                p[m] = a.pos_in[i];
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < MOVES; ++m)
+            if (pages[0][m] >= 0 && pages[1][m] >= 0) {
+                *reinterpret_cast<u32x4_nt_t *>(pool + (int64_t)pages[0][m] * a.g.page_stride + (int64_t)tp[m] * a.g.row_stride) = x[m];
+                if (lane == 0) {
+                    const int64_t i = table_index(a.g, pages[0][m], kv, tp[m]);
+                    a.weight_out[i] = w[m];
+                    a.pos_out[i] = p[m];
+                }
+            }
     }
 }
 
@@ -345,22 +373,32 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
                 if (move_bits >> k & 1) list[1 + a.cap + m++] = j0 + k;
             }
         }
+        // the tables' entries of slots below n'; those of free slots are written again with the rows that move there
         if (copy) {
-            int block, place;
-            split_slot(a.g, j0 < n ? j0 : 0, block, place);
+            typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+            typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-            for (int k = 0; k < HAVE; ++k) {
-                if (j0 + k >= stay) break;
-                if (k > 0 && ++place == a.g.page_size) {
-                    place = 0;
-                    ++block;
-                }
-                if (!(kept >> k & 1)) continue;
+            for (int k = 0; k < HAVE; k += 4) {
+                const int j = j0 + k;
+                int block, place;
+                if (j >= stay) continue;
+                split_slot(a.g, j, block, place);
                 const int page = page_of(a.g, b, block);
-                if (page < 0) continue;
                 const int64_t i = table_index(a.g, page, kv, place);
-                a.pos_out[i] = a.pos_in[i];
-                a.weight_out[i] = a.weight_in[i];
+                if (place + 4 <= a.g.page_size && j + 4 <= stay) {
+                    if (page < 0) continue;
+                    *reinterpret_cast<f4 *>(a.weight_out + i) = *reinterpret_cast<const f4 *>(a.weight_in + i);
+                    *reinterpret_cast<i4 *>(a.pos_out + i) = *reinterpret_cast<const i4 *>(a.pos_in + i);
+                } else {
+                    for (int e = 0; e < 4 && j + e < stay; ++e) {
+                        split_slot(a.g, j + e, block, place);
+                        const int pg = page_of(a.g, b, block);
+                        if (pg < 0) continue;
+                        const int64_t at = table_index(a.g, pg, kv, place);
+                        a.pos_out[at] = a.pos_in[at];
+                        a.weight_out[at] = a.weight_in[at];
+                    }
+                }
             }
         }
     }
