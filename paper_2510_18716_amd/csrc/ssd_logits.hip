@@ -5,8 +5,8 @@
 // tokens that fall into the piece are counted in LDS (whole-number atomics: their order does not matter), one count per entry with the highest bit for
 // "seen at all"; then the piece goes through once, 16 bytes of logits at a time.  Bound by HBM (the logits in, 4 bytes out each); the tokens are read
 // by every piece of the row, from L2.  256 rows of 128257 in fp32 with 1000 to 8000 tokens, shared bias and masks: 65 us, 4.2 TB/s (57 with short histories;
-pieces of 16384 77, logits and bias both in registers 70 for fp32 and 3 more than without for bf16).  64 guided rows of 16384 in bf16: 5.0 us, the launch and three
-dependent loads.
+// pieces of 16384 77, logits and bias both in registers 70 for fp32 and 3 more than without for bf16).  64 guided rows of 16384 in bf16: 5.0 us, the launch and three
+// dependent loads.
 #include <cmath>
 
 #include "ssd_device.h"
