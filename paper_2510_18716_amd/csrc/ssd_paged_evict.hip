@@ -1,11 +1,13 @@
 // ssd_paged_evict: each (sequence, kv head) of a paged cache is cut to its budget; the rows of the largest accumulated attention weight
 // stay (the top-M rule of Algorithm 1, sinks and recent tokens protected as in Sec. 3.3).
 //
-// A unit's selection is one workgroup's: the key of the last row that stays is found by a descent over the keys' bits (weight first,
-// then position; whole-number compares, so the set is exact), eight bits a step by a histogram in LDS, beginning at the first bit in which the
-// weights differ.  Up to 16384 rows a thread keeps its rows' keys in registers, and the tables are read once; longer units are read anew for every
-// step, eleven bits each.  Then every thread ranks its free slots below n' and its kept rows above by one scan over the workgroup, and the rows
-// move, in 16-byte fragments: by the same workgroup where units are many, by a second launch with more workgroups per unit otherwise.
+// Selection.  The key of the last row that stays is found by a descent over the keys' bits: the weight first, then the position; whole-number
+// compares, so the set is exact.  Up to 16384 rows a unit is one workgroup's, whose threads keep their rows' keys in registers, so that the tables
+// are read once.  Up to 256 rows that is one wave, which descends bit by bit (a ballot counts); above, ten bits a step by a histogram in LDS,
+// beginning at the first bit in which the keys differ.  Every thread ranks its free slots below n' and its kept rows above by one scan over
+// the workgroup.  A longer unit is cut into slices (the section "long units").
+// Movement.  A kept row above n' goes to the free slot of its own rank, in 16-byte fragments: by the unit's workgroup where units are many,
+// by a launch with more workgroups per unit otherwise.
 #include "ssd_paged.h"
 
 namespace ssd {
@@ -73,18 +75,22 @@ static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b
     return r;
 }
 
-static __device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += (uint32_t)__shfl_xor((int)v, o);
-    return v;
+// Inclusive sum over the lanes of a wave: rows of 16 by shifts, then the last lane of a row to the rows behind it.
+template <int CTRL, int ROWS> static __device__ __forceinline__ uint32_t dpp_add(uint32_t v) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
 }
 static __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
-    const int lane = threadIdx.x & 63;
+    v = dpp_add<0x111, 0xF>(v);
+    v = dpp_add<0x112, 0xF>(v);
+    v = dpp_add<0x114, 0xF>(v);
+    v = dpp_add<0x118, 0xF>(v);
+    v = dpp_add<0x142, 0xA>(v);
+    return dpp_add<0x143, 0xC>(v);
+}
+static __device__ __forceinline__ uint32_t wave_sum(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(v), 63); }
+static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t w = (uint32_t)__shfl_up((int)v, o);
-        v += lane >= o ? w : 0;
-    }
+    for (int o = 1; o < 64; o <<= 1) v |= (uint32_t)__shfl_xor((int)v, o);
     return v;
 }
 
@@ -92,7 +98,8 @@ static __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
 // A thread has MOVES rows' loads in flight at each of the three stages (list, block table, row); past the end it repeats the last row, which
 // writes the same again.
 static constexpr int MOVES = 8;
-static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b, int kv, const int32_t *to, const int32_t *from, int count, int thread,
+template <typename I>
+static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b, int kv, const I *to, const I *from, int count, int thread,
                                                  int threads) {
     const int lanes = 2 << a.lpr_log2, lane = thread & (lanes - 1), step = threads / lanes;
     const bool v = lane >> a.lpr_log2;
@@ -140,273 +147,727 @@ static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b,
     }
 }
 
-// KEYS: rows whose keys a thread keeps, consecutive ones; 0: none, the tables are read again for every step.  grid = (kv heads, sequences)
+// ---- the descent ---------------------------------------------------------------------------------------------------------
+
+static constexpr int BITS = 10, BINS = 1 << BITS;
+
+// Bits in which the rows that compete differ, and how many rows are protected.
+struct Spread {
+    uint32_t safe, any_w, not_all_w, any_p, not_all_p;             // any: some row has the bit, not_all: some row lacks it
+    __device__ __forceinline__ void add(uint32_t w, uint32_t p, bool in) {
+        any_w |= in ? w : 0;
+        not_all_w |= in ? ~w : 0;
+        any_p |= in ? p : 0;
+        not_all_p |= in ? ~p : 0;
+    }
+};
+
+// The last row that stays: rows with a larger key stay, of those with the same key the first `ties` in slot order.
+struct Last {
+    uint32_t w, p;
+    int ties;                                                      // 2^31 - 1: all of them
+};
+
+template <int THREADS> struct DescentLds {
+    uint32_t hist[2][BINS];
+    uint32_t red[5][THREADS / 64];
+    int found[3];
+};
+
+// each(f): f(weight key, position key) for this thread's competing rows.  left: places among them, 1 .. their number.  Both histograms are
+// clear on entry.
+template <int THREADS, typename Each>
+static __device__ __forceinline__ Last descend(DescentLds<THREADS> &lds, const Spread &sp, int left, const Each &each) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const uint32_t dw = sp.any_w & sp.not_all_w, dp = sp.any_p & sp.not_all_p;
+    int bits = dw ? 32 - __clz((int)dw) : 0;                       // open bits of the key at hand
+    uint32_t ref = bits == 32 ? 0 : sp.any_w >> bits << bits;      // (above them any row's bits are every row's)
+    uint32_t w_done = ref;
+    bool on_pos = false, whole = false;
+    for (int level = 0;; ++level) {
+        if (bits == 0) {
+            if (on_pos) break;
+            w_done = ref;
+            on_pos = true;
+            bits = dp ? 32 - __clz((int)dp) : 0;
+            ref = bits == 32 ? 0 : sp.any_p >> bits << bits;
+            if (bits == 0) break;
+        }
+        const int take = bits < BITS ? bits : BITS, shift = bits - take;
+        const uint32_t mask = (1u << take) - 1;
+        uint32_t *h = lds.hist[level & 1];
+        each([&](uint32_t w, uint32_t p) {
+            const uint32_t key = on_pos ? p : w;
+            if ((!on_pos || w == w_done) && (bits == 32 || (key ^ ref) >> bits == 0)) atomicAdd(&h[key >> shift & mask], 1u);
+        });
+        __syncthreads();
+        // the digit in which the place falls: one wave adds up the bins from the top while the others clear the next step's
+        if (tid < 64) {
+            constexpr int PER = BINS / 64;
+            uint32_t bin[PER], sum = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                bin[i] = h[BINS - 1 - (lane * PER + i)];
+                sum += bin[i];
+            }
+            const uint32_t upto = wave_scan(sum);
+            const int l = __ffsll((unsigned long long)__ballot(upto >= (uint32_t)left)) - 1;
+            uint32_t above = upto - sum;
+            int digit = -1;
+            uint32_t in_bin = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const bool here = digit < 0 && above + bin[i] >= (uint32_t)left;
+                digit = here ? BINS - 1 - (lane * PER + i) : digit;
+                in_bin = here ? bin[i] : in_bin;
+                above += digit < 0 ? bin[i] : 0;
+            }
+            if (lane == l) {
+                lds.found[0] = digit;
+                lds.found[1] = (int)above;
+                lds.found[2] = (int)in_bin;
+            }
+        }
+        if (THREADS == 64 || tid >= 64)
+            for (int i = THREADS == 64 ? tid : tid - 64; i < BINS; i += THREADS == 64 ? 64 : THREADS - 64) lds.hist[(level & 1) ^ 1][i] = 0;
+        __syncthreads();
+        ref |= (uint32_t)lds.found[0] << shift;
+        left -= lds.found[1];
+        bits = shift;
+        whole = lds.found[2] == left;                              // all of them stay: nothing below needs looking at
+        if (whole) break;
+    }
+    Last r;
+    r.w = on_pos ? w_done : ref;
+    r.p = on_pos ? ref : 0;
+    r.ties = whole ? 0x7fffffff : left;
+    return r;
+}
+
+// The same for the rows of one wave, bit by bit: how many rows have the bits found so far and a one in the next.
+template <typename Count>
+static __device__ __forceinline__ Last descend_wave(const Spread &sp, int left, int rows, const Count &count) {
+    const uint32_t dw = sp.any_w & sp.not_all_w, dp = sp.any_p & sp.not_all_p;
+    Last r;
+    r.w = sp.any_w & ~dw;
+    r.p = 0;
+    // rows: with the bits so far; `left` of them stay
+    for (uint32_t open = dw; open;) {
+        const uint32_t bit = 0x80000000u >> __clz((int)open), try_w = r.w | bit;
+        open &= ~bit;
+        const int ones = count([&](uint32_t w, uint32_t) { return ((w ^ try_w) & ~open) == 0; });
+        if (ones >= left) {
+            r.w = try_w;
+            rows = ones;
+        } else {
+            left -= ones;
+            rows -= ones;
+        }
+        if (rows == left) {
+            r.ties = 0x7fffffff;
+            return r;
+        }
+    }
+    r.p = sp.any_p & ~dp;
+    for (uint32_t open = dp; open;) {
+        const uint32_t bit = 0x80000000u >> __clz((int)open), try_p = r.p | bit;
+        open &= ~bit;
+        const int ones = count([&](uint32_t w, uint32_t p) { return w == r.w && ((p ^ try_p) & ~open) == 0; });
+        if (ones >= left) {
+            r.p = try_p;
+            rows = ones;
+        } else {
+            left -= ones;
+            rows -= ones;
+        }
+        if (rows == left) {
+            r.ties = 0x7fffffff;
+            return r;
+        }
+    }
+    r.ties = left;
+    return r;
+}
+
+// 2: stays, 1: has the last row's keys, 0: goes.  Where the descent ended early the open bits of the last keys are 0 and everything
+// at or above them stays.
+static __device__ __forceinline__ int standing(const Last &l, uint32_t w, uint32_t p) {
+    if (w != l.w) return w > l.w ? 2 : 0;
+    return p > l.p ? 2 : p == l.p ? 1 : 0;
+}
+
+// The tables' entries of rows j .. j + 3 below `stay`, from the old tables to the new.
+static __device__ __forceinline__ void copy_entries(const PagedEvictArgs &a, int b, int kv, int j, int stay) {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));
+    int block, place;
+    split_slot(a.g, j, block, place);
+    if (place + 4 <= a.g.page_size && j + 4 <= stay) {
+        const int page = page_of(a.g, b, block);
+        if (page < 0) return;
+        const int64_t i = table_index(a.g, page, kv, place);
+        *reinterpret_cast<f4 *>(a.weight_out + i) = *reinterpret_cast<const f4 *>(a.weight_in + i);
+        *reinterpret_cast<i4 *>(a.pos_out + i) = *reinterpret_cast<const i4 *>(a.pos_in + i);
+        return;
+    }
+    for (int e = 0; e < 4 && j + e < stay; ++e) {
+        split_slot(a.g, j + e, block, place);
+        const int page = page_of(a.g, b, block);
+        if (page < 0) continue;
+        const int64_t i = table_index(a.g, page, kv, place);
+        a.pos_out[i] = a.pos_in[i];
+        a.weight_out[i] = a.weight_in[i];
+    }
+}
+
+static __device__ __forceinline__ int stay_of(const PagedEvictArgs &a, int b, int n) {
+    const int want = a.budget[b] < 0 ? 0 : a.budget[b];
+    return n < want ? n : want;
+}
+static __device__ __forceinline__ bool is_safe(const PagedEvictArgs &a, int64_t total, int pos) {
+    return pos < a.n_sink || (int64_t)pos >= total - a.recent;
+}
+
+// ---- units of one workgroup ----------------------------------------------------------------------------------------------
+
+// A thread has KEYS consecutive rows.  grid = (kv heads, sequences)
 template <int THREADS, int KEYS>
 __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a, int move_here) {
-    constexpr int NW = THREADS / 64, BITS = KEYS ? 8 : 11, BINS = 1 << BITS, LEVELS = 2 * ((32 + BITS - 1) / BITS);
-    constexpr int HISTS = KEYS ? LEVELS : 1;                        // one histogram per step, or one that is cleared in between
-    __shared__ uint32_t hist[HISTS][BINS];
-    __shared__ uint32_t red[3][NW];
+    constexpr int NW = THREADS / 64, HALF = THREADS * KEYS / 2;
+    __shared__ DescentLds<THREADS> lds;
+    __shared__ uint16_t free_slots[HALF], move_slots[HALF];        // if the rows move here: at most half of them do
     const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n = clamp_len(a.g, b);
-    const int want = a.budget[b] < 0 ? 0 : a.budget[b];
-    const int stay = n < want ? n : want;
+    const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const bool copy = a.pos_out != a.pos_in;
     const int64_t total = a.g.seq_pos[b];
     int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
     if (kv == 0 && tid == 0 && a.len_out) a.len_out[b] = stay;
-    if (n == stay && !copy) {
-        if (tid == 0) list[0] = 0;
+    if (n == stay) {
+        if (tid == 0 && !move_here) list[0] = 0;
+        if (copy)
+            for (int j = 4 * tid; j < stay; j += 4 * THREADS) copy_entries(a, b, kv, j, stay);
         return;
     }
-    for (int i = tid; i < HISTS * BINS; i += THREADS) (&hist[0][0])[i] = 0;
-
-    // what a thread looks at: its own rows in registers, or all rows of the unit with stride THREADS * 4, read again
-    uint32_t wk[KEYS ? KEYS : 1], pk[KEYS ? KEYS : 1], safe_bits = 0;
-    auto is_safe = [&](int pos) { return pos < a.n_sink || (int64_t)pos >= total - a.recent; };
-    if constexpr (KEYS > 0) {
+    const int j0 = tid * KEYS;
+    uint32_t wk[KEYS], pk[KEYS], safe = 0, in = 0;                 // keys; bits: protected, below n
 #pragma unroll
-        for (int k = 0; k < KEYS; k += 4) {
-            const int j = tid * KEYS + k;
-            if (j < n) {
-                const Four r = table_rows(a, b, kv, j, n);
+    for (int k = 0; k < KEYS; k += 4) {
+        if (j0 + k < n) {
+            const Four r = table_rows(a, b, kv, j0 + k, n);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    wk[k + e] = weight_key(r.w[e]);
-                    pk[k + e] = pos_key(r.pos[e]);
-                    safe_bits |= is_safe(r.pos[e]) ? 1u << (k + e) : 0u;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) wk[k + e] = pk[k + e] = 0;
+            for (int e = 0; e < 4; ++e) {
+                wk[k + e] = weight_key(r.w[e]);
+                pk[k + e] = pos_key(r.pos[e]);
+                safe |= is_safe(a, total, r.pos[e]) ? 1u << (k + e) : 0u;
+                in |= j0 + k + e < n ? 1u << (k + e) : 0u;
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) wk[k + e] = pk[k + e] = 0;
         }
     }
-    auto each = [&](auto f) {                                      // f(weight key, position key, safe)
-        if constexpr (KEYS > 0) {
+    safe &= in;
+    // the tables' entries of slots below n'; those of free slots are written again with the rows that move there
+    if (copy)
 #pragma unroll
-            for (int k = 0; k < KEYS; ++k)
-                if (tid * KEYS + k < n) f(wk[k], pk[k], (safe_bits >> k & 1) != 0);
-        } else {
-#pragma unroll 2
-            for (int j = 4 * tid; j < n; j += 4 * THREADS) {
-                const Four r = table_rows(a, b, kv, j, n);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j + e < n) f(weight_key(r.w[e]), pos_key(r.pos[e]), is_safe(r.pos[e]));
-            }
-        }
-    };
+        for (int k = 0; k < KEYS; k += 4)
+            if (j0 + k < stay) copy_entries(a, b, kv, j0 + k, stay);
+    if (THREADS > 64) {
+        for (int i = tid; i < 2 * BINS; i += THREADS) (&lds.hist[0][0])[i] = 0;
+    }
 
-    // which rows compete and for how many places; the bits in which the weights of each kind differ
-    uint32_t last_w = 0, last_p = 0;                               // keys of the last row that stays
-    int ties = 0;                                                  // how many rows with just these keys stay
-    bool among_safe = false, compete = false;
-    if (stay < n && stay > 0) {
-        uint32_t safe_rows = 0, or_s = 0, and_s = ~0u, or_o = 0, and_o = ~0u;
-        each([&](uint32_t w, uint32_t, bool safe) {
-            safe_rows += safe;
-            or_s |= safe ? w : 0;
-            and_s &= safe ? w : ~0u;
-            or_o |= safe ? 0 : w;
-            and_o &= safe ? ~0u : w;
-        });
-        safe_rows = wave_sum(safe_rows);
-        if (lane == 0) red[0][wave] = safe_rows;
+    // protected rows, if they leave places for others; else they alone compete
+    uint32_t safe_rows = wave_sum((uint32_t)__popc(safe));
+    if (NW > 1) {
+        if (lane == 0) lds.red[0][wave] = safe_rows;
         __syncthreads();
         safe_rows = 0;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) safe_rows += red[0][i];
-        among_safe = (int)safe_rows >= stay;
-        int left = among_safe ? stay : stay - (int)safe_rows;
-        compete = left > 0;
-        uint32_t any = among_safe ? or_s : or_o, every = among_safe ? and_s : and_o;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            any |= (uint32_t)__shfl_xor((int)any, o);
-            every &= (uint32_t)__shfl_xor((int)every, o);
-        }
-        if (lane == 0) {
-            red[1][wave] = any;
-            red[2][wave] = every;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            any |= red[1][i];
-            every &= red[2][i];
-        }
-        const uint32_t differ = any ^ every;
-        int bits = differ ? 32 - __clz((int)differ) : 0;           // bits of the weight still open
-        last_w = bits == 32 ? 0 : every >> bits << bits;
-        bool on_pos = bits == 0, whole = false;
-        if (on_pos) bits = 32;
-        for (int level = 0; compete && !whole; ++level) {
-            const int take = bits < BITS ? bits : BITS, shift = bits - take;
-            uint32_t *h = hist[KEYS ? level : 0];
-            const uint32_t mask = (1u << take) - 1;
-            each([&](uint32_t w, uint32_t p, bool safe) {
-                const uint32_t key = on_pos ? p : w, ref = on_pos ? last_p : last_w;
-                const bool in = safe == among_safe && (!on_pos || w == last_w) && (bits == 32 || key >> bits == ref >> bits);
-                if (in) atomicAdd(&h[key >> shift & mask], 1u);
-            });
-            __syncthreads();
-            // the digit in which the place falls: every wave adds up the bins from the top, BINS / 64 a lane
-            constexpr int PER = BINS / 64;
-            uint32_t sum = 0, mine[PER];
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                mine[i] = h[BINS - 1 - (lane * PER + i)];
-                sum += mine[i];
-            }
-            const uint32_t upto = wave_scan(sum);
-            const int l = __ffsll((unsigned long long)__ballot(upto >= (uint32_t)left)) - 1;
-            uint32_t above = upto - sum, in_bin = 0;
-            int digit = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const bool here = above < (uint32_t)left && above + mine[i] >= (uint32_t)left;
-                if (here && in_bin == 0) {
-                    digit = BINS - 1 - (lane * PER + i);
-                    in_bin = mine[i];
-                }
-                if (in_bin == 0) above += mine[i];
-            }
-            digit = __builtin_amdgcn_readlane(digit, l);
-            above = (uint32_t)__builtin_amdgcn_readlane((int)above, l);
-            in_bin = (uint32_t)__builtin_amdgcn_readlane((int)in_bin, l);
-            left -= (int)above;
-            if (on_pos) last_p |= (uint32_t)digit << shift;
-            else last_w |= (uint32_t)digit << shift;
-            bits = shift;
-            whole = (int)in_bin == left;                           // all of them stay: nothing below needs looking at
-            if (bits == 0) {
-                if (on_pos) break;
-                on_pos = true;
-                bits = 32;
-            }
-            if constexpr (KEYS == 0) {
-                if (!whole) {
-                    __syncthreads();
-                    for (int i = tid; i < BINS; i += THREADS) hist[0][i] = 0;
-                    __syncthreads();
-                }
-            }
-        }
-        ties = whole ? n : left;
+        for (int i = 0; i < NW; ++i) safe_rows += lds.red[0][i];
     }
-    // Rows above the last one's keys stay; so do those equal to them while there are ties left.  Where the descent ended early, the bits
-    // below are 0 in the last keys, and everything at or above them stays.
-    auto level_of = [&](uint32_t w, uint32_t p) {                  // 2: stays, 1: equal, 0: goes
-        if (w != last_w) return w > last_w ? 2 : 0;
-        return p > last_p ? 2 : p == last_p ? 1 : 0;
-    };
-
-    // who stays, where slots become free, which rows move
-    constexpr int HAVE = KEYS ? KEYS : 4;
-    uint32_t seen_tie = 0, seen_free = 0, seen_move = 0;
-    for (int base = 0; base < n; base += THREADS * HAVE) {
-        const int j0 = base + tid * HAVE;
-        uint32_t kept = 0, tie = 0;
-        Four r;
-        if constexpr (KEYS == 0) {
-            if (j0 < n) r = table_rows(a, b, kv, j0, n);
-        }
+    const bool among_safe = (int)safe_rows >= stay;
+    const int left = among_safe ? stay : stay - (int)safe_rows;
+    const uint32_t compete = among_safe ? safe : in & ~safe;
+    uint32_t kept = among_safe ? 0 : safe, tie = 0;
+    Last last = {0, 0, 0};
+    if (left > 0) {
+        Spread sp = {0, 0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < HAVE; ++k) {
-            if (j0 + k >= n) continue;
-            bool safe;
-            uint32_t w, p;
-            if constexpr (KEYS > 0) {
-                safe = safe_bits >> k & 1;
-                w = wk[k];
-                p = pk[k];
-            } else {
-                safe = is_safe(r.pos[k]);
-                w = weight_key(r.w[k]);
-                p = pos_key(r.pos[k]);
+        for (int k = 0; k < KEYS; ++k) sp.add(wk[k], pk[k], compete >> k & 1);
+        sp.any_w = wave_or(sp.any_w);
+        sp.not_all_w = wave_or(sp.not_all_w);
+        sp.any_p = wave_or(sp.any_p);
+        sp.not_all_p = wave_or(sp.not_all_p);
+        if constexpr (NW == 1) {
+            last = descend_wave(sp, left, among_safe ? (int)safe_rows : n - (int)safe_rows, [&](auto f) {
+                int c = 0;
+#pragma unroll
+                for (int k = 0; k < KEYS; ++k) c += (int)__popcll(__ballot((compete >> k & 1) && f(wk[k], pk[k])));
+                return c;
+            });
+        } else {
+            if (lane == 0) {
+                lds.red[1][wave] = sp.any_w;
+                lds.red[2][wave] = sp.not_all_w;
+                lds.red[3][wave] = sp.any_p;
+                lds.red[4][wave] = sp.not_all_p;
             }
-            int lv = stay == n ? 2 : stay == 0 ? 0 : safe != among_safe ? (safe ? 2 : 0) : compete ? level_of(w, p) : 0;
-            kept |= lv == 2 ? 1u << k : 0u;
-            tie |= lv == 1 ? 1u << k : 0u;
-        }
-        if (stay < n) {
-            if (ties >= n) {
-                kept |= tie;
-            } else {                                               // equal keys: the lowest slots
-                const uint32_t c = (uint32_t)__popc(tie), up = wave_scan(c);
-                __syncthreads();
-                if (lane == 63) red[0][wave] = up;
-                __syncthreads();
-                uint32_t before = seen_tie + up - c;
-#pragma unroll
-                for (int i = 0; i < NW; ++i) {
-                    before += i < wave ? red[0][i] : 0;
-                    seen_tie += red[0][i];
-                }
-#pragma unroll
-                for (int k = 0; k < HAVE; ++k)
-                    if (tie >> k & 1) {
-                        kept |= (int)before < ties ? 1u << k : 0u;
-                        ++before;
-                    }
-            }
-            const int below = stay - j0 < 0 ? 0 : stay - j0 < HAVE ? stay - j0 : HAVE, there = n - j0 < 0 ? 0 : n - j0 < HAVE ? n - j0 : HAVE;
-            const uint32_t low = below == 32 ? ~0u : (1u << below) - 1, in = there == 32 ? ~0u : (1u << there) - 1;
-            const uint32_t free_bits = in & low & ~kept, move_bits = kept & ~low;
-            const uint32_t c = (uint32_t)__popc(free_bits) | (uint32_t)__popc(move_bits) << 16, up = wave_scan(c);
             __syncthreads();
-            if (lane == 63) red[1][wave] = up;
-            __syncthreads();
-            uint32_t before = up - c, all = 0;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
-                before += i < wave ? red[1][i] : 0;
-                all += red[1][i];
+                sp.any_w |= lds.red[1][i];
+                sp.not_all_w |= lds.red[2][i];
+                sp.any_p |= lds.red[3][i];
+                sp.not_all_p |= lds.red[4][i];
             }
-            uint32_t f = seen_free + (before & 0xffff), m = seen_move + (before >> 16);
-            seen_free += all & 0xffff;
-            seen_move += all >> 16;
+            last = descend<THREADS>(lds, sp, left, [&](auto f) {
 #pragma unroll
-            for (int k = 0; k < HAVE; ++k) {
-                if (free_bits >> k & 1) list[1 + f++] = j0 + k;
-                if (move_bits >> k & 1) list[1 + a.cap + m++] = j0 + k;
-            }
+                for (int k = 0; k < KEYS; ++k)
+                    if (compete >> k & 1) f(wk[k], pk[k]);
+            });
         }
-        // the tables' entries of slots below n'; those of free slots are written again with the rows that move there
-        if (copy) {
-            typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-            typedef int i4 __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-            for (int k = 0; k < HAVE; k += 4) {
-                const int j = j0 + k;
-                int block, place;
-                if (j >= stay) continue;
-                split_slot(a.g, j, block, place);
-                const int page = page_of(a.g, b, block);
-                const int64_t i = table_index(a.g, page, kv, place);
-                if (place + 4 <= a.g.page_size && j + 4 <= stay) {
-                    if (page < 0) continue;
-                    *reinterpret_cast<f4 *>(a.weight_out + i) = *reinterpret_cast<const f4 *>(a.weight_in + i);
-                    *reinterpret_cast<i4 *>(a.pos_out + i) = *reinterpret_cast<const i4 *>(a.pos_in + i);
-                } else {
-                    for (int e = 0; e < 4 && j + e < stay; ++e) {
-                        split_slot(a.g, j + e, block, place);
-                        const int pg = page_of(a.g, b, block);
-                        if (pg < 0) continue;
-                        const int64_t at = table_index(a.g, pg, kv, place);
-                        a.pos_out[at] = a.pos_in[at];
-                        a.weight_out[at] = a.weight_in[at];
-                    }
+        for (int k = 0; k < KEYS; ++k) {
+            const int st = standing(last, wk[k], pk[k]);
+            kept |= (compete >> k & 1) && st == 2 ? 1u << k : 0u;
+            tie |= (compete >> k & 1) && st == 1 ? 1u << k : 0u;
+        }
+        if (last.ties == 0x7fffffff) {
+            kept |= tie;
+        } else {                                                   // the lowest slots of those with the last keys
+            const uint32_t c = (uint32_t)__popc(tie), up = wave_scan(c);
+            uint32_t before = up - c;
+            if (NW > 1) {
+                if (lane == 63) lds.red[0][wave] = up;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NW; ++i) before += i < wave ? lds.red[0][i] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < KEYS; ++k)
+                if (tie >> k & 1) {
+                    kept |= (int)before < last.ties ? 1u << k : 0u;
+                    ++before;
                 }
+        }
+    }
+
+    // where slots become free, which rows move
+    const int below = stay - j0 < 0 ? 0 : stay - j0 < KEYS ? stay - j0 : KEYS;
+    const uint32_t low = (1u << below) - 1, free_bits = in & low & ~kept, move_bits = kept & ~low;
+    const uint32_t c = (uint32_t)__popc(free_bits) | (uint32_t)__popc(move_bits) << 16, up = wave_scan(c);
+    uint32_t before = up - c, all = (uint32_t)__builtin_amdgcn_readlane((int)up, 63);
+    if (NW > 1) {
+        if (lane == 63) lds.red[1][wave] = up;
+        __syncthreads();
+        all = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            before += i < wave ? lds.red[1][i] : 0;
+            all += lds.red[1][i];
+        }
+    }
+    uint32_t f = before & 0xffff, m = before >> 16;
+    const int moves = (int)(all >> 16);
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+        if (free_bits >> k & 1) {
+            if (move_here) free_slots[f] = (uint16_t)(j0 + k);
+            else list[1 + f] = j0 + k;
+            ++f;
+        }
+        if (move_bits >> k & 1) {
+            if (move_here) move_slots[m] = (uint16_t)(j0 + k);
+            else list[1 + a.cap + m] = j0 + k;
+            ++m;
+        }
+    }
+    if (!move_here) {
+        if (tid == 0) list[0] = moves;
+    } else if (moves > 0) {
+        __syncthreads();
+        move_rows(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
+    }
+}
+
+// ---- long units ------------------------------------------------------------------------------------------------------------
+//
+// The rows below n' and those above are cut into slices of equally many rows, a workgroup each; a unit's own workgroup works in between.
+//   1 slices: how many rows have which upper 11 bits of their weight, protected ones and others apart
+//   2 unit:   the bin in which the last place falls, and how many rows of a slice are above it and in it
+//   3 slices: the rows in the bin, in slot order, into one list (the memory of the moves, which come later)
+//   4 unit:   the descent among those; where each slice's free slots and moving rows begin in the lists
+//   5 slices: the lists
+//   6 as everywhere: the rows move
+static constexpr int TOP = 11, TOP_BINS = 1 << TOP, SLICES = 62;
+static constexpr int PICK = 6144;                                  // candidates whose keys fit in LDS
+
+// What step 2 and 4 leave for a unit's slices.
+struct SliceInfo {
+    int32_t kept, in_bin, first;                                   // rows above the bin, in it, and where the latter begin in the list
+    int32_t at;                                                    // where its free slots, or its moving rows, begin in the lists
+};
+struct UnitInfo {
+    int32_t among_safe, bin, left, candidates;
+    uint32_t last_w, last_p;
+    int32_t last_slot, pad;
+    SliceInfo slice[SLICES + 2];
+};
+
+struct SliceArgs {
+    PagedEvictArgs e;
+    uint32_t *hist;                                                // [units, slices + 2, 2, TOP_BINS]
+    UnitInfo *info;                                                // [units]
+    int slices;
+};
+
+struct Slices {
+    int rows, low, count;                                          // rows of a slice, slices below n', all of them
+    __device__ __forceinline__ Slices(int n, int stay, int slices) {
+        rows = ((n + slices - 1) / slices + 3) & ~3;
+        low = (stay + rows - 1) / rows;
+        count = low + (n - stay + rows - 1) / rows;
+    }
+    __device__ __forceinline__ int begin(int s, int stay) const { return s < low ? s * rows : stay + (s - low) * rows; }
+    __device__ __forceinline__ int end(int s, int n, int stay) const {
+        const int e = begin(s, stay) + rows, most = s < low ? stay : n;
+        return e < most ? e : most;
+    }
+    __device__ __forceinline__ int of(int slot, int stay) const { return slot < stay ? slot / rows : low + (slot - stay) / rows; }
+};
+
+__global__ __launch_bounds__(256) void slice_count_kernel(SliceArgs s) {
+    const PagedEvictArgs &a = s.e;
+    __shared__ uint32_t hist[2][TOP_BINS];
+    const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+    const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
+    const Slices sl(n > 0 ? n : 1, stay, s.slices);
+    if (n == stay || (int)blockIdx.x >= sl.count) return;
+    const int64_t total = a.g.seq_pos[b], unit = (int64_t)b * a.g.n_kv + kv;
+    for (int i = tid; i < 2 * TOP_BINS; i += 256) (&hist[0][0])[i] = 0;
+    __syncthreads();
+    const int end = sl.end((int)blockIdx.x, n, stay);
+#pragma unroll 4
+    for (int j = sl.begin((int)blockIdx.x, stay) + 4 * tid; j < end; j += 1024) {
+        const Four r = table_rows(a, b, kv, j, end);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j + e < end) atomicAdd(&hist[is_safe(a, total, r.pos[e])][weight_key(r.w[e]) >> (32 - TOP)], 1u);
+    }
+    __syncthreads();
+    uint4 *out = reinterpret_cast<uint4 *>(s.hist + (unit * (s.slices + 2) + blockIdx.x) * 2 * TOP_BINS);
+    for (int i = tid; i < 2 * TOP_BINS / 4; i += 256) out[i] = *reinterpret_cast<const uint4 *>(&hist[0][0] + 4 * i);
+}
+
+__global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
+    const PagedEvictArgs &a = s.e;
+    __shared__ uint32_t red[2][16];
+    __shared__ int found[3];
+    __shared__ SliceInfo info[SLICES + 2];
+    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
+    if (kv == 0 && tid == 0 && a.len_out) a.len_out[b] = stay;
+    if (n == stay) return;
+    const Slices sl(n, stay, s.slices);
+    const int64_t unit = (int64_t)b * a.g.n_kv + kv;
+    const uint32_t *hist = s.hist + unit * (s.slices + 2) * 2 * TOP_BINS;
+    // a thread has two bins of each kind, counted from the top
+    const int bin = TOP_BINS - 2 - 2 * tid;
+    uint32_t h[2][2] = {{0, 0}, {0, 0}};
+#pragma unroll 8
+    for (int i = 0; i < sl.count; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(hist + ((int64_t)i * 2 + k) * TOP_BINS + bin);
+            h[k][0] += x.y;
+            h[k][1] += x.x;
+        }
+    const uint32_t up0 = wave_scan(h[0][0] + h[0][1]), up1 = wave_scan(h[1][0] + h[1][1]);
+    if (lane == 63) {
+        red[0][wave] = up0;
+        red[1][wave] = up1;
+    }
+    __syncthreads();
+    uint32_t before[2] = {up0 - h[0][0] - h[0][1], up1 - h[1][0] - h[1][1]}, safe_rows = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        before[0] += i < wave ? red[0][i] : 0;
+        before[1] += i < wave ? red[1][i] : 0;
+        safe_rows += red[1][i];
+    }
+    const int k = (int)safe_rows >= stay;                          // 1: protected rows alone compete
+    const uint32_t left = (uint32_t)(k ? stay : stay - (int)safe_rows);
+    if (tid == 0) {
+        found[0] = TOP_BINS;                                       // no place to compete for: nothing is in or above this bin
+        found[1] = 0;
+    }
+    __syncthreads();
+    uint32_t above = k ? before[1] : before[0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t c = k ? h[1][i] : h[0][i];
+        if (left > 0 && above < left && above + c >= left) {
+            found[0] = bin + 1 - i;
+            found[1] = (int)(left - above);
+        }
+        above += c;
+    }
+    __syncthreads();
+    const int at = found[0];
+    // a wave per slice: what it has above the bin and in it
+    for (int i = wave; i < sl.count; i += 16) {
+        const uint32_t *mine = hist + ((int64_t)i * 2 + k) * TOP_BINS, *others = hist + ((int64_t)i * 2 + 1) * TOP_BINS;
+        uint32_t over = 0, safe = 0;
+#pragma unroll 8
+        for (int x = lane * 4; x < TOP_BINS; x += 256) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(mine + x);
+            over += (x > at ? v.x : 0) + (x + 1 > at ? v.y : 0) + (x + 2 > at ? v.z : 0) + (x + 3 > at ? v.w : 0);
+            if (!k) {
+                const uint4 o = *reinterpret_cast<const uint4 *>(others + x);
+                safe += o.x + o.y + o.z + o.w;
+            }
+        }
+        over = wave_sum(over);
+        safe = wave_sum(safe);
+        if (lane == 0) info[i] = SliceInfo{(int32_t)(over + safe), at < TOP_BINS ? (int32_t)mine[at] : 0, 0, 0};
+    }
+    __syncthreads();
+    if (tid < 64) {
+        const uint32_t c = tid < sl.count ? (uint32_t)info[tid].in_bin : 0, up = wave_scan(c);
+        UnitInfo *u = s.info + unit;
+        if (tid < sl.count) u->slice[tid] = SliceInfo{info[tid].kept, info[tid].in_bin, (int32_t)(up - c), 0};
+        if (tid == 63) {
+            u->among_safe = k;
+            u->bin = at;
+            u->left = found[1];
+            u->candidates = (int32_t)up;
+        }
+    }
+}
+
+// A slice's rows 1024 at a time, four a thread: body(first row of the thread, its rows or none) between barriers of its own.
+template <typename Body>
+static __device__ __forceinline__ void slice_rows(const PagedEvictArgs &a, int b, int kv, int begin, int end, const Body &body) {
+    Four r[2];
+    int j = begin + 4 * (int)threadIdx.x;
+    if (j < end) r[0] = table_rows(a, b, kv, j, end);
+    for (int base = begin; base < end; base += 1024, j += 1024) {
+        if (j + 1024 < end) r[1] = table_rows(a, b, kv, j + 1024, end);       // on its way while these are ranked
+        body(j, r[0]);
+        r[0] = r[1];
+    }
+}
+
+__global__ __launch_bounds__(256) void slice_gather_kernel(SliceArgs s) {
+    const PagedEvictArgs &a = s.e;
+    __shared__ uint32_t red[2][4];
+    const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
+    const Slices sl(n > 0 ? n : 1, stay, s.slices);
+    if (n == stay || (int)blockIdx.x >= sl.count) return;
+    const int64_t total = a.g.seq_pos[b], unit = (int64_t)b * a.g.n_kv + kv;
+    const UnitInfo *u = s.info + unit;
+    if (u->slice[blockIdx.x].in_bin == 0) return;
+    int32_t *out = a.moves + moves_of(a.cap, unit) + 1 + u->slice[blockIdx.x].first;
+    const bool among_safe = u->among_safe != 0;
+    const uint32_t bin = (uint32_t)u->bin;
+    int parity = 0;
+    const int end = sl.end((int)blockIdx.x, n, stay);
+    slice_rows(a, b, kv, sl.begin((int)blockIdx.x, stay), end, [&](int j, const Four &r) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            bits |= j + e < end && is_safe(a, total, r.pos[e]) == among_safe && weight_key(r.w[e]) >> (32 - TOP) == bin ? 1u << e : 0u;
+        const uint32_t c = (uint32_t)__popc(bits), up = wave_scan(c);
+        if (lane == 63) red[parity][wave] = up;
+        __syncthreads();
+        uint32_t at = up - c, all = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            at += i < wave ? red[parity][i] : 0;
+            all += red[parity][i];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (bits >> e & 1) out[at++] = j + e;
+        out += all;
+        parity ^= 1;
+    });
+}
+
+__global__ __launch_bounds__(1024) void slice_pick_kernel(SliceArgs s) {
+    const PagedEvictArgs &a = s.e;
+    __shared__ DescentLds<1024> lds;
+    __shared__ uint32_t cw[PICK], cp[PICK];
+    __shared__ int kept[SLICES + 2];
+    __shared__ int last_slot;
+    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
+    const int64_t unit = (int64_t)b * a.g.n_kv + kv;
+    int32_t *list = a.moves + moves_of(a.cap, unit);
+    if (n == stay) {
+        if (tid == 0) list[0] = 0;
+        return;
+    }
+    const Slices sl(n, stay, s.slices);
+    UnitInfo *u = s.info + unit;
+    const int count = u->candidates, left = u->left;
+    for (int i = tid; i < 2 * BINS; i += 1024) (&lds.hist[0][0])[i] = 0;
+    if (tid < SLICES + 2) kept[tid] = 0;
+    if (tid == 0) last_slot = 0x7fffffff;
+    auto row = [&](int i, uint32_t &w, uint32_t &p) {              // candidate i's keys
+        if (i < PICK) {
+            w = cw[i];
+            p = cp[i];
+            return;
+        }
+        int block, place;
+        split_slot(a.g, list[1 + i], block, place);
+        const int page = page_of(a.g, b, block);
+        const int64_t at = table_index(a.g, page < 0 ? 0 : page, kv, place);
+        w = page < 0 ? 0 : weight_key(a.weight_in[at]);
+        p = pos_key(page < 0 ? 0 : a.pos_in[at]);
+    };
+#pragma unroll 4
+    for (int i = tid; i < count && i < PICK; i += 1024) {
+        int block, place;
+        split_slot(a.g, list[1 + i], block, place);
+        const int page = page_of(a.g, b, block);
+        const int64_t at = table_index(a.g, page < 0 ? 0 : page, kv, place);
+        cw[i] = page < 0 ? 0 : weight_key(a.weight_in[at]);
+        cp[i] = pos_key(page < 0 ? 0 : a.pos_in[at]);
+    }
+    __syncthreads();
+    Last last = {~0u, ~0u, 0};
+    if (left > 0) {
+        Spread sp = {0, 0, 0, 0, 0};
+        for (int i = tid; i < count; i += 1024) {
+            uint32_t w, p;
+            row(i, w, p);
+            sp.add(w, p, true);
+        }
+        sp.any_w = wave_or(sp.any_w);
+        sp.not_all_w = wave_or(sp.not_all_w);
+        sp.any_p = wave_or(sp.any_p);
+        sp.not_all_p = wave_or(sp.not_all_p);
+        if (lane == 0) {
+            lds.red[1][wave] = sp.any_w;
+            lds.red[2][wave] = sp.not_all_w;
+            lds.red[3][wave] = sp.any_p;
+            lds.red[4][wave] = sp.not_all_p;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            sp.any_w |= lds.red[1][i];
+            sp.not_all_w |= lds.red[2][i];
+            sp.any_p |= lds.red[3][i];
+            sp.not_all_p |= lds.red[4][i];
+        }
+        last = descend<1024>(lds, sp, left, [&](auto f) {
+            for (int i = tid; i < count; i += 1024) {
+                uint32_t w, p;
+                row(i, w, p);
+                f(w, p);
+            }
+        });
+        if (last.ties != 0x7fffffff) {                             // the slot of the last of the equals that stay: candidates are in slot order
+            int before = 0;
+            for (int base = 0; base < count; base += 1024) {
+                const int i = base + tid;
+                uint32_t w = 0, p = 0;
+                if (i < count) row(i, w, p);
+                const bool tie = i < count && standing(last, w, p) == 1;
+                const uint32_t up = wave_scan(tie);
+                __syncthreads();
+                if (lane == 63) lds.red[0][wave] = up;
+                __syncthreads();
+                int at = before + (int)up;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    at += x < wave ? (int)lds.red[0][x] : 0;
+                    before += (int)lds.red[0][x];
+                }
+                if (tie && at == last.ties) last_slot = list[1 + i];
             }
         }
     }
-    if (tid == 0) list[0] = (int32_t)seen_move;
-    if (move_here && seen_move > 0) {
-        __syncthreads();
-        move_rows(a, b, kv, list + 1, list + 1 + a.cap, (int)seen_move, tid, THREADS);
+    __syncthreads();
+    const int ls = last_slot;
+    if (left > 0)
+        for (int i = tid; i < count; i += 1024) {
+            uint32_t w, p;
+            row(i, w, p);
+            const int st = standing(last, w, p), slot = list[1 + i];
+            if (st == 2 || (st == 1 && slot <= ls)) atomicAdd(&kept[sl.of(slot, stay)], 1);
+        }
+    __syncthreads();
+    if (tid < 64) {
+        const int begin = sl.begin(tid, stay), rows = tid < sl.count ? sl.end(tid, n, stay) - begin : 0;
+        const int k = tid < sl.count ? u->slice[tid].kept + kept[tid] : 0;
+        const uint32_t free_here = tid < sl.low ? (uint32_t)(rows - k) : 0, move_here = tid >= sl.low ? (uint32_t)k : 0;
+        const uint32_t f = wave_scan(free_here), m = wave_scan(move_here);
+        if (tid < sl.count) u->slice[tid].at = (int32_t)(tid < sl.low ? f - free_here : m - move_here);
+        if (tid == 63) {
+            u->last_w = last.w;
+            u->last_p = last.p;
+            u->last_slot = ls;
+            list[0] = (int32_t)m;
+        }
     }
+}
+
+__global__ __launch_bounds__(256) void slice_list_kernel(SliceArgs s) {
+    const PagedEvictArgs &a = s.e;
+    __shared__ uint32_t red[2][4];
+    const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
+    const Slices sl(n > 0 ? n : 1, stay, s.slices);
+    if ((int)blockIdx.x >= sl.count) return;
+    const int begin = sl.begin((int)blockIdx.x, stay), end = sl.end((int)blockIdx.x, n, stay);
+    const bool low = (int)blockIdx.x < sl.low;
+    if (low && a.pos_out != a.pos_in)
+        for (int j = begin + 4 * tid; j < end; j += 1024) copy_entries(a, b, kv, j, end);
+    if (n == stay) return;
+    const int64_t total = a.g.seq_pos[b], unit = (int64_t)b * a.g.n_kv + kv;
+    const UnitInfo *u = s.info + unit;
+    const bool among_safe = u->among_safe != 0, any_left = u->left > 0;
+    const uint32_t bin = (uint32_t)u->bin;
+    const Last last = {u->last_w, u->last_p, 0};
+    const int last_slot = u->last_slot;
+    int32_t *out = a.moves + moves_of(a.cap, unit) + 1 + (low ? 0 : a.cap) + u->slice[blockIdx.x].at;
+    int parity = 0;
+    slice_rows(a, b, kv, begin, end, [&](int j, const Four &r) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t w = weight_key(r.w[e]);
+            bool kept;
+            if (is_safe(a, total, r.pos[e]) != among_safe) {
+                kept = !among_safe;
+            } else if (!any_left || w >> (32 - TOP) != bin) {
+                kept = any_left && w >> (32 - TOP) > bin;
+            } else {
+                const int st = standing(last, w, pos_key(r.pos[e]));
+                kept = st == 2 || (st == 1 && j + e <= last_slot);
+            }
+            bits |= j + e < end && kept != low ? 1u << e : 0u;
+        }
+        const uint32_t c = (uint32_t)__popc(bits), up = wave_scan(c);
+        if (lane == 63) red[parity][wave] = up;
+        __syncthreads();
+        uint32_t at = up - c, all = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            at += i < wave ? red[parity][i] : 0;
+            all += red[parity][i];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (bits >> e & 1) out[at++] = j + e;
+        out += all;
+        parity ^= 1;
+    });
 }
 
 // grid = (kv heads, sequences, workgroups per unit)
@@ -416,7 +877,29 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
     move_rows(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)(blockIdx.z * 256 + threadIdx.x), (int)gridDim.z * 256);
 }
 
-static int evict_cap(const ssd_paged_config *c, int max_len) { return paged_reach(c, max_len) / 2 + 1; }
+// ---- launch shapes and memory ------------------------------------------------------------------------------------------------
+
+struct EvictShape {
+    int cap, slices;                                               // slices: 0 where a unit is one workgroup's
+    size_t moves, hist, info;
+};
+
+static EvictShape evict_shape(const ssd_paged_config *c, int max_len) {
+    EvictShape s;
+    const int reach = paged_reach(c, max_len);
+    const int64_t units = (int64_t)c->n_seqs * c->n_kv_heads;
+    s.cap = reach / 2 + 1;
+    s.slices = 0;
+    if (reach > 16384) {
+        const int64_t rows = (reach + 4095) / 4096, share = 2048 / units + 1;
+        s.slices = (int)(rows < share ? rows : share);
+        if (s.slices > SLICES) s.slices = SLICES;
+    }
+    s.moves = round256((size_t)moves_of(s.cap, units) * 4);
+    s.hist = s.slices ? (size_t)units * (s.slices + 2) * 2 * TOP_BINS * 4 : 0;
+    s.info = s.slices ? round256((size_t)units * sizeof(UnitInfo)) : 0;
+    return s;
+}
 
 }  // namespace ssd
 
@@ -425,7 +908,8 @@ using namespace ssd;
 extern "C" size_t ssd_paged_evict_workspace_bytes(const ssd_paged_config *cfg, int max_len) {
     clear_error();
     if (check_paged(cfg) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
-    return round256((size_t)moves_of(evict_cap(cfg, max_len), (int64_t)cfg->n_seqs * cfg->n_kv_heads) * 4);
+    const EvictShape s = evict_shape(cfg, max_len);
+    return s.moves + s.hist + s.info;
 }
 
 extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, const int32_t *block_table, const int32_t *seq_len,
@@ -446,7 +930,8 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     const void *all[] = {block_table, seq_len, seq_pos, budget, pos_in, pos_out, weight_in, weight_out, seq_len_out};
     for (const void *x : all)
         if (!aligned(x, 4)) return fail(SSD_ERR_INVALID_ARG, "tables must be aligned to their elements");
-    const size_t need = ssd_paged_evict_workspace_bytes(cfg, max_len);
+    const EvictShape shape = evict_shape(cfg, max_len);
+    const size_t need = shape.moves + shape.hist + shape.info;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
         return fail(SSD_ERR_INVALID_ARG, "workspace of %zu bytes, 256-byte aligned, needed; %zu given", need, workspace_bytes);
     PagedEvictArgs a;
@@ -462,18 +947,30 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     a.moves = static_cast<int32_t *>(workspace);
     a.n_sink = n_sink;
     a.recent = recent;
-    a.cap = evict_cap(cfg, max_len);
+    a.cap = shape.cap;
     a.lpr_log2 = __builtin_ctz((unsigned)((size_t)cfg->head_dim * paged_esize(cfg) / 16));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 units((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs);
     const int64_t n_units = (int64_t)units.x * units.y;
-    const int move_here = n_units >= 128;
     const int reach = a.g.max_len;
-    if (reach <= 256) hipLaunchKernelGGL((paged_select_kernel<64, 4>), units, dim3(64), 0, s, a, move_here);
+    const int move_here = n_units >= 128 && !shape.slices;
+    if (shape.slices) {
+        SliceArgs sa;
+        sa.e = a;
+        char *ws = static_cast<char *>(workspace);
+        sa.hist = reinterpret_cast<uint32_t *>(ws + shape.moves);
+        sa.info = reinterpret_cast<UnitInfo *>(ws + shape.moves + shape.hist);
+        sa.slices = shape.slices;
+        const dim3 slices((unsigned)shape.slices + 2, units.x, units.y);
+        hipLaunchKernelGGL(slice_count_kernel, slices, dim3(256), 0, s, sa);
+        hipLaunchKernelGGL(slice_bin_kernel, units, dim3(1024), 0, s, sa);
+        hipLaunchKernelGGL(slice_gather_kernel, slices, dim3(256), 0, s, sa);
+        hipLaunchKernelGGL(slice_pick_kernel, units, dim3(1024), 0, s, sa);
+        hipLaunchKernelGGL(slice_list_kernel, slices, dim3(256), 0, s, sa);
+    } else if (reach <= 256) hipLaunchKernelGGL((paged_select_kernel<64, 4>), units, dim3(64), 0, s, a, move_here);
     else if (reach <= 2048) hipLaunchKernelGGL((paged_select_kernel<256, 8>), units, dim3(256), 0, s, a, move_here);
     else if (reach <= 8192) hipLaunchKernelGGL((paged_select_kernel<1024, 8>), units, dim3(1024), 0, s, a, move_here);
-    else if (reach <= 16384) hipLaunchKernelGGL((paged_select_kernel<1024, 16>), units, dim3(1024), 0, s, a, move_here);
-    else hipLaunchKernelGGL((paged_select_kernel<1024, 0>), units, dim3(1024), 0, s, a, move_here);
+    else hipLaunchKernelGGL((paged_select_kernel<1024, 16>), units, dim3(1024), 0, s, a, move_here);
     if (!move_here) {
         const int64_t pieces = (a.cap + 31) / 32, enough = 2048 / n_units + 1;
         hipLaunchKernelGGL(paged_move_kernel, dim3(units.x, units.y, (unsigned)(pieces < enough ? pieces : enough)), dim3(256), 0, s, a);
