@@ -97,8 +97,7 @@ static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
 // Rows from[i] to slots to[i], i = first, first + step, ..; K and V of a row by neighbouring threads, their table entries by the first of them.
 // A thread has MOVES rows' loads in flight at each of the three stages (list, block table, row); past the end it repeats the last row, which
 // writes the same again.
-static constexpr int MOVES = 8;
-template <typename I>
+template <int MOVES, typename I>
 static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b, int kv, const I *to, const I *from, int count, int thread,
                                                  int threads) {
     const int lanes = 2 << a.lpr_log2, lane = thread & (lanes - 1), step = threads / lanes;
@@ -289,6 +288,48 @@ static __device__ __forceinline__ Last descend_wave(const Spread &sp, int left, 
     return r;
 }
 
+// Where few rows go: they are taken out one by one.  keys: this thread's; compete: which of them do; gone: the bits of rows that go are set.
+// The least key goes; of equal ones the highest slot (threads have consecutive rows).
+static constexpr int FEW = 4;
+template <int THREADS, int KEYS>
+static __device__ __forceinline__ uint32_t take_least(const uint32_t (&wk)[KEYS], const uint32_t (&pk)[KEYS], uint32_t compete, int rows,
+                                                      unsigned long long (&least)[2][THREADS / 64], int (&owner)[2][THREADS / 64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t gone = 0;
+    for (int i = 0; i < rows; ++i) {
+        unsigned long long m = ~0ull;
+        int at = 0;
+#pragma unroll
+        for (int k = 0; k < KEYS; ++k) {
+            const unsigned long long key = (unsigned long long)wk[k] << 32 | pk[k];
+            const bool less = ((compete & ~gone) >> k & 1) && key <= m;
+            m = less ? key : m;
+            at = less ? k : at;
+        }
+        unsigned long long all = wave_min_u64(m);
+        const bool any = (compete & ~gone) != 0;
+        int last = 63 - __clzll((long long)(__ballot(any && m == all) | 1));  // the highest lane that has it
+        bool ours = true;
+        if constexpr (THREADS > 64) {
+            if (lane == 0) {
+                least[i & 1][wave] = all;
+                owner[i & 1][wave] = __ballot(any) != 0;
+            }
+            __syncthreads();
+            int w = -1;
+#pragma unroll
+            for (int x = 0; x < THREADS / 64; ++x)
+                if (owner[i & 1][x] && (w < 0 || least[i & 1][x] <= all)) {
+                    w = x;
+                    all = least[i & 1][x];
+                }
+            ours = w == wave;
+        }
+        if (ours && lane == last) gone |= 1u << at;
+    }
+    return gone;
+}
+
 // 2: stays, 1: has the last row's keys, 0: goes.  Where the descent ended early the open bits of the last keys are 0 and everything
 // at or above them stays.
 static __device__ __forceinline__ int standing(const Last &l, uint32_t w, uint32_t p) {
@@ -336,6 +377,8 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     constexpr int NW = THREADS / 64, HALF = THREADS * KEYS / 2;
     __shared__ DescentLds<THREADS> lds;
     __shared__ uint16_t free_slots[HALF], move_slots[HALF];        // if the rows move here: at most half of them do
+    __shared__ unsigned long long least[2][NW];
+    __shared__ int owner[2][NW];
     const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const bool copy = a.pos_out != a.pos_in;
@@ -390,7 +433,10 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     const uint32_t compete = among_safe ? safe : in & ~safe;
     uint32_t kept = among_safe ? 0 : safe, tie = 0;
     Last last = {0, 0, 0};
-    if (left > 0) {
+    const int go = (among_safe ? (int)safe_rows : n - (int)safe_rows) - left;     // of those that compete
+    if (left > 0 && go <= FEW) {
+        kept |= compete & ~take_least<THREADS, KEYS>(wk, pk, compete, go, least, owner);
+    } else if (left > 0) {
         Spread sp = {0, 0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KEYS; ++k) sp.add(wk[k], pk[k], compete >> k & 1);
@@ -486,26 +532,29 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
         if (tid == 0) list[0] = moves;
     } else if (moves > 0) {
         __syncthreads();
-        move_rows(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
+        if (moves <= THREADS / (2 << a.lpr_log2)) move_rows<1>(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
+        else move_rows<8>(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
     }
 }
 
 // ---- long units ------------------------------------------------------------------------------------------------------------
 //
 // The rows below n' and those above are cut into slices of equally many rows, a workgroup each; a unit's own workgroup works in between.
-//   1 slices: how many rows have which upper 11 bits of their weight, protected ones and others apart
+//   1 slices: how many rows have which upper 12 bits of their weight, protected ones and others apart
 //   2 unit:   the bin in which the last place falls, and how many rows of a slice are above it and in it
 //   3 slices: the rows in the bin, in slot order, into one list (the memory of the moves, which come later)
 //   4 unit:   the descent among those; where each slice's free slots and moving rows begin in the lists
 //   5 slices: the lists
 //   6 as everywhere: the rows move
-static constexpr int TOP = 11, TOP_BINS = 1 << TOP, SLICES = 62;
+static constexpr int TOP = 12, TOP_BINS = 1 << TOP, SLICES = 62;
+static constexpr int ST = 1024;                                    // threads of a slice
 static constexpr int PICK = 6144;                                  // candidates whose keys fit in LDS
 
 // What step 2 and 4 leave for a unit's slices.
 struct SliceInfo {
     int32_t kept, in_bin, first;                                   // rows above the bin, in it, and where the latter begin in the list
     int32_t at;                                                    // where its free slots, or its moving rows, begin in the lists
+    int32_t safe;                                                  // protected rows
 };
 struct UnitInfo {
     int32_t among_safe, bin, left, candidates;
@@ -536,33 +585,45 @@ struct Slices {
     __device__ __forceinline__ int of(int slot, int stay) const { return slot < stay ? slot / rows : low + (slot - stay) / rows; }
 };
 
-__global__ __launch_bounds__(256) void slice_count_kernel(SliceArgs s) {
+__global__ __launch_bounds__(ST) void slice_count_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
     __shared__ uint32_t hist[2][TOP_BINS];
+    __shared__ uint32_t red[ST / 64];
     const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const Slices sl(n > 0 ? n : 1, stay, s.slices);
     if (n == stay || (int)blockIdx.x >= sl.count) return;
     const int64_t total = a.g.seq_pos[b], unit = (int64_t)b * a.g.n_kv + kv;
-    for (int i = tid; i < 2 * TOP_BINS; i += 256) (&hist[0][0])[i] = 0;
+    for (int i = tid; i < 2 * TOP_BINS / 4; i += ST) reinterpret_cast<uint4 *>(&hist[0][0])[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     const int end = sl.end((int)blockIdx.x, n, stay);
-#pragma unroll 4
-    for (int j = sl.begin((int)blockIdx.x, stay) + 4 * tid; j < end; j += 1024) {
+    uint32_t safe = 0;
+    for (int j = sl.begin((int)blockIdx.x, stay) + 4 * tid; j < end; j += 4 * ST) {
         const Four r = table_rows(a, b, kv, j, end);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (j + e < end) atomicAdd(&hist[is_safe(a, total, r.pos[e])][weight_key(r.w[e]) >> (32 - TOP)], 1u);
+            if (j + e < end) {
+                const bool sf = is_safe(a, total, r.pos[e]);
+                safe += sf;
+                atomicAdd(&hist[sf][weight_key(r.w[e]) >> (32 - TOP)], 1u);
+            }
     }
+    safe = wave_sum(safe);
+    if ((tid & 63) == 0) red[tid >> 6] = safe;
     __syncthreads();
+    safe = 0;
+#pragma unroll
+    for (int i = 0; i < ST / 64; ++i) safe += red[i];
+    if (tid == 0) s.info[unit].slice[blockIdx.x].safe = (int32_t)safe;
     uint4 *out = reinterpret_cast<uint4 *>(s.hist + (unit * (s.slices + 2) + blockIdx.x) * 2 * TOP_BINS);
-    for (int i = tid; i < 2 * TOP_BINS / 4; i += 256) out[i] = *reinterpret_cast<const uint4 *>(&hist[0][0] + 4 * i);
+    // the protected rows' half only where there are such rows
+    for (int i = tid; i < (safe ? 2 : 1) * TOP_BINS / 4; i += ST) out[i] = *reinterpret_cast<const uint4 *>(&hist[0][0] + 4 * i);
 }
 
 __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
-    __shared__ uint32_t red[2][16];
-    __shared__ int found[3];
+    __shared__ uint32_t red[16];
+    __shared__ int found[3], safe_of[SLICES + 2];
     __shared__ SliceInfo info[SLICES + 2];
     const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
@@ -571,71 +632,73 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     const Slices sl(n, stay, s.slices);
     const int64_t unit = (int64_t)b * a.g.n_kv + kv;
     const uint32_t *hist = s.hist + unit * (s.slices + 2) * 2 * TOP_BINS;
-    // a thread has two bins of each kind, counted from the top
-    const int bin = TOP_BINS - 2 - 2 * tid;
-    uint32_t h[2][2] = {{0, 0}, {0, 0}};
-#pragma unroll 8
-    for (int i = 0; i < sl.count; ++i)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint2 x = *reinterpret_cast<const uint2 *>(hist + ((int64_t)i * 2 + k) * TOP_BINS + bin);
-            h[k][0] += x.y;
-            h[k][1] += x.x;
-        }
-    const uint32_t up0 = wave_scan(h[0][0] + h[0][1]), up1 = wave_scan(h[1][0] + h[1][1]);
-    if (lane == 63) {
-        red[0][wave] = up0;
-        red[1][wave] = up1;
+    UnitInfo *u = s.info + unit;
+    if (tid < 64) {
+        const uint32_t c = tid < sl.count ? (uint32_t)u->slice[tid].safe : 0;
+        safe_of[tid] = (int)c;
+        const uint32_t all = wave_sum(c);
+        if (tid == 0) found[2] = (int)all;
     }
-    __syncthreads();
-    uint32_t before[2] = {up0 - h[0][0] - h[0][1], up1 - h[1][0] - h[1][1]}, safe_rows = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        before[0] += i < wave ? red[0][i] : 0;
-        before[1] += i < wave ? red[1][i] : 0;
-        safe_rows += red[1][i];
-    }
-    const int k = (int)safe_rows >= stay;                          // 1: protected rows alone compete
-    const uint32_t left = (uint32_t)(k ? stay : stay - (int)safe_rows);
     if (tid == 0) {
         found[0] = TOP_BINS;                                       // no place to compete for: nothing is in or above this bin
         found[1] = 0;
     }
     __syncthreads();
-    uint32_t above = k ? before[1] : before[0];
+    const int safe_rows = found[2], k = safe_rows >= stay;         // k = 1: protected rows alone compete
+    const uint32_t left = (uint32_t)(k ? stay : stay - safe_rows);
+    // a thread has PER bins, counted from the top
+    constexpr int PER = TOP_BINS / 1024;
+    static_assert(PER == 4, "bins are read four at a time");
+    const int bin = TOP_BINS - PER * (tid + 1);
+    uint32_t h[PER] = {0, 0, 0, 0};
+    auto add = [&](int i) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(hist + ((int64_t)i * 2 + k) * TOP_BINS + bin);
+        h[0] += x.w;
+        h[1] += x.z;
+        h[2] += x.y;
+        h[3] += x.x;
+    };
+    if (!k) {
+#pragma unroll 8
+        for (int i = 0; i < sl.count; ++i) add(i);
+    } else {
+        for (int i = 0; i < sl.count; ++i)
+            if (safe_of[i] > 0) add(i);
+    }
+    const uint32_t mine = h[0] + h[1] + h[2] + h[3], up = wave_scan(mine);
+    if (lane == 63) red[wave] = up;
+    __syncthreads();
+    uint32_t above = up - mine;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t c = k ? h[1][i] : h[0][i];
-        if (left > 0 && above < left && above + c >= left) {
-            found[0] = bin + 1 - i;
+    for (int i = 0; i < 16; ++i) above += i < wave ? red[i] : 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (left > 0 && above < left && above + h[i] >= left) {
+            found[0] = bin + PER - 1 - i;
             found[1] = (int)(left - above);
         }
-        above += c;
+        above += h[i];
     }
     __syncthreads();
     const int at = found[0];
     // a wave per slice: what it has above the bin and in it
     for (int i = wave; i < sl.count; i += 16) {
-        const uint32_t *mine = hist + ((int64_t)i * 2 + k) * TOP_BINS, *others = hist + ((int64_t)i * 2 + 1) * TOP_BINS;
-        uint32_t over = 0, safe = 0;
-#pragma unroll 8
-        for (int x = lane * 4; x < TOP_BINS; x += 256) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(mine + x);
-            over += (x > at ? v.x : 0) + (x + 1 > at ? v.y : 0) + (x + 2 > at ? v.z : 0) + (x + 3 > at ? v.w : 0);
-            if (!k) {
-                const uint4 o = *reinterpret_cast<const uint4 *>(others + x);
-                safe += o.x + o.y + o.z + o.w;
+        const uint32_t *row = hist + ((int64_t)i * 2 + k) * TOP_BINS;
+        const bool any = !k || safe_of[i] > 0;
+        uint32_t over = 0;
+        if (any)
+#pragma unroll 4
+            for (int x = lane * 4; x < TOP_BINS; x += 256) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(row + x);
+                over += (x > at ? v.x : 0) + (x + 1 > at ? v.y : 0) + (x + 2 > at ? v.z : 0) + (x + 3 > at ? v.w : 0);
             }
-        }
         over = wave_sum(over);
-        safe = wave_sum(safe);
-        if (lane == 0) info[i] = SliceInfo{(int32_t)(over + safe), at < TOP_BINS ? (int32_t)mine[at] : 0, 0, 0};
+        if (lane == 0) info[i] = SliceInfo{(int32_t)over + (k ? 0 : safe_of[i]), any && at < TOP_BINS ? (int32_t)row[at] : 0, 0, 0, 0};
     }
     __syncthreads();
     if (tid < 64) {
         const uint32_t c = tid < sl.count ? (uint32_t)info[tid].in_bin : 0, up = wave_scan(c);
-        UnitInfo *u = s.info + unit;
-        if (tid < sl.count) u->slice[tid] = SliceInfo{info[tid].kept, info[tid].in_bin, (int32_t)(up - c), 0};
+        if (tid < sl.count) u->slice[tid] = SliceInfo{info[tid].kept, info[tid].in_bin, (int32_t)(up - c), 0, safe_of[tid]};
         if (tid == 63) {
             u->among_safe = k;
             u->bin = at;
@@ -645,22 +708,22 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     }
 }
 
-// A slice's rows 1024 at a time, four a thread: body(first row of the thread, its rows or none) between barriers of its own.
+// A slice's rows 4 * ST at a time, four a thread: body(first row of the thread, its rows or none) between barriers of its own.
 template <typename Body>
 static __device__ __forceinline__ void slice_rows(const PagedEvictArgs &a, int b, int kv, int begin, int end, const Body &body) {
     Four r[2];
     int j = begin + 4 * (int)threadIdx.x;
     if (j < end) r[0] = table_rows(a, b, kv, j, end);
-    for (int base = begin; base < end; base += 1024, j += 1024) {
-        if (j + 1024 < end) r[1] = table_rows(a, b, kv, j + 1024, end);       // on its way while these are ranked
+    for (int base = begin; base < end; base += 4 * ST, j += 4 * ST) {
+        if (j + 4 * ST < end) r[1] = table_rows(a, b, kv, j + 4 * ST, end);       // on its way while these are ranked
         body(j, r[0]);
         r[0] = r[1];
     }
 }
 
-__global__ __launch_bounds__(256) void slice_gather_kernel(SliceArgs s) {
+__global__ __launch_bounds__(ST) void slice_gather_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
-    __shared__ uint32_t red[2][4];
+    __shared__ uint32_t red[2][ST / 64];
     const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const Slices sl(n > 0 ? n : 1, stay, s.slices);
@@ -683,7 +746,7 @@ __global__ __launch_bounds__(256) void slice_gather_kernel(SliceArgs s) {
         __syncthreads();
         uint32_t at = up - c, all = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < ST / 64; ++i) {
             at += i < wave ? red[parity][i] : 0;
             all += red[parity][i];
         }
@@ -817,9 +880,9 @@ __global__ __launch_bounds__(1024) void slice_pick_kernel(SliceArgs s) {
     }
 }
 
-__global__ __launch_bounds__(256) void slice_list_kernel(SliceArgs s) {
+__global__ __launch_bounds__(ST) void slice_list_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
-    __shared__ uint32_t red[2][4];
+    __shared__ uint32_t red[2][ST / 64];
     const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const Slices sl(n > 0 ? n : 1, stay, s.slices);
@@ -827,7 +890,7 @@ __global__ __launch_bounds__(256) void slice_list_kernel(SliceArgs s) {
     const int begin = sl.begin((int)blockIdx.x, stay), end = sl.end((int)blockIdx.x, n, stay);
     const bool low = (int)blockIdx.x < sl.low;
     if (low && a.pos_out != a.pos_in)
-        for (int j = begin + 4 * tid; j < end; j += 1024) copy_entries(a, b, kv, j, end);
+        for (int j = begin + 4 * tid; j < end; j += 4 * ST) copy_entries(a, b, kv, j, end);
     if (n == stay) return;
     const int64_t total = a.g.seq_pos[b], unit = (int64_t)b * a.g.n_kv + kv;
     const UnitInfo *u = s.info + unit;
@@ -858,7 +921,7 @@ __global__ __launch_bounds__(256) void slice_list_kernel(SliceArgs s) {
         __syncthreads();
         uint32_t at = up - c, all = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < ST / 64; ++i) {
             at += i < wave ? red[parity][i] : 0;
             all += red[parity][i];
         }
@@ -874,7 +937,7 @@ __global__ __launch_bounds__(256) void slice_list_kernel(SliceArgs s) {
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
     const int kv = blockIdx.x, b = blockIdx.y;
     const int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
-    move_rows(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)(blockIdx.z * 256 + threadIdx.x), (int)gridDim.z * 256);
+    move_rows<8>(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)(blockIdx.z * 256 + threadIdx.x), (int)gridDim.z * 256);
 }
 
 // ---- launch shapes and memory ------------------------------------------------------------------------------------------------
@@ -962,11 +1025,11 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
         sa.info = reinterpret_cast<UnitInfo *>(ws + shape.moves + shape.hist);
         sa.slices = shape.slices;
         const dim3 slices((unsigned)shape.slices + 2, units.x, units.y);
-        hipLaunchKernelGGL(slice_count_kernel, slices, dim3(256), 0, s, sa);
+        hipLaunchKernelGGL(slice_count_kernel, slices, dim3(ST), 0, s, sa);
         hipLaunchKernelGGL(slice_bin_kernel, units, dim3(1024), 0, s, sa);
-        hipLaunchKernelGGL(slice_gather_kernel, slices, dim3(256), 0, s, sa);
+        hipLaunchKernelGGL(slice_gather_kernel, slices, dim3(ST), 0, s, sa);
         hipLaunchKernelGGL(slice_pick_kernel, units, dim3(1024), 0, s, sa);
-        hipLaunchKernelGGL(slice_list_kernel, slices, dim3(256), 0, s, sa);
+        hipLaunchKernelGGL(slice_list_kernel, slices, dim3(ST), 0, s, sa);
     } else if (reach <= 256) hipLaunchKernelGGL((paged_select_kernel<64, 4>), units, dim3(64), 0, s, a, move_here);
     else if (reach <= 2048) hipLaunchKernelGGL((paged_select_kernel<256, 8>), units, dim3(256), 0, s, a, move_here);
     else if (reach <= 8192) hipLaunchKernelGGL((paged_select_kernel<1024, 8>), units, dim3(1024), 0, s, a, move_here);
