@@ -44,6 +44,19 @@ static __device__ __forceinline__ int64_t table_index(const PagedGeom &g, int pa
     return ((int64_t)page * g.n_kv + kv) * g.page_size + place;
 }
 
+// Inclusive sum over the lanes of a wave: rows of 16 by shifts, then the last lane of a row to the rows behind it.
+template <int CTRL, int ROWS> static __device__ __forceinline__ uint32_t dpp_add(uint32_t v) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+static __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    v = dpp_add<0x111, 0xF>(v);
+    v = dpp_add<0x112, 0xF>(v);
+    v = dpp_add<0x114, 0xF>(v);
+    v = dpp_add<0x118, 0xF>(v);
+    v = dpp_add<0x142, 0xA>(v);
+    return dpp_add<0x143, 0xC>(v);
+}
+static __device__ __forceinline__ uint32_t wave_sum(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(v), 63); }
 // Checks of the config (with the error text set), then the geometry; max_len <= 0 selects the table's reach.
 int check_paged(const ssd_paged_config *c);
 PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, int max_len);

@@ -237,19 +237,6 @@ template <typename T> static __device__ __forceinline__ void store_out(char *out
 
 static __device__ __forceinline__ int rounds_of(int n, int round) { return n == 0 ? 1 : (n + round - 1) / round; }
 
-static __device__ __forceinline__ uint32_t wave_sum_u32(uint32_t v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += (uint32_t)__shfl_xor((int)v, o);
-    return v;
-}
-static __device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t w = (uint32_t)__shfl_up((int)v, o);
-        v += lane >= o ? w : 0;
-    }
-    return v;
-}
 static __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
 // The runs: `all` rounds over at most `most` workgroups, none below two rounds where there are 256 workgroups without.
@@ -338,7 +325,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             const int seq = lane * run + i;
             if (seq < a.g.n_seqs) mine += (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
         }
-        uint32_t upto = wave_scan_u32(mine, lane);
+        uint32_t upto = wave_scan(mine);
         const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * K;
         const Runs runs(all, (uint32_t)a.workgroups);
         const uint32_t r0 = runs.start(blockIdx.x), r1 = runs.start(blockIdx.x + 1);
@@ -351,7 +338,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         for (int i0 = 0; run > 1; i0 += 64) {                       // the run's sequences, 64 at a time
             const int seq = l * run + i0 + lane;
             const bool ours = i0 + lane < run && seq < a.g.n_seqs;
-            const uint32_t up = wave_scan_u32(ours ? (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND) : 0u, lane) + before;
+            const uint32_t up = wave_scan(ours ? (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND) : 0u) + before;
             const int k = (int)__popcll(__ballot(up <= at));
             if (k < 64) {
                 b = l * run + i0 + k;
@@ -386,8 +373,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         }
         typename TT::Q q;
         TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (r < heads ? r : 0)) * (D * sizeof(T)), lane, q);
-        float *z_unit = WEIGHTS ? a.z + ((int64_t)b * a.n_heads + head0) * a.z_stride : nullptr;
-        const uint32_t z_lane = WEIGHTS ? (uint32_t)(r < heads ? r : 0) * (uint32_t)a.z_stride + 4u * (uint32_t)g : 0;
+        // the unit's logits; lanes without a head are out of the buffer's bounds, and what they store is dropped
+        __amdgpu_buffer_rsrc_t z_unit;
+        uint32_t z_lane = 0;
+        if constexpr (WEIGHTS) {
+            float *at = a.z + ((int64_t)b * a.n_heads + head0) * a.z_stride;
+            z_unit = __builtin_amdgcn_make_buffer_rsrc(at, 0, (int)(4u * (uint32_t)heads * (uint32_t)a.z_stride), 0x00027000);
+            z_lane = r < heads ? 4u * ((uint32_t)r * (uint32_t)a.z_stride + 4u * (uint32_t)g) : 0x80000000u;
+        }
 
         float m = NEG_BIG, l = 0.f;
         f32x4 o[TT::NV];
@@ -442,10 +435,11 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                 }
 #pragma unroll
                 for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
-                if constexpr (WEIGHTS)                              // lanes without a head repeat the first head's: the same values
+                if constexpr (WEIGHTS)
 #pragma unroll
                     for (int e = 0; e < NZ; e += 4)
-                        *reinterpret_cast<f32x4 *>(z_unit + (z_lane + (uint32_t)(row0 + first + 4 * e))) = f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]};
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_nt_t, f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]}), z_unit,
+                                                               (int)(z_lane + 4u * (uint32_t)(row0 + first + 4 * e)), 0, 0);
                 const bool all = __all(there == (1u << NZ) - 1u);
                 if (!all) {
 #pragma unroll
@@ -612,8 +606,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
             all += x;
             before += seq < b ? x : 0;
         }
-        all = uniform(wave_sum_u32(all)) * K;
-        before = uniform(wave_sum_u32(before)) * K;
+        all = uniform(wave_sum(all)) * K;
+        before = uniform(wave_sum(before)) * K;
     }
     // the workgroups that share a unit, and where the first one's part lies
     struct Parts { uint32_t w0, count, slot0; };
@@ -745,7 +739,8 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
     s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
     s.round = s.waves * tile;
-    s.workgroups = plain ? 0 : (int)(units * rounds < 768 ? units * rounds : 768);
+    const int64_t resident = c->head_dim == 64 ? 1024 : 768;        // 256 compute units, four or three workgroups each
+    s.workgroups = plain ? 0 : (int)(units * rounds < resident ? units * rounds : resident);
     // a stage's blocks: its rows and what lies before them in the first one; block_of allows 2^16 rows
     const int64_t most = (int64_t)(blocks_of(s.waves) - 1) * c->page_size;
     s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);

@@ -75,19 +75,6 @@ static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b
     return r;
 }
 
-// Inclusive sum over the lanes of a wave: rows of 16 by shifts, then the last lane of a row to the rows behind it.
-template <int CTRL, int ROWS> static __device__ __forceinline__ uint32_t dpp_add(uint32_t v) {
-    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
-}
-static __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
-    v = dpp_add<0x111, 0xF>(v);
-    v = dpp_add<0x112, 0xF>(v);
-    v = dpp_add<0x114, 0xF>(v);
-    v = dpp_add<0x118, 0xF>(v);
-    v = dpp_add<0x142, 0xA>(v);
-    return dpp_add<0x143, 0xC>(v);
-}
-static __device__ __forceinline__ uint32_t wave_sum(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(v), 63); }
 static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) v |= (uint32_t)__shfl_xor((int)v, o);
