@@ -42,6 +42,7 @@ struct PagedAttnArgs {
     int n_heads, group, q_tiles;
     int tile_heads;           // min(group, 16)
     int workgroups;           // 0: a workgroup takes a whole unit
+    int by_length;            // then: the longest sequences first
     int stage;                // rows whose part of the block table is in LDS at a time: a multiple of a round
     uint32_t page_magic, single;   // ceil(2^32 / page_size) and 0, or 0 and 1 where that is 2^32
     float scale;              // softmax scale * log2 e
@@ -296,6 +297,31 @@ static __device__ __forceinline__ const PagedAttnArgs &arguments() {
     return *(const PagedAttnArgs *)p;
 }
 
+// The sequence of rank `rank` by length, the longest first, equal ones in their order; n_seqs <= 64 * PER.  Every lane has PER lengths; the length
+// of that rank is found bit by bit from ballots.
+template <int PER> static __device__ __forceinline__ int by_length(const PagedAttnArgs &a, int rank, int lane) {
+    int len[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) len[i] = 64 * i + lane < a.g.n_seqs ? clamp_len(a.g, 64 * i + lane) : -1;
+    int t = 0, above = 0;                                           // the length so far, sequences that are longer
+    for (int bit = 1 << (31 - __clz(a.g.max_len)); bit; bit >>= 1) {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c += (int)__popcll(__ballot((len[i] & ~(bit - 1)) == (t | bit)));
+        if (above + c > rank) t |= bit;
+        else above += c;
+    }
+    int left = rank - above;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const unsigned long long m = __ballot(len[i] == t);
+        const int c = (int)__popcll(m);
+        if (left < c) return 64 * i + kth_set_bit(m, 0, left);
+        left -= c;
+    }
+    return 0;
+}
+
 // grid = (workgroups), or (kv heads * tiles of query heads, sequences) where a workgroup takes a whole unit
 template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs) {
@@ -314,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     const PagedAttnArgs &a = arguments();
     const uint32_t K = (uint32_t)(a.g.n_kv * a.q_tiles);
     if (a.workgroups == 0) {
-        b = (int)blockIdx.y;
+        b = a.by_length ? by_length<2>(a, (int)blockIdx.y, lane) : (int)blockIdx.y;
         ht = (int)((blockIdx.x + blockIdx.y) % K);
         t = 0;
         left = (uint32_t)rounds_of(clamp_len(a.g, b), ROUND);
@@ -721,6 +747,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
 
 struct PagedShape {
     int waves, round, q_tiles, tile_heads, workgroups, stage;
+    bool by_length;
     int64_t reach;            // rows, in whole rounds
 };
 
@@ -741,6 +768,9 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     s.round = s.waves * tile;
     const int64_t resident = c->head_dim == 64 ? 1024 : 768;        // 256 compute units, four or three workgroups each
     s.workgroups = plain ? 0 : (int)(units * rounds < resident ? units * rounds : resident);
+    // Where not all units are resident at once a late long one would run on alone; ranking costs every workgroup a microsecond (32 heads of 64 to 640
+    // rows, 64 sequences 54 us in their order and 50 by length, 128 96 and 95, of 10 to 1000 rows 94 and 89; 256 168 and 173, 16 17.3 and 19.0).
+    s.by_length = plain && s.waves == 4 && units > 1024 && c->n_seqs <= 128;
     // a stage's blocks: its rows and what lies before them in the first one; block_of allows 2^16 rows
     const int64_t most = (int64_t)(blocks_of(s.waves) - 1) * c->page_size;
     s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);
@@ -837,6 +867,7 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     a.q_tiles = shape.q_tiles;
     a.tile_heads = shape.tile_heads;
     a.workgroups = shape.workgroups;
+    a.by_length = shape.by_length;
     a.stage = shape.stage;
     a.single = cfg->page_size == 1;
     a.page_magic = (uint32_t)((0xffffffffull + (unsigned)cfg->page_size) / (unsigned)cfg->page_size);

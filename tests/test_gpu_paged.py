@@ -57,6 +57,70 @@ def test_many_sequences_of_one_head_and_few_rows():
     check_attend(bt, attend(bt))
 
 
+@pytest.mark.parametrize("most", [100, 200, 400])
+def test_many_units_of_equal_and_unequal_lengths(most):
+    """Enough units for those that are taken by a wave each, and for those taken in the order of their lengths."""
+    lens = [most, 0, 1, most, 17, most // 2, most // 2, 3] * 5
+    for dtype in ("bf16", "f32"):
+        bt = Batch(lens if dtype == "bf16" else [n // 2 for n in lens], 32, 32, 64, dtype, 16, seed=most)
+        check_attend(bt, attend(bt))
+
+
+def test_long_rows_in_a_large_batch():
+    """More sequences than a wave has lanes, rows dealt to workgroups across them; sequences without rows at both ends."""
+    rng = np.random.default_rng(1)
+    lens = [0, 0] + [int(x) for x in np.exp(rng.uniform(0, np.log(900), 150))] + [0, 800, 0]
+    check_attend_of(lens, 2, 1, 64, "bf16")
+    lens = [0] * 4300
+    for i, n in ((0, 3), (64, 1), (65, 700), (127, 5), (128, 65), (1000, 1), (2111, 1030), (4299, 7)):
+        lens[i] = n
+    check_attend_of(lens, 1, 1, 64, "f32")
+
+
+def check_attend_of(lens, H, n_kv, d, dtype):
+    say("batch of", len(lens), H, n_kv, d, dtype)
+    bt = Batch(lens, H, n_kv, d, dtype, 16, seed=len(lens))
+    check_attend(bt, attend(bt))
+
+
+@pytest.mark.parametrize("page", [1, 3, 8])
+def test_small_pages_equal_large_ones(page):
+    """Runs of rows longer than the part of the block table that a workgroup has in LDS: the same rows in pages of 64 give the same bits."""
+    B, n_kv, d, n = 24, 8, 128, 4096
+    g = torch.Generator(device="cuda").manual_seed(page)
+    lens = torch.randint(3500, n + 1, (B,), device="cuda", generator=g).to(torch.int32)
+    k, v = (torch.randn((B, n_kv, n, d), device="cuda", generator=g, dtype=torch.bfloat16) for _ in range(2))
+    q = torch.randn((B, 2 * n_kv, d), device="cuda", generator=g, dtype=torch.bfloat16)
+    got = []
+    for p in (64, page):
+        blocks = -(-n // p)
+        pad = blocks * p - n
+        table = torch.randperm(B * blocks, device="cuda", generator=g).to(torch.int32).reshape(B, blocks)
+        pools = []
+        for x in (k, v):
+            x = torch.nn.functional.pad(x, (0, 0, 0, pad)).reshape(B, n_kv, blocks, p, d).transpose(1, 2).reshape(B * blocks, n_kv, p, d)
+            pool = torch.empty_like(x)
+            pool[table.reshape(-1).long()] = x
+            pools.append(pool)
+        cfg = ssd.make_paged_config(B, 2 * n_kv, n_kv, d, "bf16", p, B * blocks, blocks)
+        out, lse = torch.zeros_like(q), torch.zeros((B, 2 * n_kv), device="cuda")
+        w_in = torch.zeros((B * blocks, n_kv, p), device="cuda")
+        w_out = torch.zeros_like(w_in)
+        ws = torch.empty(ssd.ssd_paged_workspace_bytes(cfg, n, True), dtype=torch.uint8, device="cuda")
+        ssd.ssd_paged_decode_attn(cfg, q, pools[0], pools[1], table, lens, out, lse=lse, weight_in=w_in, weight_out=w_out, max_len=n, workspace=ws)
+        w = w_out[table.reshape(-1).long()].reshape(B, blocks, n_kv, p).transpose(1, 2).reshape(B, n_kv, -1)[:, :, :n]
+        got.append((out, lse, w))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+    sums = got[0][2].sum(-1)
+    assert bool(((sums - 2.0).abs() < 1e-3).all())            # two query heads' probabilities
+    for b in (0, B - 1):
+        m = int(lens[b])
+        z = (q[b].float().reshape(n_kv, 2, d) @ k[b, :, :m].float().transpose(1, 2).contiguous()) / d ** 0.5
+        ref = (torch.softmax(z, -1) @ v[b, :, :m].float()).reshape(2 * n_kv, d)
+        assert bool(((got[0][0][b].float() - ref).abs() <= 1e-2 * (1 + ref.abs())).all())
+
+
 def test_one_long_sequence_of_one_head():
     bt = Batch([9001], 1, 1, 64, "bf16", 64, seed=4)
     check_attend(bt, attend(bt))
