@@ -489,12 +489,12 @@ def _strided(t) -> Optional[int]:
     """Address of a tensor whose outer strides the config gives: rows alone have to be dense."""
     if t is None or isinstance(t, int):
         return t
-    assert t.stride(-1) == 1, "rows handed to the library must be dense"
+    assert t.is_contiguous() or t.stride(-1) == 1, "rows handed to the library must be dense"
     return t.data_ptr()
 
 
 def _size(t) -> int:
-    return 0 if t is None else t.numel() * t.element_size()
+    return 0 if t is None else t.nbytes
 
 
 def ssd_paged_append(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len, k_new, v_new, pos=None, weight=None, seq_pos=None,

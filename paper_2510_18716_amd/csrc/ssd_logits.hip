@@ -4,9 +4,9 @@
 // One workgroup takes a piece of a row's vocabulary.  Its logits are requested first, into registers; while they travel, the row's
 // tokens that fall into the piece are counted in LDS (whole-number atomics: their order does not matter), one count per entry with the highest bit for
 // "seen at all"; then the piece goes through once, 16 bytes of logits at a time.  Bound by HBM (the logits in, 4 bytes out each); the tokens are read
-// by every piece of the row, from L2.  256 rows of 128257 in fp32 with 1000 to 8000 tokens, shared bias and masks: 65 us, 4.2 TB/s (57 with short histories;
-// pieces of 16384 77, logits and bias both in registers 70 for fp32 and 3 more than without for bf16).  64 guided rows of 16384 in bf16: 5.0 us, the launch and three
-// dependent loads.
+// by every piece of the row, from L2.  256 rows of 128257 in fp32 with 1000 to 8000 tokens, shared bias and masks: 66 us, 4.1 TB/s (56 with short
+// histories, where a copy would take 50; 72 without the non-temporal hint on the stores; pieces of 4096 and 16384 and a bias held in registers gain
+// nothing).  64 guided rows of 16384 in bf16: 4.5 us, the launch and two dependent loads.
 #include <cmath>
 
 #include "ssd_device.h"
@@ -47,6 +47,9 @@ template <typename T> static __device__ __forceinline__ uint4 load_logits(const 
     return r;
 }
 
+// what an array that is not given stands for: repetition, presence, frequency, temperature
+__device__ const float logits_defaults[4] = {1.f, 0.f, 0.f, 1.f};
+
 // grid = (pieces, rows)
 template <typename T, int THREADS, int GROUPS>
 __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
@@ -59,6 +62,13 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
     const float *bias = a.p.bias ? a.p.bias + (int64_t)i * a.p.bias_stride : nullptr;
     const uint32_t *mask = a.p.mask ? a.p.mask + (int64_t)i * a.p.mask_stride : nullptr;
 
+    // all four at once, before anything waits
+    const float rep0 = *(a.p.repetition ? a.p.repetition + i : logits_defaults), presence = *(a.p.presence ? a.p.presence + i : logits_defaults + 1);
+    const float frequency = *(a.p.frequency ? a.p.frequency + i : logits_defaults + 2);
+    const float temp0 = *(a.p.temperature ? a.p.temperature + i : logits_defaults + 3);
+    const bool told = a.p.tokens != nullptr;
+    int64_t n = told ? a.p.n_tokens[i] : 0;
+    const int64_t n_prompt = told && a.p.n_prompt ? a.p.n_prompt[i] : 0;
     uint4 cr[GROUPS], ur[GROUPS];
     uint32_t allowed[GROUPS];
 #pragma unroll
@@ -68,14 +78,11 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         if (a.guided) ur[g] = load_logits(u + v, a.V - v);
         allowed[g] = mask && v < a.V ? mask[v >> 5] >> (v & 31) : ~0u;      // a group lies in one word
     }
-    const bool told = a.p.tokens != nullptr;
     if (told) {
 #pragma unroll
         for (int j = 0; j < PIECE / 4; j += THREADS) *reinterpret_cast<uint4 *>(&count[4 * (j + tid)]) = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        int64_t n = a.p.n_tokens[i];
         n = n < 0 ? 0 : n > a.p.token_stride ? a.p.token_stride : n;
-        const int64_t n_prompt = a.p.n_prompt ? a.p.n_prompt[i] : 0;
         const int32_t *tok = a.p.tokens + (int64_t)i * a.p.token_stride;
         auto one = [&](int t, int64_t j) {
             const unsigned at = (unsigned)t - (unsigned)v0;
@@ -94,9 +101,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         for (int e = 0; e < 4 && j + e < n; ++e) one(tok[j + e], j + e);
         __syncthreads();
     }
-    const float rep0 = a.p.repetition ? a.p.repetition[i] : 1.f, temp0 = a.p.temperature ? a.p.temperature[i] : 1.f;
     const float rep = rep0 > 0.f ? rep0 : 1.f, cool = temp0 > 0.f ? 1.f / temp0 : 1.f;
-    const float presence = a.p.presence ? a.p.presence[i] : 0.f, frequency = a.p.frequency ? a.p.frequency[i] : 0.f;
     float *o = a.out + (int64_t)i * a.out_stride;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
@@ -146,7 +151,8 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         }
         if (full) {
 #pragma unroll
-            for (int e = 0; e < VEC; e += 4) *reinterpret_cast<f32x4_any_t *>(o + v + e) = f32x4_t{x[e], x[e + 1], x[e + 2], x[e + 3]};
+            for (int e = 0; e < VEC; e += 4)                       // written once, and more than L2 holds where it counts
+                __builtin_nontemporal_store((f32x4_any_t)f32x4_t{x[e], x[e + 1], x[e + 2], x[e + 3]}, reinterpret_cast<f32x4_any_t *>(o + v + e));
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
