@@ -294,6 +294,31 @@ def test_append_of_many_tokens_and_sequences():
     assert torch.equal(pos[rest, 0].reshape(-1)[:67000], torch.arange(67000, device="cuda", dtype=torch.int32))
 
 
+def test_append_of_more_than_the_memory_side_cache():
+    lens = [20001, 3000, 17000]
+    d, page, n_kv = 128, 16, 16
+    blocks = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(blocks), generator=torch.Generator().manual_seed(5)).to(torch.int32)
+    table = torch.full((3, max(blocks)), -1, dtype=torch.int32)
+    at = 0
+    for b, n in enumerate(blocks):
+        table[b, :n] = order[at:at + n]
+        at += n
+    total = sum(lens)
+    assert total * n_kv * d * 2 * 2 > 256 << 20
+    kn, vn = (torch.randn((total, n_kv, d), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    k = torch.zeros((sum(blocks), n_kv, page, d), device="cuda", dtype=torch.bfloat16)
+    v = torch.zeros_like(k)
+    cfg = ssd.make_paged_config(3, n_kv, n_kv, d, "bf16", page, sum(blocks), max(blocks))
+    start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    ssd.ssd_paged_append(cfg, k, v, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), kn, vn, new_start=torch.from_numpy(start).cuda())
+    for b, n in enumerate(lens):
+        rows = table[b, :blocks[b]].long().cuda()
+        for pool, new in ((k, kn), (v, vn)):
+            got = pool[rows].transpose(1, 2).reshape(-1, n_kv, d)
+            assert torch.equal(got[:n], new[start[b]:start[b + 1]]) and not bool(got[n:].any())
+
+
 @pytest.mark.parametrize("dtype,d,H,n_kv,page", [("bf16", 128, 8, 2, 16), ("f32", 64, 3, 3, 7), ("bf16", 64, 16, 1, 64), ("f32", 128, 6, 2, 32)])
 def test_step_is_append_and_attention(dtype, d, H, n_kv, page):
     lens = [1, 0, 16, 17, 65, 300, 2, 1200]
@@ -455,6 +480,99 @@ def test_eviction_of_a_long_sequence():
             rows = vv[table[0].long()].transpose(0, 1).reshape(n_kv, n, d)[kv, :budget]
             assert torch.equal(rows, torch.from_numpy(src).cuda().float()[:, None].expand(budget, d) + 0.5)
         assert ln.tolist() == [budget]
+
+
+def _table_case(lens, budgets, n_kv, page, weight_of, pos_of, sink, recent, totals, in_place, max_len=0, seed=1):
+    """Eviction judged by its tables and by rows that carry their own slot: sequences too long for the implementation one row at a time."""
+    say("tables", lens, budgets, page, sink, recent, in_place)
+    rng = np.random.default_rng(seed)
+    d, B = 64, len(lens)
+    blocks = [-(-n // page) for n in lens]
+    n_pages, max_blocks = sum(blocks) + 2, max(blocks)
+    order = rng.permutation(n_pages)
+    table = np.full((B, max_blocks), -1, np.int32)
+    at = 0
+    for b, n in enumerate(blocks):
+        table[b, :n] = order[at:at + n]
+        at += n
+    pos, weight = np.full((n_pages, n_kv, page), -9, np.int32), np.full((n_pages, n_kv, page), np.nan, np.float32)
+    rows = np.zeros((n_pages, n_kv, page), np.float32)
+    unit = {}
+    for b, n in enumerate(lens):
+        i = np.arange(n)
+        pages, places = table[b][i // page], i % page
+        for kv in range(n_kv):
+            p, w = pos_of(rng, n), weight_of(rng, n).astype(np.float32)
+            pos[pages, kv, places], weight[pages, kv, places], rows[pages, kv, places] = p, w, i + 1
+            unit[b, kv] = (p, w, pages, places)
+    kd = torch.from_numpy(rows).cuda()[..., None].expand(n_pages, n_kv, page, d).contiguous()
+    vd = -kd
+    pd, wd = torch.from_numpy(pos).cuda(), torch.from_numpy(weight).cuda()
+    po, wo = (pd, wd) if in_place else (torch.full_like(pd, -5), torch.full_like(wd, -5.0))
+    cfg = ssd.make_paged_config(B, n_kv, n_kv, d, "f32", page, n_pages, max_blocks)
+    ln = torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    ws = torch.full((max(1, ssd.ssd_paged_evict_workspace_bytes(cfg, max_len) // 4),), float("nan"), device="cuda")
+    ssd.ssd_paged_evict(cfg, kd, vd, torch.from_numpy(table).cuda(), ints(lens), ints(budgets), pd, po, wd, wo, ln, n_sink=sink, recent=recent, seq_pos=ints(totals),
+                        max_len=max_len, workspace=ws)
+    got_p, got_w, got_k, got_v = po.cpu().numpy(), wo.cpu().numpy(), kd.cpu().numpy(), vd.cpu().numpy()
+    assert ln.tolist() == [min(n, max(0, m)) for n, m in zip(lens, budgets)]
+    for (b, kv), (p, w, pages, places) in unit.items():
+        n, stay = lens[b], min(lens[b], max(0, budgets[b]))
+        safe = (p < sink) | (p >= totals[b] - recent)
+        with np.errstate(invalid="ignore"):
+            key = np.where(np.isnan(w), np.inf, -w.astype(np.float64))
+        best = np.lexsort((np.arange(n), p, key, np.isnan(w), ~safe))[:stay]
+        src = np.arange(stay)
+        src[~np.isin(src, best)] = np.sort(best[best >= stay])
+        np.testing.assert_array_equal(got_p[pages[:stay], kv, places[:stay]], p[src])
+        np.testing.assert_array_equal(got_w[pages[:stay], kv, places[:stay]], w[src])
+        np.testing.assert_array_equal(got_k[pages[:stay], kv, places[:stay]], np.broadcast_to((src + 1.0)[:, None], (stay, d)))
+        np.testing.assert_array_equal(got_v[pages[:stay], kv, places[:stay]], np.broadcast_to(-(src + 1.0)[:, None], (stay, d)))
+        if not in_place:                                            # nothing past n' is written
+            assert np.all(got_p[pages[stay:], kv, places[stay:]] == -5) and np.all(got_w[pages[stay:], kv, places[stay:]] == -5.0)
+
+
+WEIGHTS = {
+    "usual": lambda r, n: r.random(n) ** -0.7 - 1,
+    "zeros": lambda r, n: np.zeros(n),
+    "mostly zeros": lambda r, n: np.where(r.random(n) < 0.8, 0.0, r.random(n)),
+    "steps": lambda r, n: r.integers(0, 5, n) * 0.25,
+    "any": lambda r, n: r.choice(np.array([np.inf, -np.inf, np.nan, -0.0, 0.0, 3e38, 1e-44, -2.0, 1.0]), n),
+    "neighbours": lambda r, n: (np.float32(1).view(np.int32) + r.integers(0, 3000, n)).astype(np.int32).view(np.float32),
+}
+
+
+@pytest.mark.parametrize("name", sorted(WEIGHTS))
+@pytest.mark.parametrize("in_place", [False, True])
+def test_eviction_of_long_units_in_slices(name, in_place):
+    lens = [17000, 33001, 0, 5, 300, 16385, 20000, 20000]
+    budgets = [4000, 33000, 7, 5, 100, 16384, 1, 0]
+    upright = lambda r, n: np.arange(n)  # noqa: E731
+    mixed = lambda r, n: r.permutation(n + 40)[:n]  # noqa: E731
+    _table_case(lens, budgets, 2, 64, WEIGHTS[name], upright, 4, 100, lens, in_place)
+    _table_case(lens, [n // 2 for n in lens], 1, 24, WEIGHTS[name], mixed, 0, 7, [n + 40 for n in lens], in_place, seed=2)
+    # more protected rows than places, and positions that are held many times
+    _table_case([20000, 18000], [900, 5000], 1, 16, WEIGHTS[name], upright, 10, 6000, [20000, 18000], in_place, seed=3)
+    _table_case([20000, 17001], [7000, 50], 1, 7, WEIGHTS[name], lambda r, n: r.integers(0, 9, n), 0, 0, [20000, 17001], in_place, seed=4)
+
+
+@pytest.mark.parametrize("n", [257, 2048, 2049, 8192, 8193, 16384])
+@pytest.mark.parametrize("units", [1, 130])
+def test_eviction_where_its_launches_change(n, units):
+    """Rows moved by the unit's own workgroup or by a second launch, a few evicted rows or many."""
+    lens = [n - i % 3 for i in range(units)]
+    for budget in (n - 3, n - 9, n // 2):
+        _table_case(lens, [budget] * units, 1, 16, WEIGHTS["usual"], lambda r, m: np.arange(m), 1, 5, lens, False, seed=n)
+
+
+def test_few_evictions_among_equals():
+    for units in (1, 130):
+        lens = [300] * units
+        _table_case(lens, [297] * units, 1, 16, WEIGHTS["zeros"], lambda r, n: r.integers(0, 3, n), 0, 0, lens, False)
+        _table_case(lens, [299] * units, 1, 16, WEIGHTS["any"], lambda r, n: np.arange(n), 2, 290, lens, True)
+        _table_case([200] * units, [198] * units, 1, 16, WEIGHTS["zeros"], lambda r, n: np.zeros(n, int), 0, 0, [200] * units, False)
+        _table_case([200] * units, [150] * units, 1, 16, WEIGHTS["steps"], lambda r, n: r.integers(0, 3, n), 0, 0, [200] * units, False)
 
 
 # ---- streams, graphs ------------------------------------------------------------------------------------------------
