@@ -81,55 +81,50 @@ static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
     return v;
 }
 
-// Rows from[i] to slots to[i], i = first, first + step, ..; K and V of a row by neighbouring threads, their table entries by the first of them.
-// A thread has MOVES rows' loads in flight at each of the three stages (list, block table, row); past the end it repeats the last row, which
-// writes the same again.
+// Rows from[i] to slots to[i]: K and V of a row by neighbouring threads, MOVES rows of a thread on their way at a time (past the end it repeats
+// the last row, which writes the same again); move_entries: the tables' entries, a thread each.  No load is under a condition: the compiler would wait for
+// everything in flight.
 template <int MOVES, typename I>
 static __device__ __forceinline__ void move_rows(const PagedEvictArgs &a, int b, int kv, const I *to, const I *from, int count, int thread,
                                                  int threads) {
     const int lanes = 2 << a.lpr_log2, lane = thread & (lanes - 1), step = threads / lanes;
     const bool v = lane >> a.lpr_log2;
-    const int64_t sub = (int64_t)kv * a.g.head_stride + (int64_t)(lane & ((1 << a.lpr_log2) - 1)) * 16;
-    char *pool = (v ? a.v_pages : a.k_pages) + sub;
+    char *pool = (v ? a.v_pages : a.k_pages) + (int64_t)kv * a.g.head_stride + (int64_t)(lane & ((1 << a.lpr_log2) - 1)) * 16;
     for (int i0 = thread / lanes; i0 < count; i0 += MOVES * step) {
-        int t[MOVES], f[MOVES], tp[MOVES], fp[MOVES], pages[2][MOVES];
+        int tp[MOVES], fp[MOVES], tpage[MOVES], fpage[MOVES];
 #pragma unroll
         for (int m = 0; m < MOVES; ++m) {
             const int i = i0 + m * step < count ? i0 + m * step : count - 1;
-            t[m] = to[i];
-            f[m] = from[i];
-        }
-#pragma unroll
-        for (int m = 0; m < MOVES; ++m) {
             int block;
-            split_slot(a.g, t[m], block, tp[m]);
-            pages[0][m] = page_of(a.g, b, block);
-            split_slot(a.g, f[m], block, fp[m]);
-            pages[1][m] = page_of(a.g, b, block);
+            split_slot(a.g, to[i], block, tp[m]);
+            tpage[m] = page_of(a.g, b, block);
+            split_slot(a.g, from[i], block, fp[m]);
+            fpage[m] = page_of(a.g, b, block);
         }
         u32x4_nt_t x[MOVES];
-        float w[MOVES];
-        int p[MOVES];
-#pragma unroll
-        for (int m = 0; m < MOVES; ++m) {
-            const int page = pages[1][m] < 0 ? 0 : pages[1][m];
-            x[m] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_nt_t *>(pool + (int64_t)page * a.g.page_stride + (int64_t)fp[m] * a.g.row_stride));
-            if (lane == 0) {
-                const int64_t i = table_index(a.g, page, kv, fp[m]);
-                w[m] = a.weight_in[i];
-                p[m] = a.pos_in[i];
-            }
-        }
 #pragma unroll
         for (int m = 0; m < MOVES; ++m)
-            if (pages[0][m] >= 0 && pages[1][m] >= 0) {
-                *reinterpret_cast<u32x4_nt_t *>(pool + (int64_t)pages[0][m] * a.g.page_stride + (int64_t)tp[m] * a.g.row_stride) = x[m];
-                if (lane == 0) {
-                    const int64_t i = table_index(a.g, pages[0][m], kv, tp[m]);
-                    a.weight_out[i] = w[m];
-                    a.pos_out[i] = p[m];
-                }
-            }
+            x[m] = __builtin_nontemporal_load(
+                reinterpret_cast<const u32x4_nt_t *>(pool + (int64_t)(fpage[m] < 0 ? 0 : fpage[m]) * a.g.page_stride + (int64_t)fp[m] * a.g.row_stride));
+#pragma unroll
+        for (int m = 0; m < MOVES; ++m)
+            if (tpage[m] >= 0 && fpage[m] >= 0) *reinterpret_cast<u32x4_nt_t *>(pool + (int64_t)tpage[m] * a.g.page_stride + (int64_t)tp[m] * a.g.row_stride) = x[m];
+    }
+}
+
+template <typename I>
+static __device__ __forceinline__ void move_entries(const PagedEvictArgs &a, int b, int kv, const I *to, const I *from, int count, int thread,
+                                                    int threads) {
+    for (int i = thread; i < count; i += threads) {
+        int block, tp, fp;
+        split_slot(a.g, to[i], block, tp);
+        const int tpage = page_of(a.g, b, block);
+        split_slot(a.g, from[i], block, fp);
+        const int fpage = page_of(a.g, b, block);
+        if (tpage < 0 || fpage < 0) continue;
+        const int64_t t = table_index(a.g, tpage, kv, tp), f = table_index(a.g, fpage, kv, fp);
+        a.weight_out[t] = a.weight_in[f];
+        a.pos_out[t] = a.pos_in[f];
     }
 }
 
@@ -519,6 +514,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
         if (tid == 0) list[0] = moves;
     } else if (moves > 0) {
         __syncthreads();
+        move_entries(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
         if (moves <= THREADS / (2 << a.lpr_log2)) move_rows<1>(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
         else move_rows<8>(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
     }
@@ -920,11 +916,13 @@ __global__ __launch_bounds__(ST) void slice_list_kernel(SliceArgs s) {
     });
 }
 
-// grid = (kv heads, sequences, workgroups per unit)
+// grid = (kv heads, sequences, ENTRIES + workgroups per unit): the first ones bring the tables' entries
+static constexpr int ENTRIES = 4;
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
-    const int kv = blockIdx.x, b = blockIdx.y;
+    const int kv = blockIdx.x, b = blockIdx.y, z = (int)blockIdx.z - ENTRIES, tid = threadIdx.x;
     const int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
-    move_rows<8>(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)(blockIdx.z * 256 + threadIdx.x), (int)gridDim.z * 256);
+    if (z < 0) move_entries(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)blockIdx.z * 256 + tid, ENTRIES * 256);
+    else move_rows<2>(a, b, kv, list + 1, list + 1 + a.cap, list[0], z * 256 + tid, ((int)gridDim.z - ENTRIES) * 256);
 }
 
 // ---- launch shapes and memory ------------------------------------------------------------------------------------------------
@@ -1022,8 +1020,8 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     else if (reach <= 8192) hipLaunchKernelGGL((paged_select_kernel<1024, 8>), units, dim3(1024), 0, s, a, move_here);
     else hipLaunchKernelGGL((paged_select_kernel<1024, 16>), units, dim3(1024), 0, s, a, move_here);
     if (!move_here) {
-        const int64_t pieces = (a.cap + 31) / 32, enough = 2048 / n_units + 1;
-        hipLaunchKernelGGL(paged_move_kernel, dim3(units.x, units.y, (unsigned)(pieces < enough ? pieces : enough)), dim3(256), 0, s, a);
+        const int64_t pieces = (a.cap + 31) / 32, enough = 4096 / n_units + 1;
+        hipLaunchKernelGGL(paged_move_kernel, dim3(units.x, units.y, (unsigned)(ENTRIES + (pieces < enough ? pieces : enough))), dim3(256), 0, s, a);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSD_OK : hip_fail(e, "paged eviction launch");
