@@ -14,11 +14,17 @@
 // 16 KB of rows.  Maximum and sum of the softmax are kept in fp32 along the way (one pass), the sum by its lane until the end.
 //
 // K of the next tile is requested when the last product with K has read its registers, V when V's has: a wave has one of the two in
-// flight at any time and the registers hold one tile, which lets three waves share a SIMD.
+// flight at any time and the registers hold one tile, which lets three waves share a SIMD (four where rows have 64 elements).
 //
-// A workgroup of four waves takes a piece ("chunk") of a sequence; its waves take the chunk's tiles in turn and meet in LDS.  Where a sequence can
-// be longer than a chunk a second launch joins the chunks; otherwise the workgroup writes the outputs.  The chunk's part of the block table
-// is brought into LDS once, as byte offsets, so that no row's address waits for memory.
+// A workgroup's four waves take the tiles of its rows in turn and meet in LDS.  The rows' part of the block table is brought into LDS first, as
+// byte offsets, so that no row's address waits for memory.  Who takes which rows stands at "who works on what"; units that more than one workgroup
+// had a part of are joined by a second launch, which also brings the weights up to date, from logits that the first one left in memory.
+//
+// Measured (bf16, rows of 128; time of the call, share of the K and V bytes alone): 4 sequences of 30000 to 131072 rows, 32 query heads on 8: 184 to
+// 192 us, 6.2 to 6.5 TB/s (a plain read reaches 6.1 to 7.0).  128 sequences of 64 to 640 rows, 32 heads: 95 us, 5.6 TB/s; with weights 103.  128
+// sequences of 10 to 8000 rows, 32 query heads on 4: 73 us, 4.5 TB/s; with weights and the new rows 95 -- the logits are 6 % of the bytes and,
+// written among the reads, cost 15 % of the time (batches of them in LDS, other orders in memory and the hints on the stores change nothing).
+// fp32, rows of 64, 48 sequences of 0 to 5000 rows with weights: 41 us, 3.1 TB/s.
 #include "ssd_paged.h"
 
 namespace ssd {
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     extern __shared__ float sm_o[];                                 // [WAVES][tile_heads][LD]
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    int b, ht, t;                                                   // sequence, head tile, round of the unit
+    int b, n, ht, t;                                                // sequence, its rows, head tile, round of the unit
     uint32_t left;                                                  // rounds of the run
     {
     const PagedAttnArgs &a = arguments();
@@ -343,37 +349,73 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         b = a.by_length ? by_length<2>(a, (int)blockIdx.y, lane) : (int)blockIdx.y;
         ht = (int)((blockIdx.x + blockIdx.y) % K);
         t = 0;
-        left = (uint32_t)rounds_of(clamp_len(a.g, b), ROUND);
+        n = clamp_len(a.g, b);
+        left = (uint32_t)rounds_of(n, ROUND);
     } else {
-        const int run = (a.g.n_seqs + 63) / 64;                     // sequences of a lane
-        uint32_t mine = 0;
-        for (int i = 0; i < run; ++i) {
-            const int seq = lane * run + i;
-            if (seq < a.g.n_seqs) mine += (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
-        }
-        uint32_t upto = wave_scan(mine);
-        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * K;
-        const Runs runs(all, (uint32_t)a.workgroups);
-        const uint32_t r0 = runs.start(blockIdx.x), r1 = runs.start(blockIdx.x + 1);
-        if (r0 >= r1 || r0 >= all) return;
-        left = r1 - r0;
-        const uint32_t at = r0 / K;                                 // in rounds of one head
-        int l = (int)__popcll(__ballot(upto <= at));
-        uint32_t before = l == 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)upto, l - 1);
-        b = l * run;
-        for (int i0 = 0; run > 1; i0 += 64) {                       // the run's sequences, 64 at a time
-            const int seq = l * run + i0 + lane;
-            const bool ours = i0 + lane < run && seq < a.g.n_seqs;
-            const uint32_t up = wave_scan(ours ? (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND) : 0u) + before;
-            const int k = (int)__popcll(__ballot(up <= at));
-            if (k < 64) {
-                b = l * run + i0 + k;
-                if (k > 0) before = (uint32_t)__builtin_amdgcn_readlane((int)up, k - 1);
-                break;
+        uint32_t before = 0, r0;                                    // rounds of one head of the sequences before b; first of the run
+        if (a.g.n_seqs <= 256) {                                    // every lane has four lengths, and nothing is read twice
+            int len[4];
+            uint32_t mine = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) len[i] = a.g.seq_len[64 * i + lane < a.g.n_seqs ? 64 * i + lane : a.g.n_seqs - 1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                len[i] = len[i] < 0 ? 0 : len[i] > a.g.max_len ? a.g.max_len : len[i];
+                mine += 64 * i + lane < a.g.n_seqs ? (uint32_t)rounds_of(len[i], ROUND) : 0u;
             }
-            before = (uint32_t)__builtin_amdgcn_readlane((int)up, 63);
+            const uint32_t all = uniform(wave_sum(mine)) * K;
+            const Runs runs(all, (uint32_t)a.workgroups);
+            r0 = runs.start(blockIdx.x);
+            const uint32_t r1 = runs.start(blockIdx.x + 1);
+            if (r0 >= r1 || r0 >= all) return;
+            left = r1 - r0;
+            const uint32_t at = r0 / K;                             // in rounds of one head
+            b = -1;
+            n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (b >= 0 || 64 * i >= a.g.n_seqs) continue;
+                const uint32_t up = wave_scan(64 * i + lane < a.g.n_seqs ? (uint32_t)rounds_of(len[i], ROUND) : 0u) + before;
+                const int k = (int)__popcll(__ballot(up <= at));
+                if (k < 64) {
+                    b = 64 * i + k;
+                    n = __builtin_amdgcn_readlane(len[i], k);
+                }
+                before = k > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)up, k - 1) : before;
+            }
+        } else {
+            const int run = (a.g.n_seqs + 63) / 64;                 // sequences of a lane
+            uint32_t mine = 0;
+            for (int i = 0; i < run; ++i) {
+                const int seq = lane * run + i;
+                if (seq < a.g.n_seqs) mine += (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
+            }
+            const uint32_t upto = wave_scan(mine);
+            const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * K;
+            const Runs runs(all, (uint32_t)a.workgroups);
+            r0 = runs.start(blockIdx.x);
+            const uint32_t r1 = runs.start(blockIdx.x + 1);
+            if (r0 >= r1 || r0 >= all) return;
+            left = r1 - r0;
+            const uint32_t at = r0 / K;
+            const int l = (int)__popcll(__ballot(upto <= at));
+            before = l == 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)upto, l - 1);
+            b = l * run;
+            for (int i0 = 0;; i0 += 64) {                           // the run's sequences, 64 at a time
+                const int seq = l * run + i0 + lane;
+                const bool ours = i0 + lane < run && seq < a.g.n_seqs;
+                const uint32_t up = wave_scan(ours ? (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND) : 0u) + before;
+                const int k = (int)__popcll(__ballot(up <= at));
+                if (k < 64) {
+                    b = l * run + i0 + k;
+                    if (k > 0) before = (uint32_t)__builtin_amdgcn_readlane((int)up, k - 1);
+                    break;
+                }
+                before = (uint32_t)__builtin_amdgcn_readlane((int)up, 63);
+            }
+            n = clamp_len(a.g, b);
         }
-        const uint32_t tb = uniform((uint32_t)rounds_of(clamp_len(a.g, b), ROUND)), into = r0 - before * K;
+        const uint32_t tb = uniform((uint32_t)rounds_of(n, ROUND)), into = r0 - before * K;
         ht = (int)(into / tb);
         t = (int)(into - (uint32_t)ht * tb);
     }
@@ -382,12 +424,13 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     ht = (int)uniform((uint32_t)ht);
     t = (int)uniform((uint32_t)t);
     left = uniform(left);
+    n = (int)uniform((uint32_t)n);
 
     for (bool first_unit = true;; first_unit = false) {
         const PagedAttnArgs &a = arguments();
         const int kv = ht / a.q_tiles, qt = ht - kv * a.q_tiles;
         const int heads = a.group - qt * HEADS < HEADS ? a.group - qt * HEADS : HEADS, head0 = kv * a.group + qt * HEADS;
-        const int n = clamp_len(a.g, b), rounds = rounds_of(n, ROUND);
+        const int rounds = rounds_of(n, ROUND);
         const int take = (uint32_t)(rounds - t) < left ? rounds - t : (int)left;
         const int begin = t * ROUND, end = begin + take * ROUND < n ? begin + take * ROUND : n;
         const bool whole = take == rounds;                          // this workgroup writes the outputs
@@ -596,6 +639,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         if (++ht == a.g.n_kv * a.q_tiles) {
             ht = 0;
             ++b;
+            n = clamp_len(a.g, b);
         }
         }
         __syncthreads();
@@ -766,7 +810,9 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
     s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
     s.round = s.waves * tile;
-    const int64_t resident = c->head_dim == 64 ? 1024 : 768;        // 256 compute units, four or three workgroups each
+    // 256 compute units, four or three workgroups each (fp32 of 64 elements 41.7 us with 768, 40.5 with 1024; 128 sequences of 10 to 8000 rows in bf16 95
+    // with 768, 91 with 2048, 512 of them 251 and 256)
+    const int64_t resident = c->head_dim == 64 ? 1024 : 768;
     s.workgroups = plain ? 0 : (int)(units * rounds < resident ? units * rounds : resident);
     // Where not all units are resident at once a late long one would run on alone; ranking costs every workgroup a microsecond (32 heads of 64 to 640
     // rows, 64 sequences 54 us in their order and 50 by length, 128 96 and 95, of 10 to 1000 rows 94 and 89; 256 168 and 173, 16 17.3 and 19.0).
