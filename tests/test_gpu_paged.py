@@ -575,6 +575,52 @@ def test_few_evictions_among_equals():
         _table_case([200] * units, [150] * units, 1, 16, WEIGHTS["steps"], lambda r, n: r.integers(0, 3, n), 0, 0, [200] * units, False)
 
 
+# ---- the example ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_serving_example_serves(dtype):
+    import importlib.util
+    import os
+    import sys
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_serving.py")
+    spec = importlib.util.spec_from_file_location("paged_serving", path)
+    example = importlib.util.module_from_spec(spec)
+    sys.modules["paged_serving"] = example                  # its dataclasses look themselves up there
+    spec.loader.exec_module(example)
+    s = example.Settings(prompts=(37, 130, 8), budget=40, slack=12, steps=30, dtype=dtype)
+    calls = []
+
+    def watch(layer, st):
+        calls.append(layer)
+        if len(calls) % 11 not in (1, 6):                           # some of the 60
+            return
+        k, v, table = st["k"].float().cpu().numpy(), st["v"].float().cpu().numpy(), st["table"].cpu().numpy()
+        out, q = st["out"].float().cpu().numpy(), st["q"].float().cpu().numpy().reshape(6, s.heads, s.head_dim)
+        for b, n in enumerate(st["lens"]):
+            ref, _, _, size = paged.paged_attend(q[b], k, v, table[b], n, s.head_dim ** -0.5)
+            tol = 5e-5 * size if dtype == "f32" else 2.0 ** -8 * (size + np.abs(ref))
+            assert np.all(np.abs(out[b] - ref) <= tol + 1e-30), (layer, b)
+
+    tokens, lens, held = example.serve(s, watch)
+    assert len(calls) == s.steps * s.layers
+    assert tokens.shape == (3, 30) and bool(((tokens >= s.image_tokens[0]) & (tokens < s.image_tokens[1])).all())
+    starts = [n for p in s.prompts for n in (p, s.bare)]
+    want = [min(n, s.budget) for n in starts]
+    for step in range(s.steps):
+        if step and step % s.slack == 0:
+            want = [min(n, s.budget) for n in want]
+        want = [n + 1 for n in want]
+    assert lens == want
+    for layer in held:
+        for b, by_head in enumerate(layer):
+            total = starts[b] + s.steps
+            for kept in by_head.tolist():
+                assert len(set(kept)) == len(kept) == lens[b] and min(kept) == 0 and max(kept) == total - 1
+                assert set(range(total - s.recent, total)) <= set(kept)
+    again, _, _ = example.serve(s)
+    assert torch.equal(again, tokens)
+
+
 # ---- streams, graphs ------------------------------------------------------------------------------------------------
 
 def test_calls_run_on_the_stream_they_are_given():
