@@ -463,7 +463,7 @@ int ssd_paged_append(const ssd_paged_config *cfg, void *k_pages, void *v_pages, 
  *   weight_in, weight_out : both NULL, or tables shaped as `weight`:
  *                weight_out[row] = weight_in[row] + sum of p[h, row] over the row's query heads,
  *                for every row of every sequence; other places keep what they hold.  They may be
- *                the same array (then no page may belong to two sequences)
+ *                the same array.  No page may belong to two sequences then
  *   max_len    : no sequence holds more rows than this (0: max_blocks * page_size); it bounds the
  *                launch and the workspace.  A longer sequence is cut to it
  *   workspace  : dev scratch, 256-byte aligned, at least ssd_paged_workspace_bytes(cfg, max_len,
