@@ -18,10 +18,10 @@
 //
 // A workgroup's four waves take the tiles of its rows in turn and meet in LDS.  The rows' part of the block table is brought into LDS first, as
 // byte offsets, so that no row's address waits for memory.  Who takes which rows stands at "who works on what"; units that more than one workgroup
-// had a part of are joined by a second launch, which also brings the weights up to date, from logits that the first one left in memory.
+// had a part of are joined by a second launch, which also brings their weights up to date, from logits that the first one left in memory.
 //
 // Measured (bf16, rows of 128; time of the call, share of the K and V bytes alone): 4 sequences of 30000 to 131072 rows, 32 query heads on 8: 184 to
-// 192 us, 6.2 to 6.5 TB/s (a plain read reaches 6.1 to 7.0).  128 sequences of 64 to 640 rows, 32 heads: 95 us, 5.6 TB/s; with weights 103.  128
+// 192 us, 6.2 to 6.5 TB/s (a plain read reaches 6.1 to 7.0).  128 sequences of 64 to 640 rows, 32 heads: 92 us, 5.8 TB/s; with weights 100.  128
 // sequences of 10 to 8000 rows, 32 query heads on 4: 73 us, 4.5 TB/s; with weights and the new rows 95 -- the logits are 6 % of the bytes and,
 // written among the reads, cost 15 % of the time (batches of them in LDS, other orders in memory and the hints on the stores change nothing).
 // fp32, rows of 64, 48 sequences of 0 to 5000 rows with weights: 41 us, 3.1 TB/s.
@@ -39,8 +39,8 @@ struct PagedAttnArgs {
     float *weight_out;
     char *out;
     float *lse;
-    float *z;                 // logits (base 2) [n_seqs, n_heads, z_stride]; only where weights are wanted
-    float *lse2;              // [n_seqs, n_heads] lse (base 2) of units that one workgroup completed; only where weights are wanted
+    float *z;                 // logits (base 2) [n_seqs, n_heads, z_stride]; LATER only (see Weights)
+    float *lse2;              // [n_seqs, n_heads] lse (base 2) of units that one workgroup completed; LATER only
     float *part_o;            // [2 * workgroups, heads of a tile, D] sums of a unit's part, relative to its maximum
     float2 *part_ml;          // [2 * workgroups, heads of a tile] its maximum (base 2) and sum
     int64_t q_stride, new_stride;   // bytes
@@ -61,6 +61,7 @@ static constexpr int64_t NO_PAGE = -(1ll << 62);
 static constexpr float LN2 = 0.6931471805599453f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // block of a row: x / page_size for x < 2^16 (a chunk's rows and what lies before them in its first page), page_size <= 2^15:
@@ -267,7 +268,6 @@ struct Runs {
 // weight so far, or -1.
 template <bool QUADS>
 static __device__ __forceinline__ void add_weights(const PagedAttnArgs &a, int b, int kv, int j, int n, const f32x4 &p, int newest) {
-    typedef f32x4 f32x4_any __attribute__((aligned(4)));
     int block, place;
     split_slot(a.g, j, block, place);
     if (QUADS && j + 4 <= n) {
@@ -292,6 +292,18 @@ static __device__ __forceinline__ void add_weights(const PagedAttnArgs &a, int b
         const int64_t i = table_index(a.g, page, kv, place);
         a.weight_out[i] = (j + e == newest ? 0.f : a.weight_in[i]) + p[e];
     }
+}
+
+// Four rows' probabilities, summed over heads; z: the first head's logits of theirs, the others' `stride` apart.
+template <typename I> static __device__ __forceinline__ f32x4 probabilities(const float *z, I stride, const float *lse2, int heads) {
+    f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int h = 0; h < heads; ++h) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(z + h * stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] += fast_exp2(x[e] - lse2[h]);
+    }
+    return p;
 }
 
 // The arguments, to be read from their segment again: what one phase of the kernel needs of them does not have to stay in scalar
@@ -328,8 +340,11 @@ template <int PER> static __device__ __forceinline__ int by_length(const PagedAt
     return 0;
 }
 
+// What becomes of a tile's logits: nothing more, or they wait for the softmax's sum, in memory for the second launch or in LDS for the end of this one.
+enum Weights { NONE, LATER, HERE };
+
 // grid = (workgroups), or (kv heads * tiles of query heads, sequences) where a workgroup takes a whole unit
-template <typename T, int D, bool QUADS, bool STEP, bool WEIGHTS, int WAVES>
+template <typename T, int D, bool QUADS, bool STEP, Weights WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs) {
     typedef Tile<T, D> TT;
     constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
@@ -337,7 +352,9 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     constexpr int LD = D + 4;                                       // row of the merge area
     __shared__ int64_t pages[blocks_of(WAVES)];
     __shared__ float sm_ml[WAVES][HEADS][2];
-    extern __shared__ float sm_o[];                                 // [WAVES][tile_heads][LD]
+    __shared__ float sm_lse[HEADS];
+    __shared__ int32_t page_ids[WEIGHTS == HERE ? blocks_of(WAVES) : 1];
+    extern __shared__ __align__(16) float sm_o[];                   // [WAVES][tile_heads][LD], then (HERE) logits [tile_heads][z_stride + 4]
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     int b, n, ht, t;                                                // sequence, its rows, head tile, round of the unit
@@ -445,7 +462,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         // the unit's logits; lanes without a head are out of the buffer's bounds, and what they store is dropped
         __amdgpu_buffer_rsrc_t z_unit;
         uint32_t z_lane = 0;
-        if constexpr (WEIGHTS) {
+        if constexpr (WEIGHTS == LATER) {
             float *at = a.z + ((int64_t)b * a.n_heads + head0) * a.z_stride;
             z_unit = __builtin_amdgcn_make_buffer_rsrc(at, 0, (int)(4u * (uint32_t)heads * (uint32_t)a.z_stride), 0x00027000);
             z_lane = r < heads ? 4u * ((uint32_t)r * (uint32_t)a.z_stride + 4u * (uint32_t)g) : 0x80000000u;
@@ -465,6 +482,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             __syncthreads();                                        // the last stage's entries, and a unit's merge area, have been read
             for (int i = threadIdx.x; i < blocks; i += 64 * WAVES) {
                 const int page = page_of(a.g, b, block0 + i);
+                if constexpr (WEIGHTS == HERE) page_ids[i] = page;
                 pages[i] = page < 0 ? NO_PAGE : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
             }
             __syncthreads();
@@ -504,7 +522,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                 }
 #pragma unroll
                 for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
-                if constexpr (WEIGHTS)
+                if constexpr (WEIGHTS == HERE) {
+                    if (r < heads)
+#pragma unroll
+                        for (int e = 0; e < NZ; e += 4)
+                            *reinterpret_cast<f32x4 *>(sm_o + WAVES * heads * LD + r * ((int)a.z_stride + 4) + row0 + first + 4 * e + 4 * g) =
+                                f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]};
+                }
+                if constexpr (WEIGHTS == LATER)
 #pragma unroll
                     for (int e = 0; e < NZ; e += 4)
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_nt_t, f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]}), z_unit,
@@ -587,6 +612,31 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             }
         }
 
+        // HERE: a thread's four rows (a unit has no more of them than the workgroup has threads), their weights so far on their way while the waves meet
+        const int j = 4 * (int)threadIdx.x;
+        int64_t entry[4];
+        float w[4];
+        if constexpr (WEIGHTS == HERE)
+            if (j < n) {
+                int block = block_of(a, j), place = j - block * a.g.page_size;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int page = j + e < n ? page_ids[block] : -1;
+                    entry[e] = page < 0 ? -1 : table_index(a.g, page, kv, place);
+                    if (++place == a.g.page_size) {
+                        place = 0;
+                        ++block;
+                    }
+                }
+                if constexpr (QUADS) {
+                    const f32x4 x = *reinterpret_cast<const f32x4_any *>(a.weight_in + (entry[0] < 0 ? 0 : entry[0]));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = x[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = a.weight_in[entry[e] < 0 ? 0 : entry[e]];
+                }
+            }
         // the waves' states meet
         {
             float x, y;
@@ -626,12 +676,29 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                 if (d == 0) {
                     const float lse = top + __builtin_amdgcn_logf(sum);
                     if (a.lse) a.lse[bh] = sum == 0.f ? -INFINITY : lse * LN2;
-                    if (WEIGHTS) a.lse2[bh] = sum == 0.f ? INFINITY : lse;
+                    if (WEIGHTS == LATER) a.lse2[bh] = sum == 0.f ? INFINITY : lse;
+                    if (WEIGHTS == HERE) sm_lse[h] = sum == 0.f ? INFINITY : lse;
                 }
             } else {
                 a.part_o[(slot * a.tile_heads + h) * D + d] = acc;
                 if (d == 0) a.part_ml[slot * a.tile_heads + h] = make_float2(top, sum);
             }
+        }
+        if constexpr (WEIGHTS == HERE) {
+            __syncthreads();
+            if (j < n) {
+                const f32x4 p = probabilities(sm_o + WAVES * heads * LD + j, (int)a.z_stride + 4, sm_lse, heads);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = (newest && j + e == n - 1 ? 0.f : w[e]) + p[e];
+                if (QUADS && j + 4 <= n) {
+                    if (entry[0] >= 0) *reinterpret_cast<f32x4_any *>(a.weight_out + entry[0]) = f32x4{w[0], w[1], w[2], w[3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (entry[e] >= 0) a.weight_out[entry[e]] = w[e];
+                }
+            }
+            return;
         }
         left -= (uint32_t)take;
         if (left == 0) return;
@@ -775,27 +842,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
     __syncthreads();
     const int newest = step && a.g.seq_len[b] == n ? n - 1 : -1;
     const float *z0 = a.z + ((int64_t)b * a.n_heads + kv * a.group) * a.z_stride;
-    for (int j = first + 4 * tid; j < n; j += ((int)gridDim.z - head_blocks) * 1024) {
-        f32x4 p = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-        for (int h = 0; h < a.group; ++h) {
-            const f32x4 z = *reinterpret_cast<const f32x4 *>(z0 + (int64_t)h * a.z_stride + j);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] += fast_exp2(z[e] - lse2[h]);
-        }
-        add_weights<QUADS>(a, b, kv, j, n, p, newest);
-    }
+    for (int j = first + 4 * tid; j < n; j += ((int)gridDim.z - head_blocks) * 1024)
+        add_weights<QUADS>(a, b, kv, j, n, probabilities(z0 + j, a.z_stride, lse2, a.group), newest);
 }
 
 // ---- launch shapes ---------------------------------------------------------------------------------------------------
 
 struct PagedShape {
     int waves, round, q_tiles, tile_heads, workgroups, stage;
-    bool by_length;
+    bool by_length, here;     // here: a unit's weights are brought up to date by its own workgroup, from logits in LDS
     int64_t reach;            // rows, in whole rounds
+    size_t lds;               // where the waves meet
 };
 
-static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
+static PagedShape paged_shape(const ssd_paged_config *c, int max_len, bool weights) {
     PagedShape s;
     const int reach = paged_reach(c, max_len), group = c->n_heads / c->n_kv_heads;
     const int tile = c->dtype == SSD_BF16 ? 32 : 16;
@@ -805,8 +865,10 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     s.reach = rounds * 4 * tile;
     // A unit of few rounds is taken whole (8 units of 512 rows 9.1 us whole and 10.6 dealt, 512 of 512 24 and 30); with more rounds only where
     // units are many (512 of 1024 rows 44 and 51, of 10 to 1024 25 and 23, of 2048 84 and 91, of 10 to 2048 44 and 29; 128 of 1024 20 and 19),
-    // and where 32 bits would not hold the sums.
-    const bool plain = rounds <= 4 || (units >= 512 && rounds <= 8) || units * rounds >= 1ll << 31;
+    // and where 32 bits would not hold the sums.  With weights that saves the second launch, and pays earlier (256 units of 640 rows 25 us dealt and 17
+    // whole, 128 19.6 and 15.0, 32 12.3 and 12.6; 256 of 1000 rows 29.8 and 24.6, 128 19.4 and 20.7).
+    const bool once = weights && s.q_tiles == 1;
+    const bool plain = rounds <= (once ? 5 : 4) || (units >= (once ? 256 : 512) && rounds <= 8) || units * rounds >= 1ll << 31;
     // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
     s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
     s.round = s.waves * tile;
@@ -820,6 +882,11 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     // a stage's blocks: its rows and what lies before them in the first one; block_of allows 2^16 rows
     const int64_t most = (int64_t)(blocks_of(s.waves) - 1) * c->page_size;
     s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);
+    s.lds = (size_t)s.waves * s.tile_heads * (c->head_dim + 4) * sizeof(float);
+    // The weights are brought up to date by the unit's own workgroup, from logits in LDS (up to 66 KB), where it takes one tile of heads (2 sequences of
+    // 64 to 97 rows, 16 heads 6.5 us, by a second launch 10.2; 128 of 64 to 640 rows, 32 heads 100 and 103, 256 query heads on 32 111 and 130, on 16 with
+    // up to 500 rows 89 and 103; 64 of 1000 rows, 32 heads 192 and 187).
+    s.here = plain && s.q_tiles == 1 && s.reach <= s.stage && s.reach <= 256 * s.waves;
     return s;
 }
 
@@ -828,8 +895,8 @@ struct PagedScratch { size_t z, lse2, o, ml, all; };
 static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s, bool weights) {
     PagedScratch w;
     const size_t bh = (size_t)c->n_seqs * c->n_heads, parts = (size_t)2 * s.workgroups * s.tile_heads;
-    w.z = weights ? round256(bh * s.reach * sizeof(float)) : 0;
-    w.lse2 = weights ? round256(bh * sizeof(float)) : 0;
+    w.z = weights && !s.here ? round256(bh * s.reach * sizeof(float)) : 0;
+    w.lse2 = weights && !s.here ? round256(bh * sizeof(float)) : 0;
     w.o = round256(parts * c->head_dim * sizeof(float));
     w.ml = round256(parts * sizeof(float2));
     w.all = w.z + w.lse2 + w.o + w.ml;
@@ -839,18 +906,18 @@ static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s
 template <typename T, int D, bool QUADS, int WAVES> static void launch_paged_rows(const PagedAttnArgs &a, const PagedShape &sh, bool step, hipStream_t s) {
     const bool weights = a.weight_out != nullptr;
     const dim3 wg(64 * WAVES), grid = sh.workgroups ? dim3((unsigned)sh.workgroups) : dim3((unsigned)(a.g.n_kv * sh.q_tiles), (unsigned)a.g.n_seqs);
-    const size_t lds = (size_t)WAVES * a.tile_heads * (D + 4) * sizeof(float);
-    if (step && weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, true, WAVES>), grid, wg, lds, s, a);
-    else if (step) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, true, false, WAVES>), grid, wg, lds, s, a);
-    else if (weights) hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, true, WAVES>), grid, wg, lds, s, a);
-    else hipLaunchKernelGGL((paged_attn_kernel<T, D, QUADS, false, false, WAVES>), grid, wg, lds, s, a);
+    const auto go = [&](auto kernel, size_t lds) { hipLaunchKernelGGL(kernel, grid, wg, (unsigned)lds, s, a); };
+    const size_t here = sh.lds + (size_t)a.tile_heads * (a.z_stride + 4) * sizeof(float);
+    if (!weights) go(step ? paged_attn_kernel<T, D, QUADS, true, NONE, WAVES> : paged_attn_kernel<T, D, QUADS, false, NONE, WAVES>, sh.lds);
+    else if (sh.here) go(step ? paged_attn_kernel<T, D, QUADS, true, HERE, WAVES> : paged_attn_kernel<T, D, QUADS, false, HERE, WAVES>, here);
+    else go(step ? paged_attn_kernel<T, D, QUADS, true, LATER, WAVES> : paged_attn_kernel<T, D, QUADS, false, LATER, WAVES>, sh.lds);
 }
 
 template <typename T, int D, bool QUADS> static hipError_t launch_paged_attn(const PagedAttnArgs &a, const PagedShape &sh, bool step, hipStream_t s) {
     const bool weights = a.weight_out != nullptr;
     if (sh.waves == 1) launch_paged_rows<T, D, QUADS, 1>(a, sh, step, s);
     else launch_paged_rows<T, D, QUADS, 4>(a, sh, step, s);
-    if (!sh.workgroups && !weights) return hipGetLastError();
+    if (!sh.workgroups && (!weights || sh.here)) return hipGetLastError();
     const int64_t units = (int64_t)a.g.n_seqs * a.g.n_kv;
     const bool wide = units * a.group < 1024;
     const int head_blocks = !sh.workgroups ? 0 : wide ? a.group : (a.group + 3) / 4;
@@ -884,7 +951,7 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     if (!aligned(block_table, 4) || !aligned(seq_len, 4) || !aligned(seq_pos, 4) || !aligned(pos, 4) || !aligned(weight_in, 4) ||
         !aligned(weight_out, 4) || !aligned(lse, 4))
         return fail(SSD_ERR_INVALID_ARG, "tables must be aligned to their elements");
-    const PagedShape shape = paged_shape(cfg, max_len);
+    const PagedShape shape = paged_shape(cfg, max_len, weight_out != nullptr);
     const PagedScratch parts = paged_scratch(cfg, shape, weight_out != nullptr);
     const size_t need = parts.all;
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
@@ -934,7 +1001,7 @@ using namespace ssd;
 extern "C" size_t ssd_paged_workspace_bytes(const ssd_paged_config *cfg, int max_len, int with_weights) {
     clear_error();
     if (check_paged(cfg) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
-    return paged_scratch(cfg, paged_shape(cfg, max_len), with_weights != 0).all;
+    return paged_scratch(cfg, paged_shape(cfg, max_len, with_weights != 0), with_weights != 0).all;
 }
 
 extern "C" int ssd_paged_decode_attn(const ssd_paged_config *cfg, const void *q, const void *k_pages, const void *v_pages,

@@ -351,6 +351,48 @@ def test_step_is_append_and_attention(dtype, d, H, n_kv, page):
         check_attend(bt, (out, lse, w_out if weights else None), weight_before=torch.from_numpy(rw))
 
 
+@pytest.mark.parametrize("dtype,d,H,n_kv,page,most", [("bf16", 128, 16, 1, 16, 600), ("bf16", 128, 64, 4, 16, 1000), ("bf16", 64, 8, 8, 3, 900),
+                                                      ("bf16", 128, 4, 4, 1, 1000), ("f32", 128, 8, 4, 24, 480), ("f32", 64, 64, 4, 16, 300),
+                                                      ("bf16", 128, 8, 8, 1, 230), ("bf16", 128, 128, 8, 16, 250), ("f32", 64, 20, 1, 16, 200)])
+def test_weights_of_units_that_are_taken_whole(dtype, d, H, n_kv, page, most):
+    """Units of up to eight rounds, by a workgroup or a wave each: weights by the unit itself, or by the second launch where LDS holds only a part
+    of its block table or its heads are two tiles."""
+    lens = [most, 0, 1, most - 1, most // 2 + 1, 128, 127, 3] * (16 if most < 256 else 8)
+    say("whole", dtype, d, H, n_kv, page, most)
+    bt = Batch(lens, H, n_kv, d, dtype, page, seed=most + H, more_blocks=0)
+    bt.tabled[0, 0] = -1                                  # its first block names no page
+    bt.table = bt.tabled.cpu().numpy()
+    check_attend(bt, attend(bt))
+
+
+@pytest.mark.parametrize("dtype,d,H,n_kv,page,most", [("bf16", 128, 4, 4, 16, 1000), ("f32", 64, 10, 2, 24, 300), ("bf16", 64, 16, 8, 7, 128),
+                                                      ("bf16", 128, 2, 1, 16, 500)])
+def test_step_equals_append_and_attention_to_the_bit(dtype, d, H, n_kv, page, most):
+    lens = [most, 1, 0, most // 2, most - 1, 129, 64, 2] * (32 if most < 256 else 8)
+    say("step bits", dtype, d, H, n_kv, page, most)
+    bt = Batch(lens, H, n_kv, d, dtype, page, seed=most, more_blocks=0)
+    g = torch.Generator().manual_seed(5)
+    k_new, v_new = (torch.randn((len(lens), n_kv, d), generator=g).to(TORCH[dtype]).cuda() for _ in range(2))
+    k, v, pos, weight = bt.kd.clone(), bt.vd.clone(), bt.pos.cuda(), bt.weight.cuda()
+    ssd.ssd_paged_append(bt.cfg, k, v, bt.tabled, bt.lend, k_new, v_new, pos=pos, weight=weight)
+    got = []
+    for step in (False, True):
+        out = torch.empty((len(lens), H, d), dtype=TORCH[dtype], device="cuda")
+        lse = torch.empty((len(lens), H), device="cuda")
+        w_out = torch.full_like(weight, -3.0)
+        ws = bt.scratch(ssd.ssd_paged_workspace_bytes(bt.cfg, 0, True))
+        if step:
+            pos2 = bt.pos.cuda()
+            ssd.ssd_paged_decode_step(bt.cfg, bt.qd, k_new, v_new, bt.kd, bt.vd, bt.tabled, bt.lend, out, pos=pos2, lse=lse, weight_in=bt.weight.cuda(),
+                                      weight_out=w_out, workspace=ws)
+        else:
+            ssd.ssd_paged_decode_attn(bt.cfg, bt.qd, k, v, bt.tabled, bt.lend, out, lse=lse, weight_in=weight, weight_out=w_out, workspace=ws)
+        got.append((out, lse, w_out))
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+    assert torch.equal(pos, pos2) and torch.equal(k.nan_to_num(9.0), bt.kd.nan_to_num(9.0)) and torch.equal(v.nan_to_num(9.0), bt.vd.nan_to_num(9.0))
+
+
 # ---- eviction -----------------------------------------------------------------------------------------------------
 
 def _evict_case(lens, budgets, n_kv, d, dtype, page, sink, recent, seed, layout="heads", in_place=False, weight_of=None, pos_of=None, max_len=0, more=0):
