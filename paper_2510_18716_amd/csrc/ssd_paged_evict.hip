@@ -525,7 +525,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
 // The rows below n' and those above are cut into slices of equally many rows, a workgroup each; a unit's own workgroup works in between.
 //   1 slices: how many rows have which upper 12 bits of their weight, protected ones and others apart
 //   2 unit:   the bin in which the last place falls, and how many rows of a slice are above it and in it
-//   3 slices: the rows in the bin, in slot order, into one list (the memory of the moves, which come later)
+//   3 slices: the rows in the bin, in slot order, into one list (the memory of the moves, which come later), with their keys
 //   4 unit:   the descent among those; where each slice's free slots and moving rows begin in the lists
 //   5 slices: the lists
 //   6 as everywhere: the rows move
@@ -551,7 +551,10 @@ struct SliceArgs {
     uint32_t *hist;                                                // [units, slices + 2, 2, TOP_BINS]
     UnitInfo *info;                                                // [units]
     int slices;
+    // the first candidates' keys, where the unit's histograms were
+    __device__ __forceinline__ uint32_t *keys(int64_t unit) const { return hist + unit * (slices + 2) * 2 * TOP_BINS; }
 };
+static_assert(PICK <= 3 * TOP_BINS, "a unit has three slices' histograms or more");
 
 struct Slices {
     int rows, low, count;                                          // rows of a slice, slices below n', all of them
@@ -606,7 +609,7 @@ __global__ __launch_bounds__(ST) void slice_count_kernel(SliceArgs s) {
 __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
     __shared__ uint32_t red[16];
-    __shared__ int found[3], safe_of[SLICES + 2];
+    __shared__ int found[4], safe_of[SLICES + 2];
     __shared__ SliceInfo info[SLICES + 2];
     const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
@@ -625,6 +628,7 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     if (tid == 0) {
         found[0] = TOP_BINS;                                       // no place to compete for: nothing is in or above this bin
         found[1] = 0;
+        found[3] = 0;
     }
     __syncthreads();
     const int safe_rows = found[2], k = safe_rows >= stay;         // k = 1: protected rows alone compete
@@ -634,19 +638,31 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     static_assert(PER == 4, "bins are read four at a time");
     const int bin = TOP_BINS - PER * (tid + 1);
     uint32_t h[PER] = {0, 0, 0, 0};
-    auto add = [&](int i) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(hist + ((int64_t)i * 2 + k) * TOP_BINS + bin);
-        h[0] += x.w;
-        h[1] += x.z;
-        h[2] += x.y;
-        h[3] += x.x;
-    };
     if (!k) {
-#pragma unroll 8
-        for (int i = 0; i < sl.count; ++i) add(i);
+        constexpr int AT = 16;                                     // slices on their way at a time
+        for (int i0 = 0; i0 < sl.count; i0 += AT) {
+            uint4 x[AT];
+#pragma unroll
+            for (int i = 0; i < AT; ++i)
+                x[i] = *reinterpret_cast<const uint4 *>(hist + (int64_t)(i0 + i < sl.count ? i0 + i : sl.count - 1) * 2 * TOP_BINS + bin);
+#pragma unroll
+            for (int i = 0; i < AT; ++i) {
+                const bool real = i0 + i < sl.count;
+                h[0] += real ? x[i].w : 0;
+                h[1] += real ? x[i].z : 0;
+                h[2] += real ? x[i].y : 0;
+                h[3] += real ? x[i].x : 0;
+            }
+        }
     } else {
         for (int i = 0; i < sl.count; ++i)
-            if (safe_of[i] > 0) add(i);
+            if (safe_of[i] > 0) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(hist + ((int64_t)i * 2 + 1) * TOP_BINS + bin);
+                h[0] += x.w;
+                h[1] += x.z;
+                h[2] += x.y;
+                h[3] += x.x;
+            }
     }
     const uint32_t mine = h[0] + h[1] + h[2] + h[3], up = wave_scan(mine);
     if (lane == 63) red[wave] = up;
@@ -654,6 +670,7 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     uint32_t above = up - mine;
 #pragma unroll
     for (int i = 0; i < 16; ++i) above += i < wave ? red[i] : 0;
+    if (above == 0 && mine > 0) found[3] = bin + PER;              // no row is in this bin or above it
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         if (left > 0 && above < left && above + h[i] >= left) {
@@ -670,8 +687,7 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
         const bool any = !k || safe_of[i] > 0;
         uint32_t over = 0;
         if (any)
-#pragma unroll 4
-            for (int x = lane * 4; x < TOP_BINS; x += 256) {
+            for (int x = (at & ~3) + lane * 4; x < found[3]; x += 256) {
                 const uint4 v = *reinterpret_cast<const uint4 *>(row + x);
                 over += (x > at ? v.x : 0) + (x + 1 > at ? v.y : 0) + (x + 2 > at ? v.z : 0) + (x + 3 > at ? v.w : 0);
             }
@@ -714,7 +730,9 @@ __global__ __launch_bounds__(ST) void slice_gather_kernel(SliceArgs s) {
     const int64_t total = a.g.seq_pos[b], unit = (int64_t)b * a.g.n_kv + kv;
     const UnitInfo *u = s.info + unit;
     if (u->slice[blockIdx.x].in_bin == 0) return;
-    int32_t *out = a.moves + moves_of(a.cap, unit) + 1 + u->slice[blockIdx.x].first;
+    int32_t *out = a.moves + moves_of(a.cap, unit) + 1;
+    uint32_t *keys = s.keys(unit);
+    int first = u->slice[blockIdx.x].first;
     const bool among_safe = u->among_safe != 0;
     const uint32_t bin = (uint32_t)u->bin;
     int parity = 0;
@@ -727,16 +745,22 @@ __global__ __launch_bounds__(ST) void slice_gather_kernel(SliceArgs s) {
         const uint32_t c = (uint32_t)__popc(bits), up = wave_scan(c);
         if (lane == 63) red[parity][wave] = up;
         __syncthreads();
-        uint32_t at = up - c, all = 0;
+        int at = first + (int)(up - c);
 #pragma unroll
         for (int i = 0; i < ST / 64; ++i) {
-            at += i < wave ? red[parity][i] : 0;
-            all += red[parity][i];
+            at += i < wave ? (int)red[parity][i] : 0;
+            first += (int)red[parity][i];
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (bits >> e & 1) out[at++] = j + e;
-        out += all;
+            if (bits >> e & 1) {
+                out[at] = j + e;
+                if (at < PICK) {
+                    keys[at] = weight_key(r.w[e]);
+                    keys[PICK + at] = pos_key(r.pos[e]);
+                }
+                ++at;
+            }
         parity ^= 1;
     });
 }
@@ -774,15 +798,13 @@ __global__ __launch_bounds__(1024) void slice_pick_kernel(SliceArgs s) {
         w = page < 0 ? 0 : weight_key(a.weight_in[at]);
         p = pos_key(page < 0 ? 0 : a.pos_in[at]);
     };
-#pragma unroll 4
-    for (int i = tid; i < count && i < PICK; i += 1024) {
-        int block, place;
-        split_slot(a.g, list[1 + i], block, place);
-        const int page = page_of(a.g, b, block);
-        const int64_t at = table_index(a.g, page < 0 ? 0 : page, kv, place);
-        cw[i] = page < 0 ? 0 : weight_key(a.weight_in[at]);
-        cp[i] = pos_key(page < 0 ? 0 : a.pos_in[at]);
-    }
+    const uint32_t *keys = s.keys(unit);
+#pragma unroll
+    for (int i = tid; i < PICK; i += 1024)
+        if (i < count) {
+            cw[i] = keys[i];
+            cp[i] = keys[PICK + i];
+        }
     __syncthreads();
     Last last = {~0u, ~0u, 0};
     if (left > 0) {
