@@ -481,7 +481,8 @@ int ssd_paged_decode_attn(const ssd_paged_config *cfg, const void *q, const void
 /*
  * ssd_paged_append of one token per sequence (weight 0), then ssd_paged_decode_attn:
  * the same rows, tables and results, with the rows written on the way.  weight_in is not read at the
- * new token's place.  pos may be NULL.  No page that holds a sequence's last row may belong to two sequences.
+ * new token's place; the token of a sequence longer than max_len is left out.  pos may be NULL.
+ * No page that holds a sequence's last row may belong to two sequences.
  */
 int ssd_paged_decode_step(const ssd_paged_config *cfg, const void *q, const void *k_new, const void *v_new,
                           void *k_pages, void *v_pages, int32_t *pos, const float *weight_in, float *weight_out,
@@ -501,7 +502,7 @@ int ssd_paged_decode_step(const ssd_paged_config *cfg, const void *q, const void
  *   pos_out, weight_out : the tables after; written in slots below n'.  May be the same arrays as pos_in, weight_in
  *                         (both or neither)
  *   budget       : dev int32 [n_seqs]
- *   seq_len_out  : dev int32 [n_seqs], n' per sequence; may be NULL, must not be seq_len
+ *   seq_len_out  : dev int32 [n_seqs], n' per sequence; may be NULL, must not be seq_len, seq_pos or budget
  *   max_len, workspace : as ssd_paged_decode_attn (ssd_paged_evict_workspace_bytes)
  * The rows of K and V move in place; slots n' and above keep their contents.  Sequences that share
  * a page must not be evicted from.  Rows of entries that name no page count like others and are not moved;

@@ -995,7 +995,8 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     if (!block_table || !seq_len || !budget) return fail(SSD_ERR_INVALID_ARG, "block_table, seq_len or budget is NULL");
     if (!pos_in || !pos_out || !weight_in || !weight_out) return fail(SSD_ERR_INVALID_ARG, "pos_in, pos_out, weight_in or weight_out is NULL");
     if ((pos_in == pos_out) != (weight_in == weight_out)) return fail(SSD_ERR_INVALID_ARG, "both tables are updated in place, or neither");
-    if (seq_len_out == seq_len) return fail(SSD_ERR_INVALID_ARG, "seq_len_out must not be seq_len");
+    if (seq_len_out && (seq_len_out == seq_len || seq_len_out == seq_pos || seq_len_out == budget))
+        return fail(SSD_ERR_INVALID_ARG, "seq_len_out must not be seq_len, seq_pos or budget");
     if (n_sink < 0 || recent < 0) return fail(SSD_ERR_INVALID_ARG, "n_sink=%d and recent=%d must be >= 0", n_sink, recent);
     const void *all[] = {block_table, seq_len, seq_pos, budget, pos_in, pos_out, weight_in, weight_out, seq_len_out};
     for (const void *x : all)

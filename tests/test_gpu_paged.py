@@ -393,6 +393,27 @@ def test_step_equals_append_and_attention_to_the_bit(dtype, d, H, n_kv, page, mo
     assert torch.equal(pos, pos2) and torch.equal(k.nan_to_num(9.0), bt.kd.nan_to_num(9.0)) and torch.equal(v.nan_to_num(9.0), bt.vd.nan_to_num(9.0))
 
 
+def test_step_beyond_max_len_leaves_the_token_out():
+    lens, most = [40, 100, 101, 300], 100
+    bt = Batch(lens, 4, 2, 128, "bf16", 16, seed=9)
+    g = torch.Generator().manual_seed(6)
+    k_new, v_new = (torch.randn((4, 2, 128), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    out = torch.empty((4, 4, 128), dtype=torch.bfloat16, device="cuda")
+    w_out, pos = torch.full_like(bt.weight, -3.0).cuda(), bt.pos.cuda()
+    before = bt.kd.clone(), bt.vd.clone(), pos.clone()
+    ssd.ssd_paged_decode_step(bt.cfg, bt.qd, k_new, v_new, bt.kd, bt.vd, bt.tabled, bt.lend, out, pos=pos, weight_in=bt.weight.cuda(), weight_out=w_out,
+                              max_len=most, workspace=bt.scratch(ssd.ssd_paged_workspace_bytes(bt.cfg, most, True)))
+    weight = bt.weight.clone()
+    for b in (0, 1):                                       # these two got their token
+        page, place = int(bt.table[b, (lens[b] - 1) // 16]), (lens[b] - 1) % 16
+        before[0][page, :, place], before[1][page, :, place], before[2][page, :, place] = k_new[b], v_new[b], lens[b] - 1
+        weight[page, :, place] = 0
+    for x, y in zip(before, (bt.kd, bt.vd, pos)):
+        assert torch.equal(x.nan_to_num(9.0), y.nan_to_num(9.0))
+    bt.k, bt.v = bt.kd.cpu(), bt.vd.cpu()
+    check_attend(bt, (out, None, w_out), max_len=most, weight_before=weight)
+
+
 # ---- eviction -----------------------------------------------------------------------------------------------------
 
 def _evict_case(lens, budgets, n_kv, d, dtype, page, sink, recent, seed, layout="heads", in_place=False, weight_of=None, pos_of=None, max_len=0, more=0):

@@ -106,6 +106,24 @@ def test_eviction_refusals():
                           dict(pi=FAKE + 1, po=FAKE + 1), dict(wi=FAKE + 1, wo=FAKE + 1), dict(lo=FAKE + 65)])
 
 
+def test_lengths_after_an_eviction_need_an_array_of_their_own():
+    for same in (dict(len=FAKE + 64), dict(total=FAKE + 64), dict(budget=FAKE + 64)):
+        assert _evict(_cfg(), **same) == ssd.SSD_ERR_INVALID_ARG, same
+        assert "seq_len_out" in ssd.ssd_last_error()
+
+
+def test_attention_over_long_rows_needs_its_workspace():
+    for weights in (False, True):
+        cfg = _cfg(max_blocks=1000)
+        need = ssd.ssd_paged_workspace_bytes(cfg, 0, weights)
+        assert need > 0
+        more = {} if weights else dict(wi=None, wo=None)
+        for call in (_attn, _step):
+            for bad in (dict(ws=None), dict(ws=FAKE + 128), dict(size=need - 1)):
+                assert call(cfg, **more, **bad) == ssd.SSD_ERR_INVALID_ARG, bad
+                assert "workspace" in ssd.ssd_last_error()
+
+
 def test_workspaces_grow_with_the_bound_and_not_with_the_table():
     small, large = _cfg(), _cfg(max_blocks=1000)
     for size in (lambda c, n: ssd.ssd_paged_workspace_bytes(c, n, True), ssd.ssd_paged_evict_workspace_bytes):
