@@ -42,6 +42,7 @@ struct PagedAttnArgs {
     float *z;                 // logits (base 2) [n_seqs, n_heads, z_stride]; LATER only (see Weights)
     float *lse2;              // [n_seqs, n_heads] lse (base 2) of units that one workgroup completed; LATER only
     float *part_o;            // [2 * workgroups, heads of a tile, D] sums of a unit's part, relative to its maximum
+    uint2 *parts;             // [n_seqs, n_kv, q_tiles] where a unit's first part lies, how many workgroups share it; only where rows are dealt
     float2 *part_ml;          // [2 * workgroups, heads of a tile] its maximum (base 2) and sum
     int64_t q_stride, new_stride;   // bytes
     int64_t z_stride;         // rows, a multiple of a round
@@ -238,24 +239,31 @@ template <typename T> static __device__ __forceinline__ void store_out(char *out
 // ---- who works on what -------------------------------------------------------------------------------------------------
 //
 // A unit is a (sequence, key / value head, tile of query heads); its rows are counted in rounds of WAVES tiles.  All units' rounds, in the order
-// sequence, head, row, are dealt to the workgroups in equal runs, so that the chip is evenly loaded whatever the lengths are: a
+// sequence, head, row, are dealt to the workgroups in runs of equal cost, so that the chip is evenly loaded whatever the lengths are: a
 // workgroup finishes one unit, goes through some and begins another.  The lengths are known on the device only; every wave adds them
 // up for itself, 64 sequences (or runs of them) at a time, and finds its place by a ballot.  A unit in more than one workgroup leaves parts
-// for the second launch; a workgroup leaves at most two, the one it begins with and the one it ends with.
+// for the second launch; a workgroup leaves at most two, the one it begins with and the one it ends with.  Who has a unit's first round notes where
+// its parts are.
 
 static __device__ __forceinline__ int rounds_of(int n, int round) { return n == 0 ? 1 : (n + round - 1) / round; }
 
+// What a unit costs besides its rounds, in rounds: its queries, its part of the block table and the meeting of its waves, 4 us against 3 to 6 for a
+// round (128 sequences of 10 to 8000 rows with weights: counted as none 98 us, as one round 88, two 89, three 91; 48 of up to 5000, fp32: 39.8, 38.5, 39.6,
+// 40.8; one of 5000 rows 14.1 and 15.2).
+static constexpr int EXTRA = 1;
+static __device__ __forceinline__ uint32_t cost_of(int n, int round) { return (uint32_t)rounds_of(n, round) + EXTRA; }
+
 static __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
-// The runs: `all` rounds over at most `most` workgroups, none below two rounds where there are 256 workgroups without.
+// The runs: a cost of `all` over at most `most` workgroups, none below two where there are 256 workgroups without.
 struct Runs {
     uint32_t q, rem;
-    __device__ __forceinline__ Runs(uint32_t all, uint32_t most) {
+    __device__ __forceinline__ Runs(uint32_t q_, uint32_t rem_) : q(q_), rem(rem_) {}
+    static __device__ __forceinline__ Runs of(uint32_t all, uint32_t most) {
         uint32_t w = all / 2 > 256 ? all / 2 : 256;
         w = w < most ? w : most;
         w = w < all ? w : all;
-        q = all / w;
-        rem = all - q * w;
+        return Runs(all / w, all % w);
     }
     __device__ __forceinline__ uint32_t start(uint32_t w) const { return w * q + (w < rem ? w : rem); }
     __device__ __forceinline__ uint32_t owner(uint32_t r) const {
@@ -353,6 +361,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     __shared__ int64_t pages[blocks_of(WAVES)];
     __shared__ float sm_ml[WAVES][HEADS][2];
     __shared__ float sm_lse[HEADS];
+    __shared__ uint32_t sm_runs[2];
     __shared__ int32_t page_ids[WEIGHTS == HERE ? blocks_of(WAVES) : 1];
     extern __shared__ __align__(16) float sm_o[];                   // [WAVES][tile_heads][LD], then (HERE) logits [tile_heads][z_stride + 4]
 
@@ -378,21 +387,25 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 len[i] = len[i] < 0 ? 0 : len[i] > a.g.max_len ? a.g.max_len : len[i];
-                mine += 64 * i + lane < a.g.n_seqs ? (uint32_t)rounds_of(len[i], ROUND) : 0u;
+                mine += 64 * i + lane < a.g.n_seqs ? cost_of(len[i], ROUND) : 0u;
             }
             const uint32_t all = uniform(wave_sum(mine)) * K;
-            const Runs runs(all, (uint32_t)a.workgroups);
+            const Runs runs = Runs::of(all, (uint32_t)a.workgroups);
             r0 = runs.start(blockIdx.x);
             const uint32_t r1 = runs.start(blockIdx.x + 1);
             if (r0 >= r1 || r0 >= all) return;
             left = r1 - r0;
+            if (threadIdx.x == 0) {
+                sm_runs[0] = runs.q;
+                sm_runs[1] = runs.rem;
+            }
             const uint32_t at = r0 / K;                             // in rounds of one head
             b = -1;
             n = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (b >= 0 || 64 * i >= a.g.n_seqs) continue;
-                const uint32_t up = wave_scan(64 * i + lane < a.g.n_seqs ? (uint32_t)rounds_of(len[i], ROUND) : 0u) + before;
+                const uint32_t up = wave_scan(64 * i + lane < a.g.n_seqs ? cost_of(len[i], ROUND) : 0u) + before;
                 const int k = (int)__popcll(__ballot(up <= at));
                 if (k < 64) {
                     b = 64 * i + k;
@@ -405,15 +418,19 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             uint32_t mine = 0;
             for (int i = 0; i < run; ++i) {
                 const int seq = lane * run + i;
-                if (seq < a.g.n_seqs) mine += (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
+                if (seq < a.g.n_seqs) mine += cost_of(clamp_len(a.g, seq), ROUND);
             }
             const uint32_t upto = wave_scan(mine);
             const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * K;
-            const Runs runs(all, (uint32_t)a.workgroups);
+            const Runs runs = Runs::of(all, (uint32_t)a.workgroups);
             r0 = runs.start(blockIdx.x);
             const uint32_t r1 = runs.start(blockIdx.x + 1);
             if (r0 >= r1 || r0 >= all) return;
             left = r1 - r0;
+            if (threadIdx.x == 0) {
+                sm_runs[0] = runs.q;
+                sm_runs[1] = runs.rem;
+            }
             const uint32_t at = r0 / K;
             const int l = (int)__popcll(__ballot(upto <= at));
             before = l == 0 ? 0 : (uint32_t)__builtin_amdgcn_readlane((int)upto, l - 1);
@@ -421,7 +438,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             for (int i0 = 0;; i0 += 64) {                           // the run's sequences, 64 at a time
                 const int seq = l * run + i0 + lane;
                 const bool ours = i0 + lane < run && seq < a.g.n_seqs;
-                const uint32_t up = wave_scan(ours ? (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND) : 0u) + before;
+                const uint32_t up = wave_scan(ours ? cost_of(clamp_len(a.g, seq), ROUND) : 0u) + before;
                 const int k = (int)__popcll(__ballot(up <= at));
                 if (k < 64) {
                     b = l * run + i0 + k;
@@ -432,9 +449,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             }
             n = clamp_len(a.g, b);
         }
-        const uint32_t tb = uniform((uint32_t)rounds_of(n, ROUND)), into = r0 - before * K;
+        const uint32_t tb = uniform(cost_of(n, ROUND)), into = r0 - before * K;
         ht = (int)(into / tb);
-        t = (int)(into - (uint32_t)ht * tb);
+        t = (int)(into - (uint32_t)ht * tb) - EXTRA;
+        if (t < 0) {                                                // the run begins with what the unit costs besides
+            if (left <= (uint32_t)-t) return;
+            left -= (uint32_t)-t;
+            t = 0;
+        }
     }
     }
     b = (int)uniform((uint32_t)b);
@@ -646,7 +668,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             l = x + y;
         }
         if (!first_unit) __syncthreads();                           // a unit without rows passes no other barrier
-        if (r < heads) {
+        const int active = end - begin > (WAVES - 1) * TT::ROWS ? WAVES : end - begin > TT::ROWS ? (end - begin + TT::ROWS - 1) / TT::ROWS : 1;
+        if (r < heads && wave < active) {                           // the others have had no tile
             if (g == 0) {
                 sm_ml[wave][r][0] = m;
                 sm_ml[wave][r][1] = l;
@@ -663,9 +686,11 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             const int h = i / D, d = i % D;
             float top = sm_ml[0][h][0], sum = 0.f, acc = 0.f;
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm_ml[w][h][0]);
+            for (int w = 1; w < WAVES; ++w)
+                if (w < active) top = fmaxf(top, sm_ml[w][h][0]);
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
+                if (w >= active) break;
                 const float f = fast_exp2(sm_ml[w][h][0] - top);
                 sum = fmaf(sm_ml[w][h][1], f, sum);
                 acc = fmaf(sm_o[(w * heads + h) * LD + d], f, acc);
@@ -700,8 +725,17 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             }
             return;
         }
+        if (a.workgroups && t == 0 && threadIdx.x == 0) {           // where the parts of a unit lie is told by who has its first round
+            uint32_t count = 1;
+            if (!whole) {
+                const Runs runs{sm_runs[0], sm_runs[1]};
+                count = runs.owner(runs.start(blockIdx.x + 1) + (uint32_t)(rounds - take) - 1) - blockIdx.x + 1;
+            }
+            a.parts[(int64_t)b * (a.g.n_kv * a.q_tiles) + ht] = make_uint2((uint32_t)slot, count);
+        }
         left -= (uint32_t)take;
-        if (left == 0) return;
+        if (left <= EXTRA) return;
+        left -= EXTRA;
         t = 0;
         if (++ht == a.g.n_kv * a.q_tiles) {
             ht = 0;
@@ -727,7 +761,6 @@ static __device__ __forceinline__ float wave_max(float v) {
 // grid = (kv heads, sequences, head_blocks + a few)
 template <typename T, int D, bool QUADS, bool WIDE>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int step, int head_blocks) {
-    constexpr int ROUND = 4 * Tile<T, D>::ROWS;
     constexpr int FR = D / 4, PW = 64 / FR, NW = WIDE ? 4 : 1;      // 16-byte pieces of a part's sums; parts a wave reads side by side; waves
     __shared__ float red[2][4];
     __shared__ f32x4 sums[4][FR];
@@ -735,26 +768,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
     extern __shared__ float lse2[];                                 // [group]
     const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = clamp_len(a.g, b);
-    const uint32_t K = (uint32_t)(a.g.n_kv * a.q_tiles), tb = (uint32_t)rounds_of(n, ROUND);
-    uint32_t all = 0, before = 0;
-    if (a.workgroups > 0) {
-        for (int seq = lane; seq < a.g.n_seqs; seq += 64) {
-            const uint32_t x = (uint32_t)rounds_of(clamp_len(a.g, seq), ROUND);
-            all += x;
-            before += seq < b ? x : 0;
-        }
-        all = uniform(wave_sum(all)) * K;
-        before = uniform(wave_sum(before)) * K;
-    }
     // the workgroups that share a unit, and where the first one's part lies
-    struct Parts { uint32_t w0, count, slot0; };
+    struct Parts { uint32_t slot0, count; };
     auto parts_of = [&](int tile) {
-        if (a.workgroups == 0) return Parts{0, 1, 0};
-        const Runs runs(all, (uint32_t)a.workgroups);
-        const uint32_t u0 = before + (uint32_t)(kv * a.q_tiles + tile) * tb, w0 = runs.owner(u0);
-        return Parts{w0, runs.owner(u0 + tb - 1) - w0 + 1, 2 * w0 + (runs.start(w0) < u0 ? 1 : 0)};
+        if (a.workgroups == 0) return Parts{0, 1};
+        const uint2 p = a.parts[((int64_t)b * a.g.n_kv + kv) * a.q_tiles + tile];
+        return Parts{uniform(p.x), uniform(p.y)};
     };
-    auto slot = [&](const Parts &p, uint32_t c) { return (int64_t)(c == 0 ? p.slot0 : 2 * (p.w0 + c)) * a.tile_heads; };
+    auto slot = [&](const Parts &p, uint32_t c) { return (int64_t)(c == 0 ? p.slot0 : (p.slot0 & ~1u) + 2 * c) * a.tile_heads; };
 
     if ((int)blockIdx.z < head_blocks) {
         const int head = WIDE ? (int)blockIdx.z : (int)blockIdx.z * 4 + wave, w = WIDE ? wave : 0;
@@ -868,7 +889,7 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, bool weigh
     // and where 32 bits would not hold the sums.  With weights that saves the second launch, and pays earlier (256 units of 640 rows 25 us dealt and 17
     // whole, 128 19.6 and 15.0, 32 12.3 and 12.6; 256 of 1000 rows 29.8 and 24.6, 128 19.4 and 20.7).
     const bool once = weights && s.q_tiles == 1;
-    const bool plain = rounds <= (once ? 5 : 4) || (units >= (once ? 256 : 512) && rounds <= 8) || units * rounds >= 1ll << 31;
+    const bool plain = rounds <= (once ? 5 : 4) || (units >= (once ? 256 : 512) && rounds <= 8) || units * (rounds + EXTRA) >= 1ll << 31;
     // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
     s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
     s.round = s.waves * tile;
@@ -890,7 +911,7 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, bool weigh
     return s;
 }
 
-struct PagedScratch { size_t z, lse2, o, ml, all; };
+struct PagedScratch { size_t z, lse2, o, ml, parts, all; };
 
 static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s, bool weights) {
     PagedScratch w;
@@ -899,7 +920,8 @@ static PagedScratch paged_scratch(const ssd_paged_config *c, const PagedShape &s
     w.lse2 = weights && !s.here ? round256(bh * sizeof(float)) : 0;
     w.o = round256(parts * c->head_dim * sizeof(float));
     w.ml = round256(parts * sizeof(float2));
-    w.all = w.z + w.lse2 + w.o + w.ml;
+    w.parts = s.workgroups ? round256((size_t)c->n_seqs * c->n_kv_heads * s.q_tiles * sizeof(uint2)) : 0;
+    w.all = w.z + w.lse2 + w.o + w.ml + w.parts;
     return w;
 }
 
@@ -970,6 +992,7 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     a.lse2 = reinterpret_cast<float *>(ws + parts.z);
     a.part_o = reinterpret_cast<float *>(ws + parts.z + parts.lse2);
     a.part_ml = reinterpret_cast<float2 *>(ws + parts.z + parts.lse2 + parts.o);
+    a.parts = reinterpret_cast<uint2 *>(ws + parts.z + parts.lse2 + parts.o + parts.ml);
     a.k_new = static_cast<const char *>(k_new);
     a.v_new = static_cast<const char *>(v_new);
     a.k_dst = static_cast<char *>(k_pages);
