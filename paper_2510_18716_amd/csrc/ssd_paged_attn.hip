@@ -272,34 +272,52 @@ struct Runs {
     }
 };
 
-// Accumulated weights of rows j .. j + 3, j a multiple of four, n the sequence's rows; p their probabilities.  newest: the row without a
-// weight so far, or -1.
-template <bool QUADS>
-static __device__ __forceinline__ void add_weights(const PagedAttnArgs &a, int b, int kv, int j, int n, const f32x4 &p, int newest) {
+// Rows j .. j + 3 (j < n, a multiple of four) in the tables: where they are, negative past n and where no page is named, and their weights so far.
+struct Entries {
+    int64_t at[4];
+    float w[4];
+};
+// page(block): the block's page, or a negative number
+template <bool QUADS, typename Page>
+static __device__ __forceinline__ Entries entries_of(const PagedAttnArgs &a, int kv, int j, int n, const Page &page) {
+    Entries x;
     int block, place;
     split_slot(a.g, j, block, place);
-    if (QUADS && j + 4 <= n) {
-        const int page = page_of(a.g, b, block);
-        if (page < 0) return;
-        const int64_t i = table_index(a.g, page, kv, place);
-        f32x4 w = *reinterpret_cast<const f32x4_any *>(a.weight_in + i);
+    if constexpr (QUADS) {                                         // four places of one page
+        const int p = page(block);
+        const int64_t i = table_index(a.g, p < 0 ? 0 : p, kv, place);
+        const f32x4 w = *reinterpret_cast<const f32x4_any *>(a.weight_in + i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (j + e == newest ? 0.f : w[e]) + p[e];
-        *reinterpret_cast<f32x4_any *>(a.weight_out + i) = w;
+        for (int e = 0; e < 4; ++e) {
+            x.at[e] = p >= 0 && j + e < n ? i + e : -1;
+            x.w[e] = w[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int p = j + e < n ? page(block) : -1;
+            x.at[e] = p < 0 ? -1 : table_index(a.g, p, kv, place);
+            x.w[e] = a.weight_in[p < 0 ? 0 : x.at[e]];
+            if (++place == a.g.page_size) {
+                place = 0;
+                ++block;
+            }
+        }
+    }
+    return x;
+}
+
+// p: what is added; newest: the row without a weight so far, or -1.
+template <bool QUADS> static __device__ __forceinline__ void add_weights(const PagedAttnArgs &a, int j, int n, Entries x, const f32x4 &p, int newest) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x.w[e] = (j + e == newest ? 0.f : x.w[e]) + p[e];
+    if (QUADS && j + 4 <= n) {
+        if (x.at[0] >= 0) *reinterpret_cast<f32x4_any *>(a.weight_out + x.at[0]) = f32x4{x.w[0], x.w[1], x.w[2], x.w[3]};
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (j + e >= n) return;
-        if (e > 0 && ++place == a.g.page_size) {
-            place = 0;
-            ++block;
-        }
-        const int page = page_of(a.g, b, block);
-        if (page < 0) continue;
-        const int64_t i = table_index(a.g, page, kv, place);
-        a.weight_out[i] = (j + e == newest ? 0.f : a.weight_in[i]) + p[e];
-    }
+    for (int e = 0; e < 4; ++e)
+        if (x.at[e] >= 0) a.weight_out[x.at[e]] = x.w[e];
 }
 
 // Four rows' probabilities, summed over heads; z: the first head's logits of theirs, the others' `stride` apart.
@@ -636,29 +654,9 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
 
         // HERE: a thread's four rows (a unit has no more of them than the workgroup has threads), their weights so far on their way while the waves meet
         const int j = 4 * (int)threadIdx.x;
-        int64_t entry[4];
-        float w[4];
+        Entries entries;
         if constexpr (WEIGHTS == HERE)
-            if (j < n) {
-                int block = block_of(a, j), place = j - block * a.g.page_size;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int page = j + e < n ? page_ids[block] : -1;
-                    entry[e] = page < 0 ? -1 : table_index(a.g, page, kv, place);
-                    if (++place == a.g.page_size) {
-                        place = 0;
-                        ++block;
-                    }
-                }
-                if constexpr (QUADS) {
-                    const f32x4 x = *reinterpret_cast<const f32x4_any *>(a.weight_in + (entry[0] < 0 ? 0 : entry[0]));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = x[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = a.weight_in[entry[e] < 0 ? 0 : entry[e]];
-                }
-            }
+            if (j < n) entries = entries_of<QUADS>(a, kv, j, n, [&](int block) { return page_ids[block]; });
         // the waves' states meet
         {
             float x, y;
@@ -711,18 +709,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         }
         if constexpr (WEIGHTS == HERE) {
             __syncthreads();
-            if (j < n) {
-                const f32x4 p = probabilities(sm_o + WAVES * heads * LD + j, (int)a.z_stride + 4, sm_lse, heads);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = (newest && j + e == n - 1 ? 0.f : w[e]) + p[e];
-                if (QUADS && j + 4 <= n) {
-                    if (entry[0] >= 0) *reinterpret_cast<f32x4_any *>(a.weight_out + entry[0]) = f32x4{w[0], w[1], w[2], w[3]};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (entry[e] >= 0) a.weight_out[entry[e]] = w[e];
-                }
-            }
+            if (j < n)
+                add_weights<QUADS>(a, j, n, entries, probabilities(sm_o + WAVES * heads * LD + j, (int)a.z_stride + 4, sm_lse, heads), newest ? n - 1 : -1);
             return;
         }
         if (a.workgroups && t == 0 && threadIdx.x == 0) {           // where the parts of a unit lie is told by who has its first round
@@ -831,6 +819,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
     }
     const int first = ((int)blockIdx.z - head_blocks) * 1024;
     if (first >= n) return;
+    int j = first + 4 * tid;                                       // the tables' entries are on their way while the lse are found
+    Entries entries;
+    const auto page = [&](int block) { return page_of(a.g, b, block); };
+    if (j < n) entries = entries_of<QUADS>(a, kv, j, n, page);
     // the heads' lse: a lane takes a head of the tile and every sixteenth part
     for (int tile = 0; tile < a.q_tiles; ++tile) {
         const int h0 = tile * HEADS, h = lane & 15, heads = a.group - h0 < HEADS ? a.group - h0 : HEADS;
@@ -863,8 +855,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
     __syncthreads();
     const int newest = step && a.g.seq_len[b] == n ? n - 1 : -1;
     const float *z0 = a.z + ((int64_t)b * a.n_heads + kv * a.group) * a.z_stride;
-    for (int j = first + 4 * tid; j < n; j += ((int)gridDim.z - head_blocks) * 1024)
-        add_weights<QUADS>(a, b, kv, j, n, probabilities(z0 + j, a.z_stride, lse2, a.group), newest);
+    while (j < n) {
+        add_weights<QUADS>(a, j, n, entries, probabilities(z0 + j, a.z_stride, lse2, a.group), newest);
+        j += ((int)gridDim.z - head_blocks) * 1024;
+        if (j < n) entries = entries_of<QUADS>(a, kv, j, n, page);
+    }
 }
 
 // ---- launch shapes ---------------------------------------------------------------------------------------------------
