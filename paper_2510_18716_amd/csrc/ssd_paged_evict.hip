@@ -75,12 +75,6 @@ static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b
     return r;
 }
 
-static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v |= (uint32_t)__shfl_xor((int)v, o);
-    return v;
-}
-
 // Rows from[i] to slots to[i]: K and V of a row by neighbouring threads, MOVES rows of a thread on their way at a time (past the end it repeats
 // the last row, which writes the same again); move_entries: the tables' entries, a thread each.  No load is under a condition: the compiler would wait for
 // everything in flight.
