@@ -21,10 +21,10 @@
 // had a part of are joined by a second launch, which also brings their weights up to date, from logits that the first one left in memory.
 //
 // Measured (bf16, rows of 128; time of the call, share of the K and V bytes alone): 4 sequences of 30000 to 131072 rows, 32 query heads on 8: 184 to
-// 192 us, 6.2 to 6.5 TB/s (a plain read reaches 6.1 to 7.0).  128 sequences of 64 to 640 rows, 32 heads: 92 us, 5.8 TB/s; with weights 100.  128
-// sequences of 10 to 8000 rows, 32 query heads on 4: 73 us, 4.5 TB/s; with weights and the new rows 95 -- the logits are 6 % of the bytes and,
-// written among the reads, cost 15 % of the time (batches of them in LDS, other orders in memory and the hints on the stores change nothing).
-// fp32, rows of 64, 48 sequences of 0 to 5000 rows with weights: 41 us, 3.1 TB/s.
+// 192 us, 6.2 to 6.5 TB/s (a plain read reaches 6.1 to 7.0).  128 sequences of 64 to 640 rows, 32 heads: 92 to 95 us, 5.6 to 5.8 TB/s; with weights 99 to
+// 102.  128 sequences of 10 to 8000 rows, 32 query heads on 4: 67 us, 4.8 TB/s; with weights and the new rows 87 -- the logits are 6 % of the bytes and,
+// written among the reads, cost 16 us (batches of them in LDS, other orders in memory and the hints on the stores change nothing).
+// fp32, rows of 64, 48 sequences of 0 to 5000 rows with weights: 37 us, 3.4 TB/s.
 #include "ssd_paged.h"
 
 namespace ssd {
@@ -871,7 +871,7 @@ struct PagedShape {
     size_t lds;               // where the waves meet
 };
 
-static PagedShape paged_shape(const ssd_paged_config *c, int max_len, bool weights) {
+static PagedShape paged_shape(const ssd_paged_config *c, int max_len) {
     PagedShape s;
     const int reach = paged_reach(c, max_len), group = c->n_heads / c->n_kv_heads;
     const int tile = c->dtype == SSD_BF16 ? 32 : 16;
@@ -879,17 +879,16 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, bool weigh
     s.tile_heads = group < HEADS ? group : HEADS;
     const int64_t units = (int64_t)c->n_seqs * c->n_kv_heads * s.q_tiles, rounds = (reach + 4 * tile - 1) / (4 * tile);
     s.reach = rounds * 4 * tile;
-    // A unit of few rounds is taken whole (8 units of 512 rows 9.1 us whole and 10.6 dealt, 512 of 512 24 and 30); with more rounds only where
-    // units are many (512 of 1024 rows 44 and 51, of 10 to 1024 25 and 23, of 2048 84 and 91, of 10 to 2048 44 and 29; 128 of 1024 20 and 19),
-    // and where 32 bits would not hold the sums.  With weights that saves the second launch, and pays earlier (256 units of 640 rows 25 us dealt and 17
-    // whole, 128 19.6 and 15.0, 32 12.3 and 12.6; 256 of 1000 rows 29.8 and 24.6, 128 19.4 and 20.7).
-    const bool once = weights && s.q_tiles == 1;
-    const bool plain = rounds <= (once ? 5 : 4) || (units >= (once ? 256 : 512) && rounds <= 8) || units * (rounds + EXTRA) >= 1ll << 31;
+    // A unit of few rounds is taken whole: one launch instead of two (8 units of 400 rows 8.5 us whole and 11.0 dealt, 256 12.9 and 18.8, 128 of 640 13.9
+    // and 16.7, 32 12.2 and 11.5); with more rounds only where units are many (256 of 1000 rows 24.5 and 28.6, of 10 to 1000 18.5 and 16.6, 1024 85 and 92, 38 and
+    // 34; 128 of 1000 19.7 and 21.0, of 10 to 1000 17.7 and 13.3; 512 of 2048 84 and 91, of 10 to 2048 44 and 29; all with 16 key heads, two query heads each; weights
+    // change little), and where 32 bits would not hold the sums.
+    const bool plain = rounds <= 5 || (units >= 256 && rounds <= 8) || units * (rounds + EXTRA) >= 1ll << 31;
     // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
     s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
     s.round = s.waves * tile;
-    // 256 compute units, four or three workgroups each (fp32 of 64 elements 41.7 us with 768, 40.5 with 1024; 128 sequences of 10 to 8000 rows in bf16 95
-    // with 768, 91 with 2048, 512 of them 251 and 256)
+    // 256 compute units, four or three workgroups each; twice as many are no better (128 sequences of 10 to 8000 rows 67 and 69 us, with weights 87 and 87, of 1195 rows
+    // 63.5 and 66.7; fp32 of 64 elements, 48 of up to 5000 rows, 37.4 and 39.8, with three each 38)
     const int64_t resident = c->head_dim == 64 ? 1024 : 768;
     s.workgroups = plain ? 0 : (int)(units * rounds < resident ? units * rounds : resident);
     // Where not all units are resident at once a late long one would run on alone; ranking costs every workgroup a microsecond (32 heads of 64 to 640
@@ -968,7 +967,7 @@ static int paged_attend(const ssd_paged_config *cfg, const void *q, const void *
     if (!aligned(block_table, 4) || !aligned(seq_len, 4) || !aligned(seq_pos, 4) || !aligned(pos, 4) || !aligned(weight_in, 4) ||
         !aligned(weight_out, 4) || !aligned(lse, 4))
         return fail(SSD_ERR_INVALID_ARG, "tables must be aligned to their elements");
-    const PagedShape shape = paged_shape(cfg, max_len, weight_out != nullptr);
+    const PagedShape shape = paged_shape(cfg, max_len);
     const PagedScratch parts = paged_scratch(cfg, shape, weight_out != nullptr);
     const size_t need = parts.all;
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
@@ -1019,7 +1018,7 @@ using namespace ssd;
 extern "C" size_t ssd_paged_workspace_bytes(const ssd_paged_config *cfg, int max_len, int with_weights) {
     clear_error();
     if (check_paged(cfg) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
-    return paged_scratch(cfg, paged_shape(cfg, max_len, with_weights != 0), with_weights != 0).all;
+    return paged_scratch(cfg, paged_shape(cfg, max_len), with_weights != 0).all;
 }
 
 extern "C" int ssd_paged_decode_attn(const ssd_paged_config *cfg, const void *q, const void *k_pages, const void *v_pages,
