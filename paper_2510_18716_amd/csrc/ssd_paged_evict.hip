@@ -291,9 +291,10 @@ static __device__ __forceinline__ uint32_t take_least(const uint32_t (&wk)[KEYS]
         int last = 63 - __clzll((long long)(__ballot(any && m == all) | 1));  // the highest lane that has it
         bool ours = true;
         if constexpr (THREADS > 64) {
+            const bool some = __any(any);                          // of the whole wave: not inside the branch
             if (lane == 0) {
                 least[i & 1][wave] = all;
-                owner[i & 1][wave] = __ballot(any) != 0;
+                owner[i & 1][wave] = some;
             }
             __syncthreads();
             int w = -1;

@@ -638,6 +638,17 @@ def test_few_evictions_among_equals():
         _table_case([200] * units, [150] * units, 1, 16, WEIGHTS["steps"], lambda r, n: r.integers(0, 3, n), 0, 0, [200] * units, False)
 
 
+@pytest.mark.parametrize("n", [200, 300, 2100, 9000])
+@pytest.mark.parametrize("sink,recent", [(8, 0), (17, 5), (130, 0), (0, 180), (64, 64)])
+def test_few_evictions_beside_protected_rows(n, sink, recent):
+    """The first lanes of some waves have nothing that may go, others of the wave have; and too many protected ones for the budget."""
+    lens = [n, n - 7]
+    for go in (1, 3):
+        _table_case(lens, [n - go, n - 7 - go], 1, 16, WEIGHTS["usual"], lambda r, m: np.arange(m), sink, recent, lens, go == 1, seed=n + go)
+    for go in (1, 4):
+        _table_case(lens, [sink + recent - go] * 2, 1, 16, WEIGHTS["usual"], lambda r, m: np.arange(m), sink, recent, lens, False, seed=n + go)
+
+
 # ---- the example ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
