@@ -28,6 +28,7 @@ struct PagedEvictArgs {
     int n_sink, recent;
     int cap;
     int lpr_log2;
+    int share;
 };
 
 static __host__ __device__ inline int64_t moves_of(int cap, int64_t unit) { return unit * (2 * (int64_t)cap + 1); }
@@ -270,7 +271,9 @@ static __device__ __forceinline__ Last descend_wave(const Spread &sp, int left, 
 
 // Where few rows go: they are taken out one by one.  keys: this thread's; compete: which of them do; gone: the bits of rows that go are set.
 // The least key goes; of equal ones the highest slot (threads have consecutive rows).
-static constexpr int FEW = 4;
+// Lines where the descent takes as long: 256 units of 200 rows, 12 evictions 8.8 and 11.2 us, 24 12.6 and 10.0; of 2000, 8 15.4 and 18.2, 16 23.3 and 19.9; of 8000, 4 35.6
+// and 38.6, 6 40.5 and 39.0.
+static constexpr int few(int threads) { return threads == 64 ? 16 : threads == 256 ? 8 : 4; }
 template <int THREADS, int KEYS>
 static __device__ __forceinline__ uint32_t take_least(const uint32_t (&wk)[KEYS], const uint32_t (&pk)[KEYS], uint32_t compete, int rows,
                                                       unsigned long long (&least)[2][THREADS / 64], int (&owner)[2][THREADS / 64]) {
@@ -352,6 +355,20 @@ static __device__ __forceinline__ bool is_safe(const PagedEvictArgs &a, int64_t 
 
 // ---- units of one workgroup ----------------------------------------------------------------------------------------------
 
+// The unit of a workgroup.  Workgroups go to the eight XCDs in turn.  Where a page's entries of one head are less than a cache line, the heads that
+// share one (2^share of them) go to the same XCD, or two would read and write every line of the tables.
+static __device__ __forceinline__ void unit_of(const PagedEvictArgs &a, int &kv, int &b) {
+    kv = blockIdx.x;
+    b = blockIdx.y;
+    if (a.share == 0) return;
+    const unsigned heads = (unsigned)a.g.n_kv, i = blockIdx.y * heads + blockIdx.x, round = 8u << a.share;
+    if (i < (unsigned)a.g.n_seqs * heads / round * round) {
+        const unsigned unit = ((i / round * 8 + (i & 7)) << a.share) + (i >> 3 & ((1u << a.share) - 1));
+        b = (int)(unit / heads);
+        kv = (int)(unit - (unsigned)b * heads);
+    }
+}
+
 // A thread has KEYS consecutive rows.  grid = (kv heads, sequences)
 template <int THREADS, int KEYS>
 __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a, int move_here) {
@@ -360,7 +377,9 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     __shared__ uint16_t free_slots[HALF], move_slots[HALF];        // if the rows move here: at most half of them do
     __shared__ unsigned long long least[2][NW];
     __shared__ int owner[2][NW];
-    const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int kv, b;
+    unit_of(a, kv, b);
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const bool copy = a.pos_out != a.pos_in;
     const int64_t total = a.g.seq_pos[b];
@@ -415,7 +434,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     uint32_t kept = among_safe ? 0 : safe, tie = 0;
     Last last = {0, 0, 0};
     const int go = (among_safe ? (int)safe_rows : n - (int)safe_rows) - left;     // of those that compete
-    if (left > 0 && go <= FEW) {
+    if (left > 0 && go <= few(THREADS)) {
         kept |= compete & ~take_least<THREADS, KEYS>(wk, pk, compete, go, least, owner);
     } else if (left > 0) {
         Spread sp = {0, 0, 0, 0, 0};
@@ -1019,11 +1038,16 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     a.recent = recent;
     a.cap = shape.cap;
     a.lpr_log2 = __builtin_ctz((unsigned)((size_t)cfg->head_dim * paged_esize(cfg) / 16));
+    a.share = cfg->page_size >= 32 ? 0 : cfg->page_size >= 16 ? 1 : cfg->page_size >= 8 ? 2 : 3;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 units((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs);
     const int64_t n_units = (int64_t)units.x * units.y;
     const int reach = a.g.max_len;
-    const int move_here = n_units >= 128 && !shape.slices;
+    // Rows move by the unit's workgroup, which saves a launch, where units fill the chip (one eviction from each of 64 units of 2000 rows 7.5 us here and 9.2 by a launch, 1000 32.9 and
+    // 17.0; 128 units 39 and 28, 256 42.6 and 43.4, of 8000 rows to 4000 137 and 156); with few rows, from 128 units on (one of 129 rows 6.3 and 8.2, 100 of 250 stay 16.7 and 14.0).
+    const int move_here = n_units >= (reach <= 256 ? 128 : 256) && !shape.slices;
+    // A wave, 256 or 1024 threads per unit: the next larger take 15.6 us instead of 11.5 (12 of 200 rows, 64 units), 18.0 and 17.0 (half of 2000 rows, 32 units; 39.5 and 42.6 with 256), 38.7 and
+    // 32.0 (half of 8000); slices from 8192 rows on 38.1 and 29.2 (one of 16000 rows, 32 units; 346 and 305 for half of them, 256).
     if (shape.slices) {
         SliceArgs sa;
         sa.e = a;
