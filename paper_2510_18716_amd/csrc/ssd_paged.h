@@ -14,6 +14,7 @@ struct PagedGeom {
     int32_t n_seqs, n_kv, page_size, n_pages, max_blocks;
     int32_t max_len;                 // min(caller's bound, max_blocks * page_size)
     int32_t page_log2;               // log2 of page_size, or -1 where it is no power of two
+    int32_t share;                   // log2 of the heads whose entries of a page share a cache line of the tables
 };
 
 static __device__ __forceinline__ int clamp_len(const PagedGeom &g, int b) {
@@ -42,6 +43,22 @@ static __device__ __forceinline__ int64_t row_offset(const PagedGeom &g, int pag
 }
 static __device__ __forceinline__ int64_t table_index(const PagedGeom &g, int page, int kv, int place) {
     return ((int64_t)page * g.n_kv + kv) * g.page_size + place;
+}
+
+// The sequence and key head of a workgroup of a grid (heads, sequences).  Workgroups go to the eight XCDs in turn.  Where a page's entries of one
+// head are less than a cache line, the heads that share one go to the same XCD, or two would read and write every line of the tables (one eviction from each
+// of 256 units of 8000 rows in pages of 16 28.7 -> 20.3 us, of 16000 105 -> 64, in pages of one row 186 -> 83; 32 unequal prompts 45.1 -> 45.9; attention with
+// weights over 4096 units of 640 rows 250 -> 237; the second launch of the attention gains nothing).
+static __device__ __forceinline__ void unit_of(const PagedGeom &g, int &kv, int &b) {
+    kv = blockIdx.x;
+    b = blockIdx.y;
+    if (g.share == 0) return;
+    const unsigned heads = (unsigned)g.n_kv, i = blockIdx.y * heads + blockIdx.x, round = 8u << g.share;
+    if (i < (unsigned)g.n_seqs * heads / round * round) {
+        const unsigned unit = ((i / round * 8 + (i & 7)) << g.share) + (i >> 3 & ((1u << g.share) - 1));
+        b = (int)(unit / heads);
+        kv = (int)(unit - (unsigned)b * heads);
+    }
 }
 
 // Inclusive sum over the lanes of a wave: rows of 16 by shifts, then the last lane of a row to the rows behind it.

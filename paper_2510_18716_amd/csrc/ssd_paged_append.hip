@@ -61,6 +61,7 @@ PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, cons
     g.max_blocks = c->max_blocks;
     g.max_len = paged_reach(c, max_len);
     g.page_log2 = (c->page_size & (c->page_size - 1)) == 0 ? __builtin_ctz((unsigned)c->page_size) : -1;
+    g.share = c->page_size >= 32 ? 0 : c->page_size >= 16 ? 1 : c->page_size >= 8 ? 2 : 3;
     return g;
 }
 

@@ -390,8 +390,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
     const PagedAttnArgs &a = arguments();
     const uint32_t K = (uint32_t)(a.g.n_kv * a.q_tiles);
     if (a.workgroups == 0) {
-        b = a.by_length ? by_length<2>(a, (int)blockIdx.y, lane) : (int)blockIdx.y;
-        ht = (int)((blockIdx.x + blockIdx.y) % K);
+        int rank = (int)blockIdx.y;
+        if constexpr (WEIGHTS == HERE) unit_of(a.g, ht, rank);
+        else ht = (int)((blockIdx.x + blockIdx.y) % K);
+        b = a.by_length ? by_length<2>(a, rank, lane) : rank;
         t = 0;
         n = clamp_len(a.g, b);
         left = (uint32_t)rounds_of(n, ROUND);

@@ -28,7 +28,6 @@ struct PagedEvictArgs {
     int n_sink, recent;
     int cap;
     int lpr_log2;
-    int share;
 };
 
 static __host__ __device__ inline int64_t moves_of(int cap, int64_t unit) { return unit * (2 * (int64_t)cap + 1); }
@@ -355,20 +354,6 @@ static __device__ __forceinline__ bool is_safe(const PagedEvictArgs &a, int64_t 
 
 // ---- units of one workgroup ----------------------------------------------------------------------------------------------
 
-// The unit of a workgroup.  Workgroups go to the eight XCDs in turn.  Where a page's entries of one head are less than a cache line, the heads that
-// share one (2^share of them) go to the same XCD, or two would read and write every line of the tables.
-static __device__ __forceinline__ void unit_of(const PagedEvictArgs &a, int &kv, int &b) {
-    kv = blockIdx.x;
-    b = blockIdx.y;
-    if (a.share == 0) return;
-    const unsigned heads = (unsigned)a.g.n_kv, i = blockIdx.y * heads + blockIdx.x, round = 8u << a.share;
-    if (i < (unsigned)a.g.n_seqs * heads / round * round) {
-        const unsigned unit = ((i / round * 8 + (i & 7)) << a.share) + (i >> 3 & ((1u << a.share) - 1));
-        b = (int)(unit / heads);
-        kv = (int)(unit - (unsigned)b * heads);
-    }
-}
-
 // A thread has KEYS consecutive rows.  grid = (kv heads, sequences)
 template <int THREADS, int KEYS>
 __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a, int move_here) {
@@ -379,7 +364,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     __shared__ int owner[2][NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int kv, b;
-    unit_of(a, kv, b);
+    unit_of(a.g, kv, b);
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const bool copy = a.pos_out != a.pos_in;
     const int64_t total = a.g.seq_pos[b];
@@ -1038,7 +1023,6 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     a.recent = recent;
     a.cap = shape.cap;
     a.lpr_log2 = __builtin_ctz((unsigned)((size_t)cfg->head_dim * paged_esize(cfg) / 16));
-    a.share = cfg->page_size >= 32 ? 0 : cfg->page_size >= 16 ? 1 : cfg->page_size >= 8 ? 2 : 3;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 units((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs);
     const int64_t n_units = (int64_t)units.x * units.y;
