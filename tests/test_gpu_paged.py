@@ -649,6 +649,24 @@ def test_few_evictions_beside_protected_rows(n, sink, recent):
         _table_case(lens, [sink + recent - go] * 2, 1, 16, WEIGHTS["usual"], lambda r, m: np.arange(m), sink, recent, lens, False, seed=n + go)
 
 
+@pytest.mark.parametrize("n", [200, 300, 2100, 9000])
+def test_evictions_about_the_line_between_one_by_one_and_the_descent(n):
+    for go in (4, 5, 8, 9, 16, 17):
+        lens = [n, n - 3, n - go]
+        for weights in ("usual", "zeros"):
+            _table_case(lens, [n - go] * 3, 2, 16, WEIGHTS[weights], lambda r, m: np.arange(m), 2, 9, lens, False, seed=n + go)
+
+
+@pytest.mark.parametrize("page,units", [(16, 40), (8, 37), (1, 66), (24, 9)])
+def test_heads_that_share_cache_lines_of_the_tables(page, units):
+    """Workgroups of neighbouring heads are dealt in another order; with and without a remainder, heads that do not fill a line."""
+    for n_kv in (1, 3, 8):
+        lens = [100 + i % 7 for i in range(units)]
+        _evict_case(lens, [60] * units, n_kv, 64, "bf16", page, 1, 5, units)
+        bt = Batch(lens, n_kv, n_kv, 64, "bf16", page, seed=units)
+        check_attend(bt, attend(bt))
+
+
 # ---- the example ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
