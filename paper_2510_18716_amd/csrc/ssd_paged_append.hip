@@ -1,7 +1,7 @@
 // ssd_paged_append: new tokens' K and V rows into the pages of a cache of unequal lengths, with their entries in the tables.
 // Also the checks that every call on such a cache shares.
 //
-// Pure data movement, bound by HBM: a row is a run of adjacent lanes, 16 bytes each, on both sides.  46000 tokens of 16 KB (prompts of 64
+// Pure data movement, bound by HBM: a row is a run of adjacent lanes, 16 bytes each, on both sides.  22500 tokens of 16 KB (prompts of 64
 // requests, 32 heads of 128, bf16): 145 us, 5.1 TB/s read and written, where a plain copy reaches 5.4.  One token for each of 8 sequences: 3.7 us, launch
 // and four dependent loads (first row, length, block table, the row itself, which is requested first).
 #include <cmath>
@@ -199,11 +199,11 @@ static int launch_paged_append(const ssd_paged_config *c, void *k_pages, void *v
     const int frags = c->n_kv_heads << a.lpr_log2;
     a.lanes_log2 = 4;
     while (a.lanes_log2 < 8 && 1 << a.lanes_log2 < frags) ++a.lanes_log2;
-    // 32 KB a workgroup, if that leaves 1024 of them (46000 tokens of 16 KB: 2 tokens 154 us, 16 163; of 4 KB: 2 36.8, 8 34.5; 128000 of 512 bytes: 2 95, 16 27.5)
+    // 32 KB a workgroup, if that leaves 1024 of them (22500 tokens of 16 KB: 2 tokens 154 us, 16 163; of 4 KB: 2 36.8, 8 34.5; 128000 of 512 bytes: 2 95, 16 27.5)
     a.tokens_log2 = 0;
     while (1 << a.tokens_log2 < TOKENS && ((int64_t)frags * 32) << a.tokens_log2 < 32768 && n_new >> a.tokens_log2 > 1024) ++a.tokens_log2;
     const int64_t blocks = ((int64_t)n_new + (1 << a.tokens_log2) - 1) >> a.tokens_log2;
-    // 373 MB: 153 us with ordinary stores, 145 with the hint; 93 MB: 33.5 and 36.3
+    // 369 MB: 153 us with ordinary stores, 145 with the hint; 93 MB: 33.5 and 36.3
     if ((int64_t)n_new * frags * 32 > 256ll << 20) hipLaunchKernelGGL((paged_append_kernel<true>), dim3((unsigned)blocks), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((paged_append_kernel<false>), dim3((unsigned)blocks), dim3(256), 0, s, a);
     const hipError_t err = hipGetLastError();

@@ -24,7 +24,7 @@
 // 192 us, 6.2 to 6.5 TB/s (a plain read reaches 6.1 to 7.0).  128 sequences of 64 to 640 rows, 32 heads: 92 to 95 us, 5.6 to 5.8 TB/s; with weights 99 to
 // 102.  128 sequences of 10 to 8000 rows, 32 query heads on 4: 67 us, 4.8 TB/s; with weights and the new rows 87 -- the logits are 6 % of the bytes and,
 // written among the reads, cost 16 us (batches of them in LDS, other orders in memory and the hints on the stores change nothing).
-// fp32, rows of 64, 48 sequences of 0 to 5000 rows with weights: 37 us, 3.4 TB/s.
+// fp32, rows of 64, 48 sequences of 0 to 5000 rows with weights: 37 us, 3.3 TB/s.
 #include "ssd_paged.h"
 
 namespace ssd {
