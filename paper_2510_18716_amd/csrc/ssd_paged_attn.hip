@@ -164,13 +164,15 @@ template <int D> struct Tile<bf16_t, D> {
             for (int i = 0; i < 4; ++i) z[4 * t + i] = c[i];
         }
     }
-    // o[j] += column d = NV m + j of V, times p.  The probabilities go in as a bf16 and what it leaves out as another: 16 bits of each, as
-    // good as fp32 for the sum, at eight products more that the matrix cores have time for.
+    // o[j] += column d = NV m + j of V, times p.  The probabilities go in as a bf16 and what it leaves out as another: 15 bits of each or more,
+    // for the sum as good as fp32, at eight products more that the matrix cores have time for.  Both terms have to be above zero where p is, or an infinite
+    // element of V would give 0 * inf or inf - inf: so the first is rounded from a 256th less than p, and leaves out 2^-15 to 2^-7 of it.  That holds
+    // for p down to 2^-100; the second has to be a normal number.
     __device__ __forceinline__ void accumulate(const float (&p)[8], f32x4 (&o)[NV]) const {
         bf16x8 hi, lo;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            hi[i] = (__bf16)p[i];
+            hi[i] = (__bf16)(p[i] * (1.f - 0x1p-8f));
             lo[i] = (__bf16)(p[i] - (float)hi[i]);
         }
 #pragma unroll
