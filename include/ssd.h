@@ -507,8 +507,8 @@ int ssd_paged_decode_step(const ssd_paged_config *cfg, const void *q, const void
  *   seq_len_out  : dev int32 [n_seqs], n' per sequence; may be NULL, must not be seq_len, seq_pos or budget
  *   max_len, workspace : as ssd_paged_decode_attn (ssd_paged_evict_workspace_bytes)
  * The rows of K and V move in place; slots n' and above keep their contents.  Sequences that share
- * a page must not be evicted from.  Rows of entries that name no page count like others and are not moved;
- * their weight is taken as NaN, their position as 0.
+ * a page must not be evicted from.  Slots of entries that name no page hold no row and take none:
+ * the slots below n' that have a page get the best of the rows that exist.
  */
 size_t ssd_paged_evict_workspace_bytes(const ssd_paged_config *cfg, int max_len);
 int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, const int32_t *block_table,

@@ -69,12 +69,16 @@ def evict_order(pos, weight, total, n_sink, recent):
     return sorted(range(len(pos)), key=key)
 
 
-def evict_moves(pos, weight, total, budget, n_sink, recent):
-    """n' of one unit and the moves (slot that became free, slot its new row comes from)."""
+def evict_moves(pos, weight, total, budget, n_sink, recent, there=None):
+    """n' of one unit and the moves (slot that became free, slot its new row comes from).  there: which slots have a page, None: all; the others hold no
+    row and take none."""
     n = len(pos)
     stay = min(n, max(0, budget))
-    kept = set(evict_order(pos, weight, total, n_sink, recent)[:stay])
-    free = [j for j in range(stay) if j not in kept]
+    held = [j for j in range(n) if there is None or there[j]]
+    places = [j for j in held if j < stay]
+    order = evict_order([pos[j] for j in held], [weight[j] for j in held], total, n_sink, recent)
+    kept = set(held[i] for i in order[:len(places)])
+    free = [j for j in places if j not in kept]
     source = sorted(j for j in kept if j >= stay)
     assert len(free) == len(source)
     return stay, list(zip(free, source))

@@ -6,6 +6,7 @@
 // are read once.  Up to 256 rows that is one wave, which descends bit by bit (a ballot counts); above, ten bits a step by a histogram in LDS,
 // beginning at the first bit in which the keys differ.  Every thread ranks its free slots below n' and its kept rows above by one scan over
 // the workgroup.  A longer unit is cut into slices (the section "long units").
+// Slots whose block has no page hold no row and can take none: they are left out of the competition, and so are their places below n'.
 // Movement.  A kept row above n' goes to the free slot of its own rank, in 16-byte fragments: by the unit's workgroup where units are many,
 // by a launch with more workgroups per unit otherwise.
 //
@@ -41,7 +42,11 @@ static __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 static __device__ __forceinline__ uint32_t pos_key(int pos) { return ~((uint32_t)pos ^ 0x80000000u); }
 
-struct Four { float w[4]; int pos[4]; };
+struct Four {
+    float w[4];
+    int pos[4];
+    uint32_t there;                                                // bits: rows whose block has a page
+};
 
 // Weights and positions of rows j .. j + 3 (those below n).
 static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b, int kv, int j, int n) {
@@ -57,14 +62,16 @@ static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b
         const i4 p = *reinterpret_cast<const i4 *>(a.pos_in + i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            r.w[e] = page < 0 ? __uint_as_float(0x7fc00000u) : w[e];
-            r.pos[e] = page < 0 ? 0 : p[e];
+            r.w[e] = w[e];
+            r.pos[e] = p[e];
         }
+        r.there = page < 0 ? 0u : 15u;
         return r;
     }
+    r.there = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        r.w[e] = __uint_as_float(0x7fc00000u);
+        r.w[e] = 0.f;
         r.pos[e] = 0;
         if (j + e < n) {
             split_slot(a.g, j + e, block, place);
@@ -73,6 +80,7 @@ static __device__ __forceinline__ Four table_rows(const PagedEvictArgs &a, int b
                 const int64_t i = table_index(a.g, page, kv, place);
                 r.w[e] = a.weight_in[i];
                 r.pos[e] = a.pos_in[i];
+                r.there |= 1u << e;
             }
         }
     }
@@ -377,7 +385,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
         return;
     }
     const int j0 = tid * KEYS;
-    uint32_t wk[KEYS], pk[KEYS], safe = 0, in = 0;                 // keys; bits: protected, below n
+    uint32_t wk[KEYS], pk[KEYS], safe = 0, in = 0;                 // keys; bits: protected, below n and with a page
 #pragma unroll
     for (int k = 0; k < KEYS; k += 4) {
         if (j0 + k < n) {
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
                 wk[k + e] = weight_key(r.w[e]);
                 pk[k + e] = pos_key(r.pos[e]);
                 safe |= is_safe(a, total, r.pos[e]) ? 1u << (k + e) : 0u;
-                in |= j0 + k + e < n ? 1u << (k + e) : 0u;
+                in |= j0 + k + e < n && (r.there >> e & 1) ? 1u << (k + e) : 0u;
             }
         } else {
 #pragma unroll
@@ -404,21 +412,38 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
         for (int i = tid; i < 2 * BINS; i += THREADS) (&lds.hist[0][0])[i] = 0;
     }
 
-    // protected rows, if they leave places for others; else they alone compete
-    uint32_t safe_rows = wave_sum((uint32_t)__popc(safe));
+    // protected rows and slots without a page, at most 16384 of either
+    const int mine = n - j0 < 0 ? 0 : n - j0 < KEYS ? n - j0 : KEYS, below = stay - j0 < 0 ? 0 : stay - j0 < KEYS ? stay - j0 : KEYS;
+    const uint32_t low = (1u << below) - 1;                        // the thread's slots below n'
+    uint32_t counts = wave_sum((uint32_t)__popc(safe) | (uint32_t)(mine - __popc(in)) << 16);
     if (NW > 1) {
-        if (lane == 0) lds.red[0][wave] = safe_rows;
+        if (lane == 0) lds.red[0][wave] = counts;
         __syncthreads();
-        safe_rows = 0;
+        counts = 0;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) safe_rows += lds.red[0][i];
+        for (int i = 0; i < NW; ++i) counts += lds.red[0][i];
     }
-    const bool among_safe = (int)safe_rows >= stay;
-    const int left = among_safe ? stay : stay - (int)safe_rows;
+    const int safe_rows = (int)(counts & 0xffff), rows = n - (int)(counts >> 16);
+    int places = stay;                                             // slots below n' that can hold a row
+    if (rows < n) {
+        uint32_t c = wave_sum((uint32_t)__popc(in & low));
+        if (NW > 1) {
+            if (lane == 0) lds.red[1][wave] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) c += lds.red[1][i];
+            __syncthreads();                                       // the line is written again
+        }
+        places = (int)c;
+    }
+    // protected rows, if they leave places for others; else they alone compete
+    const bool among_safe = safe_rows >= places;
+    const int left = among_safe ? places : places - safe_rows;
     const uint32_t compete = among_safe ? safe : in & ~safe;
     uint32_t kept = among_safe ? 0 : safe, tie = 0;
     Last last = {0, 0, 0};
-    const int go = (among_safe ? (int)safe_rows : n - (int)safe_rows) - left;     // of those that compete
+    const int go = (among_safe ? safe_rows : rows - safe_rows) - left;     // of those that compete
     if (left > 0 && go <= few(THREADS)) {
         kept |= compete & ~take_least<THREADS, KEYS>(wk, pk, compete, go, least, owner);
     } else if (left > 0) {
@@ -430,7 +455,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
         sp.any_p = wave_or(sp.any_p);
         sp.not_all_p = wave_or(sp.not_all_p);
         if constexpr (NW == 1) {
-            last = descend_wave(sp, left, among_safe ? (int)safe_rows : n - (int)safe_rows, [&](auto f) {
+            last = descend_wave(sp, left, among_safe ? safe_rows : rows - safe_rows, [&](auto f) {
                 int c = 0;
 #pragma unroll
                 for (int k = 0; k < KEYS; ++k) c += (int)__popcll(__ballot((compete >> k & 1) && f(wk[k], pk[k])));
@@ -484,8 +509,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     }
 
     // where slots become free, which rows move
-    const int below = stay - j0 < 0 ? 0 : stay - j0 < KEYS ? stay - j0 : KEYS;
-    const uint32_t low = (1u << below) - 1, free_bits = in & low & ~kept, move_bits = kept & ~low;
+    const uint32_t free_bits = in & low & ~kept, move_bits = kept & ~low;
     const uint32_t c = (uint32_t)__popc(free_bits) | (uint32_t)__popc(move_bits) << 16, up = wave_scan(c);
     uint32_t before = up - c, all = (uint32_t)__builtin_amdgcn_readlane((int)up, 63);
     if (NW > 1) {
@@ -526,7 +550,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
 // ---- long units ------------------------------------------------------------------------------------------------------------
 //
 // The rows below n' and those above are cut into slices of equally many rows, a workgroup each; a unit's own workgroup works in between.
-//   1 slices: how many rows have which upper 12 bits of their weight, protected ones and others apart
+//   1 slices: how many rows have which upper 12 bits of their weight, protected ones and others apart; slots without a page
 //   2 unit:   the bin in which the last place falls, and how many rows of a slice are above it and in it
 //   3 slices: the rows in the bin, in slot order, into one list (the memory of the moves, which come later), with their keys
 //   4 unit:   the descent among those; where each slice's free slots and moving rows begin in the lists
@@ -541,6 +565,7 @@ struct SliceInfo {
     int32_t kept, in_bin, first;                                   // rows above the bin, in it, and where the latter begin in the list
     int32_t at;                                                    // where its free slots, or its moving rows, begin in the lists
     int32_t safe;                                                  // protected rows
+    int32_t gone;                                                  // slots without a page
 };
 struct UnitInfo {
     int32_t among_safe, bin, left, candidates;
@@ -577,7 +602,7 @@ struct Slices {
 __global__ __launch_bounds__(ST) void slice_count_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
     __shared__ uint32_t hist[2][TOP_BINS];
-    __shared__ uint32_t red[ST / 64];
+    __shared__ uint32_t red[2][ST / 64];
     const int kv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
     const Slices sl(n > 0 ? n : 1, stay, s.slices);
@@ -586,24 +611,38 @@ __global__ __launch_bounds__(ST) void slice_count_kernel(SliceArgs s) {
     for (int i = tid; i < 2 * TOP_BINS / 4; i += ST) reinterpret_cast<uint4 *>(&hist[0][0])[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     const int end = sl.end((int)blockIdx.x, n, stay);
-    uint32_t safe = 0;
+    uint32_t safe = 0, gone = 0;
     for (int j = sl.begin((int)blockIdx.x, stay) + 4 * tid; j < end; j += 4 * ST) {
         const Four r = table_rows(a, b, kv, j, end);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (j + e < end) {
+                if (!(r.there >> e & 1)) {
+                    ++gone;
+                    continue;
+                }
                 const bool sf = is_safe(a, total, r.pos[e]);
                 safe += sf;
                 atomicAdd(&hist[sf][weight_key(r.w[e]) >> (32 - TOP)], 1u);
             }
     }
     safe = wave_sum(safe);
-    if ((tid & 63) == 0) red[tid >> 6] = safe;
+    gone = wave_sum(gone);
+    if ((tid & 63) == 0) {
+        red[0][tid >> 6] = safe;
+        red[1][tid >> 6] = gone;
+    }
     __syncthreads();
-    safe = 0;
+    safe = gone = 0;
 #pragma unroll
-    for (int i = 0; i < ST / 64; ++i) safe += red[i];
-    if (tid == 0) s.info[unit].slice[blockIdx.x].safe = (int32_t)safe;
+    for (int i = 0; i < ST / 64; ++i) {
+        safe += red[0][i];
+        gone += red[1][i];
+    }
+    if (tid == 0) {
+        s.info[unit].slice[blockIdx.x].safe = (int32_t)safe;
+        s.info[unit].slice[blockIdx.x].gone = (int32_t)gone;
+    }
     uint4 *out = reinterpret_cast<uint4 *>(s.hist + (unit * (s.slices + 2) + blockIdx.x) * 2 * TOP_BINS);
     // the protected rows' half only where there are such rows
     for (int i = tid; i < (safe ? 2 : 1) * TOP_BINS / 4; i += ST) out[i] = *reinterpret_cast<const uint4 *>(&hist[0][0] + 4 * i);
@@ -612,7 +651,7 @@ __global__ __launch_bounds__(ST) void slice_count_kernel(SliceArgs s) {
 __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     const PagedEvictArgs &a = s.e;
     __shared__ uint32_t red[16];
-    __shared__ int found[4], safe_of[SLICES + 2];
+    __shared__ int found[5], safe_of[SLICES + 2];
     __shared__ SliceInfo info[SLICES + 2];
     const int kv = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = clamp_len(a.g, b), stay = stay_of(a, b, n);
@@ -622,11 +661,16 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
     const int64_t unit = (int64_t)b * a.g.n_kv + kv;
     const uint32_t *hist = s.hist + unit * (s.slices + 2) * 2 * TOP_BINS;
     UnitInfo *u = s.info + unit;
+    uint32_t gone = 0;                                             // of slice tid
     if (tid < 64) {
         const uint32_t c = tid < sl.count ? (uint32_t)u->slice[tid].safe : 0;
+        gone = tid < sl.count ? (uint32_t)u->slice[tid].gone : 0;
         safe_of[tid] = (int)c;
-        const uint32_t all = wave_sum(c);
-        if (tid == 0) found[2] = (int)all;
+        const uint32_t all = wave_sum(c), low = wave_sum(tid < sl.low ? gone : 0u);
+        if (tid == 0) {
+            found[2] = (int)all;
+            found[4] = stay - (int)low;
+        }
     }
     if (tid == 0) {
         found[0] = TOP_BINS;                                       // no place to compete for: nothing is in or above this bin
@@ -634,8 +678,8 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
         found[3] = 0;
     }
     __syncthreads();
-    const int safe_rows = found[2], k = safe_rows >= stay;         // k = 1: protected rows alone compete
-    const uint32_t left = (uint32_t)(k ? stay : stay - safe_rows);
+    const int safe_rows = found[2], places = found[4], k = safe_rows >= places;       // k = 1: protected rows alone compete
+    const uint32_t left = (uint32_t)(k ? places : places - safe_rows);
     // a thread has PER bins, counted from the top
     constexpr int PER = TOP_BINS / 1024;
     static_assert(PER == 4, "bins are read four at a time");
@@ -695,12 +739,12 @@ __global__ __launch_bounds__(1024) void slice_bin_kernel(SliceArgs s) {
                 over += (x > at ? v.x : 0) + (x + 1 > at ? v.y : 0) + (x + 2 > at ? v.z : 0) + (x + 3 > at ? v.w : 0);
             }
         over = wave_sum(over);
-        if (lane == 0) info[i] = SliceInfo{(int32_t)over + (k ? 0 : safe_of[i]), any && at < TOP_BINS ? (int32_t)row[at] : 0, 0, 0, 0};
+        if (lane == 0) info[i] = SliceInfo{(int32_t)over + (k ? 0 : safe_of[i]), any && at < TOP_BINS ? (int32_t)row[at] : 0, 0, 0, 0, 0};
     }
     __syncthreads();
     if (tid < 64) {
         const uint32_t c = tid < sl.count ? (uint32_t)info[tid].in_bin : 0, up = wave_scan(c);
-        if (tid < sl.count) u->slice[tid] = SliceInfo{info[tid].kept, info[tid].in_bin, (int32_t)(up - c), 0, safe_of[tid]};
+        if (tid < sl.count) u->slice[tid] = SliceInfo{info[tid].kept, info[tid].in_bin, (int32_t)(up - c), 0, safe_of[tid], (int32_t)gone};
         if (tid == 63) {
             u->among_safe = k;
             u->bin = at;
@@ -744,7 +788,7 @@ __global__ __launch_bounds__(ST) void slice_gather_kernel(SliceArgs s) {
         uint32_t bits = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            bits |= j + e < end && is_safe(a, total, r.pos[e]) == among_safe && weight_key(r.w[e]) >> (32 - TOP) == bin ? 1u << e : 0u;
+            bits |= j + e < end && (r.there >> e & 1) && is_safe(a, total, r.pos[e]) == among_safe && weight_key(r.w[e]) >> (32 - TOP) == bin ? 1u << e : 0u;
         const uint32_t c = (uint32_t)__popc(bits), up = wave_scan(c);
         if (lane == 63) red[parity][wave] = up;
         __syncthreads();
@@ -796,10 +840,10 @@ __global__ __launch_bounds__(1024) void slice_pick_kernel(SliceArgs s) {
         }
         int block, place;
         split_slot(a.g, list[1 + i], block, place);
-        const int page = page_of(a.g, b, block);
+        const int page = page_of(a.g, b, block);                   // a candidate's block has one
         const int64_t at = table_index(a.g, page < 0 ? 0 : page, kv, place);
-        w = page < 0 ? 0 : weight_key(a.weight_in[at]);
-        p = pos_key(page < 0 ? 0 : a.pos_in[at]);
+        w = weight_key(a.weight_in[at]);
+        p = pos_key(a.pos_in[at]);
     };
     const uint32_t *keys = s.keys(unit);
 #pragma unroll
@@ -874,7 +918,7 @@ __global__ __launch_bounds__(1024) void slice_pick_kernel(SliceArgs s) {
         }
     __syncthreads();
     if (tid < 64) {
-        const int begin = sl.begin(tid, stay), rows = tid < sl.count ? sl.end(tid, n, stay) - begin : 0;
+        const int begin = sl.begin(tid, stay), rows = tid < sl.count ? sl.end(tid, n, stay) - begin - u->slice[tid].gone : 0;
         const int k = tid < sl.count ? u->slice[tid].kept + kept[tid] : 0;
         const uint32_t free_here = tid < sl.low ? (uint32_t)(rows - k) : 0, move_here = tid >= sl.low ? (uint32_t)k : 0;
         const uint32_t f = wave_scan(free_here), m = wave_scan(move_here);
@@ -922,7 +966,7 @@ __global__ __launch_bounds__(ST) void slice_list_kernel(SliceArgs s) {
                 const int st = standing(last, w, pos_key(r.pos[e]));
                 kept = st == 2 || (st == 1 && j + e <= last_slot);
             }
-            bits |= j + e < end && kept != low ? 1u << e : 0u;
+            bits |= j + e < end && (r.there >> e & 1) && kept != low ? 1u << e : 0u;
         }
         const uint32_t c = (uint32_t)__popc(bits), up = wave_scan(c);
         if (lane == 63) red[parity][wave] = up;

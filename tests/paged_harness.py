@@ -122,3 +122,18 @@ def check_attend(bt, got, weights=True, max_len=0, lens=None, scale=None, table=
                 touched[page, :, place] = True
     if w is not None:
         assert np.all(w[~touched] == -3.0)            # nothing else was written
+
+
+def evict_sources(pos, weight, total, budget, n_sink, recent, there):
+    """oracle.paged.evict_moves for long units: the slot that each slot below n' has its row from."""
+    n = len(pos)
+    stay = min(n, max(0, budget))
+    held = np.nonzero(there)[0]
+    p, w = pos[held], weight[held]
+    safe = (p < n_sink) | (p >= total - recent)
+    with np.errstate(invalid="ignore"):
+        key = np.where(np.isnan(w), np.inf, -w.astype(np.float64))
+    best = held[np.lexsort((held, p, key, np.isnan(w), ~safe))[:int(np.sum(held < stay))]]
+    src = np.arange(stay)
+    src[~np.isin(src, best) & there[:stay]] = np.sort(best[best >= stay])
+    return src
