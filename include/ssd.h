@@ -524,7 +524,7 @@ int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, c
  *     v among the row's tokens:          x = x > 0 ? x / repetition[i] : x * repetition[i]
  *     n = times v is among the row's tokens from n_prompt[i] on:
  *                                        x -= frequency[i] * n + (n > 0 ? presence[i] : 0)
- *     x /= temperature[i]                (as a product with the reciprocal)
+ *     x /= temperature[i]                (as a product with the reciprocal, taken in two factors where it is no normal number)
  *     mask bit 0:                        x = -infinity, whatever it was
  * A row whose mask leaves nothing is -infinity throughout.
  */

@@ -101,7 +101,9 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         for (int e = 0; e < 4 && j + e < n; ++e) one(tok[j + e], j + e);
         __syncthreads();
     }
-    const float rep = rep0 > 0.f ? rep0 : 1.f, cool = temp0 > 0.f ? 1.f / temp0 : 1.f;
+    const float rep = rep0 > 0.f ? rep0 : 1.f, temp = temp0 > 0.f ? temp0 : 1.f;
+    // the reciprocal in two factors, 1 and a normal number: one that overflows would make NaN of 0, one below the normal numbers has fewer bits
+    const float part = temp < 0x1p-126f ? 0x1p64f : temp > 0x1p126f ? 0x1p-64f : 1.f, cool = 1.f / (temp * part);
     float *o = a.out + (int64_t)i * a.out_stride;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            x[e] = x[e] * cool;
+            x[e] = x[e] * cool * part;
             x[e] = allowed[g] >> e & 1 ? x[e] : -INFINITY;
         }
         if (full) {
