@@ -140,8 +140,11 @@ def _check(rc: int, where: str) -> None:
         raise SsdError(rc, where)
 
 
+_Tensor = torch.Tensor
+
+
 def _ptr(t) -> Optional[int]:
-    if t is None or isinstance(t, int):
+    if type(t) is not _Tensor and (t is None or isinstance(t, int)):
         return t
     assert t.is_contiguous(), "tensors handed to the library must be contiguous"
     return t.data_ptr()
@@ -164,14 +167,16 @@ def _stream(stream=None) -> Optional[int]:
     return None
 
 
+_DTYPE_CODES = {torch.bfloat16: SSD_BF16, "bf16": SSD_BF16, torch.float32: SSD_F32, "f32": SSD_F32}
+
+
 def _dtype_code(dt) -> int:
     if isinstance(dt, int):
         return dt                      # passed through; the library validates it
-    if dt in (torch.bfloat16, "bf16"):
-        return SSD_BF16
-    if dt in (torch.float32, "f32"):
-        return SSD_F32
-    raise ValueError("unsupported dtype %r" % (dt,))
+    code = _DTYPE_CODES.get(dt)
+    if code is None:
+        raise ValueError("unsupported dtype %r" % (dt,))
+    return code
 
 
 def make_config(L, B, H, d, dtype, W, S, M, R, C_, softmax_scale=0.0, spatial_row_buffer=0) -> SsdConfig:
@@ -447,6 +452,21 @@ class SsdPagedConfig(C.Structure):
         ("q_stride", C.c_int64), ("new_stride", C.c_int64),
     ]
 
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        self.__dict__.pop("strides", None)
+
+    def __getattr__(self, name):
+        """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
+        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; found when it is first asked for after a field was set."""
+        if name != "strides":
+            raise AttributeError(name)
+        d, row = self.head_dim, self.row_stride or self.head_dim
+        head = self.head_stride or row * self.page_size
+        got = self.__dict__["strides"] = ((self.page_stride or head * self.n_kv_heads, head, row, 1), (self.q_stride or self.n_heads * d, d, 1),
+                                          (self.new_stride or self.n_kv_heads * d, d, 1))
+        return got
+
 
 class SsdLogitsParams(C.Structure):
     _fields_ = [
@@ -485,12 +505,88 @@ def make_paged_config(B, H, H_kv, d, dtype, page_size, n_pages, max_blocks, soft
     return cfg
 
 
-def _strided(t) -> Optional[int]:
-    """Address of a tensor whose outer strides the config gives: rows alone have to be dense."""
+def _runs(t):
+    """A tensor's dimensions as (size, stride), those of one element left out and neighbours that are one run of memory joined."""
+    runs = []
+    for size, stride in zip(t.shape, t.stride()):
+        if size == 1:
+            continue
+        if runs and runs[-1][1] == size * stride:
+            runs[-1] = (runs[-1][0] * size, stride)
+        else:
+            runs.append((size, stride))
+    if not runs or runs[-1][1] != 1:
+        runs.append((1, 1))
+    return runs
+
+
+def _check_rows(t, what: str, n: int, stride: int, width: int) -> None:
+    """n rows of `width` elements, `stride` apart: the tensor's own rows, or memory without gaps that reaches as far."""
+    runs = _runs(t)
+    fits = runs[-1][1] == 1
+    if fits and n > 1 and len(runs) == 1:
+        fits = (n - 1) * stride + width <= runs[0][0]
+        if fits and t.dim() > 1 and t.shape[0] >= n and t.stride(0) >= width:          # rows of its own
+            fits = t.stride(0) == stride
+    elif fits and n > 0:
+        fits = runs[-1][0] >= width and (n == 1 or any(size >= n and apart == stride for size, apart in runs[:-1]))
+    if n > 0 and not fits:
+        raise ValueError("%s of shape %s, strides %s: %d rows of %d elements that lie %d apart are expected"
+                         % (what, tuple(t.shape), t.stride(), n, width, stride))
+
+
+def _check_pool(t, what: str, cfg) -> None:
+    """[n_pages, n_kv_heads, page_size, d] with the config's strides (or the same with page_size before n_kv_heads, as it lies in memory then), or
+    memory without gaps that reaches as far."""
+    want, sizes = cfg.strides[0], (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+    named = False
+    if t.dim() == 4:
+        for order in ((0, 1, 2, 3), (0, 2, 1, 3)):
+            if tuple(t.shape[i] for i in order[1:]) == sizes[1:]:
+                named = True
+                if all(size == 1 or t.stride(i) == stride for i, size, stride in zip(order, sizes, want)):
+                    return
+    fits = not named
+    if fits and t.is_contiguous():
+        fits = sum((size - 1) * stride for size, stride in zip(sizes, want)) < t.numel()
+    elif fits:
+        runs = [(size, stride) for size, stride in zip(t.shape, t.stride()) if size != 1]
+        fits = bool(runs) and runs[-1][1] == 1 and all(stride in want for _, stride in runs[:-1])
+    if not fits:
+        raise ValueError("%s of shape %s, strides %s: the config says [%d, %d, %d, %d] with strides %s" % ((what, tuple(t.shape), t.stride()) + sizes + (want,)))
+
+
+def _pool(t, what: str, cfg, want) -> Optional[int]:
+    """Address of a pool whose strides the config gives: `want`."""
+    if type(t) is _Tensor and t.stride() == want:
+        return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
-    assert t.is_contiguous() or t.stride(-1) == 1, "rows handed to the library must be dense"
+    _check_pool(t, what, cfg)
     return t.data_ptr()
+
+
+def _rows(t, what: str, n: int, heads: int, want) -> Optional[int]:
+    """Address of n rows of `heads` heads; want: the strides of [n, heads, d]."""
+    if type(t) is _Tensor and t.stride() == want:
+        return t.data_ptr()
+    if t is None or isinstance(t, int):
+        return t
+    if t.stride() != (want[0], 1) or t.shape[1] < heads * want[1]:
+        _check_rows(t, what, n, want[0], heads * want[1])
+    return t.data_ptr()
+
+
+def _vocabulary_stride(t, what: str, n: int, V: int, stride: int) -> int:
+    """How far n rows of V elements lie apart: as the caller says, or where that is 0 as the tensor does."""
+    if stride == 0:
+        runs = _runs(t)
+        if len(runs) == 1:                                         # memory without gaps: its own rows, if there are as many of them
+            stride = t.shape[-1] if t.dim() > 1 and t.shape[-1] >= V and t.numel() >= n * t.shape[-1] else V
+        else:
+            stride = next((apart for size, apart in reversed(runs[:-1]) if size >= n), V)
+    _check_rows(t, what, n, stride, V)
+    return max(stride, V)
 
 
 def _size(t) -> int:
@@ -501,9 +597,11 @@ def ssd_paged_append(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len
                      new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
     """n_new: tokens in k_new; None: its first dimension."""
     n = int(k_new.shape[0] if n_new is None else n_new)
-    _check(lib.ssd_paged_append(C.byref(cfg), _strided(k_pages), _strided(v_pages), _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len),
-                                _ptr(seq_pos), _strided(k_new), _strided(v_new), _ptr(new_start), n, _ptr(weight_new), _stream(stream)),
-           "ssd_paged_append")
+    pool, _, new = cfg.strides
+    heads = cfg.n_kv_heads
+    _check(lib.ssd_paged_append(C.byref(cfg), _pool(k_pages, "k_pages", cfg, pool), _pool(v_pages, "v_pages", cfg, pool), _ptr(pos), _ptr(weight),
+                                _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _rows(k_new, "k_new", n, heads, new), _rows(v_new, "v_new", n, heads, new),
+                                _ptr(new_start), n, _ptr(weight_new), _stream(stream)), "ssd_paged_append")
 
 
 def ssd_paged_workspace_bytes(cfg: SsdPagedConfig, max_len: int = 0, with_weights: bool = False) -> int:
@@ -512,14 +610,17 @@ def ssd_paged_workspace_bytes(cfg: SsdPagedConfig, max_len: int = 0, with_weight
 
 def ssd_paged_decode_attn(cfg: SsdPagedConfig, q, k_pages, v_pages, block_table, seq_len, out, lse=None, weight_in=None, weight_out=None,
                           max_len: int = 0, workspace=None, stream=None) -> None:
-    _check(lib.ssd_paged_decode_attn(C.byref(cfg), _strided(q), _strided(k_pages), _strided(v_pages), _ptr(weight_in), _ptr(weight_out),
-                                     _ptr(block_table), _ptr(seq_len), _ptr(out), _ptr(lse), int(max_len), _ptr(workspace), _size(workspace),
-                                     _stream(stream)), "ssd_paged_decode_attn")
+    pool, queries, _ = cfg.strides
+    _check(lib.ssd_paged_decode_attn(C.byref(cfg), _rows(q, "q", cfg.n_seqs, cfg.n_heads, queries), _pool(k_pages, "k_pages", cfg, pool),
+                                     _pool(v_pages, "v_pages", cfg, pool), _ptr(weight_in), _ptr(weight_out), _ptr(block_table), _ptr(seq_len),
+                                     _ptr(out), _ptr(lse), int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_decode_attn")
 
 
 def ssd_paged_decode_step(cfg: SsdPagedConfig, q, k_new, v_new, k_pages, v_pages, block_table, seq_len, out, pos=None, seq_pos=None, lse=None,
                           weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    _check(lib.ssd_paged_decode_step(C.byref(cfg), _strided(q), _strided(k_new), _strided(v_new), _strided(k_pages), _strided(v_pages),
+    (pool, queries, new), B, heads = cfg.strides, cfg.n_seqs, cfg.n_kv_heads
+    _check(lib.ssd_paged_decode_step(C.byref(cfg), _rows(q, "q", B, cfg.n_heads, queries), _rows(k_new, "k_new", B, heads, new),
+                                     _rows(v_new, "v_new", B, heads, new), _pool(k_pages, "k_pages", cfg, pool), _pool(v_pages, "v_pages", cfg, pool),
                                      _ptr(pos), _ptr(weight_in), _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(out),
                                      _ptr(lse), int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_decode_step")
 
@@ -530,8 +631,9 @@ def ssd_paged_evict_workspace_bytes(cfg: SsdPagedConfig, max_len: int = 0) -> in
 
 def ssd_paged_evict(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len, budget, pos_in, pos_out, weight_in, weight_out, seq_len_out=None,
                     n_sink: int = 0, recent: int = 0, seq_pos=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    _check(lib.ssd_paged_evict(C.byref(cfg), _strided(k_pages), _strided(v_pages), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(budget),
-                               int(n_sink), int(recent), _ptr(pos_in), _ptr(pos_out), _ptr(weight_in), _ptr(weight_out), _ptr(seq_len_out),
+    pool = cfg.strides[0]
+    _check(lib.ssd_paged_evict(C.byref(cfg), _pool(k_pages, "k_pages", cfg, pool), _pool(v_pages, "v_pages", cfg, pool), _ptr(block_table), _ptr(seq_len),
+                               _ptr(seq_pos), _ptr(budget), int(n_sink), int(recent), _ptr(pos_in), _ptr(pos_out), _ptr(weight_in), _ptr(weight_out), _ptr(seq_len_out),
                                int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_evict")
 
 
@@ -540,7 +642,8 @@ def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[
                        mask_shared: bool = False, logits_stride: int = 0, out_stride: int = 0, token_stride: Optional[int] = None,
                        stream=None) -> None:
     """gamma: guidance strength, None: no guidance.  bias [n_rows, V] and mask [n_rows, ceil(V / 32)], or one row of either for all
-    (bias_shared, mask_shared).  token_stride: places per row of tokens, None: its last dimension."""
+    (bias_shared, mask_shared).  token_stride: places per row of tokens, None: its last dimension.  logits_stride, out_stride 0: the tensor's own (a view of
+    a padded vocabulary may be handed over as it is)."""
     p = SsdLogitsParams()
     p.tokens, p.n_tokens, p.n_prompt = _ptr(tokens), _ptr(n_tokens), _ptr(n_prompt)
     p.repetition, p.presence, p.frequency, p.temperature = _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(temperature)
@@ -548,5 +651,14 @@ def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[
     p.token_stride = int((0 if tokens is None else tokens.shape[-1]) if token_stride is None else token_stride)
     p.bias_stride = 0 if bias_shared else int(V)
     p.mask_stride = 0 if mask_shared else -(-int(V) // 32)
-    _check(lib.ssd_logits_process(_strided(logits), int(n_rows), int(V), _dtype_code(dtype), int(logits_stride), int(gamma is not None),
-                                  float(gamma or 0.0), C.byref(p), _strided(out), int(out_stride), _stream(stream)), "ssd_logits_process")
+    if logits is not None and not isinstance(logits, int):
+        n = n_rows if gamma is None else 2 * n_rows
+        if logits_stride or logits.numel() != n * V or not logits.is_contiguous():
+            logits_stride = _vocabulary_stride(logits, "logits", n, V, logits_stride)
+        logits = logits.data_ptr()
+    if out is not None and not isinstance(out, int):
+        if out_stride or out.numel() != n_rows * V or not out.is_contiguous():
+            out_stride = _vocabulary_stride(out, "out", n_rows, V, out_stride)
+        out = out.data_ptr()
+    _check(lib.ssd_logits_process(logits, int(n_rows), int(V), _dtype_code(dtype), int(logits_stride), int(gamma is not None),
+                                  float(gamma or 0.0), C.byref(p), out, int(out_stride), _stream(stream)), "ssd_logits_process")
