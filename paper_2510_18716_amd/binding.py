@@ -589,6 +589,17 @@ def _vocabulary_stride(t, what: str, n: int, V: int, stride: int) -> int:
     return max(stride, V)
 
 
+def _per_row(t, what: str, n: int, width: int, shared: bool) -> int:
+    """The stride of an array (without gaps) with a row of `width` elements for each of n rows, or one for all: 0."""
+    if t is not None and not isinstance(t, int):
+        rows = 1 if shared else n
+        own = width if t.dim() < 2 or t.numel() == rows * width else t.shape[-1]
+        if own < width or t.numel() < rows * own:
+            raise ValueError("%s of shape %s: %d rows of %d elements are expected" % (what, tuple(t.shape), rows, width))
+        width = own
+    return 0 if shared else width
+
+
 def _size(t) -> int:
     return 0 if t is None else t.nbytes
 
@@ -649,8 +660,8 @@ def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[
     p.repetition, p.presence, p.frequency, p.temperature = _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(temperature)
     p.bias, p.mask = _ptr(bias), _ptr(mask)
     p.token_stride = int((0 if tokens is None else tokens.shape[-1]) if token_stride is None else token_stride)
-    p.bias_stride = 0 if bias_shared else int(V)
-    p.mask_stride = 0 if mask_shared else -(-int(V) // 32)
+    p.bias_stride = _per_row(bias, "bias", n_rows, int(V), bias_shared)
+    p.mask_stride = _per_row(mask, "mask", n_rows, -(-int(V) // 32), mask_shared)
     if logits is not None and not isinstance(logits, int):
         n = n_rows if gamma is None else 2 * n_rows
         if logits_stride or logits.numel() != n * V or not logits.is_contiguous():

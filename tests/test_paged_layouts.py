@@ -208,3 +208,30 @@ def test_logits_that_do_not_lie_as_said_are_refused(calls):
         with pytest.raises(ValueError, match="out of shape"):
             _logits(out, n, V, x, **kw)
     assert not calls
+
+
+def test_bias_and_mask_have_a_row_for_each_or_are_shared(calls):
+    n, V = 6, 100
+    x, out, words = torch.zeros(n, V), torch.zeros(n, V), -(-V // 32)
+
+    def strides():
+        p = calls[-1][1][7]._obj
+        return p.bias_stride, p.mask_stride
+    for bias, mask, kw, want in ((torch.zeros(n, V), torch.zeros(n, words, dtype=torch.int32), {}, (V, words)),
+                                 (torch.zeros(n, V // 4, 4), torch.zeros(2, n // 2, words, dtype=torch.int32), {}, (V, words)),
+                                 (torch.zeros(n * V), torch.zeros(n + 2, words, dtype=torch.int32), {}, (V, words)),
+                                 (torch.zeros(V), torch.zeros(1, words, dtype=torch.int32), dict(bias_shared=True, mask_shared=True), (0, 0)),
+                                 (torch.zeros(n, V), torch.zeros(words, dtype=torch.int32), dict(bias_shared=True, mask_shared=True), (0, 0)),
+                                 (torch.zeros(n, V + 28), torch.zeros(n, words + 4, dtype=torch.int32), {}, (V + 28, words + 4))):       # a padded vocabulary
+        _logits(x, n, V, out, bias=bias, mask=mask, **kw)
+        assert strides() == want
+    made = len(calls)
+    for bias in (torch.zeros(V), torch.zeros(1, V), torch.zeros(n - 1, V), torch.zeros(n, V - 1)):
+        with pytest.raises(ValueError, match="bias of shape"):
+            _logits(x, n, V, out, bias=bias)
+    with pytest.raises(ValueError, match="bias of shape"):
+        _logits(x, n, V, out, bias=torch.zeros(V - 1), bias_shared=True)
+    for mask in (torch.zeros(words, dtype=torch.int32), torch.zeros(n, words - 1, dtype=torch.int32), torch.zeros(n - 1, words, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="mask of shape"):
+            _logits(x, n, V, out, mask=mask)
+    assert len(calls) == made
