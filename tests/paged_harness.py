@@ -124,6 +124,47 @@ def check_attend(bt, got, weights=True, max_len=0, lens=None, scale=None, table=
         assert np.all(w[~touched] == -3.0)            # nothing else was written
 
 
+def outputs_of(bt, b, n=None, table=None):
+    """(out, sum p |v|) of sequence b in 64 bits."""
+    table = bt.table if table is None else table
+    out, _, _, size = paged.paged_attend(bt.q[b].float().numpy(), bt.k.float().numpy(), bt.v.float().numpy(), table[b], bt.lens[b] if n is None else n,
+                                         bt.d ** -0.5)
+    return out, size
+
+
+def fine_tolerance(dtype, ref, size):
+    """What an output may be off by if the probabilities keep 16 bits.  Logits are off by 2e-5 (check_attend) and so relative are the probabilities; their two
+    bf16 terms leave out at most 2^-15 and nothing of the largest's; exponentials, sums and the division are fp32's: 5.1e-5 of sum p |v| together.  A bf16 output is rounded once more, by at most
+    2^-8 of itself.  One row of thousands, or the second term, is more than that."""
+    return 5.1e-5 * size + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else 0.0) + 1e-30
+
+
+def check_outputs(bt, out, lens=None, table=None):
+    o = out.float().cpu().numpy()
+    for b, n in enumerate(bt.lens if lens is None else lens):
+        ref, size = outputs_of(bt, b, n, table)
+        worst = np.abs(o[b] - ref) - fine_tolerance(bt.dtype, ref, size)
+        assert worst.max() <= 0, (b, n, float(np.abs(o[b] - ref).max()), float(worst.max()))
+
+
+def cancelling(lens, H, n_kv, d, dtype, seed, device):
+    """A batch whose rows come in pairs of nearly the same key and opposite values: what is left of the output is the difference of probabilities that have
+    their first eight bits in common."""
+    bt = Batch(lens, H, n_kv, d, dtype, 16, seed=seed, device=device)
+    g = torch.Generator().manual_seed(seed)
+    bt.q.zero_()
+    bt.q[:, :, 0] = 1.0
+    for b, n in enumerate(bt.lens):
+        v = torch.randn((n_kv, d), generator=g)
+        for j in range(n):
+            at = (bt.table[b, j // 16], slice(None), j % 16)
+            bt.k[at] = 0.0
+            bt.k[at][:, 0] = torch.randint(-40, 0, (n_kv,), generator=g) * 2.0 ** -6          # exact in bf16
+            bt.v[at] = (v * (1 if j % 2 else -1)).to(bt.v.dtype)
+    bt.kd, bt.vd, bt.qd = bt.k.to(device), bt.v.to(device), bt.q.to(device)
+    return bt
+
+
 def evict_sources(pos, weight, total, budget, n_sink, recent, there):
     """oracle.paged.evict_moves for long units: the slot that each slot below n' has its row from."""
     n = len(pos)
