@@ -472,7 +472,9 @@ int ssd_paged_append(const ssd_paged_config *cfg, void *k_pages, void *v_pages, 
  * Logits that are NaN or infinite are the caller's; they reach the outputs of
  * their own sequence and heads only.  Elements of V that are infinite give what the
  * sum gives (an infinity, or NaN where its terms have both signs) as long as the row's exp(logit - largest) is
- * above 2^-100; below, they may give NaN.  What lies in a page past a sequence's end is
+ * above 2^-100; below, they may give NaN.  A sequence whose logits are all -infinity (or below -2e38) gives what one without rows
+ * gives: out = 0, lse = -infinity, weights as they were.  sum_j exp(logit - largest) |v| has to stay below fp32's
+ * largest number.  What lies in a page past a sequence's end is
  * never used, whatever bits it holds.
  */
 size_t ssd_paged_workspace_bytes(const ssd_paged_config *cfg, int max_len, int with_weights);
