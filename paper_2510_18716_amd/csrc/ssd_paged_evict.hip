@@ -998,6 +998,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
 
 struct EvictShape {
     int cap, slices;                                               // slices: 0 where a unit is one workgroup's
+    bool move_here;                                                // the unit's workgroup moves its rows, from lists in LDS
     size_t moves, hist, info;
 };
 
@@ -1012,7 +1013,10 @@ static EvictShape evict_shape(const ssd_paged_config *c, int max_len) {
         s.slices = (int)(rows < share ? rows : share);
         if (s.slices > SLICES) s.slices = SLICES;
     }
-    s.moves = round256((size_t)moves_of(s.cap, units) * 4);
+    // Rows move by the unit's workgroup, which saves a launch, where units fill the chip (one eviction from each of 64 units of 2000 rows 7.5 us here and 9.2 by a launch, 1000 32.9 and
+    // 17.0; 128 units 39 and 28, 256 42.6 and 43.4, of 8000 rows to 4000 137 and 156); with few rows, from 128 units on (one of 129 rows 6.3 and 8.2, 100 of 250 stay 16.7 and 14.0).
+    s.move_here = units >= (reach <= 256 ? 128 : 256) && !s.slices;
+    s.moves = s.move_here ? 0 : round256((size_t)moves_of(s.cap, units) * 4);
     s.hist = s.slices ? (size_t)units * (s.slices + 2) * 2 * TOP_BINS * 4 : 0;
     s.info = s.slices ? round256((size_t)units * sizeof(UnitInfo)) : 0;
     return s;
@@ -1050,7 +1054,7 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
         if (!aligned(x, 4)) return fail(SSD_ERR_INVALID_ARG, "tables must be aligned to their elements");
     const EvictShape shape = evict_shape(cfg, max_len);
     const size_t need = shape.moves + shape.hist + shape.info;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
+    if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return fail(SSD_ERR_INVALID_ARG, "workspace of %zu bytes, 256-byte aligned, needed; %zu given", need, workspace_bytes);
     PagedEvictArgs a;
     a.g = paged_geom(cfg, block_table, seq_len, seq_pos, max_len);
@@ -1071,9 +1075,7 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     const dim3 units((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs);
     const int64_t n_units = (int64_t)units.x * units.y;
     const int reach = a.g.max_len;
-    // Rows move by the unit's workgroup, which saves a launch, where units fill the chip (one eviction from each of 64 units of 2000 rows 7.5 us here and 9.2 by a launch, 1000 32.9 and
-    // 17.0; 128 units 39 and 28, 256 42.6 and 43.4, of 8000 rows to 4000 137 and 156); with few rows, from 128 units on (one of 129 rows 6.3 and 8.2, 100 of 250 stay 16.7 and 14.0).
-    const int move_here = n_units >= (reach <= 256 ? 128 : 256) && !shape.slices;
+    const int move_here = shape.move_here;
     // A wave, 256 or 1024 threads per unit: the next larger take 15.6 us instead of 11.5 (12 of 200 rows, 64 units), 18.0 and 17.0 (half of 2000 rows, 32 units; 39.5 and 42.6 with 256), 38.7 and
     // 32.0 (half of 8000); slices from 8192 rows on 38.1 and 29.2 (one of 16000 rows, 32 units; 346 and 305 for half of them, 256).
     if (shape.slices) {
