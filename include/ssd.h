@@ -414,6 +414,8 @@ int ssd_decode_step_split_rope(ssd_cache *cache, int layer_begin, int layer_end,
  *                 from which nothing is evicted needs neither.
  *   Grouped queries: query heads kv*G .. kv*G + G-1, G = n_heads / n_kv_heads,
  *   read key / value head kv.
+ *   All heads of a sequence hold the same number of rows, and an eviction has one budget for
+ *   them: spatial heads with a window beside semantic heads with a budget are the calls' above.
  */
 typedef struct ssd_paged_config {
     int32_t n_seqs;        /* B: 1..65535                                                  */
@@ -468,7 +470,8 @@ int ssd_paged_append(const ssd_paged_config *cfg, void *k_pages, void *v_pages, 
  *                launch and the workspace.  A longer sequence is cut to it
  *   workspace  : dev scratch, 256-byte aligned, at least ssd_paged_workspace_bytes(cfg, max_len,
  *                weight_out != NULL) bytes; may be NULL if that is 0.  Nothing in it has to be
- *                kept or cleared between calls
+ *                kept or cleared between calls.  It follows the bound, not the rows held: with weights up to
+ *                n_seqs * n_heads * max_len floats, rounded up, beside about 13 MB
  * Logits that are NaN or infinite are the caller's; they reach the outputs of
  * their own sequence and heads only.  Elements of V that are infinite give what the
  * sum gives (an infinity, or NaN where its terms have both signs) as long as the row's exp(logit - largest) is

@@ -6,7 +6,7 @@
 // "seen at all"; then the piece goes through once, 16 bytes of logits at a time.  Bound by HBM (the logits in, 4 bytes out each); the tokens are read
 // by every piece of the row, from L2.  256 rows of 128257 in fp32 with 1000 to 8000 tokens, shared bias and masks: 64 to 66 us, 4.1 TB/s (56 with short
 // histories, where a copy would take 50; 72 without the non-temporal hint on the stores; pieces of 4096 and 16384 and a bias held in registers gain
-// nothing).  64 guided rows of 16384 in bf16: 4.5 us, the launch and two dependent loads.
+// nothing).  64 guided rows of 16384 in bf16: 4.5 to 5.3 us, the launch and two dependent loads.
 #include <cmath>
 
 #include "ssd_device.h"

@@ -11,7 +11,7 @@
 // by a launch with more workgroups per unit otherwise.
 //
 // Measured (8 key heads, rows of 256 bytes in pages of 16 and 64): 32 sequences of 500 to 8192 rows to 1024, 46 us, of which selection takes the first 13 (latency: tables,
-// three histograms, ranks) and the rows, all units' at once, 24 at 4.9 TB/s read and written; 2 sequences of 70001 and 100000 rows to 16000, 96 us, rows 48 at 4.4 TB/s and
+// three histograms, ranks) and the rows, all units' at once, 24 at 4.9 TB/s read and written, and 9 are not accounted for; 2 sequences of 70001 and 100000 rows to 16000, 96 us, rows 48 at 4.4 TB/s and
 // five launches of 7 to 10; one of 129 rows in 512 units 4.5 us, launch and latency.
 #include "ssd_paged.h"
 
