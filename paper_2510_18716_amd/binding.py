@@ -562,7 +562,8 @@ def _pool(t, what: str, cfg, want) -> Optional[int]:
         return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
-    _check_pool(t, what, cfg)
+    if t.dim() == 4 or not t.is_contiguous() or t.numel() != cfg.n_pages * want[0] or want[0] < want[1] * cfg.n_kv_heads:
+        _check_pool(t, what, cfg)                                  # else the memory of the whole pool, in another shape
     return t.data_ptr()
 
 
@@ -572,13 +573,20 @@ def _rows(t, what: str, n: int, heads: int, want) -> Optional[int]:
         return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
-    if t.stride() != (want[0], 1) or t.shape[1] < heads * want[1]:
-        _check_rows(t, what, n, want[0], heads * want[1])
+    width = heads * want[1]
+    if t.is_contiguous() and want[0] == width and t.numel() == n * width:          # of any shape
+        return t.data_ptr()
+    if t.stride() != (want[0], 1) or t.shape[1] < width:
+        _check_rows(t, what, n, want[0], width)
     return t.data_ptr()
 
 
 def _vocabulary_stride(t, what: str, n: int, V: int, stride: int) -> int:
     """How far n rows of V elements lie apart: as the caller says, or where that is 0 as the tensor does."""
+    if t.dim() == 2 and t.shape[0] >= n > 1 and t.shape[1] >= V:
+        own, one = t.stride()
+        if one == 1 and own >= V and stride in (0, own):
+            return own
     if stride == 0:
         runs = _runs(t)
         if len(runs) == 1:                                         # memory without gaps: its own rows, if there are as many of them
