@@ -521,6 +521,83 @@ int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, c
                     const int32_t *pos_in, int32_t *pos_out, const float *weight_in, float *weight_out,
                     int32_t *seq_len_out, int max_len, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- the same cache held in 8 or 4 bits -------------------------------------- */
+
+/*
+ * Block formats (OCP microscaling).  A row of d elements is d / 32 blocks of 32; a block shares a scale 2^E, kept as the byte E + 127, and its
+ * elements x are kept as codes of x / 2^E: E4M3 numbers (one byte) or E2M1 numbers (four bits, the even element of a byte in its low bits).  The byte 255 says
+ * that all elements of the block are NaN.
+ * Writing: E is the smallest exponent with which no element of the block is off by more than half a step, that is with largest |x| <= 464 * 2^E or
+ * 7 * 2^E, at least -117 or -125; codes are rounded to the nearest, ties to the even code (the largest are 448 and 6).  A block that holds a NaN or an
+ * infinity becomes NaN.  So an element keeps 4 (2) significant bits, relative to the block's largest at least 2^-18 (2^-4) of it; elements whose rounding
+ * reaches 2^128 read back as infinities.
+ * Reading: a bf16 or fp32 number holds every value exactly.  (Pools written elsewhere: elements below 2^-126 may be read as 0.)
+ */
+typedef enum ssd_mx_format { SSD_MXFP4 = 4, SSD_MXFP8 = 8 } ssd_mx_format;
+
+/*
+ * The calls on such a cache are those on pages above, with the same tables, lengths, rules and refusals, and with
+ *   format             : ssd_mx_format, of K and V alike
+ *   k_pages, v_pages   : codes; page_stride, head_stride and row_stride of the config count elements of the format (two to a byte for
+ *                        SSD_MXFP4), multiples of 16 bytes, all 0: [n_pages, n_kv_heads, page_size, d], dense
+ *   k_scales, v_scales : dev uint8 [n_pages, n_kv_heads, page_size, d / 32], dense, 16-byte aligned
+ * and the config's dtype that of q, new rows and outputs.
+ *
+ * ssd_paged_mx_append: ssd_paged_append, the rows quantised on the way.
+ */
+int ssd_paged_mx_append(const ssd_paged_config *cfg, int format, void *k_pages, void *v_pages, uint8_t *k_scales, uint8_t *v_scales, int32_t *pos,
+                        float *weight, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, const void *k_new,
+                        const void *v_new, const int32_t *new_start, int n_new, const float *weight_new, void *stream);
+
+/*
+ * Rows of the cache in the config's dtype (exactly what they stand for): row row_start[b] + j of k_out and v_out is slot first_slot[b] + j of sequence b.
+ *   k_out, v_out : dev [n_rows, n_kv_heads, d], new_stride apart
+ *   row_start    : dev int32 [n_seqs + 1], ascending from 0 to n_rows; NULL: one row per sequence (n_rows = n_seqs)
+ *   first_slot   : dev int32 [n_seqs], NULL: 0
+ * Rows whose slot is outside the sequence's rows, or in a block without a page, are left as they were.
+ */
+int ssd_paged_mx_read(const ssd_paged_config *cfg, int format, const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                      const uint8_t *v_scales, const int32_t *block_table, const int32_t *seq_len, const int32_t *row_start, int n_rows,
+                      const int32_t *first_slot, void *k_out, void *v_out, void *stream);
+
+/*
+ * ssd_paged_decode_attn and ssd_paged_decode_step over the values that the codes stand for; a step's new row is quantised and written first, and
+ * attended to as the cache then has it.  A NaN block makes the outputs of its sequence and key head NaN (of V: in its 32 elements).
+ */
+size_t ssd_paged_mx_workspace_bytes(const ssd_paged_config *cfg, int format, int max_len, int with_weights);
+int ssd_paged_mx_decode_attn(const ssd_paged_config *cfg, int format, const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scales,
+                             const uint8_t *v_scales, const float *weight_in, float *weight_out, const int32_t *block_table, const int32_t *seq_len,
+                             void *out, float *lse, int max_len, void *workspace, size_t workspace_bytes, void *stream);
+int ssd_paged_mx_decode_step(const ssd_paged_config *cfg, int format, const void *q, const void *k_new, const void *v_new, void *k_pages, void *v_pages,
+                             uint8_t *k_scales, uint8_t *v_scales, int32_t *pos, const float *weight_in, float *weight_out,
+                             const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, void *out, float *lse, int max_len,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* ssd_paged_evict: codes and scales of the rows that move go with them. */
+size_t ssd_paged_mx_evict_workspace_bytes(const ssd_paged_config *cfg, int format, int max_len);
+int ssd_paged_mx_evict(const ssd_paged_config *cfg, int format, void *k_pages, void *v_pages, uint8_t *k_scales, uint8_t *v_scales,
+                       const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, const int32_t *budget, int n_sink, int recent,
+                       const int32_t *pos_in, int32_t *pos_out, const float *weight_in, float *weight_out, int32_t *seq_len_out, int max_len,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rotary positions with one to four axes (text; time, height and width of images and video) for batches whose tokens have positions of their
+ * own.  Pair i of every head of token t turns by the angle  pos[axis[i], t] * inv_freq[i]:  (a, b) becomes (a cos - b sin, b cos + a sin), computed in fp32
+ * and rounded once to the dtype.  The angle is that of the exact product, however far the position.
+ *   x, out      : dev [n_rows, n_heads, head_dim] of `dtype`, tokens x_stride and out_stride elements apart (0: dense), aligned to their elements.
+ *                 out may be x with the same stride, otherwise they share no memory (nor may the ranges of their rows overlap).
+ *                 Query and key heads that lie next to each other in a projection's row are one call
+ *   pos         : dev int32 [n_axes, n_rows]
+ *   axis        : dev uint8 [n_pairs], the axis whose position turns each pair; NULL with n_axes = 1.  A pair whose entry is n_axes or more stays
+ *   inv_freq    : dev float [n_pairs], finite
+ *   n_pairs     : 1..head_dim / 2; elements 2 * n_pairs and beyond of a head stay as they are (in out: are copied)
+ *   rope_layout : SSD_ROPE_HALF pairs element i with i + n_pairs; SSD_ROPE_INTERLEAVED 2i with 2i + 1
+ *   inverse     : 1 turns back, by the negative angles: the gradient of x from that of out
+ *   n_rows >= 0;  n_heads 1..4096;  head_dim even, 2..1024
+ */
+int ssd_rope_axes(const void *x, void *out, int n_rows, int n_heads, int head_dim, int dtype, int64_t x_stride, int64_t out_stride, const int32_t *pos,
+                  int n_axes, const uint8_t *axis, const float *inv_freq, int n_pairs, int rope_layout, int inverse, void *stream);
+
 /*
  * From a step's logits to those a token is sampled from.  Per output row i and
  * vocabulary entry v, in fp32 and in this order:

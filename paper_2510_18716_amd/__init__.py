@@ -14,4 +14,6 @@ from .binding import (  # noqa: F401
     ssd_dense_decode_attn, ssd_dense_decode_attn_static, SSD_DENSE_STATIC_SCRATCH_BYTES, ssd_dense_workspace_bytes, ssd_last_error, ssd_prefill_scores, ssd_version,
     SsdLogitsParams, SsdPagedConfig, make_paged_config, ssd_logits_process, ssd_paged_append, ssd_paged_decode_attn, ssd_paged_decode_step,
     ssd_paged_evict, ssd_paged_evict_workspace_bytes, ssd_paged_workspace_bytes,
+    SSD_MXFP4, SSD_MXFP8, ssd_paged_mx_append, ssd_paged_mx_decode_attn, ssd_paged_mx_decode_step, ssd_paged_mx_evict,
+    ssd_paged_mx_evict_workspace_bytes, ssd_paged_mx_read, ssd_paged_mx_workspace_bytes, ssd_rope_axes,
 )

@@ -489,6 +489,22 @@ lib.ssd_paged_evict_workspace_bytes.argtypes = [_pcfg, C.c_int]
 lib.ssd_paged_evict_workspace_bytes.restype = C.c_size_t
 lib.ssd_paged_evict.argtypes = [_pcfg] + [_vp] * 6 + [C.c_int, C.c_int] + [_vp] * 5 + [C.c_int, _vp, C.c_size_t, _vp]
 lib.ssd_paged_evict.restype = C.c_int
+lib.ssd_paged_mx_append.argtypes = [_pcfg, C.c_int] + [_vp] * 12 + [C.c_int, _vp, _vp]
+lib.ssd_paged_mx_append.restype = C.c_int
+lib.ssd_paged_mx_read.argtypes = [_pcfg, C.c_int] + [_vp] * 7 + [C.c_int] + [_vp] * 4
+lib.ssd_paged_mx_read.restype = C.c_int
+lib.ssd_paged_mx_workspace_bytes.argtypes = [_pcfg, C.c_int, C.c_int, C.c_int]
+lib.ssd_paged_mx_workspace_bytes.restype = C.c_size_t
+lib.ssd_paged_mx_decode_attn.argtypes = [_pcfg, C.c_int] + [_vp] * 11 + [C.c_int, _vp, C.c_size_t, _vp]
+lib.ssd_paged_mx_decode_attn.restype = C.c_int
+lib.ssd_paged_mx_decode_step.argtypes = [_pcfg, C.c_int] + [_vp] * 15 + [C.c_int, _vp, C.c_size_t, _vp]
+lib.ssd_paged_mx_decode_step.restype = C.c_int
+lib.ssd_paged_mx_evict_workspace_bytes.argtypes = [_pcfg, C.c_int, C.c_int]
+lib.ssd_paged_mx_evict_workspace_bytes.restype = C.c_size_t
+lib.ssd_paged_mx_evict.argtypes = [_pcfg, C.c_int] + [_vp] * 8 + [C.c_int, C.c_int] + [_vp] * 5 + [C.c_int, _vp, C.c_size_t, _vp]
+lib.ssd_paged_mx_evict.restype = C.c_int
+lib.ssd_rope_axes.argtypes = [_vp, _vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int, _vp, _vp, C.c_int, C.c_int, C.c_int, _vp]
+lib.ssd_rope_axes.restype = C.c_int
 lib.ssd_logits_process.argtypes = [_vp, C.c_int, C.c_int, C.c_int, C.c_int64, C.c_int, C.c_float, C.POINTER(SsdLogitsParams), _vp,
                                    C.c_int64, _vp]
 lib.ssd_logits_process.restype = C.c_int
@@ -654,6 +670,129 @@ def ssd_paged_evict(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len,
     _check(lib.ssd_paged_evict(C.byref(cfg), _pool(k_pages, "k_pages", cfg, pool), _pool(v_pages, "v_pages", cfg, pool), _ptr(block_table), _ptr(seq_len),
                                _ptr(seq_pos), _ptr(budget), int(n_sink), int(recent), _ptr(pos_in), _ptr(pos_out), _ptr(weight_in), _ptr(weight_out), _ptr(seq_len_out),
                                int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_evict")
+
+
+SSD_MXFP4, SSD_MXFP8 = 4, 8
+_FORMATS = {"mxfp4": SSD_MXFP4, "mxfp8": SSD_MXFP8, SSD_MXFP4: SSD_MXFP4, SSD_MXFP8: SSD_MXFP8}
+
+
+def _format_code(format) -> int:
+    if format not in _FORMATS:
+        raise ValueError("format %r: \"mxfp4\" or \"mxfp8\" is expected" % (format,))
+    return _FORMATS[format]
+
+
+def _mx_pool(t, what: str, cfg, bits: int) -> Optional[int]:
+    """Address of a pool of codes: bytes [n_pages, n_kv_heads, page_size, d * bits / 8] with the config's strides (or the same with page_size before
+    n_kv_heads, as it lies in memory then), or memory without gaps that reaches as far."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.element_size() != 1:
+        raise ValueError("%s of type %s: a pool of codes is bytes" % (what, t.dtype))
+    want = tuple(s * bits // 8 for s in cfg.strides[0][:3]) + (1,)
+    sizes = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim * bits // 8)
+    if tuple(t.shape) == sizes:
+        fits = all(size == 1 or stride == w for size, stride, w in zip(sizes, t.stride(), want))
+        if not fits and sizes[1] == sizes[2]:                      # which of the two dimensions is which, the strides say
+            fits = t.transpose(1, 2).stride() == want
+    elif t.dim() == 4 and tuple(t.transpose(1, 2).shape) == sizes:
+        fits = all(size == 1 or stride == w for size, stride, w in zip(sizes, t.transpose(1, 2).stride(), want))
+    else:
+        fits = t.is_contiguous() and sum((size - 1) * w for size, w in zip(sizes, want)) < t.numel()
+    if not fits:
+        raise ValueError("%s of shape %s, strides %s: the config says bytes [%d, %d, %d, %d] with strides %s" % ((what, tuple(t.shape), t.stride()) + sizes + (want,)))
+    return t.data_ptr()
+
+
+def _mx_scales(t, what: str, cfg) -> Optional[int]:
+    """Address of the scales [n_pages, n_kv_heads, page_size, d / 32]: bytes without gaps."""
+    if t is None or isinstance(t, int):
+        return t
+    need = cfg.n_pages * cfg.n_kv_heads * cfg.page_size * (cfg.head_dim // 32)
+    if t.element_size() != 1 or not t.is_contiguous() or t.numel() < need:
+        raise ValueError("%s of shape %s, strides %s, type %s: %d bytes without gaps are expected" % (what, tuple(t.shape), t.stride(), t.dtype, need))
+    return t.data_ptr()
+
+
+def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
+    bits = _format_code(format)
+    return (bits, _mx_pool(k_pages, "k_pages", cfg, bits), _mx_pool(v_pages, "v_pages", cfg, bits), _mx_scales(k_scales, "k_scales", cfg),
+            _mx_scales(v_scales, "v_scales", cfg))
+
+
+def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, k_new, v_new, pos=None, weight=None,
+                        seq_pos=None, new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
+    """format: "mxfp4" or "mxfp8" (SSD_MXFP4, SSD_MXFP8).  n_new: tokens in k_new; None: its first dimension."""
+    n = int(k_new.shape[0] if n_new is None else n_new)
+    new, heads = cfg.strides[2], cfg.n_kv_heads
+    bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
+    _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos),
+                                   _rows(k_new, "k_new", n, heads, new), _rows(v_new, "v_new", n, heads, new), _ptr(new_start), n, _ptr(weight_new),
+                                   _stream(stream)), "ssd_paged_mx_append")
+
+
+def ssd_paged_mx_read(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, k_out, v_out, row_start=None,
+                      first_slot=None, n_rows: Optional[int] = None, stream=None) -> None:
+    """n_rows: rows of k_out; None: its first dimension."""
+    n = int(k_out.shape[0] if n_rows is None else n_rows)
+    new, heads = cfg.strides[2], cfg.n_kv_heads
+    bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
+    _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(row_start), n, _ptr(first_slot),
+                                 _rows(k_out, "k_out", n, heads, new), _rows(v_out, "v_out", n, heads, new), _stream(stream)), "ssd_paged_mx_read")
+
+
+def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, with_weights: bool = False) -> int:
+    return lib.ssd_paged_mx_workspace_bytes(C.byref(cfg), _format_code(format), int(max_len), int(bool(with_weights)))
+
+
+def ssd_paged_mx_decode_attn(cfg: SsdPagedConfig, format, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, lse=None, weight_in=None,
+                             weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
+    bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
+    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _rows(q, "q", cfg.n_seqs, cfg.n_heads, cfg.strides[1]), k, v, ks, vs, _ptr(weight_in),
+                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(out), _ptr(lse), int(max_len), _ptr(workspace),
+                                        _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
+
+
+def ssd_paged_mx_decode_step(cfg: SsdPagedConfig, format, q, k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, pos=None,
+                             seq_pos=None, lse=None, weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
+    (_, queries, new), B, heads = cfg.strides, cfg.n_seqs, cfg.n_kv_heads
+    bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
+    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _rows(q, "q", B, cfg.n_heads, queries), _rows(k_new, "k_new", B, heads, new),
+                                        _rows(v_new, "v_new", B, heads, new), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
+                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(out), _ptr(lse), int(max_len), _ptr(workspace),
+                                        _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
+
+
+def ssd_paged_mx_evict_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0) -> int:
+    return lib.ssd_paged_mx_evict_workspace_bytes(C.byref(cfg), _format_code(format), int(max_len))
+
+
+def ssd_paged_mx_evict(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, budget, pos_in, pos_out, weight_in,
+                       weight_out, seq_len_out=None, n_sink: int = 0, recent: int = 0, seq_pos=None, max_len: int = 0, workspace=None, stream=None) -> None:
+    bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
+    _check(lib.ssd_paged_mx_evict(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(budget), int(n_sink),
+                                  int(recent), _ptr(pos_in), _ptr(pos_out), _ptr(weight_in), _ptr(weight_out), _ptr(seq_len_out), int(max_len),
+                                  _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_mx_evict")
+
+
+def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, inv_freq, axis=None, n_axes: int = 1, n_pairs: Optional[int] = None,
+                  layout: int = SSD_ROPE_HALF, inverse: bool = False, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
+    """n_pairs None: inv_freq's elements.  x_stride, out_stride 0: the tensor's own (query and key heads may be handed over where a projection has them)."""
+    width = n_heads * head_dim
+    if x is not None and not isinstance(x, int):
+        x_stride = x_stride or (x.stride(0) if x.dim() > 1 and x.shape[0] == n_rows > 1 else 0)
+        _check_rows(x, "x", n_rows, x_stride or width, width)
+        x = x.data_ptr()
+    if out is not None and not isinstance(out, int):
+        out_stride = out_stride or (out.stride(0) if out.dim() > 1 and out.shape[0] == n_rows > 1 else 0)
+        _check_rows(out, "out", n_rows, out_stride or width, width)
+        out = out.data_ptr()
+    pairs = int(inv_freq.numel() if n_pairs is None else n_pairs)
+    for t, what, most in ((pos, "pos", n_axes * n_rows), (inv_freq, "inv_freq", pairs), (axis, "axis", pairs)):
+        if t is not None and not isinstance(t, int) and (not t.is_contiguous() or t.numel() < most):
+            raise ValueError("%s of shape %s, strides %s: %d elements without gaps are expected" % (what, tuple(t.shape), t.stride(), most))
+    _check(lib.ssd_rope_axes(x, out, int(n_rows), int(n_heads), int(head_dim), _dtype_code(dtype), int(x_stride), int(out_stride), _ptr(pos), int(n_axes),
+                             _ptr(axis), _ptr(inv_freq), pairs, int(layout), int(bool(inverse)), _stream(stream)), "ssd_rope_axes")
 
 
 def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[float] = None, tokens=None, n_tokens=None, n_prompt=None,

@@ -45,6 +45,17 @@ static __device__ __forceinline__ int64_t table_index(const PagedGeom &g, int pa
     return ((int64_t)page * g.n_kv + kv) * g.page_size + place;
 }
 
+// The sequence that has a row of an array in which sequence b's rows begin at start(b): the last one that begins at or before it.
+template <typename Start> static __device__ __forceinline__ int sequence_of(const PagedGeom &g, int row, const Start &start) {
+    int lo = 0, hi = g.n_seqs;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (start(mid) <= row) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
 // The sequence and key head of a workgroup of a grid (heads, sequences).  Workgroups go to the eight XCDs in turn.  Where a page's entries of one
 // head are less than a cache line, the heads that share one go to the same XCD, or two would read and write every line of the tables (one eviction from each
 // of 256 units of 8000 rows in pages of 16 28.7 -> 20.3 us, of 16000 105 -> 64, in pages of one row 186 -> 83; 32 unequal prompts 45.1 -> 45.9; attention with
@@ -87,9 +98,10 @@ static __device__ __forceinline__ uint32_t wave_or(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_readlane((int)dpp_or<0x143, 0xC>(v), 63);
 }
 
-// Checks of the config (with the error text set), then the geometry; max_len <= 0 selects the table's reach.
-int check_paged(const ssd_paged_config *c);
-PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, int max_len);
+// Checks of the config (with the error text set), then the geometry; max_len <= 0 selects the table's reach.  bits: of an element of the pool, 0: of the
+// config's type.
+int check_paged(const ssd_paged_config *c, int bits = 0);
+PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, int max_len, int bits = 0);
 int check_max_len(const ssd_paged_config *c, int max_len);
 static inline int paged_reach(const ssd_paged_config *c, int max_len) {
     const int64_t all = (int64_t)c->max_blocks * c->page_size;

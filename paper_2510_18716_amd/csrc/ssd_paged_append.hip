@@ -10,7 +10,7 @@
 
 namespace ssd {
 
-int check_paged(const ssd_paged_config *c) {
+int check_paged(const ssd_paged_config *c, int bits) {
     if (!c) return fail(SSD_ERR_INVALID_ARG, "config is NULL");
     if (c->n_seqs < 1 || c->n_seqs > 65535) return fail(SSD_ERR_INVALID_ARG, "n_seqs=%d outside 1..65535", c->n_seqs);
     if (c->n_kv_heads < 1 || c->n_kv_heads > 1024) return fail(SSD_ERR_INVALID_ARG, "n_kv_heads=%d outside 1..1024", c->n_kv_heads);
@@ -25,11 +25,11 @@ int check_paged(const ssd_paged_config *c) {
     if (!(c->softmax_scale >= 0.f) || !std::isfinite(c->softmax_scale)) return fail(SSD_ERR_INVALID_ARG, "softmax_scale must be finite and >= 0");
     for (int i = 0; i < 3; ++i)
         if (c->reserved[i] != 0) return fail(SSD_ERR_INVALID_ARG, "reserved[%d] must be 0", i);
-    const int64_t unit = 16 / (int64_t)paged_esize(c), most = 1ll << 50;
+    const int64_t unit = 16 / (int64_t)paged_esize(c), pool_unit = bits ? 128 / bits : unit, most = 1ll << 50;
     const bool none = c->page_stride == 0 && c->head_stride == 0 && c->row_stride == 0;
     const int64_t st[3] = {c->page_stride, c->head_stride, c->row_stride};
     for (int i = 0; i < 3 && !none; ++i)
-        if (st[i] < c->head_dim || st[i] % unit != 0 || st[i] > most / ((int64_t)c->n_pages + c->n_kv_heads + c->page_size))
+        if (st[i] < c->head_dim || st[i] % pool_unit != 0 || st[i] > most / ((int64_t)c->n_pages + c->n_kv_heads + c->page_size))
             return fail(SSD_ERR_INVALID_ARG, "page_stride, head_stride and row_stride are all 0, or multiples of 16 bytes of at least head_dim elements");
     if (c->q_stride != 0 && (c->q_stride < (int64_t)c->n_heads * c->head_dim || c->q_stride % unit != 0 || c->q_stride > most / 65536))
         return fail(SSD_ERR_INVALID_ARG, "q_stride must be 0 or a multiple of 16 bytes of at least n_heads * head_dim elements");
@@ -44,13 +44,13 @@ int check_max_len(const ssd_paged_config *c, int max_len) {
     return SSD_OK;
 }
 
-PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, int max_len) {
+PagedGeom paged_geom(const ssd_paged_config *c, const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, int max_len, int bits) {
     PagedGeom g;
-    const int64_t e = (int64_t)paged_esize(c);
+    const int64_t b = bits ? bits : 8 * (int64_t)paged_esize(c);
     const bool dense = c->page_stride == 0;
-    g.row_stride = (dense ? c->head_dim : c->row_stride) * e;
-    g.head_stride = dense ? g.row_stride * c->page_size : c->head_stride * e;
-    g.page_stride = dense ? g.head_stride * c->n_kv_heads : c->page_stride * e;
+    g.row_stride = (dense ? c->head_dim : c->row_stride) * b / 8;
+    g.head_stride = dense ? g.row_stride * c->page_size : c->head_stride * b / 8;
+    g.page_stride = dense ? g.head_stride * c->n_kv_heads : c->page_stride * b / 8;
     g.block_table = block_table;
     g.seq_len = seq_len;
     g.seq_pos = seq_pos ? seq_pos : seq_len;
@@ -117,13 +117,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
         if (row < a.n_new) {
             int b = row, first = row, count = 1;
             if (a.new_start) {
-                int lo = 0, hi = a.g.n_seqs;                 // the last sequence that begins at or before the row
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) / 2;
-                    if ((in_lds ? starts[mid] : a.new_start[mid]) <= row) lo = mid;
-                    else hi = mid;
-                }
-                b = lo;
+                b = sequence_of(a.g, row, [&](int i) { return in_lds ? starts[i] : a.new_start[i]; });
                 first = in_lds ? starts[b] : a.new_start[b];
                 count = (in_lds ? starts[b + 1] : a.new_start[b + 1]) - first;
             }

@@ -13,7 +13,7 @@
 // Measured (8 key heads, rows of 256 bytes in pages of 16 and 64): 32 sequences of 500 to 8192 rows to 1024, 46 us, of which selection takes the first 13 (latency: tables,
 // three histograms, ranks) and the rows, all units' at once, 24 at 4.9 TB/s read and written, and 9 are not accounted for; 2 sequences of 70001 and 100000 rows to 16000, 96 us, rows 48 at 4.4 TB/s and
 // five launches of 7 to 10; one of 129 rows in 512 units 4.5 us, launch and latency.
-#include "ssd_paged.h"
+#include "ssd_paged_mx.h"
 
 namespace ssd {
 
@@ -28,7 +28,9 @@ struct PagedEvictArgs {
     int32_t *moves;          // per unit: count, then cap free slots, then cap slots to move from
     int n_sink, recent;
     int cap;
-    int lpr_log2;
+    int lpr_log2;            // 16-byte fragments of a row: 2 to 32
+    uint8_t *k_scales, *v_scales;    // a pool that holds codes: the blocks' shared exponents, scale_bytes of a row; or NULL
+    int scale_bytes;
 };
 
 static __host__ __device__ inline int64_t moves_of(int cap, int64_t unit) { return unit * (2 * (int64_t)cap + 1); }
@@ -131,6 +133,28 @@ static __device__ __forceinline__ void move_entries(const PagedEvictArgs &a, int
         const int64_t t = table_index(a.g, tpage, kv, tp), f = table_index(a.g, fpage, kv, fp);
         a.weight_out[t] = a.weight_in[f];
         a.pos_out[t] = a.pos_in[f];
+    }
+}
+
+// The shared exponents of moved rows, a thread each.
+template <typename I>
+static __device__ __forceinline__ void move_scales(const PagedEvictArgs &a, int b, int kv, const I *to, const I *from, int count, int thread,
+                                                   int threads) {
+    for (int i = thread; i < count; i += threads) {
+        int block, tp, fp;
+        split_slot(a.g, to[i], block, tp);
+        const int tpage = page_of(a.g, b, block);
+        split_slot(a.g, from[i], block, fp);
+        const int fpage = page_of(a.g, b, block);
+        if (tpage < 0 || fpage < 0) continue;
+        const int64_t t = table_index(a.g, tpage, kv, tp), f = table_index(a.g, fpage, kv, fp);
+        if (a.scale_bytes == 4) {
+            reinterpret_cast<uint32_t *>(a.k_scales)[t] = reinterpret_cast<const uint32_t *>(a.k_scales)[f];
+            reinterpret_cast<uint32_t *>(a.v_scales)[t] = reinterpret_cast<const uint32_t *>(a.v_scales)[f];
+        } else {
+            reinterpret_cast<uint16_t *>(a.k_scales)[t] = reinterpret_cast<const uint16_t *>(a.k_scales)[f];
+            reinterpret_cast<uint16_t *>(a.v_scales)[t] = reinterpret_cast<const uint16_t *>(a.v_scales)[f];
+        }
     }
 }
 
@@ -542,6 +566,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(PagedEvictArgs a,
     } else if (moves > 0) {
         __syncthreads();
         move_entries(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
+        if (a.k_scales) move_scales(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
         if (moves <= THREADS / (2 << a.lpr_log2)) move_rows<1>(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
         else move_rows<8>(a, b, kv, free_slots, move_slots, moves, tid, THREADS);
     }
@@ -990,8 +1015,10 @@ static constexpr int ENTRIES = 4;
 __global__ __launch_bounds__(256) void paged_move_kernel(PagedEvictArgs a) {
     const int kv = blockIdx.x, b = blockIdx.y, z = (int)blockIdx.z - ENTRIES, tid = threadIdx.x;
     const int32_t *list = a.moves + moves_of(a.cap, (int64_t)b * a.g.n_kv + kv);
-    if (z < 0) move_entries(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)blockIdx.z * 256 + tid, ENTRIES * 256);
-    else move_rows<2>(a, b, kv, list + 1, list + 1 + a.cap, list[0], z * 256 + tid, ((int)gridDim.z - ENTRIES) * 256);
+    if (z < 0) {
+        move_entries(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)blockIdx.z * 256 + tid, ENTRIES * 256);
+        if (a.k_scales) move_scales(a, b, kv, list + 1, list + 1 + a.cap, list[0], (int)blockIdx.z * 256 + tid, ENTRIES * 256);
+    } else move_rows<2>(a, b, kv, list + 1, list + 1 + a.cap, list[0], z * 256 + tid, ((int)gridDim.z - ENTRIES) * 256);
 }
 
 // ---- launch shapes and memory ------------------------------------------------------------------------------------------------
@@ -1022,24 +1049,11 @@ static EvictShape evict_shape(const ssd_paged_config *c, int max_len) {
     return s;
 }
 
-}  // namespace ssd
-
-using namespace ssd;
-
-extern "C" size_t ssd_paged_evict_workspace_bytes(const ssd_paged_config *cfg, int max_len) {
-    clear_error();
-    if (check_paged(cfg) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
-    const EvictShape s = evict_shape(cfg, max_len);
-    return s.moves + s.hist + s.info;
-}
-
-extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, const int32_t *block_table, const int32_t *seq_len,
-                               const int32_t *seq_pos, const int32_t *budget, int n_sink, int recent, const int32_t *pos_in, int32_t *pos_out,
-                               const float *weight_in, float *weight_out, int32_t *seq_len_out, int max_len, void *workspace,
-                               size_t workspace_bytes, void *stream) {
-    clear_error();
-    int rc = check_paged(cfg);
-    if (rc != SSD_OK) return rc;
+// bits: of an element of the pool
+static int paged_evict(const ssd_paged_config *cfg, int bits, void *k_pages, void *v_pages, uint8_t *k_scales, uint8_t *v_scales, const int32_t *block_table,
+                       const int32_t *seq_len, const int32_t *seq_pos, const int32_t *budget, int n_sink, int recent, const int32_t *pos_in, int32_t *pos_out,
+                       const float *weight_in, float *weight_out, int32_t *seq_len_out, int max_len, void *workspace, size_t workspace_bytes, hipStream_t s) {
+    int rc;
     if ((rc = check_max_len(cfg, max_len)) != SSD_OK) return rc;
     if (!k_pages || !v_pages || !aligned(k_pages, 16) || !aligned(v_pages, 16))
         return fail(SSD_ERR_INVALID_ARG, "k_pages and v_pages must be given, 16-byte aligned");
@@ -1057,7 +1071,7 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return fail(SSD_ERR_INVALID_ARG, "workspace of %zu bytes, 256-byte aligned, needed; %zu given", need, workspace_bytes);
     PagedEvictArgs a;
-    a.g = paged_geom(cfg, block_table, seq_len, seq_pos, max_len);
+    a.g = paged_geom(cfg, block_table, seq_len, seq_pos, max_len, bits);
     a.k_pages = static_cast<char *>(k_pages);
     a.v_pages = static_cast<char *>(v_pages);
     a.budget = budget;
@@ -1070,8 +1084,10 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     a.n_sink = n_sink;
     a.recent = recent;
     a.cap = shape.cap;
-    a.lpr_log2 = __builtin_ctz((unsigned)((size_t)cfg->head_dim * paged_esize(cfg) / 16));
-    hipStream_t s = static_cast<hipStream_t>(stream);
+    a.lpr_log2 = __builtin_ctz((unsigned)((size_t)cfg->head_dim * bits / 128));
+    a.k_scales = k_scales;
+    a.v_scales = v_scales;
+    a.scale_bytes = cfg->head_dim / 32;
     const dim3 units((unsigned)a.g.n_kv, (unsigned)a.g.n_seqs);
     const int64_t n_units = (int64_t)units.x * units.y;
     const int reach = a.g.max_len;
@@ -1101,4 +1117,44 @@ extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void 
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSD_OK : hip_fail(e, "paged eviction launch");
+}
+
+}  // namespace ssd
+
+using namespace ssd;
+
+extern "C" size_t ssd_paged_evict_workspace_bytes(const ssd_paged_config *cfg, int max_len) {
+    clear_error();
+    if (check_paged(cfg) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
+    const EvictShape s = evict_shape(cfg, max_len);
+    return s.moves + s.hist + s.info;
+}
+
+extern "C" size_t ssd_paged_mx_evict_workspace_bytes(const ssd_paged_config *cfg, int format, int max_len) {
+    clear_error();
+    if (check_mx(cfg, format) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
+    const EvictShape s = evict_shape(cfg, max_len);
+    return s.moves + s.hist + s.info;
+}
+
+extern "C" int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, const int32_t *block_table, const int32_t *seq_len,
+                               const int32_t *seq_pos, const int32_t *budget, int n_sink, int recent, const int32_t *pos_in, int32_t *pos_out,
+                               const float *weight_in, float *weight_out, int32_t *seq_len_out, int max_len, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+    clear_error();
+    const int rc = check_paged(cfg);
+    if (rc != SSD_OK) return rc;
+    return paged_evict(cfg, 8 * (int)paged_esize(cfg), k_pages, v_pages, nullptr, nullptr, block_table, seq_len, seq_pos, budget, n_sink, recent, pos_in, pos_out,
+                       weight_in, weight_out, seq_len_out, max_len, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int ssd_paged_mx_evict(const ssd_paged_config *cfg, int format, void *k_pages, void *v_pages, uint8_t *k_scales, uint8_t *v_scales,
+                                  const int32_t *block_table, const int32_t *seq_len, const int32_t *seq_pos, const int32_t *budget, int n_sink, int recent,
+                                  const int32_t *pos_in, int32_t *pos_out, const float *weight_in, float *weight_out, int32_t *seq_len_out, int max_len,
+                                  void *workspace, size_t workspace_bytes, void *stream) {
+    clear_error();
+    int rc = check_mx(cfg, format);
+    if (rc != SSD_OK || (rc = check_mx_scales(k_scales, v_scales)) != SSD_OK) return rc;
+    return paged_evict(cfg, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, seq_pos, budget, n_sink, recent, pos_in, pos_out, weight_in,
+                       weight_out, seq_len_out, max_len, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
 }

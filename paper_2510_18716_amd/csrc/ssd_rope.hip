@@ -1,0 +1,174 @@
+// ssd_rope_axes: heads of tokens turned by positions with one to four axes.
+//
+// Pair i of a token's heads turns by the angle pos[axis[i]] * inv_freq[i].  The angle's revolutions are found in 64 bits: the product is exact up to the last
+// of 53 bits and is divided by 2 pi with the quotient's rounding made up for, so that positions of 2^31 lose nothing; then the fraction of a quarter turn
+// that is left is at most pi / 4, where the series of sine and cosine up to r^11 and r^10 are below 2^-28 off.
+//
+// Bound by HBM: every element read once and written once.  A token's angles serve all its heads: they are found once per workgroup, into LDS, while the heads'
+// elements are on their way.
+#include <cmath>
+
+#include "ssd_device.h"
+
+namespace ssd {
+
+struct RopeArgs {
+    const char *x;
+    char *out;
+    const int32_t *pos;      // [axes, n]
+    const uint8_t *axis;     // [pairs], or NULL: 0
+    const float *inv_freq;   // [pairs]
+    int64_t x_stride, out_stride;   // bytes
+    int n, heads, d, pairs, axes;
+    int tokens;              // of a workgroup
+    float sign;              // -1: turned back
+};
+
+// (cos, sin) of pos * f.
+static __device__ __forceinline__ float2 turn_of(int pos, float f, float sign) {
+    const double x = (double)pos * (double)f;
+    constexpr double C = 0x1.45f306dc9c883p-3, C2 = -0x1.6b01ec5417056p-57;        // 1 / (2 pi) in two parts
+    const double r = x * C, low = __builtin_fma(x, C, -r) + x * C2;
+    const double quarter = (r - __builtin_rint(r)) * 4.0, q = __builtin_rint(quarter);
+    const float t = (float)(((quarter - q) + low * 4.0) * 0x1.921fb54442d18p+0), t2 = t * t;     // at most pi / 4
+    float s = __builtin_fmaf(t2, -2.50521084e-8f, 2.75573192e-6f);
+    s = __builtin_fmaf(t2, s, -1.98412698e-4f);
+    s = __builtin_fmaf(t2, s, 8.33333333e-3f);
+    s = __builtin_fmaf(t2, s, -1.66666667e-1f);
+    s = __builtin_fmaf(t2 * t, s, t);
+    float c = __builtin_fmaf(t2, -2.75573192e-7f, 2.48015873e-5f);
+    c = __builtin_fmaf(t2, c, -1.38888889e-3f);
+    c = __builtin_fmaf(t2, c, 4.16666667e-2f);
+    c = __builtin_fmaf(t2, c, -0.5f);
+    c = __builtin_fmaf(t2, c, 1.f);
+    const int k = (int)q & 3;
+    const float cs = k & 1 ? s : c, sn = k & 1 ? c : s;
+    return make_float2(k == 1 || k == 2 ? -cs : cs, sign * (k & 2 ? -sn : sn));
+}
+
+// N neighbouring elements.
+template <typename T, int N> struct alignas(sizeof(T) * N) Wide { T e[N]; };
+
+template <typename T> static __device__ __forceinline__ float to_f32(T x) {
+    if constexpr (sizeof(T) == 4) return x;
+    else return __uint_as_float((uint32_t)x.bits << 16);
+}
+template <typename T> static __device__ __forceinline__ T from_f32(float x) {
+    if constexpr (sizeof(T) == 4) return x;
+    else return T{(uint16_t)f32_to_bf16_bits(x)};
+}
+
+// VEC: elements of a lane's run; HALF: pair i is (i, i + pairs), else (2 i, 2 i + 1).
+template <typename T, int VEC, bool HALF> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+    extern __shared__ __align__(16) float2 turns[];               // [tokens][pairs]
+    typedef Wide<T, VEC> run_t;
+    const int t0 = (int)blockIdx.x * a.tokens, tokens = a.n - t0 < a.tokens ? a.n - t0 : a.tokens;
+    for (int i = threadIdx.x; i < tokens * a.pairs; i += 256) {
+        const int t = i / a.pairs, p = i - t * a.pairs;
+        const int axis = a.axis ? a.axis[p] : 0;
+        turns[i] = axis < a.axes ? turn_of(a.pos[(int64_t)axis * a.n + t0 + t], a.inv_freq[p], a.sign) : make_float2(1.f, 0.f);
+    }
+    __syncthreads();
+    // what a lane takes at a time: runs at i and i + pairs, or 2 VEC neighbouring elements
+    const int per_head = HALF ? a.pairs / VEC : 2 * a.pairs / VEC, rest = (a.d - 2 * a.pairs) / VEC, all = per_head + (a.x == a.out ? 0 : rest);
+    for (int i = threadIdx.x; i < tokens * a.heads * all; i += 256) {
+        const int th = i / all, c = i - th * all, t = th / a.heads, h = th - t * a.heads;
+        const T *x = reinterpret_cast<const T *>(a.x + (int64_t)(t0 + t) * a.x_stride) + (int64_t)h * a.d;
+        T *out = reinterpret_cast<T *>(a.out + (int64_t)(t0 + t) * a.out_stride) + (int64_t)h * a.d;
+        if (c >= per_head) {
+            const int at = 2 * a.pairs + (c - per_head) * VEC;
+            *reinterpret_cast<run_t *>(out + at) = *reinterpret_cast<const run_t *>(x + at);
+            continue;
+        }
+        if constexpr (HALF) {
+            run_t u = *reinterpret_cast<const run_t *>(x + c * VEC), w = *reinterpret_cast<const run_t *>(x + a.pairs + c * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float2 cs = turns[t * a.pairs + c * VEC + e];
+                const float p = to_f32<T>(u.e[e]), q = to_f32<T>(w.e[e]);
+                u.e[e] = from_f32<T>(p * cs.x - q * cs.y);
+                w.e[e] = from_f32<T>(q * cs.x + p * cs.y);
+            }
+            *reinterpret_cast<run_t *>(out + c * VEC) = u;
+            *reinterpret_cast<run_t *>(out + a.pairs + c * VEC) = w;
+        } else {
+            run_t u = *reinterpret_cast<const run_t *>(x + c * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; e += 2) {
+                const float2 cs = turns[t * a.pairs + (c * VEC + e) / 2];
+                const float p = to_f32<T>(u.e[e]), q = to_f32<T>(u.e[e + 1]);
+                u.e[e] = from_f32<T>(p * cs.x - q * cs.y);
+                u.e[e + 1] = from_f32<T>(q * cs.x + p * cs.y);
+            }
+            *reinterpret_cast<run_t *>(out + c * VEC) = u;
+        }
+    }
+}
+
+template <typename T, bool HALF> static void launch_rope(const RopeArgs &a, int vec, hipStream_t s) {
+    const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens));
+    const unsigned lds = (unsigned)(a.tokens * a.pairs * sizeof(float2));
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, a); };
+    if constexpr (sizeof(T) == 2)
+        if (vec == 8) return go(rope_kernel<T, 8, HALF>);
+    if (vec >= 4) go(rope_kernel<T, 4, HALF>);
+    else if (vec == 2 || !HALF) go(rope_kernel<T, 2, HALF>);
+    else if constexpr (HALF) go(rope_kernel<T, 1, HALF>);
+}
+
+}  // namespace ssd
+
+using namespace ssd;
+
+extern "C" int ssd_rope_axes(const void *x, void *out, int n_rows, int n_heads, int head_dim, int dtype, int64_t x_stride, int64_t out_stride,
+                             const int32_t *pos, int n_axes, const uint8_t *axis, const float *inv_freq, int n_pairs, int rope_layout, int inverse,
+                             void *stream) {
+    clear_error();
+    if (n_rows != 0 && (!x || !out || !pos)) return fail(SSD_ERR_INVALID_ARG, "x, out or pos is NULL");
+    if (!inv_freq) return fail(SSD_ERR_INVALID_ARG, "inv_freq is NULL");
+    if (dtype != SSD_F32 && dtype != SSD_BF16) return fail(SSD_ERR_INVALID_ARG, "dtype=%d is neither SSD_F32 nor SSD_BF16", dtype);
+    if (n_rows < 0) return fail(SSD_ERR_INVALID_ARG, "n_rows=%d must be >= 0", n_rows);
+    if (n_heads < 1 || n_heads > 4096) return fail(SSD_ERR_INVALID_ARG, "n_heads=%d outside 1..4096", n_heads);
+    if (head_dim < 2 || head_dim > 1024 || head_dim % 2 != 0) return fail(SSD_ERR_INVALID_ARG, "head_dim=%d must be even, 2..1024", head_dim);
+    if (n_pairs < 1 || n_pairs > head_dim / 2) return fail(SSD_ERR_INVALID_ARG, "n_pairs=%d outside 1..head_dim / 2", n_pairs);
+    if (n_axes < 1 || n_axes > 4) return fail(SSD_ERR_INVALID_ARG, "n_axes=%d outside 1..4", n_axes);
+    if (!axis && n_axes != 1) return fail(SSD_ERR_INVALID_ARG, "axis is NULL with n_axes=%d", n_axes);
+    if (rope_layout != SSD_ROPE_HALF && rope_layout != SSD_ROPE_INTERLEAVED) return fail(SSD_ERR_INVALID_ARG, "rope_layout=%d", rope_layout);
+    if (inverse != 0 && inverse != 1) return fail(SSD_ERR_INVALID_ARG, "inverse=%d is neither 0 nor 1", inverse);
+    const int64_t e = dtype == SSD_F32 ? 4 : 2, row = (int64_t)n_heads * head_dim;
+    if ((x_stride != 0 && (x_stride < row || x_stride > 1ll << 40)) || (out_stride != 0 && (out_stride < row || out_stride > 1ll << 40)))
+        return fail(SSD_ERR_INVALID_ARG, "x_stride and out_stride must be 0 or at least n_heads * head_dim");
+    if (!aligned(x, e) || !aligned(out, e) || !aligned(pos, 4) || !aligned(inv_freq, 4))
+        return fail(SSD_ERR_INVALID_ARG, "x, out, pos and inv_freq must be aligned to their elements");
+    RopeArgs a;
+    a.x_stride = (x_stride ? x_stride : row) * e;
+    a.out_stride = (out_stride ? out_stride : row) * e;
+    // Rows of one array onto themselves, or two arrays that have nothing in common
+    const char *x0 = static_cast<const char *>(x), *o0 = static_cast<const char *>(out);
+    const int64_t x_size = n_rows > 0 ? (n_rows - 1) * a.x_stride + row * e : 0, o_size = n_rows > 0 ? (n_rows - 1) * a.out_stride + row * e : 0;
+    if (x0 == o0 ? n_rows > 1 && a.x_stride != a.out_stride : x0 < o0 + o_size && o0 < x0 + x_size)
+        return fail(SSD_ERR_INVALID_ARG, "out must be x with the same stride, or share no memory with it");
+    if (n_rows == 0) return SSD_OK;
+    a.x = x0;
+    a.out = static_cast<char *>(out);
+    a.pos = pos;
+    a.axis = axis;
+    a.inv_freq = inv_freq;
+    a.n = n_rows;
+    a.heads = n_heads;
+    a.d = head_dim;
+    a.pairs = n_pairs;
+    a.axes = n_axes;
+    a.sign = inverse ? -1.f : 1.f;
+    // the longest run, up to 16 bytes, that all sizes, strides and addresses are multiples of
+    const uint64_t bits = (uint64_t)a.x_stride | (uint64_t)a.out_stride | (uintptr_t)x | (uintptr_t)out | (uint64_t)(head_dim * e) |
+                          (uint64_t)((rope_layout == SSD_ROPE_HALF ? n_pairs : 2 * n_pairs) * e) | 16u;
+    const int vec = (int)((int64_t)(bits & (0 - bits)) / e);
+    a.tokens = 1;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool half = rope_layout == SSD_ROPE_HALF;
+    if (dtype == SSD_F32) half ? launch_rope<float, true>(a, vec, s) : launch_rope<float, false>(a, vec, s);
+    else half ? launch_rope<bf16_t, true>(a, vec, s) : launch_rope<bf16_t, false>(a, vec, s);
+    const hipError_t err = hipGetLastError();
+    return err == hipSuccess ? SSD_OK : hip_fail(err, "rope launch");
+}
