@@ -454,11 +454,17 @@ class SsdPagedConfig(C.Structure):
 
     def __setattr__(self, name, value):
         super().__setattr__(name, value)
-        self.__dict__.pop("strides", None)
+        self.__dict__.clear()
 
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
-        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; found when it is first asked for after a field was set."""
+        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes and the bytes of their scales.
+        Found when they are first asked for after a field was set."""
+        if name == "mx_strides":
+            places = (self.n_pages, self.n_kv_heads, self.page_size)
+            got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,),
+                                                places[0] * places[1] * places[2] * (self.head_dim // 32)) for bits in (4, 8)}
+            return got
         if name != "strides":
             raise AttributeError(name)
         d, row = self.head_dim, self.row_stride or self.head_dim
@@ -682,15 +688,9 @@ def _format_code(format) -> int:
     return _FORMATS[format]
 
 
-def _mx_pool(t, what: str, cfg, bits: int) -> Optional[int]:
-    """Address of a pool of codes: bytes [n_pages, n_kv_heads, page_size, d * bits / 8] with the config's strides (or the same with page_size before
-    n_kv_heads, as it lies in memory then), or memory without gaps that reaches as far."""
-    if t is None or isinstance(t, int):
-        return t
+def _check_mx_pool(t, what: str, want, sizes) -> None:
     if t.element_size() != 1:
         raise ValueError("%s of type %s: a pool of codes is bytes" % (what, t.dtype))
-    want = tuple(s * bits // 8 for s in cfg.strides[0][:3]) + (1,)
-    sizes = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim * bits // 8)
     if tuple(t.shape) == sizes:
         fits = all(size == 1 or stride == w for size, stride, w in zip(sizes, t.stride(), want))
         if not fits and sizes[1] == sizes[2]:                      # which of the two dimensions is which, the strides say
@@ -701,23 +701,33 @@ def _mx_pool(t, what: str, cfg, bits: int) -> Optional[int]:
         fits = t.is_contiguous() and sum((size - 1) * w for size, w in zip(sizes, want)) < t.numel()
     if not fits:
         raise ValueError("%s of shape %s, strides %s: the config says bytes [%d, %d, %d, %d] with strides %s" % ((what, tuple(t.shape), t.stride()) + sizes + (want,)))
-    return t.data_ptr()
 
 
-def _mx_scales(t, what: str, cfg) -> Optional[int]:
-    """Address of the scales [n_pages, n_kv_heads, page_size, d / 32]: bytes without gaps."""
+def _mx_scales(t, what: str, need: int) -> Optional[int]:
+    """Address of the scales: `need` bytes without gaps."""
     if t is None or isinstance(t, int):
         return t
-    need = cfg.n_pages * cfg.n_kv_heads * cfg.page_size * (cfg.head_dim // 32)
     if t.element_size() != 1 or not t.is_contiguous() or t.numel() < need:
         raise ValueError("%s of shape %s, strides %s, type %s: %d bytes without gaps are expected" % (what, tuple(t.shape), t.stride(), t.dtype, need))
     return t.data_ptr()
 
 
+def _mx_pool(t, what: str, want, sizes) -> Optional[int]:
+    """Address of a pool of codes: bytes [n_pages, n_kv_heads, page_size, d * bits / 8] with the config's strides (or the same with page_size before
+    n_kv_heads, as it lies in memory then), or memory without gaps that reaches as far."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.stride() != want or t.shape != sizes or t.element_size() != 1:
+        _check_mx_pool(t, what, want, sizes)
+    return t.data_ptr()
+
+
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
-    bits = _format_code(format)
-    return (bits, _mx_pool(k_pages, "k_pages", cfg, bits), _mx_pool(v_pages, "v_pages", cfg, bits), _mx_scales(k_scales, "k_scales", cfg),
-            _mx_scales(v_scales, "v_scales", cfg))
+    """The format's code, and the addresses of two pools of codes and their scales."""
+    bits = _FORMATS.get(format) or _format_code(format)
+    want, sizes, need = cfg.mx_strides[bits]
+    return (bits, _mx_pool(k_pages, "k_pages", want, sizes), _mx_pool(v_pages, "v_pages", want, sizes), _mx_scales(k_scales, "k_scales", need),
+            _mx_scales(v_scales, "v_scales", need))
 
 
 def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, k_new, v_new, pos=None, weight=None,

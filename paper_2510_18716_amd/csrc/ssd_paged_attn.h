@@ -1,8 +1,10 @@
 // What the attention over a paged cache shares, whatever the pool holds: who works on which rows, the pass over a unit's tiles with the running softmax, the
 // meeting of parts, the weights, and the launches.  A tile's operands and products are the including file's: a type TT with
-//   elem, D, ROWS, NV     element type of q and the output, row length, rows of a tile, tiles of V^T P
+//   elem, D, ROWS, NO     element type of q and the output, row length, rows of a tile, accumulators
+//   RESIDENT              waves of a SIMD that the registers are to allow
 //   MX                    whether the pool holds codes with scales (the newest row of a step then goes into the pool first)
-//   Q, load_q, logits, zero_v, accumulate, column
+//   TABLE                 whether every wave keeps the addresses of its own tiles' rows (else the workgroup has the pages' in LDS)
+//   Q, load_q, head, logits, zero_v, accumulate, finish, column
 //   Rows<QUADS>           where a lane finds a tile's rows; seen() tells which of them exist
 // and functions find_k, find_v, hold_k, hold_v, request_k, request_v on them.  QUADS: four rows from a multiple of four on lie in one page.
 #pragma once
@@ -42,6 +44,7 @@ struct PagedAttnArgs {
 static constexpr int blocks_of(int waves) { return 256 * waves; }
 static constexpr int HEADS = 16;                                   // heads of a tile
 static constexpr int64_t NO_PAGE = -(1ll << 62);
+static constexpr int TABLE_TILES = 32;                             // tiles whose addresses a wave keeps, two lanes for each
 static constexpr float LN2 = 0.6931471805599453f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -58,6 +61,7 @@ static __device__ __forceinline__ int block_of(const PagedAttnArgs &a, int x) {
 struct Stage {
     const int64_t *pages;                                          // byte offsets of the blocks' pages (head included), or NO_PAGE
     const int32_t *ids;                                            // their numbers, -1 for none; where weights are brought up to date or the pool holds codes
+    int begin, b;                                                  // first row, sequence
     int lead, rows, kv;                                            // places before the first row in its page; rows; key head
 };
 
@@ -150,14 +154,14 @@ template <bool QUADS> static __device__ __forceinline__ void add_weights(const P
         if (x.at[e] >= 0) a.weight_out[x.at[e]] = x.w[e];
 }
 
-// Four rows' probabilities, summed over heads; z: the first head's logits of theirs, the others' `stride` apart.
-template <typename I> static __device__ __forceinline__ f32x4 probabilities(const float *z, I stride, const float *lse2, int heads) {
+// Four rows' probabilities, summed over heads; z: the first head's logits of theirs, the others' `stride` apart.  RAW: without the scale.
+template <bool RAW, typename I> static __device__ __forceinline__ f32x4 probabilities(const float *z, I stride, const float *lse2, int heads, float scale) {
     f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int h = 0; h < heads; ++h) {
         const f32x4 x = *reinterpret_cast<const f32x4 *>(z + h * stride);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] += fast_exp2(x[e] - lse2[h]);
+        for (int e = 0; e < 4; ++e) p[e] += fast_exp2(RAW ? fmaf(x[e], scale, -lse2[h]) : x[e] - lse2[h]);
     }
     return p;
 }
@@ -201,14 +205,14 @@ enum Weights { NONE, LATER, HERE };
 
 // grid = (workgroups), or (kv heads * tiles of query heads, sequences) where a workgroup takes a whole unit
 template <typename TT, bool QUADS, bool STEP, Weights WEIGHTS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs) {
+__global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(PagedAttnArgs) {
     typedef typename TT::elem T;
     constexpr int D = TT::D;
-    constexpr bool IDS = WEIGHTS == HERE || TT::MX;                 // the blocks' numbers are in LDS
+    constexpr bool IDS = !TT::TABLE && (WEIGHTS == HERE || TT::MX), PAGES = !TT::TABLE && !TT::MX;      // what of the blocks is in LDS
     constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
     constexpr int ROUND = WAVES * TT::ROWS;
     constexpr int LD = D + 4;                                       // row of the merge area
-    __shared__ int64_t pages[TT::MX ? 1 : blocks_of(WAVES)];
+    __shared__ int64_t pages[PAGES ? blocks_of(WAVES) : 1];
     __shared__ float sm_ml[WAVES][HEADS][2];
     __shared__ float sm_lse[HEADS];
     __shared__ uint32_t sm_runs[2];
@@ -332,7 +336,14 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             v_new = a.v_new + (int64_t)b * a.new_stride + (int64_t)kv * (D * sizeof(T));
         }
         typename TT::Q q;
-        TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (r < heads ? r : 0)) * (D * sizeof(T)), lane, q);
+        TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (TT::head(r) < heads ? TT::head(r) : 0)) * (D * sizeof(T)), lane, q);
+        int own_page = -1;                                          // HERE, TABLE: of a thread's four rows
+        if constexpr (WEIGHTS == HERE && TT::TABLE)
+            if (4 * (int)threadIdx.x < n) {
+                int block, place;
+                split_slot(a.g, 4 * (int)threadIdx.x, block, place);
+                own_page = page_of(a.g, b, block);
+            }
         // the unit's logits; lanes without a head are out of the buffer's bounds, and what they store is dropped
         __amdgpu_buffer_rsrc_t z_unit;
         uint32_t z_lane = 0;
@@ -343,31 +354,36 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         }
 
         float m = NEG_BIG, l = 0.f;
-        f32x4 o[TT::NV];
+        f32x4 o[TT::NO];
 #pragma unroll
-        for (int j = 0; j < TT::NV; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < TT::NO; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
         if constexpr (STEP && TT::MX)                               // the newest row's codes go where they belong, and are read like the others' behind the next barrier
-            if (newest) TT::put_newest(a, b, kv, n, k_new, v_new);
+            if (newest) {
+                TT::put_newest(a, b, kv, n, k_new, v_new);
+                if (TT::TABLE) __syncthreads();
+            }
 
         for (int row0 = begin; row0 < end;) {
             const PagedAttnArgs &a = arguments();
             const int rows = end - row0 < a.stage ? end - row0 : a.stage;
-            int block0, lead;
+            int block0 = 0, lead = 0;
+            if constexpr (!TT::TABLE) {
             split_slot(a.g, row0, block0, lead);
             const int blocks = block_of(a, rows - 1 + lead) + 1;
             __syncthreads();                                        // the last stage's entries, and a unit's merge area, have been read
             for (int i = threadIdx.x; i < blocks; i += 64 * WAVES) {
                 const int page = page_of(a.g, b, block0 + i);
                 if constexpr (IDS) page_ids[i] = page;
-                if constexpr (!TT::MX) pages[i] = page < 0 ? NO_PAGE : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
+                if constexpr (PAGES) pages[i] = page < 0 ? NO_PAGE : (int64_t)page * a.g.page_stride + (int64_t)kv * a.g.head_stride;
             }
             __syncthreads();
+            }
             const int last_row = newest && row0 + rows == n ? rows - 1 : 0x7fffffff;
 
             TT tl;
             typename TT::template Rows<QUADS> at;
-            const Stage st = {pages, page_ids, lead, rows, kv};
+            const Stage st = {pages, page_ids, row0, b, lead, rows, kv};
             auto request_keys = [&](int first) { request_k(std::bool_constant<STEP>(), a, at, tl, first, last_row, k_new, lane); };
             auto request_values = [&](int first) { request_v(std::bool_constant<STEP>(), a, at, tl, first, last_row, v_new, lane); };
             // One tile: its products and softmax step.  LAST: no tile follows.  Outside the last one every request is made without a condition,
@@ -383,8 +399,11 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                     hold_k(at, z[NZ - 1]);
                     request_keys(next);
                 }
+                const float scale = TT::MX ? a.scale : 1.f;          // codes: the logits stay as they are until the exponential
+                if constexpr (!TT::MX) {
 #pragma unroll
-                for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
+                    for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
+                }
                 if constexpr (WEIGHTS == HERE) {
                     if (r < heads)
 #pragma unroll
@@ -402,9 +421,10 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
 #pragma unroll
                     for (int e = 0; e < NZ; ++e) z[e] = seen.has(e) ? z[e] : NEG_BIG;
                 }
-                float top = m;
+                float top = TT::MX ? z[0] : m;
 #pragma unroll
                 for (int e = 0; e < NZ; ++e) top = fmaxf(top, z[e]);
+                if constexpr (TT::MX) top = fmaxf(m, top * scale);
                 {
                     float x, y;
                     rows_pair(top, x, y);
@@ -416,12 +436,12 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                     const float f = fast_exp2(m - top);
                     l *= f;
 #pragma unroll
-                    for (int j = 0; j < TT::NV; ++j) o[j] *= f;
+                    for (int j = 0; j < TT::NO; ++j) o[j] *= f;
                     m = top;
                 }
                 float p[NZ];
 #pragma unroll
-                for (int e = 0; e < NZ; ++e) p[e] = fast_exp2(z[e] - m);
+                for (int e = 0; e < NZ; ++e) p[e] = fast_exp2(TT::MX ? fmaf(z[e], scale, -m) : z[e] - m);
                 if (!all) {                                         // rows that do not exist: neither their p nor their V may count
 #pragma unroll
                     for (int e = 0; e < NZ; ++e)
@@ -435,7 +455,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
                 tl.accumulate(p, o);
                 if constexpr (!LAST) {
                     find_v(a, st, next, lane, at);
-                    hold_v(at, o[TT::NV - 1][0]);
+                    hold_v(at, o[TT::NO - 1][0]);
                     request_values(next);
                     asm volatile("" ::: "memory");                  // or the requests would move to the loop's head, behind K's
                 }
@@ -443,6 +463,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
             const int tiles = (rows + TT::ROWS - 1) / TT::ROWS;
             if (wave < tiles) {
                 int first = wave * TT::ROWS;
+                if constexpr (TT::TABLE) at.template begin<WAVES>(a, st, wave, lane);
                 find_k(a, st, first, lane, at);
                 request_keys(first);
                 find_v(a, st, first, lane, at);
@@ -478,7 +499,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         const int j = 4 * (int)threadIdx.x;
         Entries entries;
         if constexpr (WEIGHTS == HERE)
-            if (j < n) entries = entries_of<QUADS>(a, kv, j, n, [&](int block) { return page_ids[block]; });
+            if (j < n) entries = entries_of<QUADS>(a, kv, j, n, [&](int block) { return TT::TABLE ? own_page : page_ids[block]; });
         // the waves' states meet
         {
             float x, y;
@@ -489,14 +510,16 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         }
         if (!first_unit) __syncthreads();                           // a unit without rows passes no other barrier
         const int active = end - begin > (WAVES - 1) * TT::ROWS ? WAVES : end - begin > TT::ROWS ? (end - begin + TT::ROWS - 1) / TT::ROWS : 1;
-        if (r < heads && wave < active) {                           // the others have had no tile
-            if (g == 0) {
-                sm_ml[wave][r][0] = m;
-                sm_ml[wave][r][1] = l;
+        TT::finish(o);
+        if (TT::head(r) < heads && TT::writes(r) && wave < active) {        // the others have had no tile
+            const int h = TT::head(r);
+            if (g == 0 && r == h) {
+                sm_ml[wave][h][0] = m;
+                sm_ml[wave][h][1] = l;
             }
-            float *dst = sm_o + (wave * heads + r) * LD;
+            float *dst = sm_o + (wave * heads + h) * LD;
 #pragma unroll
-            for (int j = 0; j < TT::NV; ++j)
+            for (int j = 0; j < TT::NO; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) dst[TT::column(j, e, lane)] = o[j][e];
         }
@@ -532,7 +555,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_attn_kernel(PagedAttnArgs
         if constexpr (WEIGHTS == HERE) {
             __syncthreads();
             if (j < n)
-                add_weights<QUADS>(a, j, n, entries, probabilities(sm_o + WAVES * heads * LD + j, (int)a.z_stride + 4, sm_lse, heads), newest ? n - 1 : -1);
+                add_weights<QUADS>(a, j, n, entries, probabilities<TT::MX>(sm_o + WAVES * heads * LD + j, (int)a.z_stride + 4, sm_lse, heads, a.scale), newest ? n - 1 : -1);
             return;
         }
         if (a.workgroups && t == 0 && threadIdx.x == 0) {           // where the parts of a unit lie is told by who has its first round
@@ -680,13 +703,19 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
     const int newest = step && a.g.seq_len[b] == n ? n - 1 : -1;
     const float *z0 = a.z + ((int64_t)b * a.n_heads + kv * a.group) * a.z_stride;
     while (j < n) {
-        add_weights<QUADS>(a, j, n, entries, probabilities(z0 + j, a.z_stride, lse2, a.group), newest);
+        add_weights<QUADS>(a, j, n, entries, probabilities<TT::MX>(z0 + j, a.z_stride, lse2, a.group, a.scale), newest);
         j += ((int)gridDim.z - head_blocks) * 1024;
         if (j < n) entries = entries_of<QUADS>(a, kv, j, n, page);
     }
 }
 
 // ---- launch shapes ---------------------------------------------------------------------------------------------------
+
+// What the launch goes by of a tile: its rows, workgroups of four waves that are resident at once, whether waves keep their rows' addresses (TABLE).
+struct TileShape {
+    int rows, resident;
+    bool table;
+};
 
 struct PagedShape {
     int waves, round, q_tiles, tile_heads, workgroups, stage;
@@ -695,9 +724,9 @@ struct PagedShape {
     size_t lds;               // where the waves meet
 };
 
-// tile: rows of a tile
-static PagedShape paged_shape(const ssd_paged_config *c, int max_len, int tile) {
+static PagedShape paged_shape(const ssd_paged_config *c, int max_len, const TileShape &ts) {
     PagedShape s;
+    const int tile = ts.rows;
     const int reach = paged_reach(c, max_len), group = c->n_heads / c->n_kv_heads;
     s.q_tiles = (group + HEADS - 1) / HEADS;
     s.tile_heads = group < HEADS ? group : HEADS;
@@ -713,7 +742,7 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, int tile) 
     s.round = s.waves * tile;
     // 256 compute units, four or three workgroups each; twice as many are no better (128 sequences of 10 to 8000 rows 67 and 69 us, with weights 87 and 87, of 1195 rows
     // 63.5 and 66.7; fp32 of 64 elements, 48 of up to 5000 rows, 37.4 and 39.8, with three each 38)
-    const int64_t resident = c->head_dim == 64 ? 1024 : 768;
+    const int64_t resident = ts.resident;
     s.workgroups = plain ? 0 : (int)(units * rounds < resident ? units * rounds : resident);
     // Where not all units are resident at once a late long one would run on alone; ranking costs every workgroup a microsecond (32 heads of 64 to 640
     // rows, 64 sequences 54 us in their order and 50 by length, 128 96 and 95, of 10 to 1000 rows 94 and 89; 256 168 and 173, 16 17.3 and 19.0).
@@ -721,6 +750,7 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, int tile) 
     // a stage's blocks: its rows and what lies before them in the first one; block_of allows 2^16 rows
     const int64_t most = (int64_t)(blocks_of(s.waves) - 1) * c->page_size;
     s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);
+    if (ts.table) s.stage = TABLE_TILES * s.round;
     s.lds = (size_t)s.waves * s.tile_heads * (c->head_dim + 4) * sizeof(float);
     // The weights are brought up to date by the unit's own workgroup, from logits in LDS (up to 66 KB), where it takes one tile of heads (2 sequences of
     // 64 to 97 rows, 16 heads 6.5 us, by a second launch 10.2; 128 of 64 to 640 rows, 32 heads 100 and 103, 256 query heads on 32 111 and 130, on 16 with
@@ -788,8 +818,8 @@ struct AttendCall {
     bool step;
 };
 
-// The checks of everything but the config, then the kernels' arguments and the launch's shape.  tile: rows of a tile; bits: of an element of the pool.
-static inline int attend_args(const AttendCall &c, int tile, int bits, PagedAttnArgs &a, PagedShape &shape) {
+// The checks of everything but the config, then the kernels' arguments and the launch's shape.  bits: of an element of the pool.
+static inline int attend_args(const AttendCall &c, const TileShape &tile, int bits, PagedAttnArgs &a, PagedShape &shape) {
     int rc;
     if ((rc = check_max_len(c.cfg, c.max_len)) != SSD_OK) return rc;
     if (!c.q || !c.k_pages || !c.v_pages || !c.out) return fail(SSD_ERR_INVALID_ARG, "q, k_pages, v_pages or out is NULL");

@@ -126,11 +126,15 @@ template <typename T, int D> struct Tile;
 
 template <int D_> struct Tile<bf16_t, D_> {
     typedef bf16_t elem;
-    static constexpr bool MX = false;
+    static constexpr bool MX = false, TABLE = false;
+    static constexpr int RESIDENT = 3;
+    static __device__ __forceinline__ int head(int r) { return r; }
+    static __device__ __forceinline__ bool writes(int) { return true; }
     template <bool QUADS> using Rows = TileRows<true, QUADS>;
     static constexpr int D = D_, ROWS = 32, STEPS = D / 32;                // STEPS: 64-byte pieces of a row of K
     static constexpr int VB = D / 8;                               // bytes of a row of V in a lane: 16 or 8
-    static constexpr int NV = D / 16;                              // tiles of V^T P
+    static constexpr int NV = D / 16, NO = NV;                     // tiles of V^T P
+    static __device__ __forceinline__ void finish(f32x4 (&)[NO]) {}
     typedef uint32_t vrow_t __attribute__((ext_vector_type(VB / 4)));
     u32x4_nt_t k[2][STEPS];
     vrow_t v[8];
@@ -187,10 +191,14 @@ template <int D_> struct Tile<bf16_t, D_> {
 
 template <int D_> struct Tile<float, D_> {
     typedef float elem;
-    static constexpr bool MX = false;
+    static constexpr bool MX = false, TABLE = false;
+    static constexpr int RESIDENT = 3;
+    static __device__ __forceinline__ int head(int r) { return r; }
+    static __device__ __forceinline__ bool writes(int) { return true; }
     template <bool QUADS> using Rows = TileRows<false, QUADS>;
     static constexpr int D = D_, ROWS = 16, STEPS = D / 16;
-    static constexpr int HALVES = D / 64, NV = D / 16;
+    static constexpr int HALVES = D / 64, NV = D / 16, NO = NV;
+    static __device__ __forceinline__ void finish(f32x4 (&)[NO]) {}
     u32x4_nt_t k[1][STEPS];
     u32x4_nt_t v[4][HALVES];
     struct Q { f32x4 x[STEPS]; };
@@ -234,7 +242,7 @@ template <typename T, int D> static hipError_t launch_tiles(const PagedAttnArgs 
     return a.g.page_size % 4 == 0 ? launch_paged_attn<Tile<T, D>, true>(a, sh, step, s) : launch_paged_attn<Tile<T, D>, false>(a, sh, step, s);
 }
 
-static int tile_rows(const ssd_paged_config *c) { return c->dtype == SSD_BF16 ? 32 : 16; }
+static TileShape tile_shape(const ssd_paged_config *c) { return {c->dtype == SSD_BF16 ? 32 : 16, c->head_dim == 64 ? 1024 : 768, false}; }
 
 static int paged_attend(const AttendCall &c, hipStream_t s) {
     clear_error();
@@ -242,7 +250,7 @@ static int paged_attend(const AttendCall &c, hipStream_t s) {
     if (rc != SSD_OK) return rc;
     PagedAttnArgs a;
     PagedShape shape;
-    if ((rc = attend_args(c, tile_rows(c.cfg), 8 * (int)paged_esize(c.cfg), a, shape)) != SSD_OK) return rc;
+    if ((rc = attend_args(c, tile_shape(c.cfg), 8 * (int)paged_esize(c.cfg), a, shape)) != SSD_OK) return rc;
     hipError_t e;
     if (c.cfg->dtype == SSD_BF16) e = c.cfg->head_dim == 128 ? launch_tiles<bf16_t, 128>(a, shape, c.step, s) : launch_tiles<bf16_t, 64>(a, shape, c.step, s);
     else e = c.cfg->head_dim == 128 ? launch_tiles<float, 128>(a, shape, c.step, s) : launch_tiles<float, 64>(a, shape, c.step, s);
@@ -256,7 +264,7 @@ using namespace ssd;
 extern "C" size_t ssd_paged_workspace_bytes(const ssd_paged_config *cfg, int max_len, int with_weights) {
     clear_error();
     if (check_paged(cfg) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
-    return paged_scratch(cfg, paged_shape(cfg, max_len, tile_rows(cfg)), with_weights != 0).all;
+    return paged_scratch(cfg, paged_shape(cfg, max_len, tile_shape(cfg)), with_weights != 0).all;
 }
 
 extern "C" int ssd_paged_decode_attn(const ssd_paged_config *cfg, const void *q, const void *k_pages, const void *v_pages,

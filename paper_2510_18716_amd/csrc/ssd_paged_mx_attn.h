@@ -1,9 +1,16 @@
 // The attention over a paged cache held in 8 or 4 bits: a tile's operands from codes and scales.
 //
 // Both products run on the matrix cores in bf16, which holds every element of either format exactly; the conversion multiplies by the block's scale on the
-// way (one instruction for two elements).  A lane's part of a row of K is a run of D / 4 elements, so that with rows of 128 it has one block and one scale;
-// q is laid out alike.  V as in the tiles of plain rows: D / 16 columns of eight rows in a lane, turned by byte permutations after the conversion.
-// fp32 calls split q into three bf16 terms and the probabilities too (24 bits of both); bf16 calls take q as it is and probabilities in two terms.
+// way (one instruction for two elements).  The cores' own products of scaled blocks (v_mfma_scale_f32_16x16x128_f8f6f4, q in two terms of eight bits) would save the conversion
+// of K, but their sums are off by up to 2^-13 of sum |q k|, measured, where those of bf16 are fp32's.
+// A lane's part of a row of K is a run of D / 4 elements, so that with rows of 128 it has one block and one scale; q is laid out alike.
+// V: D / 16 columns of eight rows in a lane.  fp32 calls split q into three bf16 terms and the probabilities too (24 bits of both); bf16 calls take q as it is
+// and probabilities in two terms.
+//
+// With four bits a row's bytes are so few that instructions bound the kernel as soon as memory: 166 vector instructions for 32 rows of 128 elements, 64 of them
+// conversions (290 before: V turned by byte permutations 32, addresses added lane by lane 14, logits scaled on their own 8, the workgroup's page addresses looked
+// up in LDS; 4 sequences of 30000 to 131072 rows 63 -> 59 us, 128 of 64 to 640 rows of 32 heads 48 -> 38).  Tried and taken back: tiles of 64 rows (70 and 57 us: the
+// registers do not hold them), tiles that pass through LDS by direct loads (64 and 51).
 #pragma once
 
 #include "ssd_mx.h"
@@ -16,8 +23,25 @@ namespace ssd {
 template <int SUB, int SB, bool P16> struct MxRows;
 
 template <int SUB, int SB> struct MxRows<SUB, SB, true> {
-    int64_t off[SUB], soff[SUB];                                   // bytes from the pools' and the scales' beginnings
-    int left[SUB];                                                 // rows there are from the group's first on
+    // A lane has 16 rows of the wave's tiles in this chunk: lane SUB k + s group s of tile k.  Byte offset in the pool (the upper half below zero: no page), and
+    // first place in the tables by 16.
+    uint32_t low, group;
+    int high, next;                                                // next: the lane of the tile to come
+    int64_t off[SUB], soff[SUB];                                   // that tile's: bytes from the pools' and the scales' beginnings
+    int left[SUB];                                                 // rows there are from a group's first on
+
+    template <int WAVES> __device__ __forceinline__ void begin(const PagedAttnArgs &a, const Stage &st, int wave, int lane) {
+        static_assert(SUB * TABLE_TILES == 64, "a lane for each group of 16 rows");
+        const int x = (wave + lane / SUB * WAVES) * (16 * SUB) + lane % SUB * 16;
+        int block, place;
+        split_slot(a.g, st.begin + (x < st.rows ? x : 0), block, place);
+        const int page = page_of(a.g, st.b, block);
+        const int64_t at = row_offset(a.g, page, st.kv, place);
+        low = (uint32_t)at;
+        high = page < 0 ? -1 : (int)(at >> 32);
+        group = ((uint32_t)page * (uint32_t)a.g.n_kv + (uint32_t)st.kv) * (uint32_t)(a.g.page_size / 16) + (uint32_t)place / 16;
+        next = 0;
+    }
     struct Seen {
         int left[SUB], own;                                        // own: the lane's first row in a group
         __device__ __forceinline__ bool all() const {
@@ -49,16 +73,16 @@ template <int SUB, int SB> struct MxRows<SUB, SB, false> {
 };
 
 template <int SUB, int SB>
-static __device__ __forceinline__ void find_k(const PagedAttnArgs &a, const Stage &st, int first, int, MxRows<SUB, SB, true> &t) {
+static __device__ __forceinline__ void find_k(const PagedAttnArgs &, const Stage &st, int first, int, MxRows<SUB, SB, true> &t) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
-        const int x = first + 16 * s, y = (x < st.rows ? x : (st.rows - 1) & ~15) + st.lead;
-        const int block = block_of(a, y), place = y - block * a.g.page_size;
-        const int id = __builtin_amdgcn_readfirstlane(st.ids[block]), page = id < 0 ? 0 : id;
-        t.off[s] = row_offset(a.g, page, st.kv, place);
-        t.soff[s] = table_index(a.g, page, st.kv, place) * SB;
-        t.left[s] = id < 0 ? 0 : st.rows - x;
+        const int high = __builtin_amdgcn_readlane(t.high, t.next + s);
+        const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)t.low, t.next + s), group = (uint32_t)__builtin_amdgcn_readlane((int)t.group, t.next + s);
+        t.off[s] = high < 0 ? 0 : (int64_t)((uint64_t)(uint32_t)high << 32 | low);
+        t.soff[s] = high < 0 ? 0 : (int64_t)((uint64_t)group * (16 * SB));
+        t.left[s] = high < 0 ? 0 : st.rows - first - 16 * s;
     }
+    t.next += SUB;
 }
 template <int SUB, int SB>
 static __device__ __forceinline__ void find_v(const PagedAttnArgs &, const Stage &, int, int, MxRows<SUB, SB, true> &) {}
@@ -118,14 +142,23 @@ static __device__ __forceinline__ uint32_t take_upper(float &x) {
     return hi >> 16;
 }
 
-template <typename T, int D_, int BITS_, bool P16> struct MxTile {
+// HT: heads of a tile, 4, 8 or 16.  The matrix cores' sixteen columns hold COPIES = 16 / HT columns for a head.  With two, one takes the even elements of a
+// pair (V's columns 2 c), the other the odd ones: a pair is the operand as it comes from the conversion, two neighbouring places of the sum, and a copy has its
+// probability in one of them and nothing in the other.  So V is not turned at all, and the sums take half the registers.  With four (bf16 calls) two more take
+// the probabilities' second term.
+template <typename T, int D_, int BITS_, bool P16, int HT> struct MxTile {
     typedef T elem;
-    static constexpr bool MX = true;
+    static constexpr bool MX = true, TABLE = P16;
+    static constexpr int RESIDENT = 3;
     static constexpr int D = D_, BITS = BITS_, SB = D / 32;        // SB: bytes of a row's scales
     static constexpr int SUB = 2, ROWS = 16 * SUB;
     static constexpr int STEPS = D / 32, NV = D / 16, KE = D / 4;  // KE: elements of a row of K in a lane
     static constexpr int KW = KE * BITS / 32, VB = NV * BITS / 8;  // dwords of those; bytes of a row of V in a lane
     static constexpr int QT = sizeof(T) == 4 ? 3 : 1, PT = sizeof(T) == 4 ? 3 : 2;      // terms of q and of the probabilities
+    static constexpr int COPIES = 16 / HT, NO = COPIES == 1 ? NV : NV / 2;
+    static_assert(COPIES < 4 || PT == 2, "four copies have two terms");
+    static __device__ __forceinline__ int head(int r) { return r % HT; }
+    static __device__ __forceinline__ bool writes(int r) { return r < 2 * HT; }
     template <bool QUADS> using Rows = MxRows<SUB, SB, P16>;
     typedef typename Words<KW>::type krow_t;
     typedef std::conditional_t<VB == 2, uint16_t, typename Words<VB == 8 ? 2 : 1>::type> vrow_t;
@@ -138,6 +171,8 @@ template <typename T, int D_, int BITS_, bool P16> struct MxTile {
     std::conditional_t<P16, four_t, one_t> vs[P16 ? SUB : 4 * SUB];
     struct Q { bf16x8 x[QT][STEPS]; };
 
+    static __device__ __forceinline__ int odd(int lane) { return (lane & 15) / HT & 1; }
+    static __device__ __forceinline__ bool second(int lane) { return (lane & 15) / (2 * HT) & 1; }
     template <typename X> static __device__ __forceinline__ X load(const char *p) { return __builtin_nontemporal_load(reinterpret_cast<const X *>(p)); }
 
     static __device__ __forceinline__ void load_q(const char *row, int lane, Q &q) {
@@ -224,14 +259,26 @@ template <typename T, int D_, int BITS_, bool P16> struct MxTile {
         else vs[i / 4][i % 4 / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
     }
 
-    // o[j] += column d = NV m + j of V, times p.  The probabilities go in as terms of bf16, each the upper half of what the one before leaves; the last
-    // one of two is rounded: 16 bits of each or more (2^-17), of three 24.
-    __device__ __forceinline__ void accumulate(const float (&p)[4 * SUB], f32x4 (&o)[NV]) const {
+    // x less one of two bf16 (`which`: -1 in its place, 0 in the other's), exactly: the upper half of x, so that what is left has fewer bits.
+    static __device__ __forceinline__ float less(float x, uint32_t two, uint32_t which) {
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, two), __builtin_bit_cast(bf16x2_t, which), x, false);
+    }
+    __device__ __forceinline__ uint32_t v_pair(int i, int c, float scale) const {
+        if constexpr (VB == 8) return pair(v[i][c / 2], scale, c % 2);
+        else return pair((uint32_t)v[i], scale, c);
+    }
+
+    // Sums of V's columns times p.  The probabilities go in as terms of bf16, each the upper half of what the one before leaves: 16 bits of each (two terms; the
+    // last one rounded where a head has one column, else cut off) or 24 (three).
+    __device__ __forceinline__ void accumulate(const float (&p)[4 * SUB], f32x4 (&o)[NO]) const {
         const int lane = threadIdx.x & 63;
+        if constexpr (COPIES == 1) {
+            // -1 as the lower and as the upper of two bf16, from registers: as a constant the lower one is encoded as the fp32 number -1, which is the upper
+            uint32_t lower = 0x0000bf80u, upper = 0xbf800000u;
+            asm("" : "+s"(lower), "+s"(upper));
 #pragma unroll
-        for (int t = 0; t < SUB / 2; ++t) {
-            bf16x8 term[PT];
-            {
+            for (int t = 0; t < SUB / 2; ++t) {
+                bf16x8 term[PT];
                 float rest[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) rest[i] = p[8 * t + i];
@@ -244,36 +291,77 @@ template <typename T, int D_, int BITS_, bool P16> struct MxTile {
                         continue;
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; i += 2) d[i / 2] = __builtin_amdgcn_perm(__float_as_uint(rest[i + 1]), __float_as_uint(rest[i]), 0x07060302u);
+                    for (int i = 0; i < 8; i += 2) {
+                        const uint32_t two = __builtin_amdgcn_perm(__float_as_uint(rest[i + 1]), __float_as_uint(rest[i]), 0x07060302u);
+                        d[i / 2] = two;
+                        rest[i] = less(rest[i], two, lower);
+                        rest[i + 1] = less(rest[i + 1], two, upper);
+                    }
                     term[m] = __builtin_bit_cast(bf16x8, d);
+                }
+                float scale[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) rest[i] -= __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
+                for (int i = 0; i < 8; ++i) scale[i] = v_scale(8 * t + i, lane);
+#pragma unroll
+                for (int c = 0; c < NV / 2; ++c) {
+                    uint32_t x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = v_pair(8 * t + i, c, scale[i]);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        u32x4_nt_t w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], half ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                        for (int m = PT - 1; m >= 0; --m)
+                            o[2 * c + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), term[m], o[2 * c + half], 0, 0, 0);
+                    }
                 }
             }
-            float scale[8];
+        } else {
+            constexpr int TERMS = COPIES == 4 ? 1 : PT;
+            const uint32_t take = odd(lane) ? 0x07060c0cu : 0x0c0c0706u;        // the upper half of a number, in the copy's place
+            const uint32_t which = odd(lane) ? 0xbf800000u : 0x0000bf80u, less_first = second(lane) ? 0xffff0000u : 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) scale[i] = v_scale(8 * t + i, lane);
+            for (int t = 0; t < SUB; ++t) {
+                u32x4_nt_t term[TERMS];
 #pragma unroll
-            for (int c = 0; c < NV / 2; ++c) {
-                uint32_t x[8];
+                for (int i = 0; i < 4; ++i) {
+                    float x = p[4 * t + i];
+                    if constexpr (COPIES == 4) x -= __uint_as_float(__float_as_uint(x) & less_first);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (VB == 8) x[i] = pair(v[8 * t + i][c / 2], scale[i], c % 2);
-                    else x[i] = pair((uint32_t)v[8 * t + i], scale[i], c);
+                    for (int m = 0; m < TERMS; ++m) {
+                        const uint32_t two = __builtin_amdgcn_perm(__float_as_uint(x), 0u, take);
+                        term[m][i] = two;
+                        if (m + 1 < TERMS) x = less(x, two, which);
+                    }
                 }
+                float scale[4];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                for (int i = 0; i < 4; ++i) scale[i] = v_scale(4 * t + i, lane);
+#pragma unroll
+                for (int c = 0; c < NV / 2; ++c) {
                     u32x4_nt_t w;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], half ? 0x07060302u : 0x05040100u);
+                    for (int i = 0; i < 4; ++i) w[i] = v_pair(4 * t + i, c, scale[i]);
 #pragma unroll
-                    for (int m = PT - 1; m >= 0; --m)
-                        o[2 * c + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), term[m], o[2 * c + half], 0, 0, 0);
+                    for (int m = TERMS - 1; m >= 0; --m)
+                        o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, term[m]), o[c], 0, 0, 0);
                 }
             }
         }
     }
-    static __device__ __forceinline__ int column(int j, int i, int lane) { return NV * (4 * (lane >> 4) + i) + j; }
+    // The copies' terms meet.
+    static __device__ __forceinline__ void finish(f32x4 (&o)[NO]) {
+        if constexpr (COPIES == 4) {
+#pragma unroll
+            for (int j = 0; j < NO; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][e] += dpp_f<0x128>(o[j][e]);      // eight lanes on
+        }
+    }
+    // column of o[j][i] in lane
+    static __device__ __forceinline__ int column(int j, int i, int lane) { return NV * (4 * (lane >> 4) + i) + (COPIES == 1 ? j : 2 * j + odd(lane)); }
 
     // A step's newest row: its codes into the pool, by every workgroup that is about to read it (all write the same).
     static __device__ __forceinline__ void put_newest(const PagedAttnArgs &a, int b, int kv, int n, const char *k_new, const char *v_new) {
@@ -297,20 +385,43 @@ template <typename T, int D_, int BITS_, bool P16> struct MxTile {
     }
 };
 
+// Bytes at base + more + own, base and more being the same for all lanes: through a buffer, whose address is in scalar registers (as a pointer the compiler adds
+// it lane by lane, 14 of 250 vector instructions).  NT: read once.
+static __device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const void *base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, -1, 0x00027000);
+}
+template <typename X, int NT> static __device__ __forceinline__ X mx_load(__amdgpu_buffer_rsrc_t from, uint32_t own, uint32_t more) {
+    if constexpr (sizeof(X) == 32) {
+        const u32x4_nt_t lo = mx_load<u32x4_nt_t, NT>(from, own, more), hi = mx_load<u32x4_nt_t, NT>(from, own + 16, more);
+        return X{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    } else if constexpr (sizeof(X) == 16) {
+        return __builtin_bit_cast(X, __builtin_amdgcn_raw_buffer_load_b128(from, (int)own, (int)more, NT));
+    } else if constexpr (sizeof(X) == 8) {
+        return __builtin_bit_cast(X, __builtin_amdgcn_raw_buffer_load_b64(from, (int)own, (int)more, NT));
+    } else if constexpr (sizeof(X) == 4) {
+        return __builtin_bit_cast(X, __builtin_amdgcn_raw_buffer_load_b32(from, (int)own, (int)more, NT));
+    } else {
+        return (X)__builtin_amdgcn_raw_buffer_load_b16(from, (int)own, (int)more, NT);
+    }
+}
 template <typename Step, typename TT, int SUB, int SB>
 static __device__ __forceinline__ void request_k(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, true> &at, TT &tl, int, int, const char *, int lane) {
-    const uint32_t r = (uint32_t)lane & 15, own = r * (uint32_t)a.g.row_stride;
+    const uint32_t r = (uint32_t)lane & 15, g = (uint32_t)lane >> 4, own = r * (uint32_t)a.g.row_stride + g * (TT::KE * TT::BITS / 8);
 #pragma unroll
-    for (int s = 0; s < SUB; ++s) tl.load_k(s, a.k_pages + at.off[s] + own, reinterpret_cast<const char *>(a.k_scales) + at.soff[s] + r * SB, lane);
+    for (int s = 0; s < SUB; ++s) {
+        tl.k[s] = mx_load<typename TT::krow_t, 2>(mx_buffer(a.k_pages + at.off[s]), own, 0);
+        tl.ks[s] = __builtin_amdgcn_raw_buffer_load_b8(mx_buffer(a.k_scales + at.soff[s]), (int)(r * SB + g * TT::KE / 32), 0, 0);
+    }
 }
 template <typename Step, typename TT, int SUB, int SB>
 static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, true> &at, TT &tl, int, int, const char *, int lane) {
     const uint32_t g = (uint32_t)lane >> 4, own = 4 * g * (uint32_t)a.g.row_stride + ((uint32_t)lane & 15) * TT::VB;
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
+        const __amdgpu_buffer_rsrc_t from = mx_buffer(a.v_pages + at.off[s]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tl.v[4 * s + i] = TT::template load<typename TT::vrow_t>(a.v_pages + at.off[s] + i * a.g.row_stride + own);
-        tl.vs[s] = *reinterpret_cast<const typename TT::four_t *>(reinterpret_cast<const char *>(a.v_scales) + at.soff[s] + g * (4 * SB));
+        for (int i = 0; i < 4; ++i) tl.v[4 * s + i] = mx_load<typename TT::vrow_t, 2>(from, own, (uint32_t)i * (uint32_t)a.g.row_stride);
+        tl.vs[s] = mx_load<typename TT::four_t, 0>(mx_buffer(a.v_scales + at.soff[s]), g * (4 * SB), 0);
     }
 }
 template <typename Step, typename TT, int SUB, int SB>
@@ -327,17 +438,26 @@ static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, c
     }
 }
 
-static inline bool mx_sixteen(const PagedGeom &g) { return g.page_size % 16 == 0 && g.row_stride < 1 << 26; }
+// Whether 16 rows are neighbours, at distances that fit 32 bits.
+static inline bool mx_sixteen(const ssd_paged_config *c) {
+    return c->page_size % 16 == 0 && 16 * (c->row_stride ? c->row_stride : (int64_t)c->head_dim) < 1ll << 31;
+}
+static inline TileShape mx_tile_shape(const ssd_paged_config *c) { return {32, 768, mx_sixteen(c)}; }
 
-template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, bool step, hipStream_t s);
+template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, bool p16, bool step, hipStream_t s);
 
 #ifdef SSD_MX_ONLY
-template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, bool step, hipStream_t s) {
-    const bool p16 = mx_sixteen(a.g);
-    if (d == 128) return p16 ? launch_paged_attn<MxTile<T, 128, BITS, true>, true>(a, sh, step, s) : launch_paged_attn<MxTile<T, 128, BITS, false>, false>(a, sh, step, s);
-    return p16 ? launch_paged_attn<MxTile<T, 64, BITS, true>, true>(a, sh, step, s) : launch_paged_attn<MxTile<T, 64, BITS, false>, false>(a, sh, step, s);
+template <typename T, int D, int BITS> static hipError_t launch_mx_rows(const PagedAttnArgs &a, const PagedShape &sh, bool p16, bool step, hipStream_t s) {
+    if (!p16) return launch_paged_attn<MxTile<T, D, BITS, false, 16>, false>(a, sh, step, s);
+    if constexpr (sizeof(T) == 2)
+        if (a.group <= 4) return launch_paged_attn<MxTile<T, D, BITS, true, 4>, true>(a, sh, step, s);
+    if (a.group <= 8) return launch_paged_attn<MxTile<T, D, BITS, true, 8>, true>(a, sh, step, s);
+    return launch_paged_attn<MxTile<T, D, BITS, true, 16>, true>(a, sh, step, s);
 }
-template hipError_t launch_mx_attn<SSD_MX_ONLY>(const PagedAttnArgs &, const PagedShape &, int, bool, hipStream_t);
+template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, bool p16, bool step, hipStream_t s) {
+    return d == 128 ? launch_mx_rows<T, 128, BITS>(a, sh, p16, step, s) : launch_mx_rows<T, 64, BITS>(a, sh, p16, step, s);
+}
+template hipError_t launch_mx_attn<SSD_MX_ONLY>(const PagedAttnArgs &, const PagedShape &, int, bool, bool, hipStream_t);
 #endif
 
 }  // namespace ssd

@@ -4,21 +4,20 @@
 
 namespace ssd {
 
-static int mx_tile_rows() { return 32; }
-
 static int mx_attend(const AttendCall &c, int format, uint8_t *k_scales, uint8_t *v_scales, hipStream_t s) {
     clear_error();
     int rc = check_mx(c.cfg, format);
     if (rc != SSD_OK || (rc = check_mx_scales(k_scales, v_scales)) != SSD_OK) return rc;
     PagedAttnArgs a;
     PagedShape shape;
-    if ((rc = attend_args(c, mx_tile_rows(), format, a, shape)) != SSD_OK) return rc;
+    if ((rc = attend_args(c, mx_tile_shape(c.cfg), format, a, shape)) != SSD_OK) return rc;
     a.k_scales = k_scales;
     a.v_scales = v_scales;
     const int d = c.cfg->head_dim;
+    const bool p16 = mx_sixteen(c.cfg);
     hipError_t e;
-    if (c.cfg->dtype == SSD_BF16) e = format == SSD_MXFP8 ? launch_mx_attn<bf16_t, 8>(a, shape, d, c.step, s) : launch_mx_attn<bf16_t, 4>(a, shape, d, c.step, s);
-    else e = format == SSD_MXFP8 ? launch_mx_attn<float, 8>(a, shape, d, c.step, s) : launch_mx_attn<float, 4>(a, shape, d, c.step, s);
+    if (c.cfg->dtype == SSD_BF16) e = format == SSD_MXFP8 ? launch_mx_attn<bf16_t, 8>(a, shape, d, p16, c.step, s) : launch_mx_attn<bf16_t, 4>(a, shape, d, p16, c.step, s);
+    else e = format == SSD_MXFP8 ? launch_mx_attn<float, 8>(a, shape, d, p16, c.step, s) : launch_mx_attn<float, 4>(a, shape, d, p16, c.step, s);
     return e == hipSuccess ? SSD_OK : hip_fail(e, "paged attention launch");
 }
 
@@ -29,7 +28,7 @@ using namespace ssd;
 extern "C" size_t ssd_paged_mx_workspace_bytes(const ssd_paged_config *cfg, int format, int max_len, int with_weights) {
     clear_error();
     if (check_mx(cfg, format) != SSD_OK || check_max_len(cfg, max_len) != SSD_OK) return 0;
-    return paged_scratch(cfg, paged_shape(cfg, max_len, mx_tile_rows()), with_weights != 0).all;
+    return paged_scratch(cfg, paged_shape(cfg, max_len, mx_tile_shape(cfg)), with_weights != 0).all;
 }
 
 extern "C" int ssd_paged_mx_decode_attn(const ssd_paged_config *cfg, int format, const void *q, const void *k_pages, const void *v_pages,

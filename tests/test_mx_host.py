@@ -7,6 +7,7 @@ import torch
 
 import paper_2510_18716_amd as ssd
 from mx_harness import MxBatch
+from paper_2510_18716_amd.binding import _mx_pools
 from test_paged_host import BAD_CONFIG, _cfg
 
 FAKE = 1 << 24
@@ -160,10 +161,9 @@ def test_binding_refuses_tensors_that_lie_otherwise():
     for layout in ("rows", "both", "wide"):                          # and takes what lies as the config says, whichever way it is named
         other = MxBatch([20, 5], 4, 2, 64, "bf16", "mxfp8", 16, seed=1, layout=layout, device="cpu")
         for t in (other.kd, other.kd.transpose(1, 2)):
-            from paper_2510_18716_amd.binding import _mx_pool
-            assert _mx_pool(t, "k_pages", other.cfg, 8) == t.data_ptr()
+            assert _mx_pools(other.cfg, "mxfp8", t, t, other.ksd, other.vsd) == (8, t.data_ptr(), t.data_ptr(), other.ksd.data_ptr(), other.vsd.data_ptr())
         with pytest.raises(ValueError):
-            _mx_pool(bt.kd, "k_pages", other.cfg, 8)
+            _mx_pools(other.cfg, "mxfp8", bt.kd, other.vd, other.ksd, other.vsd)
 
 
 def test_binding_of_the_rotation_refuses_short_arrays():
