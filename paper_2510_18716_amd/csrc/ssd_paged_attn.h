@@ -3,7 +3,7 @@
 //   elem, D, ROWS, NO     element type of q and the output, row length, rows of a tile, accumulators
 //   RESIDENT              waves of a SIMD that the registers are to allow
 //   MX                    whether the pool holds codes with scales (the newest row of a step then goes into the pool first)
-//   TABLE                 whether every wave keeps the addresses of its own tiles' rows (else the workgroup has the pages' in LDS)
+//   TABLE                 whether every wave looks up the addresses of its own tiles' rows, TILES of them at a time (else the workgroup has the pages' in LDS)
 //   Q, load_q, head, logits, zero_v, accumulate, finish, column
 //   Rows<QUADS>           where a lane finds a tile's rows; seen() tells which of them exist
 // and functions find_k, find_v, hold_k, hold_v, request_k, request_v on them.  QUADS: four rows from a multiple of four on lie in one page.
@@ -44,7 +44,6 @@ struct PagedAttnArgs {
 static constexpr int blocks_of(int waves) { return 256 * waves; }
 static constexpr int HEADS = 16;                                   // heads of a tile
 static constexpr int64_t NO_PAGE = -(1ll << 62);
-static constexpr int TABLE_TILES = 32;                             // tiles whose addresses a wave keeps, two lanes for each
 static constexpr float LN2 = 0.6931471805599453f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -217,6 +216,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
     __shared__ float sm_lse[HEADS];
     __shared__ uint32_t sm_runs[2];
     __shared__ int32_t page_ids[IDS ? blocks_of(WAVES) : 1];
+    __shared__ typename TT::entry_t table[TT::ENTRIES ? WAVES * TT::ENTRIES : 1];
     extern __shared__ __align__(16) float sm_o[];                   // [WAVES][tile_heads][LD], then (HERE) logits [tile_heads][z_stride + 4]
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -337,8 +337,8 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
         }
         typename TT::Q q;
         TT::load_q(a.q + (int64_t)b * a.q_stride + (int64_t)(head0 + (TT::head(r) < heads ? TT::head(r) : 0)) * (D * sizeof(T)), lane, q);
-        int own_page = -1;                                          // HERE, TABLE: of a thread's four rows
-        if constexpr (WEIGHTS == HERE && TT::TABLE)
+        int own_page = -1;                                          // of a thread's four rows
+        if constexpr (WEIGHTS == HERE && TT::TABLE && QUADS)
             if (4 * (int)threadIdx.x < n) {
                 int block, place;
                 split_slot(a.g, 4 * (int)threadIdx.x, block, place);
@@ -463,7 +463,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
             const int tiles = (rows + TT::ROWS - 1) / TT::ROWS;
             if (wave < tiles) {
                 int first = wave * TT::ROWS;
-                if constexpr (TT::TABLE) at.template begin<WAVES>(a, st, wave, lane);
+                if constexpr (TT::TABLE) at.template begin<WAVES>(a, st, wave, lane, table + wave * TT::ENTRIES);
                 find_k(a, st, first, lane, at);
                 request_keys(first);
                 find_v(a, st, first, lane, at);
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
         const int j = 4 * (int)threadIdx.x;
         Entries entries;
         if constexpr (WEIGHTS == HERE)
-            if (j < n) entries = entries_of<QUADS>(a, kv, j, n, [&](int block) { return TT::TABLE ? own_page : page_ids[block]; });
+            if (j < n) entries = entries_of<QUADS>(a, kv, j, n, [&](int block) { return !TT::TABLE ? page_ids[block] : QUADS ? own_page : page_of(a.g, b, block); });
         // the waves' states meet
         {
             float x, y;
@@ -711,10 +711,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, int st
 
 // ---- launch shapes ---------------------------------------------------------------------------------------------------
 
-// What the launch goes by of a tile: its rows, workgroups of four waves that are resident at once, whether waves keep their rows' addresses (TABLE).
+// What the launch goes by of a tile: its rows, workgroups of four waves that are resident at once, TILES (0: no TABLE).
 struct TileShape {
     int rows, resident;
-    bool table;
+    int tiles;
 };
 
 struct PagedShape {
@@ -750,12 +750,12 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, const Tile
     // a stage's blocks: its rows and what lies before them in the first one; block_of allows 2^16 rows
     const int64_t most = (int64_t)(blocks_of(s.waves) - 1) * c->page_size;
     s.stage = (int)((most < 8192 ? most : 8192) / s.round * s.round);
-    if (ts.table) s.stage = TABLE_TILES * s.round;
+    if (ts.tiles) s.stage = ts.tiles * s.round;
     s.lds = (size_t)s.waves * s.tile_heads * (c->head_dim + 4) * sizeof(float);
     // The weights are brought up to date by the unit's own workgroup, from logits in LDS (up to 66 KB), where it takes one tile of heads (2 sequences of
     // 64 to 97 rows, 16 heads 6.5 us, by a second launch 10.2; 128 of 64 to 640 rows, 32 heads 100 and 103, 256 query heads on 32 111 and 130, on 16 with
     // up to 500 rows 89 and 103; 64 of 1000 rows, 32 heads 192 and 187).
-    s.here = plain && s.q_tiles == 1 && s.reach <= s.stage && s.reach <= 256 * s.waves;
+    s.here = plain && s.q_tiles == 1 && (ts.tiles || s.reach <= s.stage) && s.reach <= 256 * s.waves;
     return s;
 }
 

@@ -127,7 +127,8 @@ template <typename T, int D> struct Tile;
 template <int D_> struct Tile<bf16_t, D_> {
     typedef bf16_t elem;
     static constexpr bool MX = false, TABLE = false;
-    static constexpr int RESIDENT = 3;
+    static constexpr int RESIDENT = 3, ENTRIES = 0;
+    typedef int entry_t;
     static __device__ __forceinline__ int head(int r) { return r; }
     static __device__ __forceinline__ bool writes(int) { return true; }
     template <bool QUADS> using Rows = TileRows<true, QUADS>;
@@ -192,7 +193,8 @@ template <int D_> struct Tile<bf16_t, D_> {
 template <int D_> struct Tile<float, D_> {
     typedef float elem;
     static constexpr bool MX = false, TABLE = false;
-    static constexpr int RESIDENT = 3;
+    static constexpr int RESIDENT = 3, ENTRIES = 0;
+    typedef int entry_t;
     static __device__ __forceinline__ int head(int r) { return r; }
     static __device__ __forceinline__ bool writes(int) { return true; }
     template <bool QUADS> using Rows = TileRows<false, QUADS>;
@@ -242,7 +244,7 @@ template <typename T, int D> static hipError_t launch_tiles(const PagedAttnArgs 
     return a.g.page_size % 4 == 0 ? launch_paged_attn<Tile<T, D>, true>(a, sh, step, s) : launch_paged_attn<Tile<T, D>, false>(a, sh, step, s);
 }
 
-static TileShape tile_shape(const ssd_paged_config *c) { return {c->dtype == SSD_BF16 ? 32 : 16, c->head_dim == 64 ? 1024 : 768, false}; }
+static TileShape tile_shape(const ssd_paged_config *c) { return {c->dtype == SSD_BF16 ? 32 : 16, c->head_dim == 64 ? 1024 : 768, 0}; }
 
 static int paged_attend(const AttendCall &c, hipStream_t s) {
     clear_error();

@@ -18,11 +18,40 @@
 
 namespace ssd {
 
-// Where a tile's rows lie.  P16: the page size is a multiple of 16, so that 16 rows are neighbours in one page, and a group's address is the same for all
-// lanes: found in scalar registers, the lanes' part of it never changes.
-template <int SUB, int SB, bool P16> struct MxRows;
+// Where a tile's rows lie.  Every wave looks up its own tiles' pages, a chunk of them at a time.  GROUP: rows that are neighbours in one page from a multiple of GROUP on
+// (16, 4 or 1, by the page size).  With 16 a group's address is the same for all lanes: found in scalar registers, the lanes' part of it never changes.  With fewer
+// the groups' addresses are in LDS, in a place of the wave's own.
+struct MxEntry {
+    int64_t row, scales;                                           // bytes from the pools' and the scales' beginnings; row -1: no page
+};
 
-template <int SUB, int SB> struct MxRows<SUB, SB, true> {
+template <int SUB, int SB, int GROUP> struct MxRows {
+    static constexpr int LDS = 128, PER_TILE = 16 * SUB / GROUP, TILES = LDS / PER_TILE, NV = 4 * SUB / (GROUP == 4 ? 4 : 1);
+    const MxEntry *entries;                                        // of the tile to come
+    int64_t k[SUB], ks[SUB], v[NV], vs[NV];
+    uint32_t there;                                                // bit 4 t + i: row 16 t + 4 g + i
+
+    template <int WAVES> __device__ __forceinline__ void begin(const PagedAttnArgs &a, const Stage &st, int wave, int lane, MxEntry *own) {
+#pragma unroll
+        for (int i = lane; i < LDS; i += 64) {
+            const int x = (wave + i / PER_TILE * WAVES) * (16 * SUB) + i % PER_TILE * GROUP;
+            int block, place;
+            split_slot(a.g, st.begin + (x < st.rows ? x : 0), block, place);
+            const int page = page_of(a.g, st.b, block);
+            own[i] = page < 0 || x >= st.rows ? MxEntry{-1, 0} : MxEntry{row_offset(a.g, page, st.kv, place), table_index(a.g, page, st.kv, place) * SB};
+        }
+        entries = own;
+    }
+    struct Seen {
+        uint32_t there;
+        __device__ __forceinline__ bool all() const { return __all(there == (1u << 4 * SUB) - 1u); }
+        __device__ __forceinline__ bool has(int e) const { return there >> e & 1; }
+    };
+    __device__ __forceinline__ Seen seen(int) const { return Seen{there}; }
+};
+
+template <int SUB, int SB> struct MxRows<SUB, SB, 16> {
+    static constexpr int TILES = 64 / SUB, LDS = 1;                // tiles of a chunk
     // A lane has 16 rows of the wave's tiles in this chunk: lane SUB k + s group s of tile k.  Byte offset in the pool (the upper half below zero: no page), and
     // first place in the tables by 16.
     uint32_t low, group;
@@ -30,8 +59,7 @@ template <int SUB, int SB> struct MxRows<SUB, SB, true> {
     int64_t off[SUB], soff[SUB];                                   // that tile's: bytes from the pools' and the scales' beginnings
     int left[SUB];                                                 // rows there are from a group's first on
 
-    template <int WAVES> __device__ __forceinline__ void begin(const PagedAttnArgs &a, const Stage &st, int wave, int lane) {
-        static_assert(SUB * TABLE_TILES == 64, "a lane for each group of 16 rows");
+    template <int WAVES> __device__ __forceinline__ void begin(const PagedAttnArgs &a, const Stage &st, int wave, int lane, MxEntry *) {
         const int x = (wave + lane / SUB * WAVES) * (16 * SUB) + lane % SUB * 16;
         int block, place;
         split_slot(a.g, st.begin + (x < st.rows ? x : 0), block, place);
@@ -61,19 +89,8 @@ template <int SUB, int SB> struct MxRows<SUB, SB, true> {
     }
 };
 
-template <int SUB, int SB> struct MxRows<SUB, SB, false> {
-    int64_t k[SUB], ks[SUB], v[4 * SUB], vs[4 * SUB];
-    uint32_t there;                                                // bit 4 t + i: row 16 t + 4 g + i
-    struct Seen {
-        uint32_t there;
-        __device__ __forceinline__ bool all() const { return __all(there == (1u << 4 * SUB) - 1u); }
-        __device__ __forceinline__ bool has(int e) const { return there >> e & 1; }
-    };
-    __device__ __forceinline__ Seen seen(int) const { return Seen{there}; }
-};
-
 template <int SUB, int SB>
-static __device__ __forceinline__ void find_k(const PagedAttnArgs &, const Stage &st, int first, int, MxRows<SUB, SB, true> &t) {
+static __device__ __forceinline__ void find_k(const PagedAttnArgs &, const Stage &st, int first, int, MxRows<SUB, SB, 16> &t) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
         const int high = __builtin_amdgcn_readlane(t.high, t.next + s);
@@ -85,50 +102,48 @@ static __device__ __forceinline__ void find_k(const PagedAttnArgs &, const Stage
     t.next += SUB;
 }
 template <int SUB, int SB>
-static __device__ __forceinline__ void find_v(const PagedAttnArgs &, const Stage &, int, int, MxRows<SUB, SB, true> &) {}
+static __device__ __forceinline__ void find_v(const PagedAttnArgs &, const Stage &, int, int, MxRows<SUB, SB, 16> &) {}
 
-// A row's offsets in the pool and the scales; rows that do not exist get the pool's first row and `false`.
-static __device__ __forceinline__ bool mx_row_at(const PagedAttnArgs &a, const Stage &st, int x, int64_t &row, int64_t &entry) {
-    const int y = (x < st.rows ? x : st.rows - 1) + st.lead;
-    const int block = block_of(a, y), place = y - block * a.g.page_size, id = st.ids[block];
-    row = id < 0 ? 0 : row_offset(a.g, id, st.kv, place);
-    entry = id < 0 ? 0 : table_index(a.g, id, st.kv, place);
-    return id >= 0 && x < st.rows;
-}
-template <int SUB, int SB>
-static __device__ __forceinline__ void find_k(const PagedAttnArgs &a, const Stage &st, int first, int lane, MxRows<SUB, SB, false> &t) {
+template <int SUB, int SB, int GROUP>
+static __device__ __forceinline__ void find_k(const PagedAttnArgs &a, const Stage &, int, int lane, MxRows<SUB, SB, GROUP> &t) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
-        int64_t entry;
-        mx_row_at(a, st, first + 16 * s + (lane & 15), t.k[s], entry);
-        t.ks[s] = entry * SB;
+        const int r = 16 * s + (lane & 15);
+        const MxEntry e = t.entries[r / GROUP];
+        t.k[s] = (e.row < 0 ? 0 : e.row) + (int64_t)((uint32_t)(r % GROUP) * (uint64_t)a.g.row_stride);
+        t.ks[s] = e.scales + r % GROUP * SB;
     }
 }
-template <int SUB, int SB>
-static __device__ __forceinline__ void find_v(const PagedAttnArgs &a, const Stage &st, int first, int lane, MxRows<SUB, SB, false> &t) {
+template <int SUB, int SB, int GROUP>
+static __device__ __forceinline__ void find_v(const PagedAttnArgs &, const Stage &st, int first, int lane, MxRows<SUB, SB, GROUP> &t) {
+    typedef MxRows<SUB, SB, GROUP> R;
     t.there = 0;
 #pragma unroll
-    for (int i = 0; i < 4 * SUB; ++i) {
-        int64_t entry;
-        const bool is = mx_row_at(a, st, first + 16 * (i / 4) + 4 * (lane >> 4) + i % 4, t.v[i], entry);
-        t.vs[i] = entry * SB;
-        t.there |= is ? 1u << i : 0u;
+    for (int i = 0; i < R::NV; ++i) {
+        const int r = GROUP == 4 ? 16 * i + 4 * (lane >> 4) : 16 * (i / 4) + 4 * (lane >> 4) + i % 4;
+        const MxEntry e = t.entries[r / GROUP];
+        t.v[i] = e.row < 0 ? 0 : e.row;
+        t.vs[i] = e.scales;
+        const int left = e.row < 0 ? 0 : st.rows - first - r;
+#pragma unroll
+        for (int x = 0; x < (GROUP == 4 ? 4 : 1); ++x) t.there |= x < left ? 1u << (GROUP == 4 ? 4 * i + x : i) : 0u;
     }
+    t.entries += R::PER_TILE;                                       // K's were found before
 }
 
 // Requests wait for the product that has read the registers they fill (as with plain rows).
-template <int SUB, int SB> static __device__ __forceinline__ void hold_k(MxRows<SUB, SB, true> &t, float result) {
+template <int SUB, int SB> static __device__ __forceinline__ void hold_k(MxRows<SUB, SB, 16> &t, float result) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) asm volatile("" : "+s"(t.off[s]), "+s"(t.soff[s]) : "v"(result));
 }
-template <int SUB, int SB> static __device__ __forceinline__ void hold_v(MxRows<SUB, SB, true> &t, float result) { hold_k(t, result); }
-template <int SUB, int SB> static __device__ __forceinline__ void hold_k(MxRows<SUB, SB, false> &t, float result) {
+template <int SUB, int SB> static __device__ __forceinline__ void hold_v(MxRows<SUB, SB, 16> &t, float result) { hold_k(t, result); }
+template <int SUB, int SB, int GROUP> static __device__ __forceinline__ void hold_k(MxRows<SUB, SB, GROUP> &t, float result) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) asm volatile("" : "+v"(t.k[s]), "+v"(t.ks[s]) : "v"(result));
 }
-template <int SUB, int SB> static __device__ __forceinline__ void hold_v(MxRows<SUB, SB, false> &t, float result) {
+template <int SUB, int SB, int GROUP> static __device__ __forceinline__ void hold_v(MxRows<SUB, SB, GROUP> &t, float result) {
 #pragma unroll
-    for (int i = 0; i < 4 * SUB; ++i) asm volatile("" : "+v"(t.v[i]), "+v"(t.vs[i]) : "v"(result));
+    for (int i = 0; i < MxRows<SUB, SB, GROUP>::NV; ++i) asm volatile("" : "+v"(t.v[i]), "+v"(t.vs[i]) : "v"(result));
 }
 
 template <int N> struct Words { typedef uint32_t type __attribute__((ext_vector_type(N))); };
@@ -142,14 +157,18 @@ static __device__ __forceinline__ uint32_t take_upper(float &x) {
     return hi >> 16;
 }
 
+// Waves of a SIMD: fp32 rows of 128 elements need more registers than three leave (q in three terms).
+static constexpr int mx_resident(bool f32, int d) { return f32 && d == 128 ? 2 : 3; }
+
 // HT: heads of a tile, 4, 8 or 16.  The matrix cores' sixteen columns hold COPIES = 16 / HT columns for a head.  With two, one takes the even elements of a
 // pair (V's columns 2 c), the other the odd ones: a pair is the operand as it comes from the conversion, two neighbouring places of the sum, and a copy has its
 // probability in one of them and nothing in the other.  So V is not turned at all, and the sums take half the registers.  With four (bf16 calls) two more take
 // the probabilities' second term.
-template <typename T, int D_, int BITS_, bool P16, int HT> struct MxTile {
+template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
     typedef T elem;
-    static constexpr bool MX = true, TABLE = P16;
-    static constexpr int RESIDENT = 3;
+    static constexpr bool MX = true, TABLE = true, QUADS = GROUP >= 4;
+    static constexpr int RESIDENT = mx_resident(sizeof(T) == 4, D_), ENTRIES = GROUP == 16 ? 0 : MxRows<2, 1, GROUP>::LDS;
+    typedef MxEntry entry_t;
     static constexpr int D = D_, BITS = BITS_, SB = D / 32;        // SB: bytes of a row's scales
     static constexpr int SUB = 2, ROWS = 16 * SUB;
     static constexpr int STEPS = D / 32, NV = D / 16, KE = D / 4;  // KE: elements of a row of K in a lane
@@ -159,7 +178,8 @@ template <typename T, int D_, int BITS_, bool P16, int HT> struct MxTile {
     static_assert(COPIES < 4 || PT == 2, "four copies have two terms");
     static __device__ __forceinline__ int head(int r) { return r % HT; }
     static __device__ __forceinline__ bool writes(int r) { return r < 2 * HT; }
-    template <bool QUADS> using Rows = MxRows<SUB, SB, P16>;
+    template <bool> using Rows = MxRows<SUB, SB, GROUP>;
+    static constexpr int TILES = MxRows<SUB, SB, GROUP>::TILES;
     typedef typename Words<KW>::type krow_t;
     typedef std::conditional_t<VB == 2, uint16_t, typename Words<VB == 8 ? 2 : 1>::type> vrow_t;
     typedef typename Words<SB>::type four_t;                       // scales of four rows
@@ -168,7 +188,7 @@ template <typename T, int D_, int BITS_, bool P16, int HT> struct MxTile {
     krow_t k[SUB];
     uint32_t ks[SUB];
     vrow_t v[4 * SUB];
-    std::conditional_t<P16, four_t, one_t> vs[P16 ? SUB : 4 * SUB];
+    std::conditional_t<QUADS, four_t, one_t> vs[QUADS ? SUB : 4 * SUB];
     struct Q { bf16x8 x[QT][STEPS]; };
 
     static __device__ __forceinline__ int odd(int lane) { return (lane & 15) / HT & 1; }
@@ -239,7 +259,7 @@ template <typename T, int D_, int BITS_, bool P16, int HT> struct MxTile {
     __device__ __forceinline__ float v_scale(int i, int lane) const {
         const uint32_t block = (uint32_t)(lane & 15) * NV / 32;
         uint32_t w, at = 8 * block;
-        if constexpr (P16) {
+        if constexpr (QUADS) {
             if constexpr (SB == 4) {
                 w = vs[i / 4][i % 4];
             } else {
@@ -254,7 +274,7 @@ template <typename T, int D_, int BITS_, bool P16, int HT> struct MxTile {
     // A row that does not exist: neither its codes nor a scale that is NaN may count.
     __device__ __forceinline__ void zero_v(int i) {
         v[i] = vrow_t(0);
-        if constexpr (!P16) vs[i] = 0;
+        if constexpr (!QUADS) vs[i] = 0;
         else if constexpr (SB == 4) vs[i / 4][i % 4] = 0;
         else vs[i / 4][i % 4 / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
     }
@@ -405,7 +425,7 @@ template <typename X, int NT> static __device__ __forceinline__ X mx_load(__amdg
     }
 }
 template <typename Step, typename TT, int SUB, int SB>
-static __device__ __forceinline__ void request_k(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, true> &at, TT &tl, int, int, const char *, int lane) {
+static __device__ __forceinline__ void request_k(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, 16> &at, TT &tl, int, int, const char *, int lane) {
     const uint32_t r = (uint32_t)lane & 15, g = (uint32_t)lane >> 4, own = r * (uint32_t)a.g.row_stride + g * (TT::KE * TT::BITS / 8);
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
@@ -414,7 +434,7 @@ static __device__ __forceinline__ void request_k(Step, const PagedAttnArgs &a, c
     }
 }
 template <typename Step, typename TT, int SUB, int SB>
-static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, true> &at, TT &tl, int, int, const char *, int lane) {
+static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, 16> &at, TT &tl, int, int, const char *, int lane) {
     const uint32_t g = (uint32_t)lane >> 4, own = 4 * g * (uint32_t)a.g.row_stride + ((uint32_t)lane & 15) * TT::VB;
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
@@ -424,40 +444,48 @@ static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, c
         tl.vs[s] = mx_load<typename TT::four_t, 0>(mx_buffer(a.v_scales + at.soff[s]), g * (4 * SB), 0);
     }
 }
-template <typename Step, typename TT, int SUB, int SB>
-static __device__ __forceinline__ void request_k(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, false> &at, TT &tl, int, int, const char *, int lane) {
+template <typename Step, typename TT, int SUB, int SB, int GROUP>
+static __device__ __forceinline__ void request_k(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, GROUP> &at, TT &tl, int, int, const char *, int lane) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) tl.load_k(s, a.k_pages + at.k[s], reinterpret_cast<const char *>(a.k_scales) + at.ks[s], lane);
 }
-template <typename Step, typename TT, int SUB, int SB>
-static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, false> &at, TT &tl, int, int, const char *, int lane) {
+template <typename Step, typename TT, int SUB, int SB, int GROUP>
+static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, const MxRows<SUB, SB, GROUP> &at, TT &tl, int, int, const char *, int lane) {
 #pragma unroll
     for (int i = 0; i < 4 * SUB; ++i) {
-        tl.v[i] = TT::template load<typename TT::vrow_t>(a.v_pages + at.v[i] + ((uint32_t)lane & 15) * TT::VB);
-        tl.vs[i] = *reinterpret_cast<const typename TT::one_t *>(a.v_scales + at.vs[i]);
+        const char *row = a.v_pages + (GROUP == 4 ? at.v[i / 4] + i % 4 * a.g.row_stride : at.v[i]);
+        tl.v[i] = TT::template load<typename TT::vrow_t>(row + ((uint32_t)lane & 15) * TT::VB);
     }
+    typedef std::remove_reference_t<decltype(tl.vs[0])> scales_t;
+#pragma unroll
+    for (int i = 0; i < MxRows<SUB, SB, GROUP>::NV; ++i) tl.vs[i] = *reinterpret_cast<const scales_t *>(a.v_scales + at.vs[i]);
 }
 
-// Whether 16 rows are neighbours, at distances that fit 32 bits.
-static inline bool mx_sixteen(const ssd_paged_config *c) {
-    return c->page_size % 16 == 0 && 16 * (c->row_stride ? c->row_stride : (int64_t)c->head_dim) < 1ll << 31;
+// Rows that are neighbours in a page: 16 (at distances that fit 32 bits), 4 (up to eight query heads on a key head: there are no tiles of sixteen for it) or 1.
+static inline int mx_group(const ssd_paged_config *c) {
+    if (c->page_size % 16 == 0 && 16 * (c->row_stride ? c->row_stride : (int64_t)c->head_dim) < 1ll << 31) return 16;
+    return c->page_size % 4 == 0 && c->n_heads / c->n_kv_heads <= 8 ? 4 : 1;
 }
-static inline TileShape mx_tile_shape(const ssd_paged_config *c) { return {32, 768, mx_sixteen(c)}; }
+static inline TileShape mx_tile_shape(const ssd_paged_config *c) {
+    const int group = mx_group(c);
+    return {32, 256 * mx_resident(c->dtype == SSD_F32, c->head_dim), group == 16 ? 32 : group == 4 ? 16 : 4};
+}
 
-template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, bool p16, bool step, hipStream_t s);
+template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, int group, bool step, hipStream_t s);
 
 #ifdef SSD_MX_ONLY
-template <typename T, int D, int BITS> static hipError_t launch_mx_rows(const PagedAttnArgs &a, const PagedShape &sh, bool p16, bool step, hipStream_t s) {
-    if (!p16) return launch_paged_attn<MxTile<T, D, BITS, false, 16>, false>(a, sh, step, s);
+template <typename T, int D, int BITS> static hipError_t launch_mx_rows(const PagedAttnArgs &a, const PagedShape &sh, int group, bool step, hipStream_t s) {
+    if (group == 1) return launch_paged_attn<MxTile<T, D, BITS, 1, 16>, false>(a, sh, step, s);
+    if (group == 4) return launch_paged_attn<MxTile<T, D, BITS, 4, 8>, true>(a, sh, step, s);
     if constexpr (sizeof(T) == 2)
-        if (a.group <= 4) return launch_paged_attn<MxTile<T, D, BITS, true, 4>, true>(a, sh, step, s);
-    if (a.group <= 8) return launch_paged_attn<MxTile<T, D, BITS, true, 8>, true>(a, sh, step, s);
-    return launch_paged_attn<MxTile<T, D, BITS, true, 16>, true>(a, sh, step, s);
+        if (a.group <= 4) return launch_paged_attn<MxTile<T, D, BITS, 16, 4>, true>(a, sh, step, s);
+    if (a.group <= 8) return launch_paged_attn<MxTile<T, D, BITS, 16, 8>, true>(a, sh, step, s);
+    return launch_paged_attn<MxTile<T, D, BITS, 16, 16>, true>(a, sh, step, s);
 }
-template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, bool p16, bool step, hipStream_t s) {
-    return d == 128 ? launch_mx_rows<T, 128, BITS>(a, sh, p16, step, s) : launch_mx_rows<T, 64, BITS>(a, sh, p16, step, s);
+template <typename T, int BITS> hipError_t launch_mx_attn(const PagedAttnArgs &a, const PagedShape &sh, int d, int group, bool step, hipStream_t s) {
+    return d == 128 ? launch_mx_rows<T, 128, BITS>(a, sh, group, step, s) : launch_mx_rows<T, 64, BITS>(a, sh, group, step, s);
 }
-template hipError_t launch_mx_attn<SSD_MX_ONLY>(const PagedAttnArgs &, const PagedShape &, int, bool, bool, hipStream_t);
+template hipError_t launch_mx_attn<SSD_MX_ONLY>(const PagedAttnArgs &, const PagedShape &, int, int, bool, hipStream_t);
 #endif
 
 }  // namespace ssd

@@ -14,10 +14,10 @@ static int mx_attend(const AttendCall &c, int format, uint8_t *k_scales, uint8_t
     a.k_scales = k_scales;
     a.v_scales = v_scales;
     const int d = c.cfg->head_dim;
-    const bool p16 = mx_sixteen(c.cfg);
+    const int group = mx_group(c.cfg);
     hipError_t e;
-    if (c.cfg->dtype == SSD_BF16) e = format == SSD_MXFP8 ? launch_mx_attn<bf16_t, 8>(a, shape, d, p16, c.step, s) : launch_mx_attn<bf16_t, 4>(a, shape, d, p16, c.step, s);
-    else e = format == SSD_MXFP8 ? launch_mx_attn<float, 8>(a, shape, d, p16, c.step, s) : launch_mx_attn<float, 4>(a, shape, d, p16, c.step, s);
+    if (c.cfg->dtype == SSD_BF16) e = format == SSD_MXFP8 ? launch_mx_attn<bf16_t, 8>(a, shape, d, group, c.step, s) : launch_mx_attn<bf16_t, 4>(a, shape, d, group, c.step, s);
+    else e = format == SSD_MXFP8 ? launch_mx_attn<float, 8>(a, shape, d, group, c.step, s) : launch_mx_attn<float, 4>(a, shape, d, group, c.step, s);
     return e == hipSuccess ? SSD_OK : hip_fail(e, "paged attention launch");
 }
 
