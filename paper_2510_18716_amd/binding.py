@@ -788,15 +788,18 @@ def ssd_paged_mx_evict(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, 
 def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, inv_freq, axis=None, n_axes: int = 1, n_pairs: Optional[int] = None,
                   layout: int = SSD_ROPE_HALF, inverse: bool = False, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
     """n_pairs None: inv_freq's elements.  x_stride, out_stride 0: the tensor's own (query and key heads may be handed over where a projection has them)."""
-    width = n_heads * head_dim
-    if x is not None and not isinstance(x, int):
-        x_stride = x_stride or (x.stride(0) if x.dim() > 1 and x.shape[0] == n_rows > 1 else 0)
-        _check_rows(x, "x", n_rows, x_stride or width, width)
-        x = x.data_ptr()
-    if out is not None and not isinstance(out, int):
-        out_stride = out_stride or (out.stride(0) if out.dim() > 1 and out.shape[0] == n_rows > 1 else 0)
-        _check_rows(out, "out", n_rows, out_stride or width, width)
-        out = out.data_ptr()
+    rows = []
+    for t, what, stride in ((x, "x", x_stride), (out, "out", out_stride)):
+        if t is not None and not isinstance(t, int):
+            own = t.stride()
+            if len(own) == 3 and own[1] == head_dim and own[2] == 1 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
+                stride = own[0] if n_rows > 1 else 0
+            else:
+                stride = stride or (own[0] if len(own) > 1 and t.shape[0] == n_rows > 1 else 0)
+                _check_rows(t, what, n_rows, stride or n_heads * head_dim, n_heads * head_dim)
+            t = t.data_ptr()
+        rows += [t, stride]
+    x, x_stride, out, out_stride = rows
     pairs = int(inv_freq.numel() if n_pairs is None else n_pairs)
     for t, what, most in ((pos, "pos", n_axes * n_rows), (inv_freq, "inv_freq", pairs), (axis, "axis", pairs)):
         if t is not None and not isinstance(t, int) and (not t.is_contiguous() or t.numel() < most):

@@ -358,12 +358,6 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
 #pragma unroll
         for (int j = 0; j < TT::NO; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        if constexpr (STEP && TT::MX)                               // the newest row's codes go where they belong, and are read like the others' behind the next barrier
-            if (newest) {
-                TT::put_newest(a, b, kv, n, k_new, v_new);
-                if (TT::TABLE) __syncthreads();
-            }
-
         for (int row0 = begin; row0 < end;) {
             const PagedAttnArgs &a = arguments();
             const int rows = end - row0 < a.stage ? end - row0 : a.stage;
@@ -463,7 +457,19 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
             const int tiles = (rows + TT::ROWS - 1) / TT::ROWS;
             if (wave < tiles) {
                 int first = wave * TT::ROWS;
-                if constexpr (TT::TABLE) at.template begin<WAVES>(a, st, wave, lane, table + wave * TT::ENTRIES);
+                if constexpr (TT::TABLE) {
+                    if constexpr (STEP) {                           // the newest row's codes go where they belong first, by the wave that then reads them
+                        if (last_row < rows && wave == (rows - 1) / TT::ROWS % WAVES) {
+                            const typename TT::Newest x = TT::load_newest(k_new, v_new, lane);
+                            at.template begin<WAVES>(a, st, wave, lane, table + wave * TT::ENTRIES);
+                            TT::put_newest(x, a, b, kv, n, lane);
+                        } else {
+                            at.template begin<WAVES>(a, st, wave, lane, table + wave * TT::ENTRIES);
+                        }
+                    } else {
+                        at.template begin<WAVES>(a, st, wave, lane, table + wave * TT::ENTRIES);
+                    }
+                }
                 find_k(a, st, first, lane, at);
                 request_keys(first);
                 find_v(a, st, first, lane, at);

@@ -3,7 +3,8 @@
 //
 // Both are bound by HBM, the wide side by far: 256 bytes of bf16 for 64 + 4 of codes and scales.  A lane has eight elements, 16 bytes (fp32: 32) on the wide side and 4 or
 // 8 on the narrow one; the four lanes of a block find its largest element by two lane exchanges.  Scales meet in LDS and leave with the tables' entries, a
-// page's places by neighbouring threads.
+// page's places by neighbouring threads.  22500 tokens of 32 heads of 128 elements (369 MB of bf16) into four bits and back 171 us, 5.5 TB/s read and written, as a
+// plain copy does; 557 MB from eight bits 103 us, 5.4.  A few tokens: 3.5 us each way, launch and dependent loads.
 #include "ssd_mx.h"
 #include "ssd_paged_mx.h"
 
@@ -74,31 +75,60 @@ template <bool READ> static __device__ __forceinline__ void find_spots(const MxR
     __syncthreads();
 }
 
+// A thread's share of a workgroup's tokens: the q-th fragment of eight elements.
+struct Share {
+    int i, f;                // token, fragment of its heads
+    __device__ __forceinline__ Share(const MxRowsArgs &a, int q, int lane, int per_token) {
+        const int t = q / per_token;
+        i = ((int)threadIdx.x >> a.lanes_log2) + (t << (8 - a.lanes_log2));
+        f = lane + ((q - t * per_token) << a.lanes_log2);
+    }
+};
+
 template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx_append_kernel(MxRowsArgs a) {
-    constexpr int PARTS = D / 8, SB = D / 32;
+    constexpr int PARTS = D / 8, SB = D / 32, U = 2;
     typedef std::conditional_t<SB == 4, uint32_t, uint16_t> scales_t;
     __shared__ Spots sm;
     extern __shared__ __align__(16) uint8_t sm_scale[];     // [K and V][kv heads][tokens][SB]
     const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row0 = (int)blockIdx.x << a.tokens_log2;
-    const int lane = tid & ((1 << a.lanes_log2) - 1), step = 1 << a.lanes_log2, frags = a.g.n_kv * PARTS;
+    const int lane = tid & ((1 << a.lanes_log2) - 1), step = 1 << a.lanes_log2, frags = a.g.n_kv * PARTS, per_token = (frags + step - 1) >> a.lanes_log2;
+    const int mine = ((tokens + (256 >> a.lanes_log2) - 1) >> (8 - a.lanes_log2)) * per_token;
+    // what a thread reads is on its way two fragments ahead, the first ones while the tokens' places are looked up
+    Eight<T> k[U], v[U];
+    const auto load = [&](int q) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const Share x(a, q + u, lane, per_token);
+            const int row = row0 + x.i;
+            const int64_t from = (int64_t)(row < a.n ? row : a.n - 1) * a.stride + (int64_t)(x.f < frags ? x.f : lane) * (8 * (int)sizeof(T));
+            k[u] = load_eight<T>(a.k + from);
+            v[u] = load_eight<T>(a.v + from);
+        }
+    };
+    load(0);
     find_spots<false>(a, sm);
-    for (int i = tid >> a.lanes_log2; i < tokens; i += 256 >> a.lanes_log2) {
-        const int64_t at = sm.row[i];
-        if (at < 0) continue;
-        const int64_t from = (int64_t)(row0 + i) * a.stride;
-        for (int f = lane; f < frags; f += step) {
-            const int kv = f / PARTS, part = f % PARTS;
-            const Eight<T> k = load_eight<T>(a.k + from + (int64_t)f * (8 * (int)sizeof(T)));
-            const Eight<T> v = load_eight<T>(a.v + from + (int64_t)f * (8 * (int)sizeof(T)));
-            const int64_t to = at + (int64_t)kv * a.g.head_stride + part * BITS;
-            const auto put = [&](char *pool, const Eight<T> &x, int which) {
-                const uint32_t byte = mx_scale_of<BITS>(quad_max(largest_of<T>(x)));
-                const Codes<BITS> c = mx_encode<BITS, T>(x, byte);
+    for (int q = 0; q < mine; q += U) {
+        Eight<T> k0[U], v0[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            k0[u] = k[u];
+            v0[u] = v[u];
+        }
+        if (q + U < mine) load(q + U);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const Share x(a, q + u, lane, per_token);
+            if (q + u >= mine || x.i >= tokens || x.f >= frags || sm.row[x.i] < 0) continue;       // the same for the four lanes of a block
+            const int kv = x.f / PARTS, part = x.f % PARTS;
+            const int64_t to = sm.row[x.i] + (int64_t)kv * a.g.head_stride + part * BITS;
+            const auto put = [&](char *pool, const Eight<T> &e, int which) {
+                const uint32_t byte = mx_scale_of<BITS>(quad_max(largest_of<T>(e)));
+                const Codes<BITS> c = mx_encode<BITS, T>(e, byte);
                 *reinterpret_cast<Codes<BITS> *>(pool + to) = c;
-                if (part % 4 == 0) sm_scale[(((size_t)which * a.g.n_kv + kv) * tokens + i) * SB + part / 4] = (uint8_t)byte;
+                if (part % 4 == 0) sm_scale[(((size_t)which * a.g.n_kv + kv) * tokens + x.i) * SB + part / 4] = (uint8_t)byte;
             };
-            put(a.k_pages, k, 0);
-            put(a.v_pages, v, 1);
+            put(a.k_pages, k0[u], 0);
+            put(a.v_pages, v0[u], 1);
         }
     }
     __syncthreads();
@@ -114,25 +144,46 @@ template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx
     }
 }
 
-template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx_read_kernel(MxRowsArgs a) {
-    constexpr int PARTS = D / 8, SB = D / 32;
+// ONCE: the rows written are so many that whoever reads them next finds few of them in the memory-side cache, and are not to push one another out of it.
+template <typename T, int D, int BITS, bool ONCE> __global__ __launch_bounds__(256) void mx_read_kernel(MxRowsArgs a) {
+    constexpr int PARTS = D / 8, SB = D / 32, U = 4;
     __shared__ Spots sm;
     const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row0 = (int)blockIdx.x << a.tokens_log2;
-    const int lane = tid & ((1 << a.lanes_log2) - 1), step = 1 << a.lanes_log2, frags = a.g.n_kv * PARTS;
+    const int lane = tid & ((1 << a.lanes_log2) - 1), step = 1 << a.lanes_log2, frags = a.g.n_kv * PARTS, per_token = (frags + step - 1) >> a.lanes_log2;
+    const int mine = ((tokens + (256 >> a.lanes_log2) - 1) >> (8 - a.lanes_log2)) * per_token;
     find_spots<true>(a, sm);
-    for (int i = tid >> a.lanes_log2; i < tokens; i += 256 >> a.lanes_log2) {
-        const int64_t at = sm.row[i];
-        if (at < 0) continue;
-        const int64_t to = (int64_t)(row0 + i) * a.stride;
-#pragma unroll 2
-        for (int f = lane; f < frags; f += step) {
-            const int kv = f / PARTS, part = f % PARTS;
-            const int64_t from = at + (int64_t)kv * a.g.head_stride + part * BITS;
-            const int64_t scale = (sm.entry[i] + (int64_t)kv * a.g.page_size) * SB + part / 4;
-            const Codes<BITS> k = *reinterpret_cast<const Codes<BITS> *>(a.k_pages + from), v = *reinterpret_cast<const Codes<BITS> *>(a.v_pages + from);
-            const uint32_t ks = a.k_scales[scale], vs = a.v_scales[scale];
-            *reinterpret_cast<Eight<T> *>(a.k + to + (int64_t)f * (8 * (int)sizeof(T))) = mx_decode<BITS, T>(k, ks);
-            *reinterpret_cast<Eight<T> *>(a.v + to + (int64_t)f * (8 * (int)sizeof(T))) = mx_decode<BITS, T>(v, vs);
+    for (int q = 0; q < mine; q += U) {
+        Codes<BITS> k[U], v[U];
+        uint32_t ks[U], vs[U];
+        bool is[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {                        // no load is under a condition: what does not exist is the pool's first row
+            const Share x(a, q + u, lane, per_token);
+            is[u] = q + u < mine && x.i < tokens && x.f < frags;
+            const int i = is[u] ? x.i : 0, kv = is[u] ? x.f / PARTS : 0, part = x.f % PARTS;
+            const int64_t at = sm.row[i];
+            is[u] = is[u] && at >= 0;
+            const int64_t from = (is[u] ? at + (int64_t)kv * a.g.head_stride : 0) + part * BITS;
+            const int64_t scale = (is[u] ? sm.entry[i] + (int64_t)kv * a.g.page_size : 0) * SB + part / 4;
+            k[u] = *reinterpret_cast<const Codes<BITS> *>(a.k_pages + from);
+            v[u] = *reinterpret_cast<const Codes<BITS> *>(a.v_pages + from);
+            ks[u] = a.k_scales[scale];
+            vs[u] = a.v_scales[scale];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!is[u]) continue;
+            const Share x(a, q + u, lane, per_token);
+            const int64_t to = (int64_t)(row0 + x.i) * a.stride + (int64_t)x.f * (8 * (int)sizeof(T));
+            const auto put = [&](char *p, const Eight<T> &e) {
+#pragma unroll
+                for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+                    if constexpr (ONCE) __builtin_nontemporal_store(e.r[j], reinterpret_cast<u32x4_nt_t *>(p) + j);
+                    else reinterpret_cast<u32x4_nt_t *>(p)[j] = e.r[j];
+                }
+            };
+            put(a.k + to, mx_decode<BITS, T>(k[u], ks[u]));
+            put(a.v + to, mx_decode<BITS, T>(v[u], vs[u]));
         }
     }
 }
@@ -143,15 +194,20 @@ static int launch_mx_rows(const ssd_paged_config *c, int format, MxRowsArgs &a, 
     const int frags = c->n_kv_heads * c->head_dim / 8;
     a.lanes_log2 = 4;
     while (a.lanes_log2 < 8 && 1 << a.lanes_log2 < frags) ++a.lanes_log2;
+    // 64 KB of rows to a workgroup that writes the cache, 32 to one that reads it, if that leaves 1024 of them (22500 tokens of 32 heads written in 32, 64 and 128 KB, read back in 32, in 64, 16 where
+    // they were written in 128: 174, 171 and 179 us; 557 MB read in 16, 32, 64 and 128 KB 107, 103, 107 and 110)
     a.tokens_log2 = 0;
-    while (1 << a.tokens_log2 < TOKENS && ((int64_t)frags * 8 * e) << a.tokens_log2 < 16384 && a.n >> a.tokens_log2 > 1024) ++a.tokens_log2;
+    while (1 << a.tokens_log2 < TOKENS && ((int64_t)frags * 8 * e) << a.tokens_log2 < (read ? 16384 : 32768) && a.n >> a.tokens_log2 > 1024) ++a.tokens_log2;
     const dim3 grid((unsigned)(((int64_t)a.n + (1 << a.tokens_log2) - 1) >> a.tokens_log2));
     const unsigned lds = read ? 0 : (unsigned)(2 * c->n_kv_heads * (c->head_dim / 32)) << a.tokens_log2;
+    // 367 MB: 114 us with ordinary stores, 103 with the hint; 146 MB: 60 and 53; 45 MB: 33.5 either way
+    const bool once = (int64_t)a.n * frags * 16 * e > 64 << 20;
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, a); };
     const auto by_bits = [&](auto t, auto d) {
         typedef decltype(t) T;
         constexpr int D = decltype(d)::value;
-        if (read) format == SSD_MXFP8 ? go(mx_read_kernel<T, D, 8>) : go(mx_read_kernel<T, D, 4>);
+        if (read && once) format == SSD_MXFP8 ? go(mx_read_kernel<T, D, 8, true>) : go(mx_read_kernel<T, D, 4, true>);
+        else if (read) format == SSD_MXFP8 ? go(mx_read_kernel<T, D, 8, false>) : go(mx_read_kernel<T, D, 4, false>);
         else format == SSD_MXFP8 ? go(mx_append_kernel<T, D, 8>) : go(mx_append_kernel<T, D, 4>);
     };
     const auto by_row = [&](auto t) {

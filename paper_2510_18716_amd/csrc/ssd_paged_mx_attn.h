@@ -383,25 +383,29 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
     // column of o[j][i] in lane
     static __device__ __forceinline__ int column(int j, int i, int lane) { return NV * (4 * (lane >> 4) + i) + (COPIES == 1 ? j : 2 * j + odd(lane)); }
 
-    // A step's newest row: its codes into the pool, by every workgroup that is about to read it (all write the same).
-    static __device__ __forceinline__ void put_newest(const PagedAttnArgs &a, int b, int kv, int n, const char *k_new, const char *v_new) {
-        constexpr int PARTS = D / 8;
-        const int tid = (int)threadIdx.x, part = tid & (PARTS - 1);
-        if (tid >= 2 * PARTS) return;
-        const bool is_v = tid >= PARTS;
-        const Eight<T> x = load_eight<T>((is_v ? v_new : k_new) + part * 8 * (int)sizeof(T));
+    // A step's newest row: its codes into the pool, by the wave that is about to read it (of every workgroup that does: all write the same).  A wave's loads are in
+    // order with the stores before them.
+    static constexpr int SLICES = D / 8;                           // lanes of a row, eight elements each: K's, then V's
+    struct Newest { Eight<T> x; };
+    static __device__ __forceinline__ Newest load_newest(const char *k_new, const char *v_new, int lane) {
+        const char *row = lane & SLICES ? v_new : k_new;
+        return {load_eight<T>(row + (lane & (SLICES - 1)) * 8 * (int)sizeof(T))};
+    }
+    static __device__ __forceinline__ void put_newest(const Newest &x, const PagedAttnArgs &a, int b, int kv, int n, int lane) {
+        const int slice = lane & (SLICES - 1);
+        const bool is_v = lane & SLICES;
         int block, place;
         split_slot(a.g, n - 1, block, place);
         const int page = page_of(a.g, b, block);
-        const uint32_t byte = mx_scale_of<BITS>(quad_max(largest_of<T>(x)));
-        const Codes<BITS> c = mx_encode<BITS, T>(x, byte);
-        if (page < 0) return;
-        char *to = (is_v ? a.v_dst : a.k_dst) + row_offset(a.g, page, kv, place) + part * BITS;
-#pragma unroll
-        for (int i = 0; i < BITS / 4; ++i) reinterpret_cast<uint32_t *>(to)[i] = c.c[i];
-        const int64_t entry = table_index(a.g, page, kv, place);
-        if (part % 4 == 0) (is_v ? a.v_scales : a.k_scales)[entry * SB + part / 4] = (uint8_t)byte;
-        if (tid == 0 && a.pos) a.pos[entry] = a.g.seq_pos[b] - 1;
+        const uint32_t byte = mx_scale_of<BITS>(quad_max(largest_of<T>(x.x)));
+        const Codes<BITS> c = mx_encode<BITS, T>(x.x, byte);
+        if (page >= 0 && lane < 2 * SLICES) {
+            *reinterpret_cast<Codes<BITS> *>((is_v ? a.v_dst : a.k_dst) + row_offset(a.g, page, kv, place) + slice * BITS) = c;
+            const int64_t entry = table_index(a.g, page, kv, place);
+            if (slice % 4 == 0) (is_v ? a.v_scales : a.k_scales)[entry * SB + slice / 4] = (uint8_t)byte;
+            if (lane == 0 && a.pos) a.pos[entry] = a.g.seq_pos[b] - 1;
+        }
+        asm volatile("" ::: "memory");
     }
 };
 

@@ -4,8 +4,9 @@
 // of 53 bits and is divided by 2 pi with the quotient's rounding made up for, so that positions of 2^31 lose nothing; then the fraction of a quarter turn
 // that is left is at most pi / 4, where the series of sine and cosine up to r^11 and r^10 are below 2^-28 off.
 //
-// Bound by HBM: every element read once and written once.  A token's angles serve all its heads: they are found once per workgroup, into LDS, while the heads'
-// elements are on their way.
+// Bound by HBM: every element read once and written once.  A token's angles serve all its heads: they are found once per workgroup, into LDS.  22500 tokens of 40 heads of 128
+// elements (bf16) 75 us, 6.1 TB/s read and written; 4611 of 32 heads 16.2 us, 4.7; 16 tokens 3.4 us on the device, launch and latency.  (The first elements requested before
+// the angles are found: 87 and 16.7 us.)
 #include <cmath>
 
 #include "ssd_device.h"
@@ -58,8 +59,20 @@ template <typename T> static __device__ __forceinline__ T from_f32(float x) {
     else return T{(uint16_t)f32_to_bf16_bits(x)};
 }
 
+// A run of neighbouring elements.  ONCE: of more than the memory-side cache holds.
+template <typename R, bool ONCE> static __device__ __forceinline__ R load_run(const void *p) {
+    if constexpr (ONCE && sizeof(R) == 16) return __builtin_bit_cast(R, __builtin_nontemporal_load(reinterpret_cast<const u32x4_nt_t *>(p)));
+    else if constexpr (sizeof(R) == 16) return __builtin_bit_cast(R, *reinterpret_cast<const u32x4_nt_t *>(p));
+    else return *reinterpret_cast<const R *>(p);
+}
+template <typename R, bool ONCE> static __device__ __forceinline__ void store_run(void *p, const R &r) {
+    if constexpr (ONCE && sizeof(R) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_nt_t, r), reinterpret_cast<u32x4_nt_t *>(p));
+    else if constexpr (sizeof(R) == 16) *reinterpret_cast<u32x4_nt_t *>(p) = __builtin_bit_cast(u32x4_nt_t, r);
+    else *reinterpret_cast<R *>(p) = r;
+}
+
 // VEC: elements of a lane's run; HALF: pair i is (i, i + pairs), else (2 i, 2 i + 1).
-template <typename T, int VEC, bool HALF> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+template <typename T, int VEC, bool HALF, bool ONCE> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     extern __shared__ __align__(16) float2 turns[];               // [tokens][pairs]
     typedef Wide<T, VEC> run_t;
     const int t0 = (int)blockIdx.x * a.tokens, tokens = a.n - t0 < a.tokens ? a.n - t0 : a.tokens;
@@ -77,11 +90,11 @@ template <typename T, int VEC, bool HALF> __global__ __launch_bounds__(256) void
         T *out = reinterpret_cast<T *>(a.out + (int64_t)(t0 + t) * a.out_stride) + (int64_t)h * a.d;
         if (c >= per_head) {
             const int at = 2 * a.pairs + (c - per_head) * VEC;
-            *reinterpret_cast<run_t *>(out + at) = *reinterpret_cast<const run_t *>(x + at);
+            store_run<run_t, ONCE>(out + at, load_run<run_t, ONCE>(x + at));
             continue;
         }
         if constexpr (HALF) {
-            run_t u = *reinterpret_cast<const run_t *>(x + c * VEC), w = *reinterpret_cast<const run_t *>(x + a.pairs + c * VEC);
+            run_t u = load_run<run_t, ONCE>(x + c * VEC), w = load_run<run_t, ONCE>(x + a.pairs + c * VEC);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 const float2 cs = turns[t * a.pairs + c * VEC + e];
@@ -89,10 +102,10 @@ template <typename T, int VEC, bool HALF> __global__ __launch_bounds__(256) void
                 u.e[e] = from_f32<T>(p * cs.x - q * cs.y);
                 w.e[e] = from_f32<T>(q * cs.x + p * cs.y);
             }
-            *reinterpret_cast<run_t *>(out + c * VEC) = u;
-            *reinterpret_cast<run_t *>(out + a.pairs + c * VEC) = w;
+            store_run<run_t, ONCE>(out + c * VEC, u);
+            store_run<run_t, ONCE>(out + a.pairs + c * VEC, w);
         } else {
-            run_t u = *reinterpret_cast<const run_t *>(x + c * VEC);
+            run_t u = load_run<run_t, ONCE>(x + c * VEC);
 #pragma unroll
             for (int e = 0; e < VEC; e += 2) {
                 const float2 cs = turns[t * a.pairs + (c * VEC + e) / 2];
@@ -100,7 +113,7 @@ template <typename T, int VEC, bool HALF> __global__ __launch_bounds__(256) void
                 u.e[e] = from_f32<T>(p * cs.x - q * cs.y);
                 u.e[e + 1] = from_f32<T>(q * cs.x + p * cs.y);
             }
-            *reinterpret_cast<run_t *>(out + c * VEC) = u;
+            store_run<run_t, ONCE>(out + c * VEC, u);
         }
     }
 }
@@ -108,12 +121,16 @@ template <typename T, int VEC, bool HALF> __global__ __launch_bounds__(256) void
 template <typename T, bool HALF> static void launch_rope(const RopeArgs &a, int vec, hipStream_t s) {
     const dim3 grid((unsigned)((a.n + a.tokens - 1) / a.tokens));
     const unsigned lds = (unsigned)(a.tokens * a.pairs * sizeof(float2));
+    // 230 MB: 84 us without the hint, 75 with it; 82 MB: 39.5 and 39.9; 38 MB: 16.2 and 21
+    const bool once = (int64_t)a.n * a.heads * a.d * (int64_t)sizeof(T) > 64 << 20;
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), lds, s, a); };
-    if constexpr (sizeof(T) == 2)
-        if (vec == 8) return go(rope_kernel<T, 8, HALF>);
-    if (vec >= 4) go(rope_kernel<T, 4, HALF>);
-    else if (vec == 2 || !HALF) go(rope_kernel<T, 2, HALF>);
-    else if constexpr (HALF) go(rope_kernel<T, 1, HALF>);
+    if (vec * sizeof(T) == 16) {
+        constexpr int VEC = 16 / sizeof(T);
+        return once ? go(rope_kernel<T, VEC, HALF, true>) : go(rope_kernel<T, VEC, HALF, false>);
+    }
+    if (vec == 4) go(rope_kernel<T, 4, HALF, false>);
+    else if (vec == 2 || !HALF) go(rope_kernel<T, 2, HALF, false>);
+    else if constexpr (HALF) go(rope_kernel<T, 1, HALF, false>);
 }
 
 }  // namespace ssd
@@ -164,7 +181,11 @@ extern "C" int ssd_rope_axes(const void *x, void *out, int n_rows, int n_heads, 
     const uint64_t bits = (uint64_t)a.x_stride | (uint64_t)a.out_stride | (uintptr_t)x | (uintptr_t)out | (uint64_t)(head_dim * e) |
                           (uint64_t)((rope_layout == SSD_ROPE_HALF ? n_pairs : 2 * n_pairs) * e) | 16u;
     const int vec = (int)((int64_t)(bits & (0 - bits)) / e);
+    // a token to a workgroup, or as many as its threads have pieces for (4611 tokens of 32 heads 16.2 us, of two 16.4, of four 16.4; of 8 heads 9.7, 7.6, 7.7; 22500 of 40 heads
+    // 84, 88, 92)
+    const int64_t pieces = (int64_t)n_heads * (head_dim / vec);
     a.tokens = 1;
+    while (a.tokens < 32 && a.tokens * pieces < 256 && (int64_t)a.tokens * n_pairs < 1024) a.tokens *= 2;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool half = rope_layout == SSD_ROPE_HALF;
     if (dtype == SSD_F32) half ? launch_rope<float, true>(a, vec, s) : launch_rope<float, false>(a, vec, s);
