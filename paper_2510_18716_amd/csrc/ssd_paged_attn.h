@@ -34,6 +34,7 @@ struct PagedAttnArgs {
     int tile_heads;           // min(group, 16)
     int workgroups;           // 0: a workgroup takes a whole unit
     int by_length;            // then: the longest sequences first
+    int together;             // codes: heads of a sequence on one XCD, their rows share cache lines
     int stage;                // rows whose part of the block table is in LDS at a time: a multiple of a round
     uint32_t page_magic, single;   // ceil(2^32 / page_size) and 0, or 0 and 1 where that is 2^32
     float scale;              // softmax scale * log2 e
@@ -202,6 +203,20 @@ template <int PER> static __device__ __forceinline__ int by_length(const PagedAt
 // What becomes of a tile's logits: nothing more, or they wait for the softmax's sum, in memory for the second launch or in LDS for the end of this one.
 enum Weights { NONE, LATER, HERE };
 
+// The unit of a workgroup of a grid (units of a sequence, sequences) where a sequence's are to be on one XCD, as its heads' rows share cache lines: eight sequences' at
+// a time (four bits, 128 sequences of 64 to 640 rows, 32 heads side by side: rows of 128 elements 52 -> 44 us, of 64 with weights 54 -> 42).  Runs are dealt as they come:
+// with neighbours on one XCD 10 sequences of 64601 rows of 64 elements, four heads side by side, 111 -> 105 us (51 with heads apart), 128 of 10 to 8000 rows 64 -> 66.
+static __device__ __forceinline__ void heads_of(const PagedGeom &g, uint32_t units, int &unit, int &seq) {
+    const uint32_t i = blockIdx.y * units + blockIdx.x;
+    if (i < (uint32_t)g.n_seqs / 8 * 8 * units) {
+        seq = (int)(i / (8 * units) * 8 + (i & 7));
+        unit = (int)(i / 8 % units);
+    } else {
+        seq = (int)blockIdx.y;
+        unit = (int)blockIdx.x;
+    }
+}
+
 // grid = (workgroups), or (kv heads * tiles of query heads, sequences) where a workgroup takes a whole unit
 template <typename TT, bool QUADS, bool STEP, Weights WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(PagedAttnArgs) {
@@ -229,6 +244,8 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
         int rank = (int)blockIdx.y;
         if constexpr (WEIGHTS == HERE) unit_of(a.g, ht, rank);
         else ht = (int)((blockIdx.x + blockIdx.y) % K);
+        if constexpr (TT::MX)
+            if (a.together) heads_of(a.g, K, ht, rank);
         b = a.by_length ? by_length<2>(a, rank, lane) : rank;
         t = 0;
         n = clamp_len(a.g, b);
@@ -875,6 +892,7 @@ static inline int attend_args(const AttendCall &c, const TileShape &tile, int bi
     a.group = c.cfg->n_heads / c.cfg->n_kv_heads;
     a.scale = LOG2E * (c.cfg->softmax_scale != 0.f ? c.cfg->softmax_scale : 1.f / sqrtf((float)c.cfg->head_dim));
     a.k_scales = a.v_scales = nullptr;
+    a.together = a.g.head_stride < 128 && a.g.n_kv > 1;
     return SSD_OK;
 }
 

@@ -10,7 +10,7 @@
 // With four bits a row's bytes are so few that instructions bound the kernel as soon as memory: 166 vector instructions for 32 rows of 128 elements, 64 of them
 // conversions (290 before: V turned by byte permutations 32, addresses added lane by lane 14, logits scaled on their own 8, the workgroup's page addresses looked
 // up in LDS; 4 sequences of 30000 to 131072 rows 63 -> 59 us, 128 of 64 to 640 rows of 32 heads 48 -> 38).  Tried and taken back: tiles of 64 rows (70 and 57 us: the
-// registers do not hold them), tiles that pass through LDS by direct loads (64 and 51).
+// registers do not hold them; rows of 64 elements, which they hold, gain nothing), tiles that pass through LDS by direct loads (64 and 51).
 #pragma once
 
 #include "ssd_mx.h"
@@ -167,7 +167,7 @@ static constexpr int mx_resident(bool f32, int d) { return f32 && d == 128 ? 2 :
 template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
     typedef T elem;
     static constexpr bool MX = true, TABLE = true, QUADS = GROUP >= 4;
-    static constexpr int RESIDENT = mx_resident(sizeof(T) == 4, D_), ENTRIES = GROUP == 16 ? 0 : MxRows<2, 1, GROUP>::LDS;
+    static constexpr int RESIDENT = mx_resident(sizeof(T) == 4, D_), ENTRIES = GROUP == 16 ? 0 : 128;
     typedef MxEntry entry_t;
     static constexpr int D = D_, BITS = BITS_, SB = D / 32;        // SB: bytes of a row's scales
     static constexpr int SUB = 2, ROWS = 16 * SUB;
