@@ -1,7 +1,7 @@
 // What the attention over a paged cache shares, whatever the pool holds: who works on which rows, the pass over a unit's tiles with the running softmax, the
 // meeting of parts, the weights, and the launches.  A tile's operands and products are the including file's: a type TT with
 //   elem, D, ROWS, NO     element type of q and the output, row length, rows of a tile, accumulators
-//   RESIDENT              waves of a SIMD that the registers are to allow
+//   RESIDENT, EXTRA       waves of a SIMD that the registers are to allow; what a unit costs besides its rounds
 //   MX                    whether the pool holds codes with scales (the newest row of a step then goes into the pool first)
 //   TABLE                 whether every wave looks up the addresses of its own tiles' rows, TILES of them at a time (else the workgroup has the pages' in LDS)
 //   Q, load_q, head, logits, zero_v, accumulate, finish, column
@@ -83,9 +83,9 @@ static __device__ __forceinline__ int rounds_of(int n, int round) { return n == 
 
 // What a unit costs besides its rounds, in rounds: its queries, its part of the block table and the meeting of its waves, 4 us against 3 to 6 for a
 // round (128 sequences of 10 to 8000 rows with weights: counted as none 98 us, as one round 88, two 89, three 91; 48 of up to 5000, fp32: 39.8, 38.5, 39.6,
-// 40.8; one of 5000 rows 14.1 and 15.2).
-static constexpr int EXTRA = 1;
-static __device__ __forceinline__ uint32_t cost_of(int n, int round) { return (uint32_t)rounds_of(n, round) + EXTRA; }
+// 40.8; one of 5000 rows 14.1 and 15.2).  Rounds of codes are shorter, so that it counts for more of them (TT::EXTRA; 128 sequences of 10 to 8000 rows with weights and new rows, one, two
+// and three rounds: eight bits 64.4, 62.2 and 62.5, four bits 49.4, 46.2 and 45.7).
+template <int EXTRA> static __device__ __forceinline__ uint32_t cost_of(int n, int round) { return (uint32_t)rounds_of(n, round) + EXTRA; }
 
 static __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
@@ -221,7 +221,7 @@ static __device__ __forceinline__ void heads_of(const PagedGeom &g, uint32_t uni
 template <typename TT, bool QUADS, bool STEP, Weights WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(PagedAttnArgs) {
     typedef typename TT::elem T;
-    constexpr int D = TT::D;
+    constexpr int D = TT::D, EXTRA = TT::EXTRA;
     constexpr bool IDS = !TT::TABLE && (WEIGHTS == HERE || TT::MX), PAGES = !TT::TABLE && !TT::MX;      // what of the blocks is in LDS
     constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
     constexpr int ROUND = WAVES * TT::ROWS;
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 len[i] = len[i] < 0 ? 0 : len[i] > a.g.max_len ? a.g.max_len : len[i];
-                mine += 64 * i + lane < a.g.n_seqs ? cost_of(len[i], ROUND) : 0u;
+                mine += 64 * i + lane < a.g.n_seqs ? cost_of<EXTRA>(len[i], ROUND) : 0u;
             }
             const uint32_t all = uniform(wave_sum(mine)) * K;
             const Runs runs = Runs::of(all, (uint32_t)a.workgroups);
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (b >= 0 || 64 * i >= a.g.n_seqs) continue;
-                const uint32_t up = wave_scan(64 * i + lane < a.g.n_seqs ? cost_of(len[i], ROUND) : 0u) + before;
+                const uint32_t up = wave_scan(64 * i + lane < a.g.n_seqs ? cost_of<EXTRA>(len[i], ROUND) : 0u) + before;
                 const int k = (int)__popcll(__ballot(up <= at));
                 if (k < 64) {
                     b = 64 * i + k;
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
             uint32_t mine = 0;
             for (int i = 0; i < run; ++i) {
                 const int seq = lane * run + i;
-                if (seq < a.g.n_seqs) mine += cost_of(clamp_len(a.g, seq), ROUND);
+                if (seq < a.g.n_seqs) mine += cost_of<EXTRA>(clamp_len(a.g, seq), ROUND);
             }
             const uint32_t upto = wave_scan(mine);
             const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * K;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
             for (int i0 = 0;; i0 += 64) {                           // the run's sequences, 64 at a time
                 const int seq = l * run + i0 + lane;
                 const bool ours = i0 + lane < run && seq < a.g.n_seqs;
-                const uint32_t up = wave_scan(ours ? cost_of(clamp_len(a.g, seq), ROUND) : 0u) + before;
+                const uint32_t up = wave_scan(ours ? cost_of<EXTRA>(clamp_len(a.g, seq), ROUND) : 0u) + before;
                 const int k = (int)__popcll(__ballot(up <= at));
                 if (k < 64) {
                     b = l * run + i0 + k;
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
             }
             n = clamp_len(a.g, b);
         }
-        const uint32_t tb = uniform(cost_of(n, ROUND)), into = r0 - before * K;
+        const uint32_t tb = uniform(cost_of<EXTRA>(n, ROUND)), into = r0 - before * K;
         ht = (int)(into / tb);
         t = (int)(into - (uint32_t)ht * tb) - EXTRA;
         if (t < 0) {                                                // the run begins with what the unit costs besides
@@ -590,7 +590,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
             a.parts[(int64_t)b * (a.g.n_kv * a.q_tiles) + ht] = make_uint2((uint32_t)slot, count);
         }
         left -= (uint32_t)take;
-        if (left <= EXTRA) return;
+        if (left <= (uint32_t)EXTRA) return;
         left -= EXTRA;
         t = 0;
         if (++ht == a.g.n_kv * a.q_tiles) {
@@ -759,7 +759,7 @@ static PagedShape paged_shape(const ssd_paged_config *c, int max_len, const Tile
     // and 16.7, 32 12.2 and 11.5); with more rounds only where units are many (256 of 1000 rows 24.5 and 28.6, of 10 to 1000 18.5 and 16.6, 1024 85 and 92, 38 and
     // 34; 128 of 1000 19.7 and 21.0, of 10 to 1000 17.7 and 13.3; 512 of 2048 84 and 91, of 10 to 2048 44 and 29; all with 16 key heads, two query heads each; weights
     // change little), and where 32 bits would not hold the sums.
-    const bool plain = rounds <= 5 || (units >= 256 && rounds <= 8) || units * (rounds + EXTRA) >= 1ll << 31;
+    const bool plain = rounds <= 5 || (units >= 256 && rounds <= 8) || units * (rounds + 3) >= 1ll << 31;
     // Very short units, many of them: a wave each (2048 of 128 rows 25.6 us and 29.0 with four waves, of 256 45 and 47; 512 of 128 10.3 and 9.3).
     s.waves = units >= 1024 && rounds <= 2 ? 1 : 4;
     s.round = s.waves * tile;

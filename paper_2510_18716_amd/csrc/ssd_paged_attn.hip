@@ -127,7 +127,7 @@ template <typename T, int D> struct Tile;
 template <int D_> struct Tile<bf16_t, D_> {
     typedef bf16_t elem;
     static constexpr bool MX = false, TABLE = false;
-    static constexpr int RESIDENT = 3, ENTRIES = 0;
+    static constexpr int RESIDENT = 3, EXTRA = 1, ENTRIES = 0;
     typedef int entry_t;
     static __device__ __forceinline__ int head(int r) { return r; }
     static __device__ __forceinline__ bool writes(int) { return true; }
@@ -193,7 +193,7 @@ template <int D_> struct Tile<bf16_t, D_> {
 template <int D_> struct Tile<float, D_> {
     typedef float elem;
     static constexpr bool MX = false, TABLE = false;
-    static constexpr int RESIDENT = 3, ENTRIES = 0;
+    static constexpr int RESIDENT = 3, EXTRA = 1, ENTRIES = 0;
     typedef int entry_t;
     static __device__ __forceinline__ int head(int r) { return r; }
     static __device__ __forceinline__ bool writes(int) { return true; }

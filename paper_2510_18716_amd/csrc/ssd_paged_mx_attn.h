@@ -167,7 +167,7 @@ static constexpr int mx_resident(bool f32, int d) { return f32 && d == 128 ? 2 :
 template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
     typedef T elem;
     static constexpr bool MX = true, TABLE = true, QUADS = GROUP >= 4;
-    static constexpr int RESIDENT = mx_resident(sizeof(T) == 4, D_), ENTRIES = GROUP == 16 ? 0 : 128;
+    static constexpr int RESIDENT = mx_resident(sizeof(T) == 4, D_), EXTRA = BITS_ == 4 ? 3 : 2, ENTRIES = GROUP == 16 ? 0 : 128;
     typedef MxEntry entry_t;
     static constexpr int D = D_, BITS = BITS_, SB = D / 32;        // SB: bytes of a row's scales
     static constexpr int SUB = 2, ROWS = 16 * SUB;
