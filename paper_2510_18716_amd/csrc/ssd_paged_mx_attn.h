@@ -182,13 +182,12 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
     static constexpr int TILES = MxRows<SUB, SB, GROUP>::TILES;
     typedef typename Words<KW>::type krow_t;
     typedef std::conditional_t<VB == 2, uint16_t, typename Words<VB == 8 ? 2 : 1>::type> vrow_t;
-    typedef typename Words<SB>::type four_t;                       // scales of four rows
     typedef std::conditional_t<SB == 2, uint16_t, uint32_t> one_t;  // of one
 
     krow_t k[SUB];
     uint32_t ks[SUB];
     vrow_t v[4 * SUB];
-    std::conditional_t<QUADS, four_t, one_t> vs[QUADS ? SUB : 4 * SUB];
+    uint32_t vs[QUADS ? SUB : 4 * SUB];                            // V's scales: QUADS of row 4 g + lane % 4 of a group, else of row i
     struct Q { bf16x8 x[QT][STEPS]; };
 
     static __device__ __forceinline__ int odd(int lane) { return (lane & 15) / HT & 1; }
@@ -255,28 +254,25 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
                         : mx_pair<BITS, BITS == 4 ? 3 : 1>(codes, scale);
     }
 
-    // Scale of row i in the lane's block of V.
+    // Scale of row i in the lane's block of V, the byte (lane % 16) NV / 32 of the row's; four neighbouring lanes have four rows'.
     __device__ __forceinline__ float v_scale(int i, int lane) const {
         const uint32_t block = (uint32_t)(lane & 15) * NV / 32;
-        uint32_t w, at = 8 * block;
+        uint32_t w;
         if constexpr (QUADS) {
-            if constexpr (SB == 4) {
-                w = vs[i / 4][i % 4];
-            } else {
-                w = vs[i / 4][i % 4 / 2];
-                at += 16 * (i % 2);
-            }
+            const int x = (int)vs[i / 4];
+            w = (uint32_t)(i % 4 == 0 ? __builtin_amdgcn_update_dpp(0, x, 0x00, 0xF, 0xF, true) : i % 4 == 1 ? __builtin_amdgcn_update_dpp(0, x, 0x55, 0xF, 0xF, true)
+                           : i % 4 == 2 ? __builtin_amdgcn_update_dpp(0, x, 0xAA, 0xF, 0xF, true) : __builtin_amdgcn_update_dpp(0, x, 0xFF, 0xF, 0xF, true));
         } else {
             w = vs[i];
         }
-        return __uint_as_float(__builtin_amdgcn_ubfe(w, at, 8) << 23);
+        w &= 0xffu << 8 * block;
+        return __uint_as_float(__builtin_amdgcn_alignbit(w, w, 8 * block + 9));        // the byte to the exponent's place
     }
     // A row that does not exist: neither its codes nor a scale that is NaN may count.
     __device__ __forceinline__ void zero_v(int i) {
         v[i] = vrow_t(0);
         if constexpr (!QUADS) vs[i] = 0;
-        else if constexpr (SB == 4) vs[i / 4][i % 4] = 0;
-        else vs[i / 4][i % 4 / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+        else if ((int)(threadIdx.x & 3) == i % 4) vs[i / 4] = 0;
     }
 
     // x less one of two bf16 (`which`: -1 in its place, 0 in the other's), exactly: the upper half of x, so that what is left has fewer bits.
@@ -445,7 +441,7 @@ static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, c
         const __amdgpu_buffer_rsrc_t from = mx_buffer(a.v_pages + at.off[s]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) tl.v[4 * s + i] = mx_load<typename TT::vrow_t, 2>(from, own, (uint32_t)i * (uint32_t)a.g.row_stride);
-        tl.vs[s] = mx_load<typename TT::four_t, 0>(mx_buffer(a.v_scales + at.soff[s]), g * (4 * SB), 0);
+        tl.vs[s] = mx_load<typename TT::one_t, 0>(mx_buffer(a.v_scales + at.soff[s]), (4 * g + (lane & 3)) * SB, 0);
     }
 }
 template <typename Step, typename TT, int SUB, int SB, int GROUP>
@@ -460,9 +456,9 @@ static __device__ __forceinline__ void request_v(Step, const PagedAttnArgs &a, c
         const char *row = a.v_pages + (GROUP == 4 ? at.v[i / 4] + i % 4 * a.g.row_stride : at.v[i]);
         tl.v[i] = TT::template load<typename TT::vrow_t>(row + ((uint32_t)lane & 15) * TT::VB);
     }
-    typedef std::remove_reference_t<decltype(tl.vs[0])> scales_t;
 #pragma unroll
-    for (int i = 0; i < MxRows<SUB, SB, GROUP>::NV; ++i) tl.vs[i] = *reinterpret_cast<const scales_t *>(a.v_scales + at.vs[i]);
+    for (int i = 0; i < MxRows<SUB, SB, GROUP>::NV; ++i)
+        tl.vs[i] = *reinterpret_cast<const typename TT::one_t *>(a.v_scales + at.vs[i] + (GROUP == 4 ? (lane & 3) * SB : 0));
 }
 
 // Rows that are neighbours in a page: 16 (at distances that fit 32 bits), 4 (up to eight query heads on a key head: there are no tiles of sixteen for it) or 1.
