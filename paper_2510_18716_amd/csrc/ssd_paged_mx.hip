@@ -100,7 +100,7 @@ template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx
         for (int u = 0; u < U; ++u) {
             const Share x(a, q + u, lane, per_token);
             const int row = row0 + x.i;
-            const int64_t from = (int64_t)(row < a.n ? row : a.n - 1) * a.stride + (int64_t)(x.f < frags ? x.f : lane) * (8 * (int)sizeof(T));
+            const int64_t from = (int64_t)(row < a.n ? row : a.n - 1) * a.stride + (int64_t)(x.f < frags ? x.f : 0) * (8 * (int)sizeof(T));
             k[u] = load_eight<T>(a.k + from);
             v[u] = load_eight<T>(a.v + from);
         }
