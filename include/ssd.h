@@ -529,8 +529,8 @@ int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, c
  * that all elements of the block are NaN.
  * Writing: E is the smallest exponent with which no element of the block is off by more than half a step, that is with largest |x| <= 464 * 2^E or
  * 7 * 2^E, at least -117 or -125; codes are rounded to the nearest, ties to the even code (the largest are 448 and 6).  A block that holds a NaN or an
- * infinity becomes NaN.  So an element keeps 4 (2) significant bits, relative to the block's largest at least 2^-18 (2^-4) of it; elements whose rounding
- * reaches 2^128 read back as infinities.
+ * infinity becomes NaN.  So an element is off by at most 2^-4 (2^-2) of itself or, where that is more, 2^-17 (2^-3) of its block's largest; elements whose
+ * rounding reaches 2^128 read back as infinities, whose products may give NaN.
  * Reading: a bf16 or fp32 number holds every value exactly.  (Pools written elsewhere: elements below 2^-126 may be read as 0.)
  */
 typedef enum ssd_mx_format { SSD_MXFP4 = 4, SSD_MXFP8 = 8 } ssd_mx_format;
@@ -593,7 +593,7 @@ int ssd_paged_mx_evict(const ssd_paged_config *cfg, int format, void *k_pages, v
  *   n_pairs     : 1..head_dim / 2; elements 2 * n_pairs and beyond of a head stay as they are (in out: are copied)
  *   rope_layout : SSD_ROPE_HALF pairs element i with i + n_pairs; SSD_ROPE_INTERLEAVED 2i with 2i + 1
  *   inverse     : 1 turns back, by the negative angles: the gradient of x from that of out
- *   n_rows >= 0;  n_heads 1..4096;  head_dim even, 2..1024
+ *   n_rows      : 0 .. 2^24 - 1;  n_heads 1..4096;  head_dim even, 2..1024;  strides up to 2^28
  */
 int ssd_rope_axes(const void *x, void *out, int n_rows, int n_heads, int head_dim, int dtype, int64_t x_stride, int64_t out_stride, const int32_t *pos,
                   int n_axes, const uint8_t *axis, const float *inv_freq, int n_pairs, int rope_layout, int inverse, void *stream);

@@ -144,7 +144,7 @@ extern "C" int ssd_rope_axes(const void *x, void *out, int n_rows, int n_heads, 
     if (n_rows != 0 && (!x || !out || !pos)) return fail(SSD_ERR_INVALID_ARG, "x, out or pos is NULL");
     if (!inv_freq) return fail(SSD_ERR_INVALID_ARG, "inv_freq is NULL");
     if (dtype != SSD_F32 && dtype != SSD_BF16) return fail(SSD_ERR_INVALID_ARG, "dtype=%d is neither SSD_F32 nor SSD_BF16", dtype);
-    if (n_rows < 0) return fail(SSD_ERR_INVALID_ARG, "n_rows=%d must be >= 0", n_rows);
+    if (n_rows < 0 || n_rows >= 1 << 24) return fail(SSD_ERR_INVALID_ARG, "n_rows=%d outside 0..2^24 - 1", n_rows);
     if (n_heads < 1 || n_heads > 4096) return fail(SSD_ERR_INVALID_ARG, "n_heads=%d outside 1..4096", n_heads);
     if (head_dim < 2 || head_dim > 1024 || head_dim % 2 != 0) return fail(SSD_ERR_INVALID_ARG, "head_dim=%d must be even, 2..1024", head_dim);
     if (n_pairs < 1 || n_pairs > head_dim / 2) return fail(SSD_ERR_INVALID_ARG, "n_pairs=%d outside 1..head_dim / 2", n_pairs);
@@ -153,8 +153,8 @@ extern "C" int ssd_rope_axes(const void *x, void *out, int n_rows, int n_heads, 
     if (rope_layout != SSD_ROPE_HALF && rope_layout != SSD_ROPE_INTERLEAVED) return fail(SSD_ERR_INVALID_ARG, "rope_layout=%d", rope_layout);
     if (inverse != 0 && inverse != 1) return fail(SSD_ERR_INVALID_ARG, "inverse=%d is neither 0 nor 1", inverse);
     const int64_t e = dtype == SSD_F32 ? 4 : 2, row = (int64_t)n_heads * head_dim;
-    if ((x_stride != 0 && (x_stride < row || x_stride > 1ll << 40)) || (out_stride != 0 && (out_stride < row || out_stride > 1ll << 40)))
-        return fail(SSD_ERR_INVALID_ARG, "x_stride and out_stride must be 0 or at least n_heads * head_dim");
+    if ((x_stride != 0 && (x_stride < row || x_stride > 1ll << 28)) || (out_stride != 0 && (out_stride < row || out_stride > 1ll << 28)))
+        return fail(SSD_ERR_INVALID_ARG, "x_stride and out_stride must be 0 or n_heads * head_dim .. 2^28");
     if (!aligned(x, e) || !aligned(out, e) || !aligned(pos, 4) || !aligned(inv_freq, 4))
         return fail(SSD_ERR_INVALID_ARG, "x, out, pos and inv_freq must be aligned to their elements");
     RopeArgs a;

@@ -131,8 +131,8 @@ def _rope(**kw):
 
 def test_rope_refusals():
     for bad in (dict(x=None), dict(out=None), dict(pos=None), dict(inv=None), dict(x=FAKE + 2), dict(out=2 * FAKE + 1), dict(x=FAKE + 1, t=1), dict(pos=FAKE + 2), dict(inv=FAKE + 2),
-                dict(n=-1), dict(H=0), dict(H=4097), dict(d=0), dict(d=63), dict(d=1026), dict(t=2), dict(pairs=0), dict(pairs=33), dict(axes=0), dict(axes=5), dict(axis=None),
-                dict(layout=0), dict(layout=3), dict(inverse=2), dict(xs=127), dict(os=64), dict(xs=-128), dict(xs=1 << 41)):
+                dict(n=-1), dict(n=1 << 24), dict(H=0), dict(H=4097), dict(d=0), dict(d=63), dict(d=1026), dict(t=2), dict(pairs=0), dict(pairs=33), dict(axes=0), dict(axes=5), dict(axis=None),
+                dict(layout=0), dict(layout=3), dict(inverse=2), dict(xs=127), dict(os=64), dict(xs=-128), dict(xs=(1 << 28) + 1)):
         assert _rope(**bad) == BAD, bad
         assert ssd.ssd_last_error() != ""
     assert _rope(n=0) == ssd.SSD_OK and _rope(n=0, x=None, out=None, pos=None) == ssd.SSD_OK
