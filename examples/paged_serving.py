@@ -9,9 +9,10 @@ A small random model stands in for the network; what it shows is the order of th
                ssd_paged_evict     when the rows added since the last one fill the slack
                ssd_logits_process  guidance of each request's two sequences, penalties, the tokens that are images'
 
-Every request is two sequences, one with its prompt and one without most of it (classifier-free guidance), so that their lengths differ.
+Every request is two sequences, one with its prompt and one without most of it (classifier-free guidance), so that their lengths differ.  With `pool` "mxfp8" or "mxfp4"
+the rows are held in 8 or 4 bits and the calls are the ssd_paged_mx_ ones; with `columns` queries and keys turn by positions in time, height and width (ssd_rope_axes).
 
-    python examples/paged_serving.py
+    python examples/paged_serving.py [mxfp8 | mxfp4]
 """
 from __future__ import annotations
 
@@ -44,6 +45,8 @@ class Settings:
     gamma: float = 3.0
     temperature: float = 0.9
     repetition: float = 1.1
+    pool: str = "plain"                     # or "mxfp8", "mxfp4"
+    columns: int = 0                        # of the image, if queries and keys turn by their positions
     steps: int = 40
     seed: int = 0
 
@@ -91,24 +94,49 @@ def serve(s: Settings, watch=None):
     seq_pos = seq_len.clone()
     budget = torch.full((B,), s.budget, dtype=torch.int32, device=dev)
     shape = (B * blocks, Hk, s.page)
-    k = [torch.zeros(shape + (d,), device=dev, dtype=dt) for _ in range(s.layers)]
-    v = [torch.zeros(shape + (d,), device=dev, dtype=dt) for _ in range(s.layers)]
+    bits = {"plain": 0, "mxfp8": 8, "mxfp4": 4}[s.pool]
+    row = (d * bits // 8,) if bits else (d,)
+    k = [torch.zeros(shape + row, device=dev, dtype=torch.uint8 if bits else dt) for _ in range(s.layers)]
+    v = [torch.zeros_like(x) for x in k]
+    scales = [[torch.zeros(shape + (d // 32,), device=dev, dtype=torch.uint8) for _ in "kv"] for _ in range(s.layers if bits else 0)]
     pos = [torch.zeros(shape, dtype=torch.int32, device=dev) for _ in range(s.layers)]
     mass = [torch.zeros(shape, device=dev) for _ in range(s.layers)]
     # rows of the projections are (H + 2 Hk) * d long: q, k and v are read where they lie
     cfg = ssd.make_paged_config(B, H, Hk, d, s.dtype, s.page, B * blocks, blocks, q_stride=(H + 2 * Hk) * d, new_stride=(H + 2 * Hk) * d)
-    work = torch.empty(max(ssd.ssd_paged_workspace_bytes(cfg, most, True), ssd.ssd_paged_evict_workspace_bytes(cfg, most)), dtype=torch.uint8, device=dev)
+    if bits:
+        sizes = ssd.ssd_paged_mx_workspace_bytes(cfg, s.pool, most, True), ssd.ssd_paged_mx_evict_workspace_bytes(cfg, s.pool, most)
+    else:
+        sizes = ssd.ssd_paged_workspace_bytes(cfg, most, True), ssd.ssd_paged_evict_workspace_bytes(cfg, most)
+    work = torch.empty(max(sizes), dtype=torch.uint8, device=dev)
     after = torch.zeros_like(seq_len)
 
     def parts(x):
         """Views of a projection's q, k and v."""
         return x[:, :H * d], x[:, H * d:(H + Hk) * d], x[:, (H + Hk) * d:]
 
+    def on_pool(name, l, *args, first=(), **more):
+        """A paged call on layer l's pool: (config, first.., pool, args..), of the kind that the pool is."""
+        if bits:
+            getattr(ssd, "ssd_paged_mx_" + name)(cfg, s.pool, *first, k[l], v[l], *scales[l], *args, **more)
+        else:
+            getattr(ssd, "ssd_paged_" + name)(cfg, *first, k[l], v[l], *args, **more)
+
+    pairs = d // 2
+    axis = torch.tensor([i * 3 // pairs for i in range(pairs)], dtype=torch.uint8, device=dev)
+    inv_freq = torch.tensor([10000.0 ** (-i / pairs) for i in range(pairs)], device=dev)
+
+    def turned(rows, time, i):
+        """Rows of projections whose queries and keys turn by their tokens' positions: time, and the i-th image token's row and column (or the time again)."""
+        if s.columns:
+            pos = torch.stack([time, time if i is None else time - i % s.columns, time if i is None else time - i + i % s.columns]).to(torch.int32)
+            ssd.ssd_rope_axes(rows, rows, len(rows), H + Hk, d, s.dtype, pos, inv_freq, axis=axis, n_axes=3)
+        return rows
+
     def cut(host_lens):
         nonlocal table
         for l in range(s.layers):
-            ssd.ssd_paged_evict(cfg, k[l], v[l], table, seq_len, budget, pos[l], pos[l], mass[l], mass[l], after, n_sink=s.sinks, recent=s.recent,
-                                seq_pos=seq_pos, max_len=most, workspace=work)
+            on_pool("evict", l, table, seq_len, budget, pos[l], pos[l], mass[l], mass[l], after, n_sink=s.sinks, recent=s.recent, seq_pos=seq_pos, max_len=most,
+                    workspace=work)
         seq_len.copy_(after)
         host_lens = [min(n, s.budget) for n in host_lens]
         for b, n in enumerate(host_lens):
@@ -118,7 +146,7 @@ def serve(s: Settings, watch=None):
 
     # the prompts
     for l in range(s.layers):
-        rows = (embed[prompt] @ qkv[l]).to(dt)
+        rows = turned((embed[prompt] @ qkv[l]).to(dt), torch.cat([torch.arange(n, device=dev) for n in lens]), None)
         qp, kp, vp = parts(rows)
         scores = torch.zeros((len(prompt), Hk), device=dev)
         for b, n in enumerate(lens):                                         # one sequence's heads are the units of one call
@@ -128,8 +156,7 @@ def serve(s: Settings, watch=None):
             one = torch.empty((H, n), device=dev)
             ssd.ssd_prefill_scores(Q, K, H, n, d, s.dtype, one)
             scores[part] = one.reshape(Hk, H // Hk, n).sum(1).t()
-        ssd.ssd_paged_append(cfg, k[l], v[l], table, seq_len, kp, vp, pos=pos[l], weight=mass[l], seq_pos=seq_pos, new_start=start.to(dev),
-                             weight_new=scores)
+        on_pool("append", l, table, seq_len, kp, vp, pos=pos[l], weight=mass[l], seq_pos=seq_pos, new_start=start.to(dev), weight_new=scores)
     lens = cut(lens)
 
     # the tokens
@@ -154,13 +181,13 @@ def serve(s: Settings, watch=None):
         since += 1
         x = embed[token].repeat_interleave(2, 0)
         for l in range(s.layers):
-            rows = (x @ qkv[l]).to(dt)
+            rows = turned((x @ qkv[l]).to(dt), seq_pos - 1, step)
             q, k_new, v_new = parts(rows)
             out = torch.empty((B, H, d), device=dev, dtype=dt)
-            ssd.ssd_paged_decode_step(cfg, q, k_new, v_new, k[l], v[l], table, seq_len, out, pos=pos[l], seq_pos=seq_pos, weight_in=mass[l],
-                                      weight_out=mass[l], max_len=most, workspace=work)
+            on_pool("decode_step", l, table, seq_len, out, first=(q, k_new, v_new), pos=pos[l], seq_pos=seq_pos, weight_in=mass[l], weight_out=mass[l],
+                    max_len=most, workspace=work)
             if watch is not None:
-                watch(l, {"q": q, "k": k[l], "v": v[l], "table": table, "lens": lens, "out": out})
+                watch(l, {"q": q, "k": k[l], "v": v[l], "scales": scales[l] if bits else None, "table": table, "lens": lens, "out": out})
             x = x + out.reshape(B, D).float() @ back[l]
         x = x / x.norm(dim=-1, keepdim=True) * D ** 0.5
         ssd.ssd_logits_process(x @ head, n_req, s.vocab, "f32", logits, gamma=s.gamma, tokens=told, n_tokens=n_told, mask=mask, mask_shared=True, **per_row)
@@ -172,7 +199,7 @@ def serve(s: Settings, watch=None):
 
 
 def main():
-    s = Settings()
+    s = Settings(pool=sys.argv[1], columns=24) if len(sys.argv) > 1 else Settings()
     tokens, lens, held = serve(s)
     for i, p in enumerate(s.prompts):
         print("request %d: prompt of %d tokens, %d rows held, tokens %s ..." % (i, p, lens[2 * i], tokens[i, :8].tolist()))

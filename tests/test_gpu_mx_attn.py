@@ -56,9 +56,33 @@ def test_many_units(fmt, n_kv, B, n):
     check_written(bt, step)
 
 
+@pytest.mark.parametrize("H,n_kv,dtype,fmt,page", [(128, 8, "bf16", "mxfp4", 16), (128, 8, "f32", "mxfp8", 7), (40, 8, "bf16", "mxfp8", 20)])
+def test_weights_from_logits_in_lds_at_their_largest(H, n_kv, dtype, fmt, page):
+    """Units of up to 1000 rows taken whole, up to sixteen query heads on a key head."""
+    lens = [1000 - 31 * i if i % 3 else i for i in range(33)]
+    bt = MxBatch(lens, H, n_kv, 64, dtype, fmt, page, seed=23, layout="rows")
+    check(bt, attend(bt))
+
+
+@pytest.mark.parametrize("n_kv,q", [(4, 2), (1, 5), (3, 17)])
+def test_runs_that_begin_and_end_anywhere(n_kv, q):
+    """Many units of one or a few rounds between long ones: runs that begin, end or lie in what a unit costs besides its rounds."""
+    for fmt in ("mxfp4", "mxfp8"):
+        lens = [5000, 1, 0, 130, 127, 900, 3, 2600, 0, 0, 129, 64, 1500, 31, 400]
+        bt = MxBatch(lens, n_kv * q, n_kv, 64, "bf16", fmt, 32, seed=24)
+        for max_len in (0, 2000):
+            check(bt, attend(bt, max_len=max_len), max_len=max_len)
+        step = new_rows(bt, len(lens), seed=25)
+        check(bt, attend(bt, step=step), step=step)
+        check_written(bt, step)
+
+
 def test_more_than_256_sequences_dealt():
     bt = MxBatch([1 + (53 * i) % 90 for i in range(299)] + [4000], 2, 1, 64, "bf16", "mxfp4", 16, seed=7)
     check(bt, attend(bt, weights=True))
+    step = new_rows(bt, 300, seed=26)
+    check(bt, attend(bt, step=step), step=step)
+    check_written(bt, step)
 
 
 def test_pages_that_do_not_exist():
@@ -270,3 +294,32 @@ def test_a_run_of_all_calls():
         bt.weightd = wout
         for b in range(B):                                          # every token's weight came from softmaxes: H of them a step
             assert np.isfinite(wout.cpu().numpy()[bt.table[b][np.arange(lens[b]) // page], :, np.arange(lens[b]) % page]).all()
+
+
+@pytest.mark.parametrize("pool,dtype", [("mxfp4", "bf16"), ("mxfp8", "f32")])
+def test_the_serving_example_on_a_quantised_pool(pool, dtype):
+    import importlib.util
+    import os
+    import sys
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_serving.py")
+    spec = importlib.util.spec_from_file_location("paged_serving", path)
+    example = importlib.util.module_from_spec(spec)
+    sys.modules["paged_serving"] = example
+    spec.loader.exec_module(example)
+    s = example.Settings(prompts=(37, 130, 8), budget=40, slack=12, steps=30, dtype=dtype, pool=pool, columns=6)
+    calls = []
+
+    def watch(layer, st):
+        calls.append(layer)
+        if len(calls) % 11 not in (1, 6):                            # some of the 60
+            return
+        k, v = (mx.decode(x.cpu().numpy(), y.cpu().numpy(), pool) for x, y in zip((st["k"], st["v"]), st["scales"]))
+        table, out, q = st["table"].cpu().numpy(), st["out"].float().cpu().numpy(), st["q"].float().cpu().numpy().reshape(6, s.heads, s.head_dim)
+        for b, n in enumerate(st["lens"]):
+            ref, _, _, size = paged.paged_attend(q[b], k, v, table[b], n, s.head_dim ** -0.5)
+            tol = 5e-5 * size if dtype == "f32" else 2.0 ** -8 * (size + np.abs(ref))
+            assert np.all(np.abs(out[b] - ref) <= tol + 1e-30), (layer, b)
+
+    tokens, lens, held = example.serve(s, watch)
+    assert len(calls) == s.steps * s.layers and tokens.shape == (3, 30)
+    assert bool(((tokens >= s.image_tokens[0]) & (tokens < s.image_tokens[1])).all()) and max(lens) <= s.budget + s.slack
