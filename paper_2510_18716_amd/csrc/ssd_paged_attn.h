@@ -2,7 +2,7 @@
 // meeting of parts, the weights, and the launches.  A tile's operands and products are the including file's: a type TT with
 //   elem, D, ROWS, NO     element type of q and the output, row length, rows of a tile, accumulators
 //   RESIDENT, EXTRA       waves of a SIMD that the registers are to allow; what a unit costs besides its rounds
-//   MX                    whether the pool holds codes with scales (the newest row of a step then goes into the pool first)
+//   MX                    whether the pool holds codes with scales (TABLE then; the newest row of a step goes into the pool first)
 //   TABLE                 whether every wave looks up the addresses of its own tiles' rows, TILES of them at a time (else the workgroup has the pages' in LDS)
 //   Q, load_q, head, logits, zero_v, accumulate, finish, column
 //   Rows<QUADS>           where a lane finds a tile's rows; seen() tells which of them exist
@@ -60,7 +60,7 @@ static __device__ __forceinline__ int block_of(const PagedAttnArgs &a, int x) {
 // A chunk of rows whose part of the block table is in LDS.
 struct Stage {
     const int64_t *pages;                                          // byte offsets of the blocks' pages (head included), or NO_PAGE
-    const int32_t *ids;                                            // their numbers, -1 for none; where weights are brought up to date or the pool holds codes
+    const int32_t *ids;                                            // their numbers, -1 for none; HERE (see Weights) only
     int begin, b;                                                  // first row, sequence
     int lead, rows, kv;                                            // places before the first row in its page; rows; key head
 };
@@ -222,7 +222,7 @@ template <typename TT, bool QUADS, bool STEP, Weights WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(PagedAttnArgs) {
     typedef typename TT::elem T;
     constexpr int D = TT::D, EXTRA = TT::EXTRA;
-    constexpr bool IDS = !TT::TABLE && (WEIGHTS == HERE || TT::MX), PAGES = !TT::TABLE && !TT::MX;      // what of the blocks is in LDS
+    constexpr bool PAGES = !TT::TABLE, IDS = PAGES && WEIGHTS == HERE;      // what of the blocks is in LDS
     constexpr int NZ = TT::ROWS / 4;                                // logits of a lane
     constexpr int ROUND = WAVES * TT::ROWS;
     constexpr int LD = D + 4;                                       // row of the merge area

@@ -224,10 +224,6 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
         k[s] = load<krow_t>(row + (uint32_t)(lane >> 4) * (KE * BITS / 8));
         ks[s] = (uint32_t)*reinterpret_cast<const uint8_t *>(scales + (uint32_t)(lane >> 4) * KE / 32);
     }
-    __device__ __forceinline__ uint32_t word(const krow_t &x, int i) const {
-        if constexpr (KW == 1) return x;
-        else return x[i];
-    }
 
     __device__ __forceinline__ void logits(const Q &q, float (&z)[4 * SUB]) const {
 #pragma unroll
@@ -238,7 +234,7 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
             for (int s = 0; s < STEPS; ++s) {
                 u32x4_nt_t w;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = BITS == 4 ? pair(word(k[t], s), scale, i) : pair(word(k[t], 2 * s + i / 2), scale, i % 2);
+                for (int i = 0; i < 4; ++i) w[i] = BITS == 4 ? pair(k[t][s], scale, i) : pair(k[t][2 * s + i / 2], scale, i % 2);
 #pragma unroll
                 for (int m = QT - 1; m >= 0; --m) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q.x[m][s], c, 0, 0, 0);
             }

@@ -47,8 +47,8 @@ static __device__ __forceinline__ float2 turn_of(int pos, float f, float sign) {
     return make_float2(k == 1 || k == 2 ? -cs : cs, sign * (k & 2 ? -sn : sn));
 }
 
-// N neighbouring elements.
-template <typename T, int N> struct alignas(sizeof(T) * N) Wide { T e[N]; };
+// N neighbouring elements.  Two may lie anywhere (interleaved pairs in rows at odd addresses).
+template <typename T, int N> struct alignas(N == 2 ? sizeof(T) : sizeof(T) * N) Wide { T e[N]; };
 
 template <typename T> static __device__ __forceinline__ float to_f32(T x) {
     if constexpr (sizeof(T) == 4) return x;
