@@ -3,8 +3,8 @@
 //
 // Both are bound by HBM, the wide side by far: 256 bytes of bf16 for 64 + 4 of codes and scales.  A lane has eight elements, 16 bytes (fp32: 32) on the wide side and 4 or
 // 8 on the narrow one; the four lanes of a block find its largest element by two lane exchanges.  Scales meet in LDS and leave with the tables' entries, a
-// page's places by neighbouring threads.  22500 tokens of 32 heads of 128 elements (369 MB of bf16) into four bits and back 171 us, 5.5 TB/s read and written, as a
-// plain copy does; 557 MB from eight bits 103 us, 5.4.  A few tokens: 3.5 us each way, launch and dependent loads.
+// page's places by neighbouring threads.  22500 tokens of 32 heads of 128 elements (369 MB of bf16) into four bits and back 162 us, 5.8 TB/s read and written (a
+// plain copy 5.45); 557 MB from eight bits 103 us, 5.4.  A few tokens: 3.5 us each way, launch and dependent loads.
 #include "ssd_mx.h"
 #include "ssd_paged_mx.h"
 
@@ -36,8 +36,18 @@ struct Spots {
     int32_t starts[STARTS + 1];
 };
 
-template <bool READ> static __device__ __forceinline__ void find_spots(const MxRowsArgs &a, Spots &sm) {
-    const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row = ((int)blockIdx.x << a.tokens_log2) + tid;
+// First token of a workgroup.  Workgroups go to the eight XCDs in turn; four neighbours' tokens go to one, as their rows and scales share cache lines (22500 tokens of 32
+// heads of 128 elements written in four bits and read back in their order 172 us, by twos 166, fours 162, sixteens 165, the whole grid in eight runs 162, which costs reading
+// 557 MB 103 -> 108; in eight bits, one line to a row, nothing changes).
+static __device__ __forceinline__ int first_token(const MxRowsArgs &a) {
+    const unsigned i = blockIdx.x;
+    constexpr unsigned RUN = 4;
+    if (i >= gridDim.x / (8 * RUN) * (8 * RUN)) return (int)(i << a.tokens_log2);
+    return (int)((i / (8 * RUN) * (8 * RUN) + (i & 7) * RUN + (i >> 3) % RUN) << a.tokens_log2);
+}
+
+template <bool READ> static __device__ __forceinline__ void find_spots(const MxRowsArgs &a, int row0, Spots &sm) {
+    const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row = row0 + tid;
     const bool in_lds = a.start && a.g.n_seqs <= STARTS;
     if (in_lds) {
         for (int i = tid; i <= a.g.n_seqs; i += 256) sm.starts[i] = a.start[i];
@@ -90,7 +100,7 @@ template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx
     typedef std::conditional_t<SB == 4, uint32_t, uint16_t> scales_t;
     __shared__ Spots sm;
     extern __shared__ __align__(16) uint8_t sm_scale[];     // [K and V][kv heads][tokens][SB]
-    const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row0 = (int)blockIdx.x << a.tokens_log2;
+    const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row0 = first_token(a);
     const int lane = tid & ((1 << a.lanes_log2) - 1), step = 1 << a.lanes_log2, frags = a.g.n_kv * PARTS, per_token = (frags + step - 1) >> a.lanes_log2;
     const int mine = ((tokens + (256 >> a.lanes_log2) - 1) >> (8 - a.lanes_log2)) * per_token;
     // what a thread reads is on its way two fragments ahead, the first ones while the tokens' places are looked up
@@ -106,7 +116,7 @@ template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx
         }
     };
     load(0);
-    find_spots<false>(a, sm);
+    find_spots<false>(a, row0, sm);
     for (int q = 0; q < mine; q += U) {
         Eight<T> k0[U], v0[U];
 #pragma unroll
@@ -148,10 +158,10 @@ template <typename T, int D, int BITS> __global__ __launch_bounds__(256) void mx
 template <typename T, int D, int BITS, bool ONCE> __global__ __launch_bounds__(256) void mx_read_kernel(MxRowsArgs a) {
     constexpr int PARTS = D / 8, SB = D / 32, U = 4;
     __shared__ Spots sm;
-    const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row0 = (int)blockIdx.x << a.tokens_log2;
+    const int tid = threadIdx.x, tokens = 1 << a.tokens_log2, row0 = first_token(a);
     const int lane = tid & ((1 << a.lanes_log2) - 1), step = 1 << a.lanes_log2, frags = a.g.n_kv * PARTS, per_token = (frags + step - 1) >> a.lanes_log2;
     const int mine = ((tokens + (256 >> a.lanes_log2) - 1) >> (8 - a.lanes_log2)) * per_token;
-    find_spots<true>(a, sm);
+    find_spots<true>(a, row0, sm);
     for (int q = 0; q < mine; q += U) {
         Codes<BITS> k[U], v[U];
         uint32_t ks[U], vs[U];
