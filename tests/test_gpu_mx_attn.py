@@ -215,6 +215,84 @@ def test_captured_steps_follow_the_lengths(fmt):
             assert torch.equal(bt.kd, eager.kd) and torch.equal(bt.vsd, eager.vsd) and torch.equal(bt.posd, eager.posd)
 
 
+def test_two_streams_at_once():
+    """Steps with weights of two pools on two streams, each with a workspace of its own: the bits of either alone."""
+    batches = [MxBatch([3000, 40, 900], 8, 2, 128, "bf16", "mxfp8", 16, seed=27), MxBatch([2000, 1999, 7, 0], 4, 4, 64, "f32", "mxfp4", 24, seed=28)]
+    calls = []
+    for i, bt in enumerate(batches):
+        step = [x.cuda() for x in new_rows(bt, len(bt.lens), seed=29 + i)]
+        ws = bt.scratch(ssd.ssd_paged_mx_workspace_bytes(bt.cfg, bt.fmt, 0, True))
+        o = [torch.zeros((len(bt.lens), bt.H, bt.d), dtype=bt.qd.dtype, device="cuda"), torch.zeros((len(bt.lens), bt.H), device="cuda"), torch.zeros_like(bt.weightd)]
+        calls.append((bt, step, ws, o, torch.cuda.Stream()))
+
+    def call(bt, step, ws, o, stream):
+        ssd.ssd_paged_mx_decode_step(bt.cfg, bt.fmt, bt.qd, *step, *bt.pools, bt.tabled, bt.lend, o[0], pos=bt.posd, lse=o[1], weight_in=bt.weightd, weight_out=o[2],
+                                     workspace=ws, stream=stream)
+
+    alone = []
+    for c in calls:
+        torch.cuda.synchronize()
+        call(*c)
+        torch.cuda.synchronize()
+        alone.append([x.clone() for x in c[3]])
+    for _ in range(5):
+        for x in calls[0][3] + calls[1][3]:
+            x.zero_()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for c in calls:
+                call(*c)
+        torch.cuda.synchronize()
+        for c, want in zip(calls, alone):
+            for x, y in zip(c[3], want):
+                assert torch.equal(x, y)
+
+
+def test_captured_rotation_append_and_read_follow_positions_and_lengths():
+    """A chunk of rows rotated, stored and read back as one graph, replayed while lengths and positions go on; every replay against the eager calls."""
+    fmt, n, n_kv, d = "mxfp4", 6, 2, 64
+    make = lambda: MxBatch([40, 90], 2, n_kv, d, "bf16", fmt, 16, seed=30, more_blocks=3, spare=6)  # noqa: E731
+    pair = []
+    for _ in range(2):
+        bt = make()
+        bt.table[0, 3:6], bt.table[1, 6:9] = [p for p in range(bt.n_pages) if p not in bt.table][:3], [p for p in range(bt.n_pages) if p not in bt.table][3:6]
+        bt.to_device()
+        k, v = (x.cuda() for x in new_rows(bt, n, seed=31))
+        at = torch.tensor([[38, 39, 87, 88, 89, 90]], dtype=torch.int32, device="cuda")
+        pair.append((bt, k, torch.zeros_like(k), v, at, torch.zeros_like(k), torch.zeros_like(k)))
+    start = torch.tensor([0, 2, 6], dtype=torch.int32, device="cuda")
+    inv = torch.tensor([10000.0 ** (-i / 32) for i in range(32)], device="cuda")
+
+    def call(bt, k, turned, v, at, k_out, v_out):
+        ssd.ssd_rope_axes(k, turned, n, n_kv, d, "bf16", at, inv)
+        ssd.ssd_paged_mx_append(bt.cfg, fmt, *bt.pools, bt.tabled, bt.lend, turned, v, pos=bt.posd, new_start=start)
+        ssd.ssd_paged_mx_read(bt.cfg, fmt, *bt.pools, bt.tabled, bt.lend, k_out, v_out, row_start=start, first_slot=first)
+
+    first = pair[0][0].lend - torch.tensor([2, 4], dtype=torch.int32, device="cuda")
+    for x in pair:
+        call(*x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*pair[0])
+    for replay in range(5):
+        for x in pair:
+            x[0].lend += torch.tensor([2, 4], dtype=torch.int32, device="cuda")
+            x[4].add_(3)
+            x[1].mul_(-1.25)
+        first += torch.tensor([2, 4], dtype=torch.int32, device="cuda")
+        graph.replay()
+        torch.cuda.synchronize()
+        call(*pair[1])
+        torch.cuda.synchronize()
+        for i in (2, 5, 6):
+            assert torch.equal(pair[0][i], pair[1][i]), (replay, i)
+        for x, y in zip(pair[0][0].pools + (pair[0][0].posd,), pair[1][0].pools + (pair[1][0].posd,)):
+            assert torch.equal(x, y), replay
+        held = mx.held(pair[0][2].double().cpu().numpy(), fmt)
+        assert np.array_equal(pair[0][5].float().cpu().numpy(), held), replay
+
+
 @pytest.mark.parametrize("fmt,dtype,d,page,n_kv,lens,budget", [("mxfp4", "bf16", 128, 16, 2, [129, 129, 40, 0], 128), ("mxfp8", "f32", 64, 24, 3, [500, 1000, 10], 100),
                                                               ("mxfp4", "f32", 64, 1, 1, [60, 61], 33), ("mxfp8", "bf16", 128, 32, 8, [3000, 900], 1000),
                                                               ("mxfp4", "bf16", 64, 16, 1, [20000, 17000], 5000)] +
