@@ -522,6 +522,6 @@ int ssd_cache_export(ssd_cache *cache, int layer, int32_t *pos, int32_t *count, 
 
 const char *ssd_last_error(void) { return g_err; }
 
-int ssd_version(void) { return 200; }
+int ssd_version(void) { return 300; }
 
 }  // extern "C"

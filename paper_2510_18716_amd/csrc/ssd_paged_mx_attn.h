@@ -7,10 +7,12 @@
 // V: D / 16 columns of eight rows in a lane.  fp32 calls split q into three bf16 terms and the probabilities too (24 bits of both); bf16 calls take q as it is
 // and probabilities in two terms.
 //
-// With four bits a row's bytes are so few that instructions bound the kernel as soon as memory: 166 vector instructions for 32 rows of 128 elements, 64 of them
-// conversions (290 before: V turned by byte permutations 32, addresses added lane by lane 14, logits scaled on their own 8, the workgroup's page addresses looked
-// up in LDS; 4 sequences of 30000 to 131072 rows 63 -> 59 us, 128 of 64 to 640 rows of 32 heads 48 -> 38).  Tried and taken back: tiles of 64 rows (70 and 57 us: the
-// registers do not hold them; rows of 64 elements, which they hold, gain nothing), tiles that pass through LDS by direct loads (64 and 51).
+// With four bits a row's bytes are so few that instructions bound the kernel as soon as memory: 190 vector instructions for 32 rows of 128 elements (all of a
+// launch's over its tiles), 64 of them conversions.  4 sequences of 30000 to 131072 rows, 32 query heads on 8: 58 us with the second launch, 5.4 TB/s; 128 of 64 to 640 rows of
+// 32 heads with weights 43 us, 3.5 TB/s: there the units' beginnings, a length, block table entries and rows one after the other, are half the time.  What was there before: V turned by
+// byte permutations (32 instructions), addresses added lane by lane (14), logits scaled on their own (8), the workgroup's page addresses looked up in LDS: 63 and 51 us.
+// Tried and taken back then: tiles of 64 rows (70 and 57 us: the registers do not hold them; rows of 64 elements, which they hold, gain nothing), tiles that pass
+// through LDS by direct loads (64 and 51).
 #pragma once
 
 #include "ssd_mx.h"
