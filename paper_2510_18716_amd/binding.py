@@ -454,17 +454,20 @@ class SsdPagedConfig(C.Structure):
 
     def __setattr__(self, name, value):
         super().__setattr__(name, value)
-        self.__dict__.clear()
+        self.__dict__.pop("strides", None)
+        self.__dict__.pop("mx_strides", None)
 
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
-        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes, their bytes and those of their scales.
+        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes, their bytes and those of their
+        scales, and by 0 those of an element of q, new rows and outputs.
         Found when they are first asked for after a field was set."""
         if name == "mx_strides":
             places = (self.n_pages, self.n_kv_heads, self.page_size)
             n = places[0] * places[1] * places[2]
             got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,),
                                                 n * (self.head_dim * bits // 8), n * (self.head_dim // 32)) for bits in (4, 8)}
+            got[0] = 4 if self.dtype == SSD_F32 else 2
             return got
         if name != "strides":
             raise AttributeError(name)
@@ -723,6 +726,13 @@ def _mx_pool(t, what: str, want, sizes, n: int) -> Optional[int]:
     return t.data_ptr()
 
 
+def _sized(t, what: str, size: int):
+    """A tensor, if its elements have `size` bytes."""
+    if type(t) is _Tensor and t.element_size() != size:
+        raise ValueError("%s of type %s: elements of %d bytes are expected" % (what, t.dtype, size))
+    return t
+
+
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
     """The format's code, and the addresses of two pools of codes and their scales."""
     bits = _FORMATS.get(format) or _format_code(format)
@@ -735,21 +745,22 @@ def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales,
                         seq_pos=None, new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
     """format: "mxfp4" or "mxfp8" (SSD_MXFP4, SSD_MXFP8).  n_new: tokens in k_new; None: its first dimension."""
     n = int(k_new.shape[0] if n_new is None else n_new)
-    new, heads = cfg.strides[2], cfg.n_kv_heads
+    new, heads, size = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos),
-                                   _rows(k_new, "k_new", n, heads, new), _rows(v_new, "v_new", n, heads, new), _ptr(new_start), n, _ptr(weight_new),
-                                   _stream(stream)), "ssd_paged_mx_append")
+                                   _rows(_sized(k_new, "k_new", size), "k_new", n, heads, new), _rows(_sized(v_new, "v_new", size), "v_new", n, heads, new),
+                                   _ptr(new_start), n, _ptr(weight_new), _stream(stream)), "ssd_paged_mx_append")
 
 
 def ssd_paged_mx_read(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, k_out, v_out, row_start=None,
                       first_slot=None, n_rows: Optional[int] = None, stream=None) -> None:
     """n_rows: rows of k_out; None: its first dimension."""
     n = int(k_out.shape[0] if n_rows is None else n_rows)
-    new, heads = cfg.strides[2], cfg.n_kv_heads
+    new, heads, size = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(row_start), n, _ptr(first_slot),
-                                 _rows(k_out, "k_out", n, heads, new), _rows(v_out, "v_out", n, heads, new), _stream(stream)), "ssd_paged_mx_read")
+                                 _rows(_sized(k_out, "k_out", size), "k_out", n, heads, new), _rows(_sized(v_out, "v_out", size), "v_out", n, heads, new),
+                                 _stream(stream)), "ssd_paged_mx_read")
 
 
 def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, with_weights: bool = False) -> int:
@@ -758,19 +769,20 @@ def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, 
 
 def ssd_paged_mx_decode_attn(cfg: SsdPagedConfig, format, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, lse=None, weight_in=None,
                              weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
+    size = cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _rows(q, "q", cfg.n_seqs, cfg.n_heads, cfg.strides[1]), k, v, ks, vs, _ptr(weight_in),
-                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(out), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _rows(_sized(q, "q", size), "q", cfg.n_seqs, cfg.n_heads, cfg.strides[1]), k, v, ks, vs, _ptr(weight_in),
+                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(_sized(out, "out", size)), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
 
 
 def ssd_paged_mx_decode_step(cfg: SsdPagedConfig, format, q, k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, pos=None,
                              seq_pos=None, lse=None, weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    (_, queries, new), B, heads = cfg.strides, cfg.n_seqs, cfg.n_kv_heads
+    (_, queries, new), B, heads, size = cfg.strides, cfg.n_seqs, cfg.n_kv_heads, cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _rows(q, "q", B, cfg.n_heads, queries), _rows(k_new, "k_new", B, heads, new),
-                                        _rows(v_new, "v_new", B, heads, new), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
-                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(out), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _rows(_sized(q, "q", size), "q", B, cfg.n_heads, queries), _rows(_sized(k_new, "k_new", size), "k_new", B, heads, new),
+                                        _rows(_sized(v_new, "v_new", size), "v_new", B, heads, new), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
+                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(_sized(out, "out", size)), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
 
 
@@ -789,10 +801,10 @@ def ssd_paged_mx_evict(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, 
 def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, inv_freq, axis=None, n_axes: int = 1, n_pairs: Optional[int] = None,
                   layout: int = SSD_ROPE_HALF, inverse: bool = False, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
     """n_pairs None: inv_freq's elements.  x_stride, out_stride 0: the tensor's own (query and key heads may be handed over where a projection has them)."""
-    rows = []
+    rows, code = [], _dtype_code(dtype)
     for t, what, stride in ((x, "x", x_stride), (out, "out", out_stride)):
         if t is not None and not isinstance(t, int):
-            own = t.stride()
+            own = _sized(t, what, 4 if code == SSD_F32 else 2).stride()
             if len(own) == 3 and own[1] == head_dim and own[2] == 1 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
                 stride = own[0] if n_rows > 1 else 0
             else:
@@ -805,7 +817,7 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
     for t, what, most in ((pos, "pos", n_axes * n_rows), (inv_freq, "inv_freq", pairs), (axis, "axis", pairs)):
         if t is not None and not isinstance(t, int) and (not t.is_contiguous() or t.numel() < most):
             raise ValueError("%s of shape %s, strides %s: %d elements without gaps are expected" % (what, tuple(t.shape), t.stride(), most))
-    _check(lib.ssd_rope_axes(x, out, int(n_rows), int(n_heads), int(head_dim), _dtype_code(dtype), int(x_stride), int(out_stride), _ptr(pos), int(n_axes),
+    _check(lib.ssd_rope_axes(x, out, int(n_rows), int(n_heads), int(head_dim), code, int(x_stride), int(out_stride), _ptr(pos), int(n_axes),
                              _ptr(axis), _ptr(inv_freq), pairs, int(layout), int(bool(inverse)), _stream(stream)), "ssd_rope_axes")
 
 

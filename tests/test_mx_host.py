@@ -175,3 +175,25 @@ def test_binding_of_the_rotation_refuses_short_arrays():
         a.update(bad)
         with pytest.raises(ValueError):
             ssd.ssd_rope_axes(a.pop("x"), a.pop("out"), 4, 2, 64, "f32", a.pop("pos"), a.pop("inv_freq"), n_axes=2, **a)
+
+
+def test_binding_refuses_elements_of_another_size():
+    bt = MxBatch([20, 5], 4, 2, 64, "bf16", "mxfp4", 16, seed=1, device="cpu")
+    new, wrong = torch.zeros((2, 2, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 64))
+    out, wide = torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros((2, 4, 64))
+    head, tail = (bt.cfg, "mxfp4"), (bt.tabled, bt.lend)
+    for call in (lambda: ssd.ssd_paged_mx_append(*head, *bt.pools, *tail, wrong, new), lambda: ssd.ssd_paged_mx_append(*head, *bt.pools, *tail, new, wrong),
+                 lambda: ssd.ssd_paged_mx_read(*head, *bt.pools, *tail, wrong, new), lambda: ssd.ssd_paged_mx_read(*head, *bt.pools, *tail, new, wrong),
+                 lambda: ssd.ssd_paged_mx_decode_attn(*head, wide, *bt.pools, *tail, out), lambda: ssd.ssd_paged_mx_decode_attn(*head, out, *bt.pools, *tail, wide),
+                 lambda: ssd.ssd_paged_mx_decode_step(*head, out, wrong, new, *bt.pools, *tail, out), lambda: ssd.ssd_paged_mx_decode_step(*head, out, new, wrong, *bt.pools, *tail, out),
+                 lambda: ssd.ssd_rope_axes(wide, wide, 2, 4, 64, "bf16", bt.lend, torch.ones(32)), lambda: ssd.ssd_rope_axes(out, out, 2, 4, 64, "f32", bt.lend, torch.ones(32))):
+        with pytest.raises(ValueError, match="bytes are expected"):
+            call()
+
+
+def test_what_a_user_keeps_at_a_config_stays():
+    cfg = ssd.make_paged_config(2, 4, 2, 64, "bf16", 16, 4, 2)
+    cfg.note = "kept"
+    assert cfg.strides and cfg.mx_strides
+    cfg.page_size = 32
+    assert cfg.note == "kept" and cfg.strides[0][1] == 32 * 64 and cfg.mx_strides[8][0][1] == 32 * 64
