@@ -805,7 +805,7 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
     for t, what, stride in ((x, "x", x_stride), (out, "out", out_stride)):
         if t is not None and not isinstance(t, int):
             own = _sized(t, what, 4 if code == SSD_F32 else 2).stride()
-            if len(own) == 3 and own[1] == head_dim and own[2] == 1 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
+            if len(own) == 3 and own[1] == head_dim and own[2] == 1 and own[0] > 0 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
                 stride = own[0] if n_rows > 1 else 0
             else:
                 stride = stride or (own[0] if len(own) > 1 and t.shape[0] == n_rows > 1 else 0)

@@ -197,3 +197,12 @@ def test_what_a_user_keeps_at_a_config_stays():
     assert cfg.strides and cfg.mx_strides
     cfg.page_size = 32
     assert cfg.note == "kept" and cfg.strides[0][1] == 32 * 64 and cfg.mx_strides[8][0][1] == 32 * 64
+
+
+def test_binding_of_the_rotation_refuses_broadcast_rows():
+    """One row in the place of many has no second row to read or write."""
+    x, pos, inv = torch.zeros((4, 2, 64)), torch.zeros((1, 4), dtype=torch.int32), torch.ones(32)
+    for one in (x[:1].expand(4, 2, 64), x[:1, :1].expand(4, 2, 64), x.flatten(1)[:1].expand(4, 128)):
+        for a, b in ((one, x), (x, one)):
+            with pytest.raises(ValueError):
+                ssd.ssd_rope_axes(a, b, 4, 2, 64, "f32", pos, inv)
