@@ -168,6 +168,7 @@ def _stream(stream=None) -> Optional[int]:
 
 
 _DTYPE_CODES = {torch.bfloat16: SSD_BF16, "bf16": SSD_BF16, torch.float32: SSD_F32, "f32": SSD_F32}
+_DTYPES = {SSD_BF16: torch.bfloat16, SSD_F32: torch.float32}
 
 
 def _dtype_code(dt) -> int:
@@ -460,14 +461,14 @@ class SsdPagedConfig(C.Structure):
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
         [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes, their bytes and those of their
-        scales, and by 0 those of an element of q, new rows and outputs.
+        scales, and by 0 the type of q, new rows and outputs.
         Found when they are first asked for after a field was set."""
         if name == "mx_strides":
             places = (self.n_pages, self.n_kv_heads, self.page_size)
             n = places[0] * places[1] * places[2]
             got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,),
                                                 n * (self.head_dim * bits // 8), n * (self.head_dim // 32)) for bits in (4, 8)}
-            got[0] = 4 if self.dtype == SSD_F32 else 2
+            got[0] = _DTYPES.get(self.dtype, torch.bfloat16)
             return got
         if name != "strides":
             raise AttributeError(name)
@@ -726,11 +727,24 @@ def _mx_pool(t, what: str, want, sizes, n: int) -> Optional[int]:
     return t.data_ptr()
 
 
-def _sized(t, what: str, size: int):
-    """A tensor, if its elements have `size` bytes."""
-    if type(t) is _Tensor and t.element_size() != size:
-        raise ValueError("%s of type %s: elements of %d bytes are expected" % (what, t.dtype, size))
+def _sized(t, what: str, dtype):
+    """A tensor whose elements have the size of dtype's, or whatever else stands for one."""
+    if type(t) is _Tensor and t.dtype is not dtype and t.element_size() != dtype.itemsize:
+        raise ValueError("%s of type %s: elements of %d bytes are expected" % (what, t.dtype, dtype.itemsize))
     return t
+
+
+def _mx_rows(t, what: str, n: int, heads: int, want, dtype) -> Optional[int]:
+    """_rows of elements of dtype's size, as many as the call takes."""
+    if type(t) is _Tensor:
+        if t.dtype is not dtype:
+            _sized(t, what, dtype)
+        if t.stride() == want:
+            size = t.shape
+            if size[0] < n or size[1] < heads or size[2] < want[1]:
+                raise ValueError("%s of shape %s: [%d, %d, %d] is expected" % (what, tuple(size), n, heads, want[1]))
+            return t.data_ptr()
+    return _rows(t, what, n, heads, want)
 
 
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
@@ -745,10 +759,10 @@ def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales,
                         seq_pos=None, new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
     """format: "mxfp4" or "mxfp8" (SSD_MXFP4, SSD_MXFP8).  n_new: tokens in k_new; None: its first dimension."""
     n = int(k_new.shape[0] if n_new is None else n_new)
-    new, heads, size = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
+    new, heads, dtype = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos),
-                                   _rows(_sized(k_new, "k_new", size), "k_new", n, heads, new), _rows(_sized(v_new, "v_new", size), "v_new", n, heads, new),
+                                   _mx_rows(k_new, "k_new", n, heads, new, dtype), _mx_rows(v_new, "v_new", n, heads, new, dtype),
                                    _ptr(new_start), n, _ptr(weight_new), _stream(stream)), "ssd_paged_mx_append")
 
 
@@ -756,10 +770,10 @@ def ssd_paged_mx_read(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v
                       first_slot=None, n_rows: Optional[int] = None, stream=None) -> None:
     """n_rows: rows of k_out; None: its first dimension."""
     n = int(k_out.shape[0] if n_rows is None else n_rows)
-    new, heads, size = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
+    new, heads, dtype = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(row_start), n, _ptr(first_slot),
-                                 _rows(_sized(k_out, "k_out", size), "k_out", n, heads, new), _rows(_sized(v_out, "v_out", size), "v_out", n, heads, new),
+                                 _mx_rows(k_out, "k_out", n, heads, new, dtype), _mx_rows(v_out, "v_out", n, heads, new, dtype),
                                  _stream(stream)), "ssd_paged_mx_read")
 
 
@@ -769,20 +783,20 @@ def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, 
 
 def ssd_paged_mx_decode_attn(cfg: SsdPagedConfig, format, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, lse=None, weight_in=None,
                              weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    size = cfg.mx_strides[0]
+    dtype = cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _rows(_sized(q, "q", size), "q", cfg.n_seqs, cfg.n_heads, cfg.strides[1]), k, v, ks, vs, _ptr(weight_in),
-                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(_sized(out, "out", size)), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", cfg.n_seqs, cfg.n_heads, cfg.strides[1], dtype), k, v, ks, vs, _ptr(weight_in),
+                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(_sized(out, "out", dtype)), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
 
 
 def ssd_paged_mx_decode_step(cfg: SsdPagedConfig, format, q, k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, pos=None,
                              seq_pos=None, lse=None, weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    (_, queries, new), B, heads, size = cfg.strides, cfg.n_seqs, cfg.n_kv_heads, cfg.mx_strides[0]
+    (_, queries, new), B, heads, dtype = cfg.strides, cfg.n_seqs, cfg.n_kv_heads, cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _rows(_sized(q, "q", size), "q", B, cfg.n_heads, queries), _rows(_sized(k_new, "k_new", size), "k_new", B, heads, new),
-                                        _rows(_sized(v_new, "v_new", size), "v_new", B, heads, new), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
-                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(_sized(out, "out", size)), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", B, cfg.n_heads, queries, dtype), _mx_rows(k_new, "k_new", B, heads, new, dtype),
+                                        _mx_rows(v_new, "v_new", B, heads, new, dtype), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
+                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(_sized(out, "out", dtype)), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
 
 
@@ -802,9 +816,10 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
                   layout: int = SSD_ROPE_HALF, inverse: bool = False, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
     """n_pairs None: inv_freq's elements.  x_stride, out_stride 0: the tensor's own (query and key heads may be handed over where a projection has them)."""
     rows, code = [], _dtype_code(dtype)
+    held = _DTYPES.get(code, torch.bfloat16)                          # another code is refused by the library
     for t, what, stride in ((x, "x", x_stride), (out, "out", out_stride)):
         if t is not None and not isinstance(t, int):
-            own = _sized(t, what, 4 if code == SSD_F32 else 2).stride()
+            own = _sized(t, what, held).stride()
             if len(own) == 3 and own[1] == head_dim and own[2] == 1 and own[0] > 0 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
                 stride = own[0] if n_rows > 1 else 0
             else:

@@ -206,3 +206,19 @@ def test_binding_of_the_rotation_refuses_broadcast_rows():
         for a, b in ((one, x), (x, one)):
             with pytest.raises(ValueError):
                 ssd.ssd_rope_axes(a, b, 4, 2, 64, "f32", pos, inv)
+
+
+def test_binding_refuses_fewer_rows_than_the_call_takes():
+    bt = MxBatch([20, 5], 4, 2, 64, "bf16", "mxfp4", 16, seed=1, device="cpu")
+    head, tail = (bt.cfg, "mxfp4"), (bt.tabled, bt.lend)
+    rows, few, heads, short = (torch.zeros(s, dtype=torch.bfloat16) for s in ((3, 2, 64), (2, 2, 64), (3, 1, 64), (3, 2, 32)))
+    out, one = torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros((1, 4, 64), dtype=torch.bfloat16)
+    starts = torch.tensor([0, 2, 3], dtype=torch.int32)
+    for call in (lambda x: ssd.ssd_paged_mx_append(*head, *bt.pools, *tail, x, rows, new_start=starts, n_new=3), lambda x: ssd.ssd_paged_mx_read(*head, *bt.pools, *tail, rows, x, row_start=starts, n_rows=3)):
+        for x in (few, heads, short, rows[:, :1]):
+            with pytest.raises(ValueError):
+                call(x)
+    with pytest.raises(ValueError):
+        ssd.ssd_paged_mx_decode_attn(*head, one, *bt.pools, *tail, out)
+    with pytest.raises(ValueError):
+        ssd.ssd_paged_mx_decode_step(*head, out, few[:1], few, *bt.pools, *tail, out)
