@@ -461,14 +461,15 @@ class SsdPagedConfig(C.Structure):
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
         [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes, their bytes and those of their
-        scales, and by 0 the type of q, new rows and outputs.
+        scales, and by 0 the type of q, new rows and outputs, the bytes of q and those of a token's new rows.
         Found when they are first asked for after a field was set."""
         if name == "mx_strides":
             places = (self.n_pages, self.n_kv_heads, self.page_size)
             n = places[0] * places[1] * places[2]
             got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,),
                                                 n * (self.head_dim * bits // 8), n * (self.head_dim // 32)) for bits in (4, 8)}
-            got[0] = _DTYPES.get(self.dtype, torch.bfloat16)
+            size = _DTYPES.get(self.dtype, torch.bfloat16).itemsize * self.head_dim
+            got[0] = _DTYPES.get(self.dtype, torch.bfloat16), self.n_seqs * self.n_heads * size, self.n_kv_heads * size
             return got
         if name != "strides":
             raise AttributeError(name)
@@ -734,17 +735,23 @@ def _sized(t, what: str, dtype):
     return t
 
 
-def _mx_rows(t, what: str, n: int, heads: int, want, dtype) -> Optional[int]:
-    """_rows of elements of dtype's size, as many as the call takes."""
+def _mx_rows(t, what: str, cfg, n: int, heads: int, want, n_bytes: int) -> Optional[int]:
+    """_rows of the config's type, as many as the call takes; n_bytes: of all of them."""
     if type(t) is _Tensor:
-        if t.dtype is not dtype:
-            _sized(t, what, dtype)
-        if t.stride() == want:
-            size = t.shape
-            if size[0] < n or size[1] < heads or size[2] < want[1]:
-                raise ValueError("%s of shape %s: [%d, %d, %d] is expected" % (what, tuple(size), n, heads, want[1]))
+        if t.nbytes == n_bytes and t.stride() == want:
             return t.data_ptr()
+        _sized(t, what, cfg.mx_strides[0][0])
+        if t.stride() == want and any(have < need for have, need in zip(t.shape, (n, heads, cfg.head_dim))):
+            raise ValueError("%s of shape %s: [%d, %d, %d] is expected" % (what, tuple(t.shape), n, heads, cfg.head_dim))
     return _rows(t, what, n, heads, want)
+
+
+def _mx_out(t, dtype, n_bytes: int) -> Optional[int]:
+    """Address of an attention's output, which has as many bytes as its queries."""
+    if type(t) is _Tensor and t.nbytes != n_bytes:
+        if _sized(t, "out", dtype).nbytes < n_bytes:
+            raise ValueError("out of shape %s: %d elements are expected" % (tuple(t.shape), n_bytes // dtype.itemsize))
+    return _ptr(t)
 
 
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
@@ -759,10 +766,10 @@ def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales,
                         seq_pos=None, new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
     """format: "mxfp4" or "mxfp8" (SSD_MXFP4, SSD_MXFP8).  n_new: tokens in k_new; None: its first dimension."""
     n = int(k_new.shape[0] if n_new is None else n_new)
-    new, heads, dtype = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
+    new, heads, n_bytes = cfg.strides[2], cfg.n_kv_heads, n * cfg.mx_strides[0][2]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos),
-                                   _mx_rows(k_new, "k_new", n, heads, new, dtype), _mx_rows(v_new, "v_new", n, heads, new, dtype),
+                                   _mx_rows(k_new, "k_new", cfg, n, heads, new, n_bytes), _mx_rows(v_new, "v_new", cfg, n, heads, new, n_bytes),
                                    _ptr(new_start), n, _ptr(weight_new), _stream(stream)), "ssd_paged_mx_append")
 
 
@@ -770,10 +777,10 @@ def ssd_paged_mx_read(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v
                       first_slot=None, n_rows: Optional[int] = None, stream=None) -> None:
     """n_rows: rows of k_out; None: its first dimension."""
     n = int(k_out.shape[0] if n_rows is None else n_rows)
-    new, heads, dtype = cfg.strides[2], cfg.n_kv_heads, cfg.mx_strides[0]
+    new, heads, n_bytes = cfg.strides[2], cfg.n_kv_heads, n * cfg.mx_strides[0][2]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(row_start), n, _ptr(first_slot),
-                                 _mx_rows(k_out, "k_out", n, heads, new, dtype), _mx_rows(v_out, "v_out", n, heads, new, dtype),
+                                 _mx_rows(k_out, "k_out", cfg, n, heads, new, n_bytes), _mx_rows(v_out, "v_out", cfg, n, heads, new, n_bytes),
                                  _stream(stream)), "ssd_paged_mx_read")
 
 
@@ -783,20 +790,21 @@ def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, 
 
 def ssd_paged_mx_decode_attn(cfg: SsdPagedConfig, format, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, lse=None, weight_in=None,
                              weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    dtype = cfg.mx_strides[0]
+    dtype, q_bytes, _ = cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", cfg.n_seqs, cfg.n_heads, cfg.strides[1], dtype), k, v, ks, vs, _ptr(weight_in),
-                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _ptr(_sized(out, "out", dtype)), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", cfg, cfg.n_seqs, cfg.n_heads, cfg.strides[1], q_bytes), k, v, ks, vs, _ptr(weight_in),
+                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _mx_out(out, dtype, q_bytes), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
 
 
 def ssd_paged_mx_decode_step(cfg: SsdPagedConfig, format, q, k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, pos=None,
                              seq_pos=None, lse=None, weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    (_, queries, new), B, heads, dtype = cfg.strides, cfg.n_seqs, cfg.n_kv_heads, cfg.mx_strides[0]
+    (_, queries, new), (dtype, q_bytes, n_bytes), B, heads = cfg.strides, cfg.mx_strides[0], cfg.n_seqs, cfg.n_kv_heads
+    n_bytes *= B
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", B, cfg.n_heads, queries, dtype), _mx_rows(k_new, "k_new", B, heads, new, dtype),
-                                        _mx_rows(v_new, "v_new", B, heads, new, dtype), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
-                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(_sized(out, "out", dtype)), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", cfg, B, cfg.n_heads, queries, q_bytes), _mx_rows(k_new, "k_new", cfg, B, heads, new, n_bytes),
+                                        _mx_rows(v_new, "v_new", cfg, B, heads, new, n_bytes), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
+                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _mx_out(out, dtype, q_bytes), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
 
 
@@ -816,10 +824,12 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
                   layout: int = SSD_ROPE_HALF, inverse: bool = False, x_stride: int = 0, out_stride: int = 0, stream=None) -> None:
     """n_pairs None: inv_freq's elements.  x_stride, out_stride 0: the tensor's own (query and key heads may be handed over where a projection has them)."""
     rows, code = [], _dtype_code(dtype)
-    held = _DTYPES.get(code, torch.bfloat16)                          # another code is refused by the library
+    held = torch.float32 if code == SSD_F32 else torch.bfloat16      # another code is refused by the library
     for t, what, stride in ((x, "x", x_stride), (out, "out", out_stride)):
         if t is not None and not isinstance(t, int):
-            own = _sized(t, what, held).stride()
+            if t.dtype is not held:
+                _sized(t, what, held)
+            own = t.stride()
             if len(own) == 3 and own[1] == head_dim and own[2] == 1 and own[0] > 0 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
                 stride = own[0] if n_rows > 1 else 0
             else:

@@ -218,7 +218,8 @@ def test_binding_refuses_fewer_rows_than_the_call_takes():
         for x in (few, heads, short, rows[:, :1]):
             with pytest.raises(ValueError):
                 call(x)
-    with pytest.raises(ValueError):
-        ssd.ssd_paged_mx_decode_attn(*head, one, *bt.pools, *tail, out)
+    for q, o in ((one, out), (out, one), (out, out[:, :2])):
+        with pytest.raises(ValueError):
+            ssd.ssd_paged_mx_decode_attn(*head, q, *bt.pools, *tail, o)
     with pytest.raises(ValueError):
         ssd.ssd_paged_mx_decode_step(*head, out, few[:1], few, *bt.pools, *tail, out)
