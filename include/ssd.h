@@ -589,7 +589,7 @@ int ssd_paged_mx_evict(const ssd_paged_config *cfg, int format, void *k_pages, v
  *                 Query and key heads that lie next to each other in a projection's row are one call
  *   pos         : dev int32 [n_axes, n_rows]
  *   axis        : dev uint8 [n_pairs], the axis whose position turns each pair; NULL with n_axes = 1.  A pair whose entry is n_axes or more stays
- *   inv_freq    : dev float [n_pairs], finite
+ *   inv_freq    : dev float [n_pairs], of at most 2^20 in size
  *   n_pairs     : 1..head_dim / 2; elements 2 * n_pairs and beyond of a head stay as they are (in out: are copied)
  *   rope_layout : SSD_ROPE_HALF pairs element i with i + n_pairs; SSD_ROPE_INTERLEAVED 2i with 2i + 1
  *   inverse     : 1 turns back, by the negative angles: the gradient of x from that of out

@@ -1,8 +1,8 @@
 // ssd_rope_axes: heads of tokens turned by positions with one to four axes.
 //
-// Pair i of a token's heads turns by the angle pos[axis[i]] * inv_freq[i].  The angle's revolutions are found in 64 bits: the product is exact up to the last
-// of 53 bits and is divided by 2 pi with the quotient's rounding made up for, so that positions of 2^31 lose nothing; then the fraction of a quarter turn
-// that is left is at most pi / 4, where the series of sine and cosine up to r^11 and r^10 are below 2^-28 off.
+// Pair i of a token's heads turns by the angle pos[axis[i]] * inv_freq[i].  The angle's revolutions are found in 64 bits: the product and what its rounding
+// left out (it has up to 55 bits) are divided by 2 pi with the quotient's rounding made up for, so that positions of 2^31 lose nothing; then the fraction of a quarter
+// turn that is left is at most pi / 4, where the series of sine and cosine up to r^11 and r^10 are below 2^-28 off.
 //
 // Bound by HBM: every element read once and written once.  A token's angles serve all its heads: they are found once per workgroup, into LDS.  22500 tokens of 40 heads of 128
 // elements (bf16) 75 us, 6.1 TB/s read and written; 4611 of 32 heads 16.2 us, 4.7; 16 tokens 3.4 us on the device, launch and latency.  (The first elements requested before
@@ -25,13 +25,14 @@ struct RopeArgs {
     float sign;              // -1: turned back
 };
 
-// (cos, sin) of pos * f.
+// (cos, sin) of pos * f.  Products and sums stay apart: r less its whole turns, taken from x * C in one step, would have what `low` adds already.
 static __device__ __forceinline__ float2 turn_of(int pos, float f, float sign) {
-    const double x = (double)pos * (double)f;
+#pragma clang fp contract(off)
+    const double x = (double)pos * (double)f, rest = __builtin_fma((double)pos, (double)f, -x);
     constexpr double C = 0x1.45f306dc9c883p-3, C2 = -0x1.6b01ec5417056p-57;        // 1 / (2 pi) in two parts
-    const double r = x * C, low = __builtin_fma(x, C, -r) + x * C2;
-    const double quarter = (r - __builtin_rint(r)) * 4.0, q = __builtin_rint(quarter);
-    const float t = (float)(((quarter - q) + low * 4.0) * 0x1.921fb54442d18p+0), t2 = t * t;     // at most pi / 4
+    const double r = x * C, low = __builtin_fma(x, C, -r) + __builtin_fma(x, C2, rest * C);
+    const double quarter = (r - __builtin_rint(r)) * 4.0, q0 = __builtin_rint(quarter), part = (quarter - q0) + low * 4.0, q1 = __builtin_rint(part);
+    const float t = (float)((part - q1) * 0x1.921fb54442d18p+0), t2 = t * t;     // at most pi / 4
     float s = __builtin_fmaf(t2, -2.50521084e-8f, 2.75573192e-6f);
     s = __builtin_fmaf(t2, s, -1.98412698e-4f);
     s = __builtin_fmaf(t2, s, 8.33333333e-3f);
@@ -42,7 +43,7 @@ static __device__ __forceinline__ float2 turn_of(int pos, float f, float sign) {
     c = __builtin_fmaf(t2, c, 4.16666667e-2f);
     c = __builtin_fmaf(t2, c, -0.5f);
     c = __builtin_fmaf(t2, c, 1.f);
-    const int k = (int)q & 3;
+    const int k = ((int)q0 + (int)q1) & 3;
     const float cs = k & 1 ? s : c, sn = k & 1 ? c : s;
     return make_float2(k == 1 || k == 2 ? -cs : cs, sign * (k & 2 ? -sn : sn));
 }

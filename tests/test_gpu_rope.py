@@ -63,6 +63,18 @@ def test_far_positions(far):
     _check(out, x, pos, None, inv, ssd.SSD_ROPE_HALF, False, "f32")
 
 
+@pytest.mark.parametrize("most", [4.0, 1000.0, 2.0 ** 20])
+def test_far_positions_at_large_frequencies(most):
+    """Products of 55 bits, angles up to 2^51."""
+    x, pos, _, _ = _inputs(60, 2, 64, 32, 1, (1 << 31) - 1, seed=7)
+    pos[0, 0], pos[0, 1] = (1 << 31) - 1, -(1 << 31)
+    inv = (torch.rand(32, generator=torch.Generator().manual_seed(8)) + 1) * (most / 2)
+    inv[0], inv[1] = most, -most
+    out = torch.empty_like(x, device="cuda")
+    ssd.ssd_rope_axes(x.cuda(), out, 60, 2, 64, "f32", pos.cuda(), inv.cuda())
+    _check(out, x, pos, None, inv, ssd.SSD_ROPE_HALF, False, "f32")
+
+
 @pytest.mark.parametrize("dtype,gap,at", [("bf16", 256, 0), ("bf16", 3, 1), ("f32", 1, 0), ("f32", 6, 2), ("bf16", 4, 4), ("bf16", 2, 2)])
 def test_strides_and_odd_addresses(dtype, gap, at):
     """Heads inside a projection's rows, which may lie at any element; the rest of the rows stays."""
