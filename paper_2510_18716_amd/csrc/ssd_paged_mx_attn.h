@@ -282,8 +282,9 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
         else return pair((uint32_t)v[i], scale, c);
     }
 
-    // Sums of V's columns times p.  The probabilities go in as terms of bf16, each the upper half of what the one before leaves: 16 bits of each (two terms; the
-    // last one rounded where a head has one column, else cut off) or 24 (three).
+    // Sums of V's columns times p.  The probabilities go in as terms of bf16, each the upper half of what the one before leaves: 16 bits of each (two terms) or 24 (three, which
+    // leave nothing).  The second of two is rounded: cut off, it would leave out up to 2^-15 of every probability, all on one side, where the sum of the softmax has them
+    // whole; half a step added to its bits does it, since no p is below zero (eight of 200 vector instructions of a tile; nothing in the times).
     __device__ __forceinline__ void accumulate(const float (&p)[4 * SUB], f32x4 (&o)[NO]) const {
         const int lane = threadIdx.x & 63;
         if constexpr (COPIES == 1) {
@@ -336,6 +337,7 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
             constexpr int TERMS = COPIES == 4 ? 1 : PT;
             const uint32_t take = odd(lane) ? 0x07060c0cu : 0x0c0c0706u;        // the upper half of a number, in the copy's place
             const uint32_t which = odd(lane) ? 0xbf800000u : 0x0000bf80u, less_first = second(lane) ? 0xffff0000u : 0u;
+            const uint32_t half = COPIES == 4 ? (second(lane) ? 0x8000u : 0u) : PT == 2 ? 0x8000u : 0u;       // of the last term's step
 #pragma unroll
             for (int t = 0; t < SUB; ++t) {
                 u32x4_nt_t term[TERMS];
@@ -345,7 +347,7 @@ template <typename T, int D_, int BITS_, int GROUP, int HT> struct MxTile {
                     if constexpr (COPIES == 4) x -= __uint_as_float(__float_as_uint(x) & less_first);
 #pragma unroll
                     for (int m = 0; m < TERMS; ++m) {
-                        const uint32_t two = __builtin_amdgcn_perm(__float_as_uint(x), 0u, take);
+                        const uint32_t two = __builtin_amdgcn_perm(__float_as_uint(x) + (m + 1 == TERMS ? half : 0u), 0u, take);
                         term[m][i] = two;
                         if (m + 1 < TERMS) x = less(x, two, which);
                     }
