@@ -72,6 +72,38 @@ template <typename R, bool ONCE> static __device__ __forceinline__ void store_ru
     else *reinterpret_cast<R *>(p) = r;
 }
 
+// N pairs (p[e], q[e * STEP]) turned by t = (cos, sin), or left to the bit where t is STAY: as a turn by no angle an infinity would give its partner 0 * inf.
+static constexpr float STAY = 2.f;
+template <int N, int STEP, typename T> static __device__ __forceinline__ void turn_pairs(T *p, T *q, const float2 *turns) {
+    float2 t[N];
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        t[e] = turns[e];
+        most = fmaxf(most, t[e].x);
+    }
+    T x[N], y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float a = to_f32<T>(p[e * STEP]), b = to_f32<T>(q[e * STEP]);
+        x[e] = from_f32<T>(a * t[e].x - b * t[e].y);
+        y[e] = from_f32<T>(b * t[e].x + a * t[e].y);
+    }
+    if (most == STAY) {                                             // rare, so asked once for all (4611 tokens of 32 heads 16.2 us; asked for every pair 17.3)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (t[e].x == STAY) {
+                x[e] = p[e * STEP];
+                y[e] = q[e * STEP];
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        p[e * STEP] = x[e];
+        q[e * STEP] = y[e];
+    }
+}
+
 // VEC: elements of a lane's run; HALF: pair i is (i, i + pairs), else (2 i, 2 i + 1).
 template <typename T, int VEC, bool HALF, bool ONCE> __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     extern __shared__ __align__(16) float2 turns[];               // [tokens][pairs]
@@ -80,7 +112,7 @@ template <typename T, int VEC, bool HALF, bool ONCE> __global__ __launch_bounds_
     for (int i = threadIdx.x; i < tokens * a.pairs; i += 256) {
         const int t = i / a.pairs, p = i - t * a.pairs;
         const int axis = a.axis ? a.axis[p] : 0;
-        turns[i] = axis < a.axes ? turn_of(a.pos[(int64_t)axis * a.n + t0 + t], a.inv_freq[p], a.sign) : make_float2(1.f, 0.f);
+        turns[i] = axis < a.axes ? turn_of(a.pos[(int64_t)axis * a.n + t0 + t], a.inv_freq[p], a.sign) : make_float2(STAY, 0.f);
     }
     __syncthreads();
     // what a lane takes at a time: runs at i and i + pairs, or 2 VEC neighbouring elements
@@ -96,24 +128,12 @@ template <typename T, int VEC, bool HALF, bool ONCE> __global__ __launch_bounds_
         }
         if constexpr (HALF) {
             run_t u = load_run<run_t, ONCE>(x + c * VEC), w = load_run<run_t, ONCE>(x + a.pairs + c * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float2 cs = turns[t * a.pairs + c * VEC + e];
-                const float p = to_f32<T>(u.e[e]), q = to_f32<T>(w.e[e]);
-                u.e[e] = from_f32<T>(p * cs.x - q * cs.y);
-                w.e[e] = from_f32<T>(q * cs.x + p * cs.y);
-            }
+            turn_pairs<VEC, 1>(u.e, w.e, turns + t * a.pairs + c * VEC);
             store_run<run_t, ONCE>(out + c * VEC, u);
             store_run<run_t, ONCE>(out + a.pairs + c * VEC, w);
         } else {
             run_t u = load_run<run_t, ONCE>(x + c * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; e += 2) {
-                const float2 cs = turns[t * a.pairs + (c * VEC + e) / 2];
-                const float p = to_f32<T>(u.e[e]), q = to_f32<T>(u.e[e + 1]);
-                u.e[e] = from_f32<T>(p * cs.x - q * cs.y);
-                u.e[e + 1] = from_f32<T>(q * cs.x + p * cs.y);
-            }
+            turn_pairs<VEC / 2, 2>(u.e, u.e + 1, turns + t * a.pairs + c * VEC / 2);
             store_run<run_t, ONCE>(out + c * VEC, u);
         }
     }
