@@ -728,6 +728,21 @@ def _mx_pool(t, what: str, want, sizes, n: int) -> Optional[int]:
     return t.data_ptr()
 
 
+def _table(t, what: str, n: int, dtype) -> Optional[int]:
+    """Address of at least n elements without gaps, of dtype (or whole numbers of its size where it is one of those)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype and (t.element_size() != dtype.itemsize or not _is_whole(t.dtype) or not _is_whole(dtype)):
+        raise ValueError("%s of type %s: %s, elements of %d bytes are expected" % (what, t.dtype, dtype, dtype.itemsize))
+    if t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s of shape %s, strides %s: %d elements without gaps are expected" % (what, tuple(t.shape), t.stride(), n))
+    return t.data_ptr()
+
+
+def _is_whole(dtype) -> bool:
+    return not dtype.is_floating_point and not dtype.is_complex
+
+
 def _sized(t, what: str, dtype):
     """A tensor whose elements have the size of dtype's, or whatever else stands for one."""
     if type(t) is _Tensor and t.dtype is not dtype and t.element_size() != dtype.itemsize:
@@ -828,7 +843,7 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
     for t, what, stride in ((x, "x", x_stride), (out, "out", out_stride)):
         if t is not None and not isinstance(t, int):
             if t.dtype is not held:
-                _sized(t, what, held)
+                raise ValueError("%s of type %s: %s, elements of %d bytes are expected" % (what, t.dtype, held, held.itemsize))
             own = t.stride()
             if len(own) == 3 and own[1] == head_dim and own[2] == 1 and own[0] > 0 and t.shape == (n_rows, n_heads, head_dim) and stride in (0, own[0]):
                 stride = own[0] if n_rows > 1 else 0
@@ -839,11 +854,9 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
         rows += [t, stride]
     x, x_stride, out, out_stride = rows
     pairs = int(inv_freq.numel() if n_pairs is None else n_pairs)
-    for t, what, most in ((pos, "pos", n_axes * n_rows), (inv_freq, "inv_freq", pairs), (axis, "axis", pairs)):
-        if t is not None and not isinstance(t, int) and (not t.is_contiguous() or t.numel() < most):
-            raise ValueError("%s of shape %s, strides %s: %d elements without gaps are expected" % (what, tuple(t.shape), t.stride(), most))
-    _check(lib.ssd_rope_axes(x, out, int(n_rows), int(n_heads), int(head_dim), code, int(x_stride), int(out_stride), _ptr(pos), int(n_axes),
-                             _ptr(axis), _ptr(inv_freq), pairs, int(layout), int(bool(inverse)), _stream(stream)), "ssd_rope_axes")
+    _check(lib.ssd_rope_axes(x, out, int(n_rows), int(n_heads), int(head_dim), code, int(x_stride), int(out_stride),
+                             _table(pos, "pos", n_axes * n_rows, torch.int32), int(n_axes), _table(axis, "axis", pairs, torch.uint8),
+                             _table(inv_freq, "inv_freq", pairs, torch.float32), pairs, int(layout), int(bool(inverse)), _stream(stream)), "ssd_rope_axes")
 
 
 def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[float] = None, tokens=None, n_tokens=None, n_prompt=None,
