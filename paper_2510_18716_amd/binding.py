@@ -461,15 +461,14 @@ class SsdPagedConfig(C.Structure):
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
         [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes, their bytes and those of their
-        scales, and by 0 the type of q, new rows and outputs, the bytes of q and those of a token's new rows.
+        scales, and by 0 the type of q, new rows and outputs and the elements of an output.
         Found when they are first asked for after a field was set."""
         if name == "mx_strides":
             places = (self.n_pages, self.n_kv_heads, self.page_size)
             n = places[0] * places[1] * places[2]
             got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,),
                                                 n * (self.head_dim * bits // 8), n * (self.head_dim // 32)) for bits in (4, 8)}
-            size = _DTYPES.get(self.dtype, torch.bfloat16).itemsize * self.head_dim
-            got[0] = _DTYPES.get(self.dtype, torch.bfloat16), self.n_seqs * self.n_heads * size, self.n_kv_heads * size
+            got[0] = _DTYPES.get(self.dtype, torch.bfloat16), self.n_seqs * self.n_heads * self.head_dim
             return got
         if name != "strides":
             raise AttributeError(name)
@@ -743,30 +742,17 @@ def _is_whole(dtype) -> bool:
     return not dtype.is_floating_point and not dtype.is_complex
 
 
-def _sized(t, what: str, dtype):
-    """A tensor whose elements have the size of dtype's, or whatever else stands for one."""
-    if type(t) is _Tensor and t.dtype is not dtype and t.element_size() != dtype.itemsize:
-        raise ValueError("%s of type %s: elements of %d bytes are expected" % (what, t.dtype, dtype.itemsize))
-    return t
-
-
-def _mx_rows(t, what: str, cfg, n: int, heads: int, want, n_bytes: int) -> Optional[int]:
-    """_rows of the config's type, as many as the call takes; n_bytes: of all of them."""
-    if type(t) is _Tensor:
-        if t.nbytes == n_bytes and t.stride() == want:
-            return t.data_ptr()
-        _sized(t, what, cfg.mx_strides[0][0])
-        if t.stride() == want and any(have < need for have, need in zip(t.shape, (n, heads, cfg.head_dim))):
-            raise ValueError("%s of shape %s: [%d, %d, %d] is expected" % (what, tuple(t.shape), n, heads, cfg.head_dim))
-    return _rows(t, what, n, heads, want)
-
-
-def _mx_out(t, dtype, n_bytes: int) -> Optional[int]:
-    """Address of an attention's output, which has as many bytes as its queries."""
-    if type(t) is _Tensor and t.nbytes != n_bytes:
-        if _sized(t, "out", dtype).nbytes < n_bytes:
-            raise ValueError("out of shape %s: %d elements are expected" % (tuple(t.shape), n_bytes // dtype.itemsize))
-    return _ptr(t)
+def _mx_rows(t, what: str, n: int, heads: int, d: int, want, dtype) -> Optional[int]:
+    """Address of n rows of `heads` heads of d elements of dtype; want: the strides of [n, heads, d]."""
+    if type(t) is _Tensor and t.dtype is dtype and t.stride() == want and t.shape == (n, heads, d):
+        return t.data_ptr()
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype:
+        raise ValueError("%s of type %s: %s, elements of %d bytes are expected" % (what, t.dtype, dtype, dtype.itemsize))
+    if t.dim() != 2 or t.stride() != (want[0], 1) or t.shape[0] < n or t.shape[1] < heads * d:      # else where a projection has them
+        _check_rows(t, what, n, want[0], heads * d)
+    return t.data_ptr()
 
 
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
@@ -781,10 +767,10 @@ def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales,
                         seq_pos=None, new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
     """format: "mxfp4" or "mxfp8" (SSD_MXFP4, SSD_MXFP8).  n_new: tokens in k_new; None: its first dimension."""
     n = int(k_new.shape[0] if n_new is None else n_new)
-    new, heads, n_bytes = cfg.strides[2], cfg.n_kv_heads, n * cfg.mx_strides[0][2]
+    rows = n, cfg.n_kv_heads, cfg.head_dim, cfg.strides[2], cfg.mx_strides[0][0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos),
-                                   _mx_rows(k_new, "k_new", cfg, n, heads, new, n_bytes), _mx_rows(v_new, "v_new", cfg, n, heads, new, n_bytes),
+                                   _mx_rows(k_new, "k_new", *rows), _mx_rows(v_new, "v_new", *rows),
                                    _ptr(new_start), n, _ptr(weight_new), _stream(stream)), "ssd_paged_mx_append")
 
 
@@ -792,10 +778,10 @@ def ssd_paged_mx_read(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v
                       first_slot=None, n_rows: Optional[int] = None, stream=None) -> None:
     """n_rows: rows of k_out; None: its first dimension."""
     n = int(k_out.shape[0] if n_rows is None else n_rows)
-    new, heads, n_bytes = cfg.strides[2], cfg.n_kv_heads, n * cfg.mx_strides[0][2]
+    rows = n, cfg.n_kv_heads, cfg.head_dim, cfg.strides[2], cfg.mx_strides[0][0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
     _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(row_start), n, _ptr(first_slot),
-                                 _mx_rows(k_out, "k_out", cfg, n, heads, new, n_bytes), _mx_rows(v_out, "v_out", cfg, n, heads, new, n_bytes),
+                                 _mx_rows(k_out, "k_out", *rows), _mx_rows(v_out, "v_out", *rows),
                                  _stream(stream)), "ssd_paged_mx_read")
 
 
@@ -805,21 +791,20 @@ def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, 
 
 def ssd_paged_mx_decode_attn(cfg: SsdPagedConfig, format, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, lse=None, weight_in=None,
                              weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    dtype, q_bytes, _ = cfg.mx_strides[0]
+    dtype, size = cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", cfg, cfg.n_seqs, cfg.n_heads, cfg.strides[1], q_bytes), k, v, ks, vs, _ptr(weight_in),
-                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _mx_out(out, dtype, q_bytes), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", cfg.n_seqs, cfg.n_heads, cfg.head_dim, cfg.strides[1], dtype), k, v, ks, vs, _ptr(weight_in),
+                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _table(out, "out", size, dtype), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
 
 
 def ssd_paged_mx_decode_step(cfg: SsdPagedConfig, format, q, k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, pos=None,
                              seq_pos=None, lse=None, weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    (_, queries, new), (dtype, q_bytes, n_bytes), B, heads = cfg.strides, cfg.mx_strides[0], cfg.n_seqs, cfg.n_kv_heads
-    n_bytes *= B
+    (_, queries, new), (dtype, size), B, d = cfg.strides, cfg.mx_strides[0], cfg.n_seqs, cfg.head_dim
+    rows = B, cfg.n_kv_heads, d, new, dtype
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", cfg, B, cfg.n_heads, queries, q_bytes), _mx_rows(k_new, "k_new", cfg, B, heads, new, n_bytes),
-                                        _mx_rows(v_new, "v_new", cfg, B, heads, new, n_bytes), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
-                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _mx_out(out, dtype, q_bytes), _ptr(lse), int(max_len), _ptr(workspace),
+    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", B, cfg.n_heads, d, queries, dtype), _mx_rows(k_new, "k_new", *rows), _mx_rows(v_new, "v_new", *rows), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
+                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _table(out, "out", size, dtype), _ptr(lse), int(max_len), _ptr(workspace),
                                         _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
 
 
