@@ -460,14 +460,13 @@ class SsdPagedConfig(C.Structure):
 
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
-        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes, their bytes and those of their
+        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes and the bytes of their
         scales, and by 0 the type of q, new rows and outputs and the elements of an output.
         Found when they are first asked for after a field was set."""
         if name == "mx_strides":
             places = (self.n_pages, self.n_kv_heads, self.page_size)
-            n = places[0] * places[1] * places[2]
-            got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,),
-                                                n * (self.head_dim * bits // 8), n * (self.head_dim // 32)) for bits in (4, 8)}
+            scales = places[0] * places[1] * places[2] * (self.head_dim // 32)
+            got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,), scales) for bits in (4, 8)}
             got[0] = _DTYPES.get(self.dtype, torch.bfloat16), self.n_seqs * self.n_heads * self.head_dim
             return got
         if name != "strides":
@@ -717,13 +716,14 @@ def _mx_scales(t, what: str, need: int) -> Optional[int]:
     return t.data_ptr()
 
 
-def _mx_pool(t, what: str, want, sizes, n: int) -> Optional[int]:
+def _mx_pool(t, what: str, want, sizes) -> Optional[int]:
     """Address of a pool of codes: bytes [n_pages, n_kv_heads, page_size, d * bits / 8] with the config's strides (or the same with page_size before
     n_kv_heads, as it lies in memory then), or memory without gaps that reaches as far."""
+    if type(t) is _Tensor and t.stride() == want and t.shape == sizes and t.element_size() == 1:
+        return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
-    if t.stride() != want or t.nbytes != n:                       # bytes of another shape do not have these strides and as many of them
-        _check_mx_pool(t, what, want, sizes)
+    _check_mx_pool(t, what, want, sizes)
     return t.data_ptr()
 
 
@@ -758,8 +758,8 @@ def _mx_rows(t, what: str, n: int, heads: int, d: int, want, dtype) -> Optional[
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
     """The format's code, and the addresses of two pools of codes and their scales."""
     bits = _FORMATS.get(format) or _format_code(format)
-    want, sizes, n, need = cfg.mx_strides[bits]
-    return (bits, _mx_pool(k_pages, "k_pages", want, sizes, n), _mx_pool(v_pages, "v_pages", want, sizes, n), _mx_scales(k_scales, "k_scales", need),
+    want, sizes, need = cfg.mx_strides[bits]
+    return (bits, _mx_pool(k_pages, "k_pages", want, sizes), _mx_pool(v_pages, "v_pages", want, sizes), _mx_scales(k_scales, "k_scales", need),
             _mx_scales(v_scales, "v_scales", need))
 
 

@@ -161,3 +161,22 @@ def test_rows_that_do_not_reach_as_far(stub, arg):
         for bad in (good[:2, :2 * heads * D].unflatten(1, (2 * heads, D)), good[:2, :heads * D], good[:2, :heads * D].unflatten(1, (heads, D)), good[:3, :heads * D],
                     good[:, :heads * D].unflatten(1, (heads, D))[:, :heads - 1], good[:1, :heads * D].expand(B, heads * D), good[:, :heads * D].unflatten(1, (heads, D)).transpose(1, 2)):
             refused(stub, lambda: _call(name, a, **{arg: bad}))
+
+
+@pytest.mark.parametrize("arg", ["k_pages", "v_pages"])
+def test_pools_that_do_not_reach_as_far_or_are_not_bytes(stub, arg):
+    """Pages farther apart than their rows need."""
+    gap = 4 * KV * PAGE * D // 2
+    memory = torch.zeros(PAGES * gap + 64, dtype=torch.uint8)
+    a = _args(page_stride=2 * gap, head_stride=PAGE * D, row_stride=D)
+    good = memory.as_strided((PAGES, KV, PAGE, D // 2), (gap, PAGE * D // 2, D // 2, 1))
+    a.update(k_pages=good, v_pages=good)
+    for name in CALLS:
+        taken(stub, lambda: _call(name, a))
+        for bad in (memory.as_strided((PAGES // 3, 3 * KV, PAGE, D // 2), good.stride()), memory.as_strided((PAGES // 3, KV, 3 * PAGE, D // 2), good.stride()), good[:-1],
+                    torch.zeros(PAGES * gap, dtype=torch.int16).as_strided((PAGES // 3, KV, PAGE, D // 2), good.stride())):
+            refused(stub, lambda: _call(name, a, **{arg: bad}))
+    dense = _args()
+    for bad in (torch.zeros((PAGES, KV, PAGE, D // 4), dtype=torch.int16), torch.zeros((PAGES, KV, PAGE, D // 2), dtype=torch.int16)):
+        for name in CALLS:
+            refused(stub, lambda: _call(name, dense, **{arg: bad}))
