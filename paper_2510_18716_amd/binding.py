@@ -168,7 +168,6 @@ def _stream(stream=None) -> Optional[int]:
 
 
 _DTYPE_CODES = {torch.bfloat16: SSD_BF16, "bf16": SSD_BF16, torch.float32: SSD_F32, "f32": SSD_F32}
-_DTYPES = {SSD_BF16: torch.bfloat16, SSD_F32: torch.float32}
 
 
 def _dtype_code(dt) -> int:
@@ -445,6 +444,17 @@ def ssd_dense_decode_attn_static(q, K, V, out, B: int, H: int, d: int, dtype, n_
 
 # ---- serving batches of unequal lengths: the cache in pages, the step's logits ----
 
+SSD_MXFP4, SSD_MXFP8 = 4, 8
+_FORMATS = {"mxfp4": SSD_MXFP4, "mxfp8": SSD_MXFP8, SSD_MXFP4: SSD_MXFP4, SSD_MXFP8: SSD_MXFP8}
+_INT, _F32 = torch.int32, torch.float32
+
+
+def _format_code(format) -> int:
+    if format not in _FORMATS:
+        raise ValueError("format %r: \"mxfp4\" or \"mxfp8\" is expected" % (format,))
+    return _FORMATS[format]
+
+
 class SsdPagedConfig(C.Structure):
     _fields_ = [
         ("n_seqs", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
@@ -460,14 +470,10 @@ class SsdPagedConfig(C.Structure):
 
     def __getattr__(self, name):
         """strides: what the config says of the pool, q and new rows as torch says it of tensors [n_pages, n_kv_heads, page_size, d],
-        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: of pools of codes in bytes, by their elements' bits, with their sizes and the bytes of their
-        scales, and by 0 the type of q, new rows and outputs and the elements of an output.
+        [n_seqs, n_heads, d] and [n_new, n_kv_heads, d]; mx_strides: by a format's name or bits, what the calls on quantised pages expect of their tensors (_mx_call).
         Found when they are first asked for after a field was set."""
         if name == "mx_strides":
-            places = (self.n_pages, self.n_kv_heads, self.page_size)
-            scales = places[0] * places[1] * places[2] * (self.head_dim // 32)
-            got = self.__dict__[name] = {bits: (tuple(s * bits // 8 for s in self.strides[0][:3]) + (1,), places + (self.head_dim * bits // 8,), scales) for bits in (4, 8)}
-            got[0] = _DTYPES.get(self.dtype, torch.bfloat16), self.n_seqs * self.n_heads * self.head_dim
+            got = self.__dict__[name] = {key: _mx_call(self, bits) for key, bits in _FORMATS.items()}
             return got
         if name != "strides":
             raise AttributeError(name)
@@ -682,14 +688,21 @@ def ssd_paged_evict(cfg: SsdPagedConfig, k_pages, v_pages, block_table, seq_len,
                                int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_evict")
 
 
-SSD_MXFP4, SSD_MXFP8 = 4, 8
-_FORMATS = {"mxfp4": SSD_MXFP4, "mxfp8": SSD_MXFP8, SSD_MXFP4: SSD_MXFP4, SSD_MXFP8: SSD_MXFP8}
+def _mx_call(cfg, bits: int) -> tuple:
+    """What the calls on quantised pages expect of their tensors: (strides of a pool in bytes, its sizes [n_pages, n_kv_heads, page_size, bytes of a row], whether it has no gaps,
+    bits, bytes of the scales, and for the calls' own arguments (_rows_of q, _rows_of new rows, type of outputs, elements of an output, an lse, a list of sequences,
+    the block table and a table of the pool))."""
+    n, kv, page, d, B, H = cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim, cfg.n_seqs, cfg.n_heads
+    pool, q, new = cfg.strides
+    row, dtype = d * bits // 8, torch.float32 if cfg.dtype == SSD_F32 else torch.bfloat16            # another type is refused by the library
+    strides = tuple(s * bits // 8 for s in pool[:3]) + (1,)
+    return (strides, (n, kv, page, row), strides == (kv * page * row, page * row, row, 1), bits, n * kv * page * (d // 32),
+            (_rows_of(H, d, q, dtype), _rows_of(kv, d, new, dtype), dtype, B * H * d, B * H, B, B * cfg.max_blocks, n * kv * page))
 
 
-def _format_code(format) -> int:
-    if format not in _FORMATS:
-        raise ValueError("format %r: \"mxfp4\" or \"mxfp8\" is expected" % (format,))
-    return _FORMATS[format]
+def _rows_of(heads: int, d: int, strides: tuple, dtype) -> tuple:
+    """(heads, d, strides of [n, heads, d], type, bytes of a row where rows have no gaps between them, or 0)."""
+    return heads, d, strides, dtype, heads * d * dtype.itemsize if strides[0] == heads * d else 0
 
 
 def _check_mx_pool(t, what: str, want, sizes) -> None:
@@ -709,27 +722,31 @@ def _check_mx_pool(t, what: str, want, sizes) -> None:
 
 def _mx_scales(t, what: str, need: int) -> Optional[int]:
     """Address of the scales: `need` bytes without gaps."""
-    if t is None or isinstance(t, int):
+    if type(t) is not _Tensor and (t is None or isinstance(t, int)):
         return t
     if t.nbytes < need or not t.is_contiguous():
         raise ValueError("%s of shape %s, strides %s, type %s: %d bytes without gaps are expected" % (what, tuple(t.shape), t.stride(), t.dtype, need))
     return t.data_ptr()
 
 
-def _mx_pool(t, what: str, want, sizes) -> Optional[int]:
+def _mx_pool(t, what: str, strides, sizes, dense) -> Optional[int]:
     """Address of a pool of codes: bytes [n_pages, n_kv_heads, page_size, d * bits / 8] with the config's strides (or the same with page_size before
     n_kv_heads, as it lies in memory then), or memory without gaps that reaches as far."""
-    if type(t) is _Tensor and t.stride() == want and t.shape == sizes and t.element_size() == 1:
+    if type(t) is _Tensor and t.shape == sizes and (t.is_contiguous() if dense else t.stride() == strides) and t.element_size() == 1:
         return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
-    _check_mx_pool(t, what, want, sizes)
+    _check_mx_pool(t, what, strides, sizes)
     return t.data_ptr()
 
 
 def _table(t, what: str, n: int, dtype) -> Optional[int]:
     """Address of at least n elements without gaps, of dtype (or whole numbers of its size where it is one of those)."""
-    if t is None or isinstance(t, int):
+    if t is None:
+        return None
+    if type(t) is _Tensor and t.dtype is dtype and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    if isinstance(t, int):
         return t
     if t.dtype is not dtype and (t.element_size() != dtype.itemsize or not _is_whole(t.dtype) or not _is_whole(dtype)):
         raise ValueError("%s of type %s: %s, elements of %d bytes are expected" % (what, t.dtype, dtype, dtype.itemsize))
@@ -742,47 +759,48 @@ def _is_whole(dtype) -> bool:
     return not dtype.is_floating_point and not dtype.is_complex
 
 
-def _mx_rows(t, what: str, n: int, heads: int, d: int, want, dtype) -> Optional[int]:
-    """Address of n rows of `heads` heads of d elements of dtype; want: the strides of [n, heads, d]."""
-    if type(t) is _Tensor and t.dtype is dtype and t.stride() == want and t.shape == (n, heads, d):
+def _mx_rows(t, what: str, n: int, rows) -> Optional[int]:
+    """Address of n rows; rows: _rows_of them."""
+    heads, d, strides, dtype, dense = rows
+    if type(t) is _Tensor and t.dtype is dtype and (t.nbytes == n * dense and t.is_contiguous() if dense else t.stride() == strides and t.shape == (n, heads, d)):
         return t.data_ptr()
     if t is None or isinstance(t, int):
         return t
     if t.dtype is not dtype:
         raise ValueError("%s of type %s: %s, elements of %d bytes are expected" % (what, t.dtype, dtype, dtype.itemsize))
-    if t.dim() != 2 or t.stride() != (want[0], 1) or t.shape[0] < n or t.shape[1] < heads * d:      # else where a projection has them
-        _check_rows(t, what, n, want[0], heads * d)
+    if t.dim() != 2 or t.stride() != (strides[0], 1) or t.shape[0] < n or t.shape[1] < heads * d:        # else where a projection has them
+        _check_rows(t, what, n, strides[0], heads * d)
     return t.data_ptr()
 
 
 def _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales):
     """The format's code, and the addresses of two pools of codes and their scales."""
-    bits = _FORMATS.get(format) or _format_code(format)
-    want, sizes, need = cfg.mx_strides[bits]
-    return (bits, _mx_pool(k_pages, "k_pages", want, sizes), _mx_pool(v_pages, "v_pages", want, sizes), _mx_scales(k_scales, "k_scales", need),
-            _mx_scales(v_scales, "v_scales", need))
+    strides, sizes, dense, bits, scales, _ = cfg.mx_strides.get(format) or _format_code(format)
+    return (bits, _mx_pool(k_pages, "k_pages", strides, sizes, dense), _mx_pool(v_pages, "v_pages", strides, sizes, dense), _mx_scales(k_scales, "k_scales", scales),
+            _mx_scales(v_scales, "v_scales", scales))
 
 
 def ssd_paged_mx_append(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, k_new, v_new, pos=None, weight=None,
                         seq_pos=None, new_start=None, n_new: Optional[int] = None, weight_new=None, stream=None) -> None:
     """format: "mxfp4" or "mxfp8" (SSD_MXFP4, SSD_MXFP8).  n_new: tokens in k_new; None: its first dimension."""
     n = int(k_new.shape[0] if n_new is None else n_new)
-    rows = n, cfg.n_kv_heads, cfg.head_dim, cfg.strides[2], cfg.mx_strides[0][0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _ptr(pos), _ptr(weight), _ptr(block_table), _ptr(seq_len), _ptr(seq_pos),
-                                   _mx_rows(k_new, "k_new", *rows), _mx_rows(v_new, "v_new", *rows),
-                                   _ptr(new_start), n, _ptr(weight_new), _stream(stream)), "ssd_paged_mx_append")
+    _, new, _, _, _, seqs, blocks, places = cfg.mx_strides[bits][5]
+    _check(lib.ssd_paged_mx_append(C.byref(cfg), bits, k, v, ks, vs, _table(pos, "pos", places, _INT), _table(weight, "weight", places, _F32),
+                                   _table(block_table, "block_table", blocks, _INT), _table(seq_len, "seq_len", seqs, _INT), _table(seq_pos, "seq_pos", seqs, _INT),
+                                   _mx_rows(k_new, "k_new", n, new), _mx_rows(v_new, "v_new", n, new), _table(new_start, "new_start", seqs + 1, _INT), n,
+                                   _table(weight_new, "weight_new", n * new[0], _F32), _stream(stream)), "ssd_paged_mx_append")
 
 
 def ssd_paged_mx_read(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, k_out, v_out, row_start=None,
                       first_slot=None, n_rows: Optional[int] = None, stream=None) -> None:
     """n_rows: rows of k_out; None: its first dimension."""
     n = int(k_out.shape[0] if n_rows is None else n_rows)
-    rows = n, cfg.n_kv_heads, cfg.head_dim, cfg.strides[2], cfg.mx_strides[0][0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(row_start), n, _ptr(first_slot),
-                                 _mx_rows(k_out, "k_out", *rows), _mx_rows(v_out, "v_out", *rows),
-                                 _stream(stream)), "ssd_paged_mx_read")
+    _, new, _, _, _, seqs, blocks, _ = cfg.mx_strides[bits][5]
+    _check(lib.ssd_paged_mx_read(C.byref(cfg), bits, k, v, ks, vs, _table(block_table, "block_table", blocks, _INT), _table(seq_len, "seq_len", seqs, _INT),
+                                 _table(row_start, "row_start", seqs + 1, _INT), n, _table(first_slot, "first_slot", seqs, _INT), _mx_rows(k_out, "k_out", n, new),
+                                 _mx_rows(v_out, "v_out", n, new), _stream(stream)), "ssd_paged_mx_read")
 
 
 def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, with_weights: bool = False) -> int:
@@ -791,21 +809,23 @@ def ssd_paged_mx_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0, 
 
 def ssd_paged_mx_decode_attn(cfg: SsdPagedConfig, format, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, lse=None, weight_in=None,
                              weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    dtype, size = cfg.mx_strides[0]
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", cfg.n_seqs, cfg.n_heads, cfg.head_dim, cfg.strides[1], dtype), k, v, ks, vs, _ptr(weight_in),
-                                        _ptr(weight_out), _ptr(block_table), _ptr(seq_len), _table(out, "out", size, dtype), _ptr(lse), int(max_len), _ptr(workspace),
-                                        _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
+    queries, _, dtype, size, heads, seqs, blocks, places = cfg.mx_strides[bits][5]
+    _check(lib.ssd_paged_mx_decode_attn(C.byref(cfg), bits, _mx_rows(q, "q", seqs, queries), k, v, ks, vs,
+                                        _table(weight_in, "weight_in", places, _F32), _table(weight_out, "weight_out", places, _F32),
+                                        _table(block_table, "block_table", blocks, _INT), _table(seq_len, "seq_len", seqs, _INT), _table(out, "out", size, dtype),
+                                        _table(lse, "lse", heads, _F32), int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_mx_decode_attn")
 
 
 def ssd_paged_mx_decode_step(cfg: SsdPagedConfig, format, q, k_new, v_new, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, out, pos=None,
                              seq_pos=None, lse=None, weight_in=None, weight_out=None, max_len: int = 0, workspace=None, stream=None) -> None:
-    (_, queries, new), (dtype, size), B, d = cfg.strides, cfg.mx_strides[0], cfg.n_seqs, cfg.head_dim
-    rows = B, cfg.n_kv_heads, d, new, dtype
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", B, cfg.n_heads, d, queries, dtype), _mx_rows(k_new, "k_new", *rows), _mx_rows(v_new, "v_new", *rows), k, v, ks, vs, _ptr(pos), _ptr(weight_in), _ptr(weight_out),
-                                        _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _table(out, "out", size, dtype), _ptr(lse), int(max_len), _ptr(workspace),
-                                        _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
+    queries, new, dtype, size, heads, n, blocks, places = cfg.mx_strides[bits][5]
+    _check(lib.ssd_paged_mx_decode_step(C.byref(cfg), bits, _mx_rows(q, "q", n, queries), _mx_rows(k_new, "k_new", n, new),
+                                        _mx_rows(v_new, "v_new", n, new), k, v, ks, vs, _table(pos, "pos", places, _INT), _table(weight_in, "weight_in", places, _F32),
+                                        _table(weight_out, "weight_out", places, _F32), _table(block_table, "block_table", blocks, _INT),
+                                        _table(seq_len, "seq_len", n, _INT), _table(seq_pos, "seq_pos", n, _INT), _table(out, "out", size, dtype),
+                                        _table(lse, "lse", heads, _F32), int(max_len), _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_mx_decode_step")
 
 
 def ssd_paged_mx_evict_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int = 0) -> int:
@@ -815,9 +835,12 @@ def ssd_paged_mx_evict_workspace_bytes(cfg: SsdPagedConfig, format, max_len: int
 def ssd_paged_mx_evict(cfg: SsdPagedConfig, format, k_pages, v_pages, k_scales, v_scales, block_table, seq_len, budget, pos_in, pos_out, weight_in,
                        weight_out, seq_len_out=None, n_sink: int = 0, recent: int = 0, seq_pos=None, max_len: int = 0, workspace=None, stream=None) -> None:
     bits, k, v, ks, vs = _mx_pools(cfg, format, k_pages, v_pages, k_scales, v_scales)
-    _check(lib.ssd_paged_mx_evict(C.byref(cfg), bits, k, v, ks, vs, _ptr(block_table), _ptr(seq_len), _ptr(seq_pos), _ptr(budget), int(n_sink),
-                                  int(recent), _ptr(pos_in), _ptr(pos_out), _ptr(weight_in), _ptr(weight_out), _ptr(seq_len_out), int(max_len),
-                                  _ptr(workspace), _size(workspace), _stream(stream)), "ssd_paged_mx_evict")
+    _, _, _, _, _, seqs, blocks, places = cfg.mx_strides[bits][5]
+    _check(lib.ssd_paged_mx_evict(C.byref(cfg), bits, k, v, ks, vs, _table(block_table, "block_table", blocks, _INT), _table(seq_len, "seq_len", seqs, _INT),
+                                  _table(seq_pos, "seq_pos", seqs, _INT), _table(budget, "budget", seqs, _INT), int(n_sink), int(recent),
+                                  _table(pos_in, "pos_in", places, _INT), _table(pos_out, "pos_out", places, _INT), _table(weight_in, "weight_in", places, _F32),
+                                  _table(weight_out, "weight_out", places, _F32), _table(seq_len_out, "seq_len_out", seqs, _INT), int(max_len), _ptr(workspace),
+                                  _size(workspace), _stream(stream)), "ssd_paged_mx_evict")
 
 
 def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, inv_freq, axis=None, n_axes: int = 1, n_pairs: Optional[int] = None,
@@ -840,8 +863,8 @@ def ssd_rope_axes(x, out, n_rows: int, n_heads: int, head_dim: int, dtype, pos, 
     x, x_stride, out, out_stride = rows
     pairs = int(inv_freq.numel() if n_pairs is None else n_pairs)
     _check(lib.ssd_rope_axes(x, out, int(n_rows), int(n_heads), int(head_dim), code, int(x_stride), int(out_stride),
-                             _table(pos, "pos", n_axes * n_rows, torch.int32), int(n_axes), _table(axis, "axis", pairs, torch.uint8),
-                             _table(inv_freq, "inv_freq", pairs, torch.float32), pairs, int(layout), int(bool(inverse)), _stream(stream)), "ssd_rope_axes")
+                             _table(pos, "pos", n_axes * n_rows, _INT), int(n_axes), _table(axis, "axis", pairs, torch.uint8),
+                             _table(inv_freq, "inv_freq", pairs, _F32), pairs, int(layout), int(bool(inverse)), _stream(stream)), "ssd_rope_axes")
 
 
 def ssd_logits_process(logits, n_rows: int, V: int, dtype, out, gamma: Optional[float] = None, tokens=None, n_tokens=None, n_prompt=None,

@@ -180,3 +180,25 @@ def test_pools_that_do_not_reach_as_far_or_are_not_bytes(stub, arg):
     for bad in (torch.zeros((PAGES, KV, PAGE, D // 4), dtype=torch.int16), torch.zeros((PAGES, KV, PAGE, D // 2), dtype=torch.int16)):
         for name in CALLS:
             refused(stub, lambda: _call(name, dense, **{arg: bad}))
+
+
+@pytest.mark.parametrize("arg", ["block_table", "seq_len", "seq_pos", "budget", "new_start", "row_start", "first_slot", "seq_len_out", "pos", "pos_in", "pos_out", "weight", "weight_in",
+                                 "weight_out", "weight_new", "lse"])
+def test_tables_of_another_type_or_with_fewer_entries(stub, arg):
+    """torch's whole numbers have 64 bits where nothing else is said."""
+    for name in _users(arg):
+        a = _args()
+        t = a[arg]
+        for other in (torch.int64, torch.int16, torch.uint8, BF16, torch.float64, F32 if t.dtype is INT else INT):
+            refused(stub, lambda: _call(name, a, **{arg: t.to(other)}))
+        for bad in (t.flatten()[:-1], t.flatten()[::2], torch.zeros((2,) + t.shape, dtype=t.dtype).transpose(0, -1)):
+            refused(stub, lambda: _call(name, a, **{arg: bad}))
+        taken(stub, lambda: _call(name, a, **{arg: torch.zeros(t.numel() + 3, dtype=t.dtype)}))
+
+
+@pytest.mark.parametrize("arg", ["k_scales", "v_scales"])
+def test_scales_that_are_fewer_or_lie_apart(stub, arg):
+    for name in CALLS:
+        a = _args()
+        for bad in (a[arg].flatten()[:-1], a[arg].transpose(1, 2), a[arg][:-1]):
+            refused(stub, lambda: _call(name, a, **{arg: bad}))
