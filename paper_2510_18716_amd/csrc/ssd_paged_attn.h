@@ -46,6 +46,9 @@ static constexpr int blocks_of(int waves) { return 256 * waves; }
 static constexpr int HEADS = 16;                                   // heads of a tile
 static constexpr int64_t NO_PAGE = -(1ll << 62);
 static constexpr float LN2 = 0.6931471805599453f;
+// Logits (base 2, scaled) beyond which the product with the scale is rounded before the maximum is taken off, as the maximum was: in one step, exactly, it would leave the maximum's
+// rounding, which is the same factor for all rows, but beyond 2^31 an infinite one.
+static constexpr float FAR = 1024.f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
@@ -154,14 +157,16 @@ template <bool QUADS> static __device__ __forceinline__ void add_weights(const P
         if (x.at[e] >= 0) a.weight_out[x.at[e]] = x.w[e];
 }
 
-// Four rows' probabilities, summed over heads; z: the first head's logits of theirs, the others' `stride` apart.  RAW: without the scale.
+// Four rows' probabilities, summed over heads; z: the first head's logits of theirs, the others' `stride` apart.  RAW: without the scale.  The product with it is rounded before
+// the lse, rounded at its size, is taken off: in one step a large logit would be left with what the lse's rounding took.
 template <bool RAW, typename I> static __device__ __forceinline__ f32x4 probabilities(const float *z, I stride, const float *lse2, int heads, float scale) {
+#pragma clang fp contract(off)
     f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int h = 0; h < heads; ++h) {
         const f32x4 x = *reinterpret_cast<const f32x4 *>(z + h * stride);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] += fast_exp2(RAW ? fmaf(x[e], scale, -lse2[h]) : x[e] - lse2[h]);
+        for (int e = 0; e < 4; ++e) p[e] += fast_exp2((RAW ? x[e] * scale : x[e]) - lse2[h]);
     }
     return p;
 }
@@ -410,7 +415,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
                     hold_k(at, z[NZ - 1]);
                     request_keys(next);
                 }
-                const float scale = TT::MX ? a.scale : 1.f;          // codes: the logits stay as they are until the exponential
+                float scale = TT::MX ? a.scale : 1.f;                // codes: the logits stay as they are until the exponential
                 if constexpr (!TT::MX) {
 #pragma unroll
                     for (int e = 0; e < NZ; ++e) z[e] *= a.scale;
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
                 const bool all = seen.all();
                 if (!all) {
 #pragma unroll
-                    for (int e = 0; e < NZ; ++e) z[e] = seen.has(e) ? z[e] : NEG_BIG;
+                    for (int e = 0; e < NZ; ++e) z[e] = seen.has(e) ? z[e] : TT::MX ? -INFINITY : NEG_BIG;
                 }
                 float top = TT::MX ? z[0] : m;
 #pragma unroll
@@ -443,6 +448,12 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
                     halves_pair(top, x, y);
                     top = fmaxf(x, y);
                 }
+                if constexpr (TT::MX)
+                    if (__any(fabsf(top) > FAR)) {                  // the maximum's rounding is no longer small beside 1
+#pragma unroll
+                        for (int e = 0; e < NZ; ++e) z[e] *= scale;
+                        scale = 1.f;
+                    }
                 if (__any(top > m)) {                               // a larger logit: what is summed so far shrinks
                     const float f = fast_exp2(m - top);
                     l *= f;
