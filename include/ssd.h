@@ -529,8 +529,8 @@ int ssd_paged_evict(const ssd_paged_config *cfg, void *k_pages, void *v_pages, c
  * that all elements of the block are NaN.
  * Writing: E is the smallest exponent with which no element of the block is off by more than half a step, that is with largest |x| <= 464 * 2^E or
  * 7 * 2^E, at least -117 or -125; codes are rounded to the nearest, ties to the even code (the largest are 448 and 6).  A block that holds a NaN or an
- * infinity becomes NaN.  So an element is off by at most 2^-4 (2^-2) of itself or, where that is more, 2^-17 (2^-3) of its block's largest; elements whose
- * rounding reaches 2^128 read back as infinities, whose products may give NaN.
+ * infinity becomes NaN.  So an element is off by at most 2^-4 (2^-2) of itself or, where that is more, 2^-17 (2^-3) of its block's largest or, where E is at its
+ * least, 2^-127; elements whose rounding reaches 2^128 read back as infinities, whose products may give NaN.
  * Reading: a bf16 or fp32 number holds every value exactly.  (Pools written elsewhere: elements below 2^-126 may be read as 0.)
  */
 typedef enum ssd_mx_format { SSD_MXFP4 = 4, SSD_MXFP8 = 8 } ssd_mx_format;

@@ -3,8 +3,9 @@
 //
 // E is the smallest exponent with which no element is off by more than half a step: largest |x| <= 464 * 2^E or 7 * 2^E, half a step above the largest
 // element there is (448, 6).  Elements are rounded to the nearest, ties to the even code; division by 2^E is exact, so a code follows from the definition
-// alone.  E is at least -117 (-125): every element but 0 is then a normal number of fp32 and bf16.  The instructions that convert (v_cvt_scalef32_*) take the
-// scale as the fp32 number 2^E, round so, and give NaN for the scale byte 255; checked for every scale and code, and for ties, on the device.
+// alone.  E is at least -117 (-125): every element but 0 is then a normal number of fp32 and bf16, and in blocks of
+// smaller numbers half of the smallest step stays 2^-127.  The instructions that convert (v_cvt_scalef32_*) take the scale as the fp32 number 2^E, round so, and give NaN for
+// the scale byte 255; checked for every scale and code, and for ties, on the device.
 #pragma once
 
 #include "ssd_device.h"
