@@ -562,7 +562,9 @@ int ssd_paged_mx_read(const ssd_paged_config *cfg, int format, const void *k_pag
 
 /*
  * ssd_paged_decode_attn and ssd_paged_decode_step over the values that the codes stand for; a step's new row is quantised and written first, and
- * attended to as the cache then has it.  A NaN block makes the outputs of its sequence and key head NaN (of V: in its 32 elements).
+ * attended to as the cache then has it.  A NaN block makes the outputs of its sequence and key head NaN (of V: in its 32 elements).  So does E4M3's NaN code in K, which the
+ * library does not write.  In V that code, or an element that reads as an infinity, makes its own column NaN or infinite, and may make the other column of its pair, 2 c
+ * and 2 c + 1, NaN; no other output is touched.
  */
 size_t ssd_paged_mx_workspace_bytes(const ssd_paged_config *cfg, int format, int max_len, int with_weights);
 int ssd_paged_mx_decode_attn(const ssd_paged_config *cfg, int format, const void *q, const void *k_pages, const void *v_pages, const uint8_t *k_scales,
