@@ -68,6 +68,11 @@ class PagePool:
             self.table[seq, len(self.held[seq])] = -1
 
 
+def positions(time, i, columns):
+    """Positions [3, tokens] of tokens at these times: for the i-th token of an image its time, its row and its column, counted from the image's beginning; i None: the time thrice."""
+    return torch.stack([time, time if i is None else time - i + i // columns, time if i is None else time - i + i % columns]).to(torch.int32)
+
+
 def serve(s: Settings, watch=None):
     """Returns (tokens [requests, steps], rows held, positions held per layer).  watch(layer, state): called after each layer's attention."""
     dev, dt = "cuda", torch.bfloat16 if s.dtype == "bf16" else torch.float32
@@ -126,10 +131,9 @@ def serve(s: Settings, watch=None):
     inv_freq = torch.tensor([10000.0 ** (-i / pairs) for i in range(pairs)], device=dev)
 
     def turned(rows, time, i):
-        """Rows of projections whose queries and keys turn by their tokens' positions: time, and the i-th image token's row and column (or the time again)."""
+        """Rows of projections whose queries and keys turn by their tokens' positions."""
         if s.columns:
-            pos = torch.stack([time, time if i is None else time - i % s.columns, time if i is None else time - i + i % s.columns]).to(torch.int32)
-            ssd.ssd_rope_axes(rows, rows, len(rows), H + Hk, d, s.dtype, pos, inv_freq, axis=axis, n_axes=3)
+            ssd.ssd_rope_axes(rows, rows, len(rows), H + Hk, d, s.dtype, positions(time, i, s.columns), inv_freq, axis=axis, n_axes=3)
         return rows
 
     def cut(host_lens):
