@@ -171,6 +171,12 @@ template <bool RAW, typename I> static __device__ __forceinline__ f32x4 probabil
     return p;
 }
 
+template <int N> static __device__ __forceinline__ float largest(const float (&z)[N], float x) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x = fmaxf(x, z[e]);
+    return x;
+}
+
 // The arguments, to be read from their segment again: what one phase of the kernel needs of them does not have to stay in scalar
 // registers through the others (there are too few: they would be kept in vector registers' lanes, and those in scratch memory).
 static __device__ __forceinline__ const PagedAttnArgs &arguments() {
@@ -433,14 +439,24 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_nt_t, f32x4{z[e], z[e + 1], z[e + 2], z[e + 3]}), z_unit,
                                                                (int)(z_lane + 4u * (uint32_t)(row0 + first + 4 * e)), 0, 0);
                 const bool all = seen.all();
+                // Codes: the maximum and whether a logit is far are found before the branch and again in it, though the branch is rare.  Read first behind a branch that jumps
+                // over some of the other side's instructions, the matrix cores' results would be read before they are there: the compiler then counts the wait along the longer
+                // way alone (maxima that were wrong now and then, in outputs only the last bits, as long as what a maximum missed was below 2^127).  A ballot stays where it stands.
+                float top = m;
+                bool far = false;
+                if constexpr (TT::MX) {
+                    top = largest(z, z[0]) * scale;
+                    far = __any(fabsf(top) > FAR);
+                }
                 if (!all) {
 #pragma unroll
                     for (int e = 0; e < NZ; ++e) z[e] = seen.has(e) ? z[e] : TT::MX ? -INFINITY : NEG_BIG;
+                    if constexpr (TT::MX) {
+                        top = largest(z, z[0]) * scale;
+                        far = __any(fabsf(top) > FAR);
+                    }
                 }
-                float top = TT::MX ? z[0] : m;
-#pragma unroll
-                for (int e = 0; e < NZ; ++e) top = fmaxf(top, z[e]);
-                if constexpr (TT::MX) top = fmaxf(m, top * scale);
+                top = TT::MX ? fmaxf(m, top) : largest(z, top);
                 {
                     float x, y;
                     rows_pair(top, x, y);
@@ -449,7 +465,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
                     top = fmaxf(x, y);
                 }
                 if constexpr (TT::MX)
-                    if (__any(fabsf(top) > FAR)) {                  // the maximum's rounding is no longer small beside 1
+                    if (far) {                                      // the maximum's rounding may be no longer small beside 1
 #pragma unroll
                         for (int e = 0; e < NZ; ++e) z[e] *= scale;
                         scale = 1.f;
