@@ -7,7 +7,7 @@
 // V: D / 16 columns of eight rows in a lane.  fp32 calls split q into three bf16 terms and the probabilities too (24 bits of both); bf16 calls take q as it is
 // and probabilities in two terms.
 //
-// With four bits a row's bytes are so few that instructions bound the kernel as soon as memory: 190 vector instructions for 32 rows of 128 elements (all of a
+// With four bits a row's bytes are so few that instructions bound the kernel as soon as memory: 199 vector instructions for 32 rows of 128 elements (all of a
 // launch's over its tiles), 64 of them conversions.  4 sequences of 30000 to 131072 rows, 32 query heads on 8: 58 us with the second launch, 5.4 TB/s; 128 of 64 to 640 rows of
 // 32 heads with weights 43 us, 3.5 TB/s: there the units' beginnings, a length, block table entries and rows one after the other, are half the time.  What was there before: V turned by
 // byte permutations (32 instructions), addresses added lane by lane (14), logits scaled on their own (8), the workgroup's page addresses looked up in LDS: 63 and 51 us.
