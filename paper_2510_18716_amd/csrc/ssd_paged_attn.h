@@ -441,7 +441,7 @@ __global__ __launch_bounds__(64 * WAVES, TT::RESIDENT) void paged_attn_kernel(Pa
                 const bool all = seen.all();
                 // Codes: the maximum and whether a logit is far are found before the branch and again in it, though the branch is rare.  Read first behind a branch that jumps
                 // over some of the other side's instructions, the matrix cores' results would be read before they are there: the compiler then counts the wait along the longer
-                // way alone (maxima that were wrong now and then, in outputs only the last bits, as long as what a maximum missed was below 2^127).  A ballot stays where it stands.
+                // way alone (maxima of sums that lacked a part: in outputs the last bits, and infinities where the part was above 127).  A ballot stays where it stands.
                 float top = m;
                 bool far = false;
                 if constexpr (TT::MX) {
